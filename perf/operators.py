@@ -264,8 +264,8 @@ def _own(s):
                               inverse=case["inverse"])
     pc = ebd.PagedCache(s["K"], s["V"], s["blocks"], s["seq_len"], s["status"])
     if op == "append":
-        ebd.ebd_paged_append(pc, s["k"], s["v"], s["cu"], s["max_new"], table=s["table"],
-                             layout=layout, q=s["q"], q_out=s["out"])
+        ebd.ebd_paged_append(pc, s["k"], s["v"], s["cu"], table=s["table"], layout=layout,
+                             q=s["q"], q_out=s["out"])
         return {"K": s["K"], "V": s["V"], "q": s["out"]}
     if op == "gather":
         out = ebd.CompactCache(s["Kc"], s["Vc"], s["logw"], s["idx"], s["n_kept"], s["status"])
