@@ -76,6 +76,9 @@ typedef enum { EBD_RANGE_BOUND = 0, EBD_RANGE_EXACT = 1 } ebd_range_mode;
                                  unspecified (but every write stays in bounds)       */
 #define EBD_DEV_TIMEOUT 0x4   /* an in-kernel pipeline wait hit its bound and the
                                  kernel returned early; outputs are unspecified      */
+#define EBD_DEV_RANGE 0x8     /* a position, page number, length or token range lies
+                                 outside what the call was given; that entry was
+                                 skipped or clamped (no access leaves the buffers)    */
 
 /* Tail design.  POISSON: independent Bernoulli(pi_i) draws (Section 3.3).
  * SYSTEMATIC: fixed-size systematic sampling at the same pi_i (Hajek 1964;
@@ -415,6 +418,139 @@ ebd_status ebd_certificate_update(const float* radius, int32_t n_layers, int32_t
                                   int32_t n_q_heads, int32_t head_stride, float tau,
                                   int32_t first_step, float* step_mean, float* cert,
                                   int32_t* red_flag, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged cache: the serving steps that fill and read a KV cache before (and
+ * beside) its eviction.  The paper evicts a finished prefill cache and names
+ * no layout for it; these entry points build that cache page by page, attend
+ * new tokens to it and hand an eviction's kept rows to the compact cache.
+ *
+ * New tokens of all sequences are packed one after another: sequence b's are
+ * the packed tokens cu_new[b] .. cu_new[b+1] - 1 (device [B+1] int32,
+ * non-decreasing, from 0 to n_tokens; a sequence may have none).  seq_len[b]
+ * counts the tokens of sequence b INCLUDING its new ones, so packed token t of
+ * sequence b sits at position seq_len[b] - (cu_new[b+1] - t).  Lengths, offsets
+ * and the block table are read on the device only: a captured graph follows
+ * their current values.  An entry outside its range raises EBD_DEV_RANGE and is
+ * skipped or clamped; no access leaves the buffers.
+ * ------------------------------------------------------------------------- */
+
+/* A pool of pages and the block table that deals them to sequences.  Position
+ * j of sequence b, KV head h, channel c of K is element
+ *   block_table[b * max_blocks + j / page_size] * page_stride + h * head_stride
+ *     + (j % page_size) * row_stride + c
+ * of K_pages (V alike): both [page, head, row, d] and [page, row, head, d]
+ * pools, and pools with K and V side by side in a page, are strides of this. */
+typedef struct {
+  int32_t dtype;       /* ebd_dtype of K, V and of the q, k, v of the calls      */
+  int32_t batch;       /* B, sequences                                           */
+  int32_t n_kv_heads;  /* Hkv                                                    */
+  int32_t head_dim;    /* d                                                      */
+  int32_t page_size;   /* positions per page: a power of two, 8 .. 1024          */
+  int32_t n_pages;     /* pages in the pool                                      */
+  int32_t max_blocks;  /* row length of block_table                              */
+  int32_t reserved;    /* 0                                                      */
+  int64_t page_stride; /* elements                                               */
+  int64_t head_stride;
+  int64_t row_stride;          /* >= d                                           */
+  void* K_pages;               /* device                                         */
+  void* V_pages;               /* device                                         */
+  const int32_t* block_table;  /* device [B, max_blocks]                         */
+  const int32_t* seq_len;      /* device [B]                                     */
+} ebd_paged_cache;
+
+/* Which channels of a head turn together, for R = rotary_dim:
+ * HALF (i, i + R/2), PAIRS (2i, 2i + 1), i < R/2; channels >= R stay. */
+typedef enum { EBD_ROTARY_HALF = 0, EBD_ROTARY_PAIRS = 1 } ebd_rotary_layout;
+
+/*
+ * Table of the rotation: table[p, i] = mscale * (cos, sin)(p * inv_freq[i]),
+ * p < n_pos, i < n_freq, formed in float64 and rounded once.  Frequency
+ * scaling for long contexts is in inv_freq and mscale.
+ *   inv_freq device [n_freq] float64
+ *   table    device [n_pos, n_freq, 2] float32 out, 8-byte aligned
+ */
+ebd_status ebd_rotary_table(const double* inv_freq, int32_t n_freq, int32_t n_pos, double mscale,
+                            float* table, void* stream);
+
+/*
+ * Rotary positions: y[t, h] = x[t, h] with its first rotary_dim channels turned
+ * by the angles of positions[t] (float32 arithmetic, one rounding); inverse
+ * turns them back, which is also the gradient of the forward call.
+ *   x, y       device (dtype): element (t, h, c) at t * token_stride +
+ *              h * head_stride + c; y may be x (same strides)
+ *   positions  device [n_tokens] int32; outside [0, n_pos): EBD_DEV_RANGE, the
+ *              nearest row of the table is used
+ *   table      device [n_pos, rotary_dim / 2, 2] float32
+ *   dev_status device int32, nullable
+ * Rows on 16-byte boundaries with (half layout) rotary_dim / 2 or (pairs)
+ * rotary_dim a multiple of 16 bytes move in 16-byte accesses; any other half
+ * layout moves by elements, any other pairs layout by pairs (which then need
+ * even strides and head_dim: EBD_ERR_UNSUPPORTED otherwise).
+ */
+ebd_status ebd_rotary(ebd_dtype dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                      int32_t rotary_dim, ebd_rotary_layout layout, int32_t inverse, const void* x,
+                      int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions,
+                      const float* table, int32_t n_pos, void* y, int64_t y_token_stride,
+                      int64_t y_head_stride, int32_t* dev_status, void* stream);
+
+/*
+ * Append of the new tokens' keys and values to the paged cache, keys turned to
+ * their positions on the way; with n_q_heads > 0 the queries are turned by the
+ * same launch.  Positions past the block table, or on a page outside the
+ * pool, are dropped (EBD_DEV_RANGE).
+ *   k_new, v_new device (dtype) [n_tokens, Hkv, d] with token and head strides
+ *   table        device [n_pos, rotary_dim / 2, 2] float32; NULL: keys go in
+ *                as they are (rotary_dim, layout, n_pos unused, n_q_heads 0)
+ *   q, q_out     device (dtype) [n_tokens, n_q_heads, d], strided; q_out may be q
+ *   dev_status   device int32, required
+ * Alignment as for ebd_rotary.
+ */
+ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, const int32_t* cu_new,
+                            const void* k_new, int64_t k_token_stride, int64_t k_head_stride,
+                            const void* v_new, int64_t v_token_stride, int64_t v_head_stride,
+                            const float* table, int32_t n_pos, int32_t rotary_dim,
+                            ebd_rotary_layout layout, int32_t n_q_heads, const void* q,
+                            int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                            int64_t q_out_token_stride, int64_t q_out_head_stride,
+                            int32_t* dev_status, void* stream);
+
+/*
+ * Causal attention of the new tokens over the paged cache (their own keys and
+ * values are appended first): for packed token t at position p and query head
+ * kvh * G + g, over positions max(0, p - window + 1) <= j <= p (window 0: all),
+ *   y = sum_j softmax_j(scale * q . k_j) v_j,   lse = log sum_j e^(scale q . k_j).
+ * A token with no such position (a sequence shorter than its new tokens) gets
+ * y = 0, lse = -inf.  Pages and rows past a sequence's length are not used,
+ * whatever they hold.
+ *   max_new    largest cu_new[b+1] - cu_new[b] (host bound; more: EBD_DEV_RANGE)
+ *   q          device (dtype) [n_tokens, Hq, d] with token and head strides
+ *   y          device (dtype) [n_tokens, Hq, d] out, dense
+ *   lse        device [n_tokens, Hq] float32 out, nullable
+ *   dev_status device int32, required
+ * Supports d in {64, 128}, G = Hq / Hkv <= 128; q, y and every cached row on
+ * 16-byte boundaries (EBD_ERR_INVALID otherwise).  Products accumulate in
+ * float32; softmax statistics and partial outputs are float32.
+ */
+size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cache, int32_t n_q_heads,
+                                           int32_t max_new);
+ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens, int32_t max_new,
+                               int32_t n_q_heads, const int32_t* cu_new, const void* q,
+                               int64_t q_token_stride, int64_t q_head_stride, float scale,
+                               int32_t window, void* y, float* lse, int32_t* dev_status,
+                               void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ebd_gather out of a paged cache: row p < min(n_kept, capacity) of unit
+ * (b, kvh) of K_c, V_c [B,Hkv,cap,d] receives the cached row at position
+ * idx_c[b,kvh,p].  A position outside [0, seq_len[b]) is skipped, as ebd_gather
+ * does; one on a page outside the pool is skipped with EBD_DEV_RANGE.  With
+ * idx_c = 0, 1, 2, ... it lays a paged cache out densely (for ebd_score).
+ * Needs d * elem a multiple of 16 bytes and rows on 16-byte boundaries.
+ */
+ebd_status ebd_paged_gather(const ebd_paged_cache* cache, const int32_t* idx_c,
+                            const int32_t* n_kept, int32_t capacity, void* K_c, void* V_c,
+                            int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -55,6 +55,11 @@ ebd_status launch_gather_range(const ebd_design* d, ebd_dtype dtype, const void*
 
 bool aligned16(const void* p);
 
+// Validation of a paged cache shared by its entry points, and whether every
+// row of it starts on a 16-byte boundary (paged.cu).
+ebd_status check_paged(const ebd_paged_cache* cache);
+bool paged_aligned16(const ebd_paged_cache* cache);
+
 // Address under which kernels read a caller's buffer: device or managed memory
 // as is, page-locked host memory through its device mapping (read over the
 // host link); nullptr for memory the device cannot address (evict.cu).

@@ -1,0 +1,350 @@
+// Rotary positions: the (cos, sin) table, the rotation of queries or keys, and
+// the append of new keys and values to a paged cache with the rotation on the
+// way.
+//
+// Pair i of a head (channels (i, i + R/2) in the half layout, (2i, 2i + 1) in
+// the pairs layout, R = rotary_dim) at position p turns by p * f_i:
+//   a' = a cos - b sin,  b' = b cos + a sin,
+// in float32, rounded once to the tensor's type.  The inverse (sin -> -sin) is
+// also the gradient, the rotation being orthogonal.  Channels from R on are
+// copied.
+//
+// Both kernels only move data (3 FMAs per element moved), so what bounds them
+// is HBM at large sizes and the launch's load chain at small ones.  A warp
+// takes one token (append: its sequence, position and page are then found once
+// per warp, the sequence by a ballot over 32 offsets at a time) and its lanes
+// take (head, 16-byte chunk pair): neighbouring lanes read neighbouring chunks
+// of a head's row, and a lane keeps one chunk's cosines and sines in registers
+// for all heads it walks, four rows in flight.  Small calls give every lane one
+// chunk pair (a token then spans several warps), so that a decode step costs
+// one pass of the load chain.
+#include <cuda_runtime.h>
+
+#include "common.cuh"
+#include "internal.h"
+#include "paged.cuh"
+
+namespace ebd {
+
+constexpr int kRotWarps = 8;
+
+__global__ void rotary_table_kernel(const double* __restrict__ inv_freq, int n_freq,
+                                    long long total, double mscale, float2* __restrict__ table) {
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < total;
+       i += (long long)gridDim.x * blockDim.x) {
+    const long long pos = i / n_freq;
+    double s, c;
+    // double: a float32 angle of a position near 10^5 is off by 4e-3 radians
+    sincos((double)pos * inv_freq[i - pos * n_freq], &s, &c);
+    table[i] = make_float2((float)(c * mscale), (float)(s * mscale));
+  }
+}
+
+// VEC elements of T as one access.
+template <typename T, int VEC>
+struct alignas(VEC * sizeof(T)) Chunk {
+  T e[VEC];
+};
+
+__device__ __forceinline__ void from_f32(float x, float& y) { y = x; }
+__device__ __forceinline__ void from_f32(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
+
+// One set of rows: element (token t, head h, channel c) at p[t * ts + h * hs + c].
+struct Rows {
+  const void* p;
+  long long ts, hs;
+};
+
+struct RotaryArgs {
+  Rows x;                // q (append) or x (rotary)
+  Rows y;                // its destination
+  Rows k, v;             // append only
+  void *K_pages, *V_pages;
+  PagedView pv;
+  const int32_t* cu;         // append: [batch + 1]
+  const int32_t* positions;  // rotary: [n_tokens]
+  const float2* table;       // [n_pos, rot / 2]; null: no rotation
+  int n_pos;
+  int n_tokens, n_x, n_kv;   // heads of x; kv heads (0: rotary)
+  int units;                 // chunk pairs (half) or chunks (pairs) of a row
+  int rot_units;             // how many of them are rotated
+  int half_off;              // half layout: rot / 2
+  int rot;
+  int parts;                 // warps per token
+  float sin_sign;            // -1: inverse
+  int32_t* dev_status;
+};
+
+// A lane's share of one row: chunk c1, and in the half layout c2.
+template <typename T, int VEC, bool PAIRS>
+struct Piece {
+  Chunk<T, VEC> a, b;
+};
+
+// HALF layout: unit u < rot_units is the chunk pair (u VEC, rot / 2 + u VEC);
+// later units are the chunk pairs of the copied channels, in order.
+template <typename T, int VEC, bool PAIRS>
+__device__ __forceinline__ void unit_channels(const RotaryArgs& a, int u, int& c1, int& c2) {
+  if (PAIRS) {
+    c1 = u * VEC;
+    c2 = -1;
+  } else if (u < a.rot_units) {
+    c1 = u * VEC;
+    c2 = a.half_off + u * VEC;
+  } else {
+    c1 = a.rot + (u - a.rot_units) * VEC;
+    c2 = -1;
+  }
+}
+
+template <typename T, int VEC, bool PAIRS, bool APPEND>
+__global__ void __launch_bounds__(kRotWarps * 32) rotary_kernel(const RotaryArgs a) {
+  constexpr int kRows = 4;  // rows in flight per lane
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * kRotWarps + (threadIdx.x >> 5);
+  const int t = (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
+  if (t >= a.n_tokens) return;
+
+  int pos, b = 0, page = -1;
+  if (APPEND) {
+    b = sequence_of(a.cu, a.pv.batch, t, lane);
+    if (b >= a.pv.batch) {  // past the last sequence: no place for it
+      if (lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
+      return;
+    }
+    pos = a.pv.seq_len[b] - (a.cu[b + 1] - t);
+    page = page_of(a.pv, b, pos);
+    if (page < 0 && lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
+  } else {
+    pos = a.positions[t];
+  }
+  const int tpos = min(max(pos, 0), a.n_pos - 1);
+  if (a.table && tpos != pos && lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
+
+  constexpr int kFreq = PAIRS ? VEC / 2 : VEC;
+  float cs[kFreq], sn[kFreq];
+  auto load_angles = [&](int u) {
+    if (u >= a.rot_units) return;
+    const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * kFreq;
+#pragma unroll
+    for (int i = 0; i < kFreq; ++i) {
+      const float2 f = __ldg(row + i);
+      cs[i] = f.x;
+      sn[i] = f.y * a.sin_sign;
+    }
+  };
+  auto turn = [&](Piece<T, VEC, PAIRS>& r) {
+    if (PAIRS) {
+#pragma unroll
+      for (int i = 0; i < kFreq; ++i) {
+        const float p = to_f32(r.a.e[2 * i]), q = to_f32(r.a.e[2 * i + 1]);
+        from_f32(p * cs[i] - q * sn[i], r.a.e[2 * i]);
+        from_f32(q * cs[i] + p * sn[i], r.a.e[2 * i + 1]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kFreq; ++i) {
+        const float p = to_f32(r.a.e[i]), q = to_f32(r.b.e[i]);
+        from_f32(p * cs[i] - q * sn[i], r.a.e[i]);
+        from_f32(q * cs[i] + p * sn[i], r.b.e[i]);
+      }
+    }
+  };
+
+  const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
+  const int total = heads * a.units, stride = 32 * a.parts;
+  const bool fixed = stride % a.units == 0;  // the lane keeps its unit from head to head
+  int i0 = part * 32 + lane;
+  if (fixed && i0 < total) load_angles(i0 % a.units);
+  for (; i0 < total; i0 += kRows * stride) {
+    Piece<T, VEC, PAIRS> r[kRows];
+    T* dst[kRows];
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      const int i = i0 + k * stride;
+      dst[k] = nullptr;
+      if (i < total) {
+        const int h = i / a.units, u = i - h * a.units;
+        int c1, c2;
+        unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
+        const T* src;
+        if (!APPEND || h < a.n_x) {
+          src = (const T*)a.x.p + t * a.x.ts + h * a.x.hs;
+          dst[k] = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
+        } else {
+          const bool is_v = h >= a.n_x + a.n_kv;
+          const int kh = h - a.n_x - (is_v ? a.n_kv : 0);
+          const Rows& s = is_v ? a.v : a.k;
+          src = (const T*)s.p + t * s.ts + kh * s.hs;
+          if (page >= 0)
+            dst[k] = (T*)(is_v ? a.V_pages : a.K_pages) + slot_offset(a.pv, page, kh, pos);
+        }
+        if (dst[k]) {
+          r[k].a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
+          if (c2 >= 0) r[k].b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kRows; ++k) {
+      if (!dst[k]) continue;
+      const int i = i0 + k * stride;
+      const int h = i / a.units, u = i - h * a.units;
+      int c1, c2;
+      unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
+      if (u < a.rot_units && !(APPEND && h >= a.n_x + a.n_kv)) {
+        if (!fixed) load_angles(u);
+        turn(r[k]);
+      }
+      *reinterpret_cast<Chunk<T, VEC>*>(dst[k] + c1) = r[k].a;
+      if (c2 >= 0) *reinterpret_cast<Chunk<T, VEC>*>(dst[k] + c2) = r[k].b;
+    }
+  }
+}
+
+// A row access of `vec` elements is aligned at every (token, head).
+static bool rows_aligned(const Rows& r, int vec, int elem) {
+  return ((uintptr_t)r.p % (vec * elem)) == 0 && r.ts % vec == 0 && r.hs % vec == 0;
+}
+
+template <typename T, int VEC, bool PAIRS, bool APPEND>
+static ebd_status launch_rotary_v(RotaryArgs a, int head_dim, cudaStream_t s) {
+  const int rot = a.table ? a.rot : 0;
+  a.rot = rot;
+  a.half_off = rot / 2;
+  a.rot_units = PAIRS ? rot / VEC : rot / 2 / VEC;
+  a.units = a.rot_units + (head_dim - rot) / VEC;
+  const int chunks = (a.n_x + (APPEND ? 2 * a.n_kv : 0)) * a.units;
+  // one chunk pair per lane while the call has fewer warps than the GPU holds
+  // (latency), four rows per lane beyond that
+  const int few = (chunks + 127) / 128, many = (chunks + 31) / 32;
+  a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
+  const long long blocks = ((long long)a.n_tokens * a.parts + kRotWarps - 1) / kRotWarps;
+  if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
+  rotary_kernel<T, VEC, PAIRS, APPEND><<<(unsigned)blocks, kRotWarps * 32, 0, s>>>(a);
+  return launch_status();
+}
+
+// 16-byte accesses where every row and the rotated part allow them; otherwise
+// single elements (half) or single pairs (pairs).
+template <typename T, bool APPEND>
+static ebd_status launch_rotary_t(const RotaryArgs& a, int head_dim, bool pairs, bool cache_ok,
+                                  cudaStream_t s) {
+  constexpr int kWide = 16 / (int)sizeof(T);
+  const int rot = a.table ? a.rot : 0;
+  const bool wide = (pairs ? rot : rot / 2) % kWide == 0 && head_dim % kWide == 0 && cache_ok &&
+                    (a.n_x == 0 || (rows_aligned(a.x, kWide, sizeof(T)) &&
+                                    rows_aligned(a.y, kWide, sizeof(T)))) &&
+                    (!APPEND || (rows_aligned(a.k, kWide, sizeof(T)) &&
+                                 rows_aligned(a.v, kWide, sizeof(T))));
+  if (pairs) {
+    // an odd head_dim or stride would split a pair's 2-element access
+    const bool two = head_dim % 2 == 0 &&
+                     (a.n_x == 0 || (rows_aligned(a.x, 2, sizeof(T)) &&
+                                     rows_aligned(a.y, 2, sizeof(T)))) &&
+                     (!APPEND || (rows_aligned(a.k, 2, sizeof(T)) &&
+                                  rows_aligned(a.v, 2, sizeof(T)) &&
+                                  a.pv.page_stride % 2 == 0 && a.pv.head_stride % 2 == 0 &&
+                                  a.pv.row_stride % 2 == 0 &&
+                                  (uintptr_t)a.K_pages % (2 * sizeof(T)) == 0 &&
+                                  (uintptr_t)a.V_pages % (2 * sizeof(T)) == 0));
+    if (wide) return launch_rotary_v<T, kWide, true, APPEND>(a, head_dim, s);
+    if (two) return launch_rotary_v<T, 2, true, APPEND>(a, head_dim, s);
+    return EBD_ERR_UNSUPPORTED;
+  }
+  if (wide) return launch_rotary_v<T, kWide, false, APPEND>(a, head_dim, s);
+  return launch_rotary_v<T, 1, false, APPEND>(a, head_dim, s);
+}
+
+}  // namespace ebd
+
+using namespace ebd;
+
+extern "C" ebd_status ebd_rotary_table(const double* inv_freq, int32_t n_freq, int32_t n_pos,
+                                       double mscale, float* table, void* stream) {
+  if (!inv_freq || !table || n_freq < 1 || n_pos < 1) return EBD_ERR_INVALID;
+  if ((uintptr_t)table % 8 != 0) return EBD_ERR_INVALID;
+  const long long total = (long long)n_freq * n_pos;
+  long long blocks = (total + 255) / 256;
+  if (blocks > (long long)sm_count() * 16) blocks = (long long)sm_count() * 16;
+  rotary_table_kernel<<<(unsigned)blocks, 256, 0, (cudaStream_t)stream>>>(
+      inv_freq, n_freq, total, mscale, (float2*)table);
+  return launch_status();
+}
+
+extern "C" ebd_status ebd_rotary(ebd_dtype dtype, int32_t n_tokens, int32_t n_heads,
+                                 int32_t head_dim, int32_t rotary_dim, ebd_rotary_layout layout,
+                                 int32_t inverse, const void* x, int64_t x_token_stride,
+                                 int64_t x_head_stride, const int32_t* positions,
+                                 const float* table, int32_t n_pos, void* y,
+                                 int64_t y_token_stride, int64_t y_head_stride,
+                                 int32_t* dev_status, void* stream) {
+  if (dtype != EBD_F32 && dtype != EBD_BF16) return EBD_ERR_INVALID;
+  if (layout != EBD_ROTARY_HALF && layout != EBD_ROTARY_PAIRS) return EBD_ERR_INVALID;
+  if (n_tokens < 0 || n_heads < 1 || head_dim < 1 || n_pos < 1) return EBD_ERR_INVALID;
+  if (rotary_dim < 2 || rotary_dim > head_dim || rotary_dim % 2 != 0) return EBD_ERR_INVALID;
+  if (n_tokens == 0) return EBD_OK;
+  if (!x || !y || !positions || !table || (uintptr_t)table % 8 != 0) return EBD_ERR_INVALID;
+  RotaryArgs a = {};
+  a.x = Rows{x, x_token_stride, x_head_stride};
+  a.y = Rows{y, y_token_stride, y_head_stride};
+  a.positions = positions;
+  a.table = (const float2*)table;
+  a.n_pos = n_pos;
+  a.n_tokens = n_tokens;
+  a.n_x = n_heads;
+  a.rot = rotary_dim;
+  a.sin_sign = inverse ? -1.f : 1.f;
+  a.dev_status = dev_status;
+  const bool pairs = layout == EBD_ROTARY_PAIRS;
+  cudaStream_t s = (cudaStream_t)stream;
+  return dtype == EBD_F32 ? launch_rotary_t<float, false>(a, head_dim, pairs, true, s)
+                          : launch_rotary_t<__nv_bfloat16, false>(a, head_dim, pairs, true, s);
+}
+
+extern "C" ebd_status ebd_paged_append(
+    const ebd_paged_cache* cache, int32_t n_tokens, const int32_t* cu_new, const void* k_new,
+    int64_t k_token_stride, int64_t k_head_stride, const void* v_new, int64_t v_token_stride,
+    int64_t v_head_stride, const float* table, int32_t n_pos, int32_t rotary_dim,
+    ebd_rotary_layout layout, int32_t n_q_heads, const void* q, int64_t q_token_stride,
+    int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+    int32_t* dev_status, void* stream) {
+  const ebd_status st = check_paged(cache);
+  if (st != EBD_OK) return st;
+  if (layout != EBD_ROTARY_HALF && layout != EBD_ROTARY_PAIRS) return EBD_ERR_INVALID;
+  if (n_tokens < 0 || n_q_heads < 0) return EBD_ERR_INVALID;
+  if (table && (n_pos < 1 || rotary_dim < 2 || rotary_dim > cache->head_dim ||
+                rotary_dim % 2 != 0 || (uintptr_t)table % 8 != 0))
+    return EBD_ERR_INVALID;
+  if (n_q_heads > 0 && !table) return EBD_ERR_INVALID;  // nothing to do to q
+  if (n_tokens == 0) return EBD_OK;
+  if (!cu_new || !k_new || !v_new || !dev_status || (n_q_heads > 0 && (!q || !q_out)))
+    return EBD_ERR_INVALID;
+  RotaryArgs a = {};
+  a.x = Rows{q, q_token_stride, q_head_stride};
+  a.y = Rows{q_out, q_out_token_stride, q_out_head_stride};
+  a.k = Rows{k_new, k_token_stride, k_head_stride};
+  a.v = Rows{v_new, v_token_stride, v_head_stride};
+  a.K_pages = cache->K_pages;
+  a.V_pages = cache->V_pages;
+  a.pv = paged_view(*cache);
+  a.cu = cu_new;
+  a.table = (const float2*)table;
+  a.n_pos = table ? n_pos : 0x7fffffff;
+  a.n_tokens = n_tokens;
+  a.n_x = n_q_heads;
+  a.n_kv = cache->n_kv_heads;
+  a.rot = rotary_dim;
+  a.sin_sign = 1.f;
+  a.dev_status = dev_status;
+  const int eb = cache->dtype == EBD_F32 ? 4 : 2;
+  const int wide = 16 / eb;
+  const bool cache_ok = aligned16(cache->K_pages) && aligned16(cache->V_pages) &&
+                        cache->page_stride % wide == 0 && cache->head_stride % wide == 0 &&
+                        cache->row_stride % wide == 0;
+  const bool pairs = layout == EBD_ROTARY_PAIRS && table;
+  cudaStream_t s = (cudaStream_t)stream;
+  return cache->dtype == EBD_F32
+             ? launch_rotary_t<float, true>(a, cache->head_dim, pairs, cache_ok, s)
+             : launch_rotary_t<__nv_bfloat16, true>(a, cache->head_dim, pairs, cache_ok, s);
+}

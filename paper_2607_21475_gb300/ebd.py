@@ -14,6 +14,7 @@ is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from dataclasses import dataclass
 
@@ -33,6 +34,9 @@ __all__ = [
     "ebd_check_stalled_wait", "design_for",
     "CompactCache",
     "alloc_compact", "ABI_FUNCTIONS",
+    "EBD_DEV_RANGE", "EBD_ROTARY_HALF", "EBD_ROTARY_PAIRS", "EbdPagedCache", "PagedCache",
+    "alloc_paged", "rotary_frequencies", "ebd_rotary_table", "ebd_rotary", "ebd_paged_append",
+    "ebd_paged_attention_workspace_bytes", "ebd_paged_attention", "ebd_paged_gather",
 ]
 
 EBD_OK = 0
@@ -40,6 +44,8 @@ EBD_F32, EBD_BF16 = 0, 1
 EBD_RANGE_BOUND, EBD_RANGE_EXACT = 0, 1
 EBD_DEV_CAPACITY, EBD_DEV_NONFINITE, EBD_DEV_TIMEOUT = 0x1, 0x2, 0x4
 EBD_SAMPLING_POISSON, EBD_SAMPLING_SYSTEMATIC = 0, 1
+EBD_DEV_RANGE = 0x8
+EBD_ROTARY_HALF, EBD_ROTARY_PAIRS = 0, 1
 
 # Every symbol include/ebd.h declares.
 ABI_FUNCTIONS = (
@@ -48,7 +54,8 @@ ABI_FUNCTIONS = (
     "ebd_gather", "ebd_decode_workspace_bytes", "ebd_workspace_bytes", "ebd_certified_decode",
     "ebd_certified_decode_static", "ebd_certificate_update", "ebd_append", "ebd_reevict",
     "ebd_gather_queries", "ebd_variance_contributions", "ebd_block_scores",
-    "ebd_check_stalled_wait",
+    "ebd_check_stalled_wait", "ebd_rotary_table", "ebd_rotary", "ebd_paged_append",
+    "ebd_paged_attention_workspace_bytes", "ebd_paged_attention", "ebd_paged_gather",
 )
 
 
@@ -69,6 +76,19 @@ class EbdDesign(ctypes.Structure):
     ]
 
 
+class EbdPagedCache(ctypes.Structure):
+    """Mirror of ``ebd_paged_cache`` in include/ebd.h."""
+    _fields_ = [
+        ("dtype", ctypes.c_int32), ("batch", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+        ("max_blocks", ctypes.c_int32), ("reserved", ctypes.c_int32),
+        ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+        ("row_stride", ctypes.c_int64), ("K_pages", ctypes.c_void_p),
+        ("V_pages", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+        ("seq_len", ctypes.c_void_p),
+    ]
+
+
 _LIB = None
 
 
@@ -86,7 +106,9 @@ def lib():
         L = ctypes.CDLL(LIB)
         c_void_p, i32, u64, f32, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_uint64,
                                        ctypes.c_float, ctypes.c_size_t)
+        i64, f64 = ctypes.c_int64, ctypes.c_double
         P = ctypes.POINTER(EbdDesign)
+        C = ctypes.POINTER(EbdPagedCache)
         sig = {
             "ebd_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "ebd_abi_version": (i32, []),
@@ -131,6 +153,20 @@ def lib():
             "ebd_block_scores": (ctypes.c_int, [i32, i32, i32, c_void_p, c_void_p, c_void_p, i32,
                                                 i32, i32, c_void_p, c_void_p]),
             "ebd_check_stalled_wait": (ctypes.c_int, [c_void_p, c_void_p]),
+            "ebd_rotary_table": (ctypes.c_int, [c_void_p, i32, i32, f64, c_void_p, c_void_p]),
+            "ebd_rotary": (ctypes.c_int, [ctypes.c_int, i32, i32, i32, i32, ctypes.c_int, i32,
+                                          c_void_p, i64, i64, c_void_p, c_void_p, i32, c_void_p,
+                                          i64, i64, c_void_p, c_void_p]),
+            "ebd_paged_append": (ctypes.c_int, [C, i32, c_void_p, c_void_p, i64, i64, c_void_p,
+                                                i64, i64, c_void_p, i32, i32, ctypes.c_int, i32,
+                                                c_void_p, i64, i64, c_void_p, i64, i64, c_void_p,
+                                                c_void_p]),
+            "ebd_paged_attention_workspace_bytes": (sz, [C, i32, i32]),
+            "ebd_paged_attention": (ctypes.c_int, [C, i32, i32, i32, c_void_p, c_void_p, i64, i64,
+                                                   f32, i32, c_void_p, c_void_p, c_void_p,
+                                                   c_void_p, sz, c_void_p]),
+            "ebd_paged_gather": (ctypes.c_int, [C, c_void_p, c_void_p, i32, c_void_p, c_void_p,
+                                                c_void_p, c_void_p]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -493,4 +529,229 @@ def ebd_block_scores(contrib: torch.Tensor, idx_c: torch.Tensor, n_kept: torch.T
         _ptr(idx_c, torch.int32, (B, H, cap), "idx_c"), _ptr(n_kept, torch.int32, (B, H), "n_kept"),
         cap, int(block), int(n_blocks), _ptr(out, torch.float32, (B, H, n_blocks), "out"),
         _stream(stream)))
+    return out
+
+
+# ---------------------------------------------------------------- paged cache
+@dataclass
+class PagedCache:
+    """A pool of pages and the block table that deals them to sequences.
+
+    K_pages and V_pages are [n_pages, Hkv, page_size, d] tensors of equal
+    strides with the last dimension contiguous (views of another order, such
+    as ``pool.transpose(1, 2)`` of a [n_pages, page_size, Hkv, d] pool, serve
+    as they are); block_table [B, max_blocks] and seq_len [B] are int32.
+    seq_len counts the new tokens of the call it is passed to."""
+    K_pages: torch.Tensor
+    V_pages: torch.Tensor
+    block_table: torch.Tensor
+    seq_len: torch.Tensor
+    dev_status: torch.Tensor  # [1] int32
+
+
+def alloc_paged(batch, n_kv_heads, n_pages, page_size, head_dim, max_blocks, dtype,
+                device) -> PagedCache:
+    """Caller-side allocation of a paged cache: empty pages, an all-zero block
+    table and lengths of zero."""
+    shape = (n_pages, n_kv_heads, page_size, head_dim)
+    i = torch.int32
+    return PagedCache(torch.empty(shape, dtype=dtype, device=device),
+                      torch.empty(shape, dtype=dtype, device=device),
+                      torch.zeros((batch, max_blocks), dtype=i, device=device),
+                      torch.zeros((batch,), dtype=i, device=device),
+                      torch.zeros((1,), dtype=i, device=device))
+
+
+def _paged(pc: PagedCache) -> EbdPagedCache:
+    K, V, bt, n = pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len
+    if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride():
+        raise ValueError("K_pages and V_pages must be [n_pages, Hkv, page_size, d] tensors of "
+                         "equal shapes and strides")
+    if not (K.is_cuda and V.is_cuda and bt.is_cuda and n.is_cuda):
+        raise ValueError("a paged cache's tensors must be CUDA tensors")
+    if V.dtype != K.dtype:
+        raise TypeError(f"V_pages has dtype {V.dtype}, expected {K.dtype}")
+    if bt.dtype != torch.int32 or n.dtype != torch.int32:
+        raise TypeError("block_table and seq_len must be int32")
+    B = n.shape[0]
+    if bt.dim() != 2 or n.dim() != 1 or bt.shape[0] != B or not (
+            bt.is_contiguous() and n.is_contiguous()):
+        raise ValueError("block_table must be a contiguous [B, max_blocks] and seq_len a "
+                         "contiguous [B] tensor")
+    n_pages, H, page, d = K.shape
+    ps, hs, rs, cs = K.stride()
+    if cs != 1:
+        raise ValueError("the last dimension of K_pages and V_pages must be contiguous")
+    return EbdPagedCache(_dtype_code(K), B, H, d, page, n_pages, bt.shape[1], 0, ps, hs, rs,
+                         K.data_ptr(), V.data_ptr(), bt.data_ptr(), n.data_ptr())
+
+
+def _rows(t, dtype, n_tokens, n_heads, head_dim, name):
+    """(address, token stride, head stride) of a [T, H, d] tensor with any
+    token and head strides."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if tuple(t.shape) != (n_tokens, n_heads, head_dim):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected "
+                         f"{(n_tokens, n_heads, head_dim)}")
+    ts, hs, cs = t.stride()
+    if cs != 1 and head_dim > 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    return t.data_ptr(), ts, hs
+
+
+def _rotary_rows(table):
+    if table.dim() != 3 or table.shape[2] != 2:
+        raise ValueError(f"table has shape {tuple(table.shape)}, expected [n_pos, rotary_dim / 2, 2]")
+    return _ptr(table, torch.float32, name="table"), table.shape[0], 2 * table.shape[1]
+
+
+def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none",
+                       factor: float = 1.0, original_positions: int = 4096,
+                       fast_turns: float = 32.0, slow_turns: float = 1.0):
+    """(inv_freq [rotary_dim / 2] float64 on the CPU, mscale) for
+    ``ebd_rotary_table``: f_i = base^(-2i / R), and for contexts `factor` times
+    the original length
+
+    - "linear": every f_i / factor (positions compressed);
+    - "base": base * factor^(R / (R - 2)): the slowest pair slows by `factor`,
+      the fastest stays;
+    - "parts": a pair that makes at least `fast_turns` turns over
+      `original_positions` stays, one that makes at most `slow_turns` slows by
+      `factor`, in between the two are mixed linearly in the pair's index; the
+      table grows by mscale = 0.1 ln(factor) + 1."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise ValueError("rotary_dim must be even and at least 2")
+    if not base > 1 or not factor >= 1:
+        raise ValueError("base must be above 1 and factor at least 1")
+    if scaling not in ("none", "linear", "base", "parts"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    if scaling == "base" and rotary_dim > 2:
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    i = torch.arange(0, rotary_dim, 2, dtype=torch.float64)
+    f = base ** (-i / rotary_dim)
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling == "parts":
+        if not fast_turns > slow_turns > 0:
+            raise ValueError("parts scaling needs fast_turns > slow_turns > 0")
+        # index at which a pair makes n turns over original_positions
+        at = [rotary_dim / 2 * math.log(original_positions / (2 * math.pi * n)) / math.log(base)
+              for n in (fast_turns, slow_turns)]
+        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rotary_dim // 2 - 1)
+        slow = ((i / 2 - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        return f * (1 - slow) + f / factor * slow, 0.1 * math.log(factor) + 1.0
+    return f, 1.0
+
+
+def ebd_rotary_table(inv_freq: torch.Tensor, n_pos: int, mscale: float = 1.0, table=None,
+                     device=None, stream=None) -> torch.Tensor:
+    """(cos, sin) of positions 0 .. n_pos - 1: float32 [n_pos, R / 2, 2] from the
+    float64 frequencies [R / 2] (moved to `device` when they are on the CPU)."""
+    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1:
+        raise TypeError("inv_freq must be a one-dimensional float64 tensor")
+    if table is None:
+        dev = inv_freq.device if inv_freq.is_cuda else (device or "cuda")
+        table = torch.empty((n_pos, inv_freq.shape[0], 2), dtype=torch.float32, device=dev)
+    f = inv_freq.to(table.device)
+    _check("ebd_rotary_table", lib().ebd_rotary_table(
+        _ptr(f, name="inv_freq"), f.shape[0], int(n_pos), float(mscale),
+        _ptr(table, torch.float32, (n_pos, f.shape[0], 2), "table"), _stream(stream)))
+    return table
+
+
+def ebd_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, out=None,
+               layout: int = EBD_ROTARY_HALF, inverse: bool = False, dev_status=None,
+               stream=None) -> torch.Tensor:
+    """x [T, H, d] (any token and head strides) turned to positions [T] (int32)
+    with the table's rows; `inverse` turns back (the gradient).  out may be x."""
+    if x.dim() != 3:
+        raise ValueError("x must be [T, H, d]")
+    T, H, d = x.shape
+    if out is None:
+        out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
+    tab, n_pos, rot = _rotary_rows(table)
+    xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
+    yp, yt, yh = _rows(out, x.dtype, T, H, d, "out")
+    _check("ebd_rotary", lib().ebd_rotary(
+        _dtype_code(x), T, H, d, rot, int(layout), 1 if inverse else 0, xp, xt, xh,
+        _ptr(positions, torch.int32, (T,), "positions"), tab, n_pos, yp, yt, yh,
+        _ptr(dev_status, torch.int32, (1,), "dev_status"), _stream(stream)))
+    return out
+
+
+def ebd_paged_append(pc: PagedCache, k_new: torch.Tensor, v_new: torch.Tensor,
+                     cu_new: torch.Tensor, table=None, layout: int = EBD_ROTARY_HALF, q=None,
+                     q_out=None, stream=None) -> PagedCache:
+    """Write the packed new tokens' keys (turned by the table, when given) and
+    values into their pages; with q and q_out also the turned queries.
+    k_new, v_new: [T, Hkv, d]; q, q_out: [T, Hq, d]; cu_new: [B + 1] int32."""
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    T, H, d = k_new.shape[0], c.n_kv_heads, c.head_dim
+    kp, kt, kh = _rows(k_new, dt, T, H, d, "k_new")
+    vp, vt, vh = _rows(v_new, dt, T, H, d, "v_new")
+    tab, n_pos, rot = (None, 0, 0) if table is None else _rotary_rows(table)
+    hq, qp, qt, qh, op, ot, oh = 0, None, 0, 0, None, 0, 0
+    if q is not None:
+        if q.dim() != 3 or q_out is None:
+            raise ValueError("q must be [T, Hq, d] and come with q_out")
+        hq = q.shape[1]
+        qp, qt, qh = _rows(q, dt, T, hq, d, "q")
+        op, ot, oh = _rows(q_out, dt, T, hq, d, "q_out")
+    _check("ebd_paged_append", lib().ebd_paged_append(
+        ctypes.byref(c), T, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"), kp, kt, kh, vp,
+        vt, vh, tab, n_pos, rot, int(layout), hq, qp, qt, qh, op, ot, oh,
+        _ptr(pc.dev_status, torch.int32, (1,), "dev_status"), _stream(stream)))
+    return pc
+
+
+def ebd_paged_attention_workspace_bytes(pc: PagedCache, n_q_heads: int, max_new: int) -> int:
+    return int(lib().ebd_paged_attention_workspace_bytes(ctypes.byref(_paged(pc)), int(n_q_heads),
+                                                         int(max_new)))
+
+
+def ebd_paged_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, max_new: int,
+                        y=None, lse=None, scale=None, window: int = 0, workspace=None,
+                        stream=None):
+    """Causal attention of the packed new tokens q [T, Hq, d] over the paged
+    cache that already holds their keys and values: y [T, Hq, d] in q's type and
+    the log-sum-exp [T, Hq].  max_new: the most new tokens of any sequence;
+    scale defaults to d^-1/2; window 0 sees every earlier position."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, d]")
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    T, hq, d = q.shape[0], q.shape[1], c.head_dim
+    qp, qt, qh = _rows(q, dt, T, hq, d, "q")
+    if y is None:
+        y = torch.empty((T, hq, d), dtype=dt, device=q.device)
+    if lse is None:
+        lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+    L = lib()
+    ref = ctypes.byref(c)
+    ws, wsb = _workspace(L.ebd_paged_attention_workspace_bytes(ref, hq, int(max_new)), q.device,
+                         workspace)
+    _check("ebd_paged_attention", L.ebd_paged_attention(
+        ref, T, int(max_new), hq, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"), qp, qt, qh,
+        d ** -0.5 if scale is None else float(scale), int(window), _ptr(y, dt, (T, hq, d), "y"),
+        _ptr(lse, torch.float32, (T, hq), "lse"),
+        _ptr(pc.dev_status, torch.int32, (1,), "dev_status"), ws, wsb, _stream(stream)))
+    return y, lse
+
+
+def ebd_paged_gather(pc: PagedCache, out: CompactCache, stream=None) -> CompactCache:
+    """Copy the cached rows named by out.idx_c into out.K_c / out.V_c."""
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    B, H, cap, d = c.batch, c.n_kv_heads, out.capacity, c.head_dim
+    _check("ebd_paged_gather", lib().ebd_paged_gather(
+        ctypes.byref(c), _ptr(out.idx_c, torch.int32, (B, H, cap), "idx_c"),
+        _ptr(out.n_kept, torch.int32, (B, H), "n_kept"), cap,
+        _ptr(out.K_c, dt, (B, H, cap, d), "K_c"), _ptr(out.V_c, dt, (B, H, cap, d), "V_c"),
+        _ptr(out.dev_status, torch.int32, (1,), "dev_status"), _stream(stream)))
     return out
