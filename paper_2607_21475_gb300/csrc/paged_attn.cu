@@ -13,25 +13,13 @@
 
 #include "common.cuh"
 #include "internal.h"
-#include "paged.cuh"
+#include "paged_attn.cuh"
 
 namespace ebd {
 
 constexpr int kAttnRows = 32;
 constexpr int kAttnKeys = 64;
 constexpr int kAttnThreads = 128;
-
-struct PagedAttnArgs {
-  const void *q, *K_pages, *V_pages;
-  PagedView pv;
-  const int32_t* cu;
-  long long q_ts, q_hs;
-  void* y;
-  float* lse;  // nullable
-  int n_tokens, max_new, group, window;
-  float scale2;  // scale * log2(e)
-  int32_t* dev_status;
-};
 
 template <int D>
 struct SimtLayout {
@@ -221,10 +209,9 @@ using namespace ebd;
 
 extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cache,
                                                       int32_t n_q_heads, int32_t max_new) {
-  (void)cache;
-  (void)n_q_heads;
-  (void)max_new;
-  return 0;
+  if (check_paged(cache) != EBD_OK || n_q_heads < 1 || max_new < 1) return 0;
+  if (cache->dtype != EBD_BF16) return 0;
+  return paged_split_bytes(sm_count(), kTcAttnRows, cache->head_dim);
 }
 
 extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens,
@@ -248,9 +235,9 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride % wide != 0 ||
       q_head_stride % wide != 0)
     return EBD_ERR_INVALID;
-  if (ws_bytes < ebd_paged_attention_workspace_bytes(cache, n_q_heads, max_new))
-    return EBD_ERR_CAPACITY;
-  (void)workspace;
+  const size_t need = ebd_paged_attention_workspace_bytes(cache, n_q_heads, max_new);
+  if (ws_bytes < need) return EBD_ERR_CAPACITY;
+  if (need > 0 && (!workspace || !aligned16(workspace))) return EBD_ERR_INVALID;
   PagedAttnArgs a = {};
   a.q = q;
   a.K_pages = cache->K_pages;
@@ -271,6 +258,8 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   if (cache->dtype == EBD_F32)
     return cache->head_dim == 128 ? launch_paged_simt<float, 128>(a, s)
                                   : launch_paged_simt<float, 64>(a, s);
-  return cache->head_dim == 128 ? launch_paged_simt<__nv_bfloat16, 128>(a, s)
-                                : launch_paged_simt<__nv_bfloat16, 64>(a, s);
+  const int n_cta = sm_count();
+  paged_split_layout(a, workspace, n_cta, kTcAttnRows);
+  a.min_share = 2;
+  return launch_paged_tc(a, *cache, n_cta, s);
 }

@@ -1,0 +1,253 @@
+// Work split and partial results shared by the paged-attention kernels.
+//
+// An item is one (sequence, KV head, m-tile): up to BM rows (row = new token x
+// query head of the group, token-major) over the key tiles of BN positions
+// that at least one row sees.  Items in order of (sequence, head, m-tile) form
+// one line of key tiles, and CTA c of n takes the tiles
+// [c share, (c + 1) share), whatever items they belong to: every CTA gets the
+// same number of tiles however ragged the batch is.  A CTA's range is cut at
+// item boundaries into pieces; the pieces of an item that more than one CTA
+// holds leave (o / l, log2-sum) in the workspace and a merge kernel joins them
+// in CTA order, so results do not depend on timing.  The lengths are on the
+// device only, so one warp of each CTA finds the CTA's place on that line.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "common.cuh"
+#include "internal.h"
+#include "paged.cuh"
+
+namespace ebd {
+
+// What a CTA leaves for the merge: whether its first piece continues an item
+// that an earlier CTA began (1: and does not end it, 2: and ends it), and the
+// item that its last piece begins without ending (b < 0: none).
+struct PieceRecord {
+  int cont;
+  int b, h, m;
+};
+
+struct PagedAttnArgs {
+  const void *q, *K_pages, *V_pages;
+  PagedView pv;
+  const int32_t* cu;
+  long long q_ts, q_hs;
+  void* y;
+  float* lse;  // nullable
+  int n_tokens, max_new, group, window;
+  float scale2;  // scale * log2(e)
+  int32_t* dev_status;
+  // split results: slot 2 c of CTA c for a piece that continues an item, slot
+  // 2 c + 1 for one that begins an item without ending it
+  PieceRecord* rec;  // [n_cta]
+  float* part_lse;   // [2 n_cta][BM], log2 units
+  float* part_o;     // [2 n_cta][BM][D]
+  int min_share;     // fewest key tiles per CTA
+};
+
+// Key tiles [kb, ke) of m-tile m; a tile with nothing to see keeps one (fully
+// masked) tile, so that its rows get written.
+template <int BM, int BN>
+__device__ __forceinline__ void item_range(const PagedAttnArgs& a, const SeqSpan& sp, int m,
+                                           int& kb, int& ke) {
+  const int row0 = m * BM, last = min(sp.n * a.group, row0 + BM) - 1;
+  const int p0 = sp.len - sp.n;
+  const int k_end = p0 + last / a.group + 1;  // <= len
+  kb = 0;
+  ke = 1;
+  if (k_end > 0) {
+    if (a.window > 0) kb = max(0, p0 + row0 / a.group - a.window + 1) / BN;
+    ke = (k_end + BN - 1) / BN;
+  }
+}
+
+struct WorkStart {
+  int b, h, m, cur;
+  long long count;  // key tiles of this CTA
+};
+
+__device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += u;
+  }
+  return v;
+}
+
+// Key tiles of one head of the sequences base + lane (lane = 0..31).
+template <int BM, int BN>
+__device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int base, int lane,
+                                                    bool report) {
+  const int b = base + lane;
+  SeqSpan sp = {};
+  if (b < a.pv.batch) {
+    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
+    if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
+  }
+  const int mt = (sp.n * a.group + BM - 1) / BM;
+  long long c = 0;
+  for (int m = 0; m < min(mt, 4); ++m) {
+    int kb, ke;
+    item_range<BM, BN>(a, sp, m, kb, ke);
+    c += ke - kb;
+  }
+  // long chunks: the warp walks the remaining m-tiles of one sequence together
+  for (uint32_t left = __ballot_sync(0xffffffffu, mt > 4); left; left &= left - 1) {
+    const int src = __ffs(left) - 1;
+    SeqSpan s;
+    s.n = __shfl_sync(0xffffffffu, sp.n, src);
+    s.len = __shfl_sync(0xffffffffu, sp.len, src);
+    const int k = (s.n * a.group + BM - 1) / BM;
+    long long sum = 0;
+    for (int m = 4 + lane; m < k; m += 32) {
+      int kb, ke;
+      item_range<BM, BN>(a, s, m, kb, ke);
+      sum += ke - kb;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == src) c += sum;
+  }
+  return c;
+}
+
+// The first tile and the number of tiles of CTA `cta`; one whole warp.
+template <int BM, int BN>
+__device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
+                                               int lane) {
+  const int H = a.pv.n_kv_heads;
+  long long total = 0;
+  for (int base = 0; base < a.pv.batch; base += 32)
+    total += H * sequence_tiles<BM, BN>(a, base, lane, cta == 0);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  const long long share = max((long long)a.min_share, (total + n_cta - 1) / n_cta);
+  long long at = cta * share;
+  WorkStart w = {0, 0, 0, 0, 0};
+  if (at >= total) return w;
+  w.count = min(share, total - at);
+  long long c = 0;
+  for (int base = 0; base < a.pv.batch; base += 32) {
+    c = sequence_tiles<BM, BN>(a, base, lane, false);
+    const long long upto = warp_scan_add(c * H, lane);
+    const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
+    if (past) {
+      const int src = __ffs(past) - 1;
+      at -= __shfl_sync(0xffffffffu, upto - c * H, src);
+      c = __shfl_sync(0xffffffffu, c, src);
+      w.b = base + src;
+      break;
+    }
+    at -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  w.h = (int)(at / c);
+  at -= w.h * c;
+  const SeqSpan sp = seq_span(a.pv, a.cu, w.b, a.n_tokens, a.max_new);
+  const int mt = (sp.n * a.group + BM - 1) / BM;
+  for (int base = 0; base < mt; base += 32) {
+    int kb = 0, ke = 0;
+    if (base + lane < mt) item_range<BM, BN>(a, sp, base + lane, kb, ke);
+    const long long upto = warp_scan_add(ke - kb, lane);
+    const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
+    if (past) {
+      const int src = __ffs(past) - 1;
+      at -= __shfl_sync(0xffffffffu, upto - (ke - kb), src);
+      w.m = base + src;
+      w.cur = __shfl_sync(0xffffffffu, kb, src) + (int)at;
+      break;
+    }
+    at -= __shfl_sync(0xffffffffu, upto, 31);
+  }
+  return w;
+}
+
+// Walks a CTA's pieces; every role of the CTA walks the same ones.
+template <int BM, int BN>
+struct PieceWalk {
+  int b, h, m, mt;
+  SeqSpan sp;
+  int kb, ke;    // the item's tiles
+  int cur, end;  // this piece's
+  long long left;
+
+  __device__ __forceinline__ PieceWalk(const PagedAttnArgs& a, const WorkStart& w)
+      : b(w.b), h(w.h), m(w.m), left(w.count) {
+    if (left <= 0) return;
+    load(a);
+    cur = w.cur;
+    end = (int)min((long long)ke, cur + left);
+  }
+  __device__ __forceinline__ void load(const PagedAttnArgs& a) {
+    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
+    mt = (sp.n * a.group + BM - 1) / BM;
+    item_range<BM, BN>(a, sp, m, kb, ke);
+  }
+  __device__ __forceinline__ bool live() const { return left > 0; }
+  __device__ __forceinline__ int rows(const PagedAttnArgs& a) const {
+    return min(BM, sp.n * a.group - m * BM);
+  }
+  // Slot of this piece's partial result; -1: the piece is a whole item.
+  __device__ __forceinline__ int slot(int cta) const {
+    return cur > kb ? 2 * cta : (end < ke ? 2 * cta + 1 : -1);
+  }
+  __device__ __forceinline__ void next(const PagedAttnArgs& a) {
+    left -= end - cur;
+    if (left <= 0) return;
+    if (++m < mt) {
+      item_range<BM, BN>(a, sp, m, kb, ke);
+    } else {
+      m = 0;
+      if (++h == a.pv.n_kv_heads) {
+        h = 0;
+        do {
+          if (++b >= a.pv.batch) {  // the arrays changed under the call: stop
+            left = 0;
+            return;
+          }
+          load(a);
+        } while (mt == 0);
+      } else {
+        item_range<BM, BN>(a, sp, m, kb, ke);
+      }
+    }
+    cur = kb;
+    end = (int)min((long long)ke, cur + left);
+  }
+};
+
+// One thread of each CTA writes its record (before the merge kernel's wait).
+template <int BM, int BN>
+__device__ __forceinline__ void write_record(const PagedAttnArgs& a, const WorkStart& w, int cta) {
+  PieceRecord r = {0, -1, 0, 0};
+  PieceWalk<BM, BN> p(a, w);
+  bool first = true;
+  for (; p.live(); p.next(a)) {
+    if (first && p.cur > p.kb) r.cont = p.end < p.ke ? 1 : 2;
+    else if (p.end < p.ke) {
+      r.b = p.b;
+      r.h = p.h;
+      r.m = p.m;
+    }
+    first = false;
+  }
+  a.rec[cta] = r;
+}
+
+// Joins the pieces of split items.  `a` as the attention kernel had it, rows_per_item = its BM.
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int rows_per_item,
+                              int n_cta, cudaStream_t s);
+
+// Bytes of the split results of n_cta CTAs.
+size_t paged_split_bytes(int n_cta, int rows_per_item, int head_dim);
+// Points a's split arrays into the workspace.
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int rows_per_item);
+
+ebd_status launch_paged_tc(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
+                           cudaStream_t s);
+constexpr int kTcAttnRows = 256;
+
+}  // namespace ebd

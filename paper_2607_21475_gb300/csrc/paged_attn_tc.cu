@@ -1,0 +1,540 @@
+// Paged attention on the 5th-generation tensor cores: bf16, head_dim 64 / 128,
+// more than a few rows per (sequence, KV head).
+//
+// An item is 256 rows as two MMA tiles X = A, B of 128 rows; keys come in tiles
+// of 128.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
+// the softmax warps turn S_X into weights P_X, and O_X += P_X V with P_X read
+// from tensor memory.  While the softmax of one X runs, the tensor cores work
+// for the other.  Tensor memory (512 columns): O_A, O_B (128 columns each, D
+// used), S_A, S_B (128 columns each); P_X (bf16) overwrites the first 64
+// columns of S_X.
+//
+// The softmax keeps one row per thread.  Its reference m moves only when a
+// tile's maximum exceeds it by more than 2^8 (in the weight), so that O_X is
+// rarely rescaled; the result is the same, sums and weights being relative to
+// the same m.  Weights are rounded to bf16 for the second product (their sum is
+// of the unrounded ones), which costs at most 2^-8 of the largest value, as
+// the result's own rounding does.
+//
+// Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warp 8 issues the
+// MMAs, warp 9 the TMA copies of K and V (one box per page and 64 channels;
+// pages past the sequence's end are read past the pool's end, which fills
+// zeros), warps 10-11 bring the query rows into the swizzled layout and clear
+// the value rows of a tile past the sequence's end (weight 0 times whatever a
+// page holds there must stay 0).
+//
+// Every wait is bounded (~2 s): a timeout raises EBD_DEV_TIMEOUT, the roles
+// leave their loops, copies and MMAs in flight are waited for and the tensor
+// memory is released.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include <mutex>
+
+#include "decode_tile.cuh"
+#include "paged_attn.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+
+namespace ebd {
+
+constexpr int kTcBM = kTcAttnRows;
+constexpr int kTcBN = 128;
+constexpr int kTcAttnThreads = 384;
+
+template <int D>
+struct PagedTcLayout {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kBox = 128 * 128;  // 128 rows x 64 bf16
+  static constexpr int kTile = kHalves * kBox;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr int kQ = 0;  // two tiles
+  static constexpr int kKV = 2 * kTile;
+  static constexpr int kBar = kKV + kStages * kTile;
+  static constexpr int kBytes = kBar + 512 + 1024;  // + alignment slack
+};
+
+struct TcBars {
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t fixed, done;
+  uint64_t kv_full[10], kv_empty[10];
+};
+
+// Recomputes 16-channel groups of one row's output whose products came out
+// NaN: a weight of 0 times a hidden value that is NaN or infinite, or a value
+// that the row does see.  Reads only positions [k_lo, k_hi), which it sees, with
+// the row's reference and sum of the fast path; writes mean of the weighted
+// values (bf16 to y, or float32 to a partial result).
+template <int D>
+__device__ __noinline__ void redo_groups(const PagedAttnArgs& a, int b, int h, int token, int g,
+                                         int k_lo, int k_hi, float base, float inv,
+                                         uint32_t groups, __nv_bfloat16* y, float* part) {
+  const uint4* q = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + token * a.q_ts +
+                                                  (h * a.group + g) * a.q_hs);
+  for (int c = 0; c < D; c += 16) {
+    if (!(groups >> (c / 16) & 1)) continue;
+    float acc[16] = {};
+    for (int pos = k_lo; pos < k_hi; ++pos) {
+      const int page = page_of(a.pv, b, pos);
+      if (page < 0) continue;
+      const long long off = slot_offset(a.pv, page, h, pos);
+      const uint4* k = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.K_pages + off);
+      float s = 0.f;
+      for (int i = 0; i < D / 8; ++i) {
+        const uint4 x = q[i], z = k[i];
+        s = fmaf(bf16_lo(x.x), bf16_lo(z.x), fmaf(bf16_hi(x.x), bf16_hi(z.x), s));
+        s = fmaf(bf16_lo(x.y), bf16_lo(z.y), fmaf(bf16_hi(x.y), bf16_hi(z.y), s));
+        s = fmaf(bf16_lo(x.z), bf16_lo(z.z), fmaf(bf16_hi(x.z), bf16_hi(z.z), s));
+        s = fmaf(bf16_lo(x.w), bf16_lo(z.w), fmaf(bf16_hi(x.w), bf16_hi(z.w), s));
+      }
+      const float p = exp2f(fmaf(s, a.scale2, -base));
+      const __nv_bfloat16* v = (const __nv_bfloat16*)a.V_pages + off + c;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (y) y[c + i] = __float2bfloat16_rn(acc[i] * inv);
+      else part[c + i] = acc[i] * inv;
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kTcAttnThreads, 1)
+    paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK,
+                         const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs a) {
+  using L = PagedTcLayout<D>;
+  constexpr int KS = L::kStages;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  TcBars* bar = reinterpret_cast<TcBars*>(smem + L::kBar);
+  __shared__ WorkStart start_s;
+  __shared__ uint32_t tmem_s;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int cta = blockIdx.x;
+  if (warp == 8) {
+    tmem_alloc(&tmem_s, 512);
+    tmem_relinquish();
+  } else if (warp == 9) {
+    if (lane == 0) {
+      mbar_init(&bar->q_full, 64);
+      mbar_init(&bar->q_empty, 1);
+      for (int x = 0; x < 2; ++x) {
+        mbar_init(&bar->s_full[x], 1);
+        mbar_init(&bar->p_full[x], 128);
+        mbar_init(&bar->o_full[x], 1);
+      }
+      mbar_init(&bar->fixed, 64);
+      mbar_init(&bar->done, 1);
+      for (int s = 0; s < KS; ++s) {
+        mbar_init(&bar->kv_full[s], 1);
+        mbar_init(&bar->kv_empty[s], 1);
+      }
+      fence_barrier_init();
+    }
+  } else if (warp == 0) {
+    const WorkStart w = find_work<kTcBM, kTcBN>(a, cta, gridDim.x, lane);
+    if (lane == 0) start_s = w;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_s;
+  const uint32_t tO[2] = {tmem, tmem + 128}, tS[2] = {tmem + 256, tmem + 384};
+  PieceWalk<kTcBM, kTcBN> w(a, start_s);
+  bool ok = true;
+
+  // 384 x 168 registers at launch: 64512 = 256 x 208 + 128 x 88
+  if (warp < 8) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ---------------- softmax and epilogue: one row per thread
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t sS = tS[x] + lane_base, sO = tO[x] + lane_base;
+    uint32_t it = 0;  // tiles of X so far: barrier phases
+    if (threadIdx.x == 0) write_record<kTcBM, kTcBN>(a, start_s, cta);  // while the first tile loads
+    __syncwarp();
+    for (; ok && w.live(); w.next(a)) {
+      const int rows = w.rows(a);
+      if (x * 128 >= rows) continue;  // no row of this X
+      const int r = min(x * 128 + row, rows - 1);  // rows past the end repeat the last one
+      const int tok = (w.m * kTcBM + r) / a.group, g = w.m * kTcBM + r - tok * a.group;
+      const int pos = w.sp.len - w.sp.n + tok;
+      const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+      float m = -INFINITY, l = 0.f;
+      for (int j = w.cur; j < w.end; ++j, ++it) {
+        const int k0 = j * kTcBN;
+        if (!mbar_wait_warp(&bar->s_full[x], it & 1)) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        uint32_t s[2][64];
+        tmem_ld64(sS, s[0]);
+        tmem_ld64(sS + 64, s[1]);
+        tmem_ld_wait();
+        if (__any_sync(0xffffffffu, hi - k0 < kTcBN || lo > k0)) {
+          const int chi = hi - k0, clo = lo - k0;
+#pragma unroll
+          for (int i = 0; i < 128; ++i)
+            if (i >= chi || i < clo) s[i >> 6][i & 63] = __float_as_uint(-INFINITY);
+        }
+        float t4[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t4[i] = __uint_as_float(s[0][i]);
+#pragma unroll
+        for (int i = 4; i < 128; ++i)
+          t4[i & 3] = fmaxf(t4[i & 3], __uint_as_float(s[i >> 6][i & 63]));
+        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+        const bool grow = m > -INFINITY && (top - m) * a.scale2 > kRescaleLog2;
+        if (__any_sync(0xffffffffu, grow)) {
+          // O_X holds the tiles before this one: wait for their product
+          if (!mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const float m1 = fmaxf(m, top);
+          const float f = m > -INFINITY ? exp2f((m - m1) * a.scale2) : 1.f;
+          l *= f;
+          m = m1;
+          // 16 columns at a time: the 128 logits stay in registers meanwhile
+#pragma unroll 1
+          for (int c = 0; c < D; c += 16) {
+            uint32_t o[16];
+            tmem_ld16(sO + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(sO + c, o);
+          }
+        } else if (m == -INFINITY) {
+          m = top;  // nothing but zeros in O_X so far
+        }
+        const float base = m == -INFINITY ? 0.f : m * a.scale2;
+        const float2 sc2 = make_float2(a.scale2, a.scale2), nb = make_float2(-base, -base);
+        float2 sum = make_float2(0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t p[32];
+#pragma unroll
+          for (int i = 0; i < 32; ++i) {
+            float2 e = __ffma2_rn(make_float2(__uint_as_float(s[c][2 * i]),
+                                              __uint_as_float(s[c][2 * i + 1])),
+                                  sc2, nb);
+            e.x = exp2f(e.x);
+            e.y = exp2f(e.y);
+            sum = __fadd2_rn(sum, e);
+            p[i] = pack_bf16(e.x, e.y);
+          }
+          tmem_st32(sS + c * 32, p);
+        }
+        l += sum.x + sum.y;
+        tmem_st_wait();
+        tc_fence_before();
+        mbar_arrive(&bar->p_full[x]);
+      }
+      if (!ok) break;
+      if (!mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
+        ok = false;
+        break;
+      }
+      tc_fence_after();
+      const int slot = w.slot(cta);
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const bool mine = x * 128 + row < rows;
+      const float lse2 = l == 0.f ? -INFINITY : m * a.scale2 + log2f(l);
+      const long long out = (long long)(w.sp.t0 + tok) * (a.pv.n_kv_heads * a.group) +
+                            w.h * a.group + g;
+      const size_t prow = (size_t)slot * kTcBM + x * 128 + row;
+      uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
+#pragma unroll
+      for (int c = 0; c < D; c += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        tmem_ld32(sO + c, o);
+        tmem_ld_wait();
+        float z0 = 0.f, z1 = 0.f;  // NaN where an output is NaN or infinite
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          z0 = fmaf(__uint_as_float(o[i]), 0.f, z0);
+          z1 = fmaf(__uint_as_float(o[16 + i]), 0.f, z1);
+        }
+        nan_groups |= (z0 != z0 ? 1u : 0u) << (c / 16) | (z1 != z1 ? 2u : 0u) << (c / 16);
+        if (!mine) {
+        } else if (slot >= 0) {
+          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            dst[i] = make_float4(
+                __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
+                __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
+        } else {
+          uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.y + out * D + c);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t q[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              q[e] = pack_bf16(__uint_as_float(o[8 * i + 2 * e]) * inv,
+                               __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+            dst[i] = make_uint4(q[0], q[1], q[2], q[3]);
+          }
+        }
+      }
+      if (mine) {
+        if (slot >= 0) a.part_lse[prow] = lse2;
+        else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
+        if (nan_groups)
+          redo_groups<D>(a, w.b, w.h, w.sp.t0 + tok, g, max(lo, w.cur * kTcBN),
+                         min(hi, w.end * kTcBN), m == -INFINITY ? 0.f : m * a.scale2, inv,
+                         nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
+                         slot < 0 ? nullptr : a.part_o + prow * D);
+      }
+      __syncwarp();
+      tc_fence_before();  // the reads of O_X, before the next item's first product
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+  }
+  if (warp == 8) {
+    // ---------------- MMA issue
+    if (lane == 0) {
+      const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
+      const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
+      const uint32_t qb = smem_u32(smem + L::kQ), kvb = smem_u32(smem + L::kKV);
+      uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
+      uint32_t it[2] = {0, 0}, items = 0, fixes = 0;
+      auto s_mma = [&](int x, uint32_t kslot) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (uint32_t)((kk >> 2) * L::kBox + (kk & 3) * 32);
+          umma_bf16(tS[x], umma_desc_k_sw128(qb + x * L::kTile + off),
+                    umma_desc_k_sw128(kvb + kslot * L::kTile + off), idesc_s, kk > 0);
+        }
+        umma_commit(&bar->s_full[x]);
+      };
+      auto o_mma = [&](int x, uint32_t vslot, bool acc) {
+#pragma unroll
+        for (int kk = 0; kk < kTcBN / 16; ++kk)
+          umma_bf16_ta(tO[x], tS[x] + kk * 8,
+                       umma_desc_mn_sw128(kvb + vslot * L::kTile + kk * 2048, L::kBox), idesc_o,
+                       acc || kk > 0);
+        umma_commit(&bar->o_full[x]);
+      };
+      auto step = [&]() {
+        if (++slot == KS) {
+          slot = 0;
+          ph ^= 1;
+        }
+      };
+      for (; ok && w.live(); w.next(a), ++items) {
+        const int nx = w.rows(a) > 128 ? 2 : 1;
+        const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
+        ok = mbar_wait_bounded(&bar->q_full, items & 1) &&
+             mbar_wait_bounded(&bar->kv_full[slot], ph);
+        if (!ok) break;
+        tc_fence_after();
+        for (int x = 0; ok && x < nx; ++x) {
+          // S_X overwrites the last item's P_X: its product has to be done
+          if (it[x] > 0) ok = mbar_wait_bounded(&bar->o_full[x], (it[x] - 1) & 1);
+          if (ok) s_mma(x, slot);
+        }
+        if (!ok) break;
+        umma_commit(&bar->kv_empty[slot]);
+        if (w.end - w.cur == 1) umma_commit(&bar->q_empty);
+        step();
+        for (int j = w.cur; ok && j < w.end; ++j) {
+          const uint32_t vslot = slot;
+          ok = mbar_wait_bounded(&bar->kv_full[slot], ph);
+          if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
+          if (!ok) break;
+          step();
+          const bool more = j + 1 < w.end;
+          const uint32_t kslot = slot;
+          for (int x = 0; ok && x < nx; ++x) {
+            ok = mbar_wait_bounded(&bar->p_full[x], it[x] & 1);
+            if (!ok) break;
+            tc_fence_after();
+            o_mma(x, vslot, j > w.cur);
+            if (x + 1 == nx) umma_commit(&bar->kv_empty[vslot]);
+            if (more) {
+              if (x == 0) ok = mbar_wait_bounded(&bar->kv_full[kslot], ph);
+              // S_X overwrites P_X: its product has to be done
+              ok = ok && mbar_wait_bounded(&bar->o_full[x], it[x] & 1);
+              if (!ok) break;
+              tc_fence_after();
+              s_mma(x, kslot);
+              if (x + 1 == nx) umma_commit(&bar->kv_empty[kslot]);
+              if (x + 1 == nx && j + 2 == w.end) umma_commit(&bar->q_empty);
+            }
+            ++it[x];
+          }
+          if (ok && more) step();
+        }
+      }
+      umma_commit(&bar->done);
+      mbar_wait_bounded(&bar->done, 0);
+    }
+    __syncwarp();
+  } else if (warp == 9) {
+    // ---------------- K and V copies
+    uint32_t slot = 0, ph = 0, issued = 0;
+    const int page = 1 << a.pv.page_shift;
+    const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
+    bool bad = false;
+    for (; ok && w.live(); w.next(a)) {
+      for (int j = w.cur; ok && j < w.end; ++j) {
+        // lane i: one box of the tile (keys bx * box .., channels half * 64 ..)
+        const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
+        const int pos = j * kTcBN + bx * box;
+        int pg = a.pv.n_pages;  // past the pool where there is none
+        if (bx < boxes && pos < w.sp.len) {
+          const int p = page_of(a.pv, w.b, pos);
+          if (p >= 0) pg = p;
+          else bad = true;
+        }
+        for (int kv = 0; ok && kv < 2; ++kv) {
+          if (issued >= KS && !mbar_wait_warp(&bar->kv_empty[slot], ph ^ 1)) {
+            ok = false;
+            break;
+          }
+          if (lane == 0) mbar_arrive_expect_tx(&bar->kv_full[slot], L::kTile);
+          __syncwarp();
+          if (bx < boxes)
+            tma_load_4d(smem + L::kKV + slot * L::kTile + half * L::kBox + bx * box * 128,
+                        kv ? &tmV : &tmK, half * 64, pos & (page - 1), w.h, pg,
+                        &bar->kv_full[slot]);
+          __syncwarp();
+          ++issued;
+          if (++slot == KS) {
+            slot = 0;
+            ph ^= 1;
+          }
+        }
+      }
+    }
+    if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
+    // every copy has landed before the block may end
+    for (uint32_t i = issued > KS ? issued - KS : 0; i < issued; ++i)
+      mbar_wait_bounded(&bar->kv_full[i % KS], (i / KS) & 1);
+  } else if (warp > 9) {
+    // ---------------- query rows; value rows past the end
+    const int tid = threadIdx.x - 320;
+    constexpr int CH = D / 8;  // 16-byte chunks per row
+    uint32_t items = 0, tile0 = 0;  // tiles before this piece: ring position 2 tile
+    for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
+      if (items > 0 && !mbar_wait_bounded(&bar->q_empty, (items - 1) & 1)) {
+        ok = false;
+        break;
+      }
+      const int rows = w.rows(a);
+      const int c = tid % CH, padded = rows > 128 ? 256 : 128;
+      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (long long)w.sp.t0 * a.q_ts +
+                               (long long)(w.h * a.group) * a.q_hs + c * 8;
+      for (int r = tid / CH; r < padded; r += 64 / CH) {
+        unsigned char* dst = smem + L::kQ + (r >> 7) * L::kTile + (c >> 3) * L::kBox +
+                             (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
+        if (r < rows) {
+          const int tok = (w.m * kTcBM + r) / a.group, g = w.m * kTcBM + r - tok * a.group;
+          cp_async16(dst, q + tok * a.q_ts + g * a.q_hs);
+        } else {
+          *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+        }
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+      fence_proxy_async_smem();
+      mbar_arrive(&bar->q_full);
+      if (w.sp.len < w.end * kTcBN) {
+        // the piece's last value tile: ring position 2 (tile0 + tiles) - 1.  Its
+        // stage's phase is certain only once the piece's last S product is done
+        // (q_empty): every earlier copy has landed by then, and no later one
+        // can take the stage before the rows are cleared.
+        const uint32_t at = 2 * (tile0 + (w.end - w.cur)) - 1;
+        if (!mbar_wait_bounded(&bar->q_empty, items & 1) ||
+            !mbar_wait_bounded(&bar->kv_full[at % KS], (at / KS) & 1)) {
+          ok = false;
+          break;
+        }
+        const int first = w.sp.len - (w.end - 1) * kTcBN;  // rows from here on are cleared
+        unsigned char* v = smem + L::kKV + (at % KS) * L::kTile;
+        for (int i = max(first, 0) * 8 + tid; i < kTcBN * 8; i += 64)
+#pragma unroll
+          for (int h = 0; h < L::kHalves; ++h)
+            *reinterpret_cast<uint4*>(v + h * L::kBox + i * 16) = make_uint4(0, 0, 0, 0);
+        fence_proxy_async_smem();
+        mbar_arrive(&bar->fixed);
+      }
+    }
+  }
+  if (!ok) raise_status(a.dev_status, EBD_DEV_TIMEOUT);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+static PFN_cuTensorMapEncodeTiled_v12000 paged_encoder() {
+  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+  static std::once_flag once;
+  std::call_once(once, [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess)
+      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+  });
+  return fn;
+}
+
+// [page, head, row, channel] of one pool; box: 64 channels x rows of one page.
+static bool encode_pool(CUtensorMap* map, const ebd_paged_cache& c, const void* base,
+                        int box_rows) {
+  auto enc = paged_encoder();
+  if (!enc) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page_size,
+                              (cuuint64_t)c.n_kv_heads, (cuuint64_t)c.n_pages};
+  // a dimension of one entry never steps: any valid stride will do for it
+  auto bytes = [&](int64_t s, int n) { return (cuuint64_t)(n > 1 ? s * 2 : c.head_dim * 2); };
+  const cuuint64_t strides[3] = {bytes(c.row_stride, c.page_size),
+                                 bytes(c.head_stride, c.n_kv_heads),
+                                 bytes(c.page_stride, c.n_pages)};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box,
+             one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
+                              cudaStream_t s) {
+  CUtensorMap tmK, tmV;
+  const int box = c.page_size < kTcBN ? c.page_size : kTcBN;
+  if (!encode_pool(&tmK, c, c.K_pages, box) || !encode_pool(&tmV, c, c.V_pages, box))
+    return EBD_ERR_CUDA;
+  constexpr int smem = PagedTcLayout<D>::kBytes;
+  if (cudaFuncSetAttribute(paged_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           smem) != cudaSuccess)
+    return EBD_ERR_CUDA;
+  paged_attn_tc_kernel<D><<<n_cta, kTcAttnThreads, smem, s>>>(tmK, tmV, a);
+  return launch_status();
+}
+
+ebd_status launch_paged_tc(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
+                           cudaStream_t s) {
+  const ebd_status st =
+      c.head_dim == 128 ? launch_tc_t<128>(a, c, n_cta, s) : launch_tc_t<64>(a, c, n_cta, s);
+  if (st != EBD_OK) return st;
+  return launch_paged_merge(a, true, c.head_dim, kTcAttnRows, n_cta, s);
+}
+
+}  // namespace ebd

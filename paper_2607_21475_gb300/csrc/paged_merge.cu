@@ -1,0 +1,128 @@
+// Joins the pieces of attention items that several CTAs worked on:
+//   y = sum_p 2^(s_p - M) o_p / sum_p 2^(s_p - M),  lse = (M + log2 sum_p 2^(s_p - M)) ln 2,
+// over the pieces p in CTA order, with o_p each piece's own weighted mean and
+// s_p its log2-sum (M the largest).  A warp joins one row; the partial results
+// were written just before and come from L2.  Launched as a programmatic
+// dependent of the attention kernel.
+#include <cuda_runtime.h>
+#include <math.h>
+
+#include "decode_tile.cuh"
+#include "paged_attn.cuh"
+
+namespace ebd {
+
+constexpr int kMergeWarps = 8;
+
+__device__ __forceinline__ void store_row(float* p, int lane, float4 v) {
+  reinterpret_cast<float4*>(p)[lane] = v;
+}
+__device__ __forceinline__ void store_row(float* p, int lane, float2 v) {
+  reinterpret_cast<float2*>(p)[lane] = v;
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, int lane, float4 v) {
+  reinterpret_cast<uint2*>(p)[lane] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
+}
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, int lane, float2 v) {
+  reinterpret_cast<uint32_t*>(p)[lane] = pack_bf16(v.x, v.y);
+}
+__device__ __forceinline__ void add_scaled(float4& o, float f, const float4& v) {
+  o.x = fmaf(f, v.x, o.x);
+  o.y = fmaf(f, v.y, o.y);
+  o.z = fmaf(f, v.z, o.z);
+  o.w = fmaf(f, v.w, o.w);
+}
+__device__ __forceinline__ void add_scaled(float2& o, float f, const float2& v) {
+  o.x = fmaf(f, v.x, o.x);
+  o.y = fmaf(f, v.y, o.y);
+}
+__device__ __forceinline__ float4 scaled(const float4& v, float f) {
+  return make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+}
+__device__ __forceinline__ float2 scaled(const float2& v, float f) {
+  return make_float2(v.x * f, v.y * f);
+}
+
+// VT: the float vector that a lane of a warp owns of a row (D / 32 floats).
+template <typename T, typename VT>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    paged_merge_kernel(const PagedAttnArgs a, int bm, int n_cta) {
+  grid_dependency_wait();
+  const int c0 = blockIdx.x, lane = threadIdx.x & 31;
+  const PieceRecord r = a.rec[c0];
+  if (r.b < 0) return;
+  const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
+  const int rows = min(bm, sp.n * a.group - r.m * bm);
+  // the item goes on through the first pieces of the following CTAs
+  int c1 = c0 + 1;
+  while (c1 + 1 < n_cta && a.rec[c1].cont == 1) ++c1;
+  constexpr int D = 32 * (int)(sizeof(VT) / 4);
+  const int hq = a.pv.n_kv_heads * a.group;
+  for (int row = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); row < rows;
+       row += gridDim.y * kMergeWarps) {
+    float M = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32)
+      M = fmaxf(M, a.part_lse[(size_t)(2 * c + (c == c0)) * bm + row]);
+    M = warp_max(M);
+    const float base = M == -INFINITY ? 0.f : M;
+    float sum = 0.f;
+    VT o = {};
+#pragma unroll 4
+    for (int c = c0; c <= c1; ++c) {
+      const size_t slot = (size_t)(2 * c + (c == c0)) * bm + row;
+      const VT v = reinterpret_cast<const VT*>(a.part_o + slot * D)[lane];
+      const float f = exp2f(a.part_lse[slot] - base);
+      sum += f;
+      add_scaled(o, f, v);
+    }
+    const int t = (r.m * bm + row) / a.group, g = (r.m * bm + row) - t * a.group;
+    const long long out = (long long)(sp.t0 + t) * hq + r.h * a.group + g;
+    store_row((T*)a.y + out * D, lane, scaled(o, sum == 0.f ? 0.f : 1.f / sum));
+    if (a.lse && lane == 0)
+      a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  }
+}
+
+size_t paged_split_bytes(int n_cta, int rows_per_item, int head_dim) {
+  const size_t rows = (size_t)2 * n_cta * rows_per_item;
+  return align_up(n_cta * sizeof(PieceRecord), 256) + align_up(rows * 4, 256) +
+         rows * head_dim * 4;
+}
+
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int rows_per_item) {
+  char* p = (char*)ws;
+  a.rec = (PieceRecord*)p;
+  p += align_up(n_cta * sizeof(PieceRecord), 256);
+  a.part_lse = (float*)p;
+  p += align_up((size_t)2 * n_cta * rows_per_item * 4, 256);
+  a.part_o = (float*)p;
+}
+
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int rows_per_item,
+                              int n_cta, cudaStream_t s) {
+  if (n_cta <= 1) return EBD_OK;
+  cudaLaunchConfig_t cfg = {};
+  int by = (rows_per_item + kMergeWarps - 1) / kMergeWarps;
+  cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
+  cfg.blockDim = dim3(kMergeWarps * 32);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  cudaError_t e;
+  if (bf16)
+    e = head_dim == 128
+            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float4>, a, rows_per_item,
+                                 n_cta)
+            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float2>, a, rows_per_item,
+                                 n_cta);
+  else
+    e = head_dim == 128
+            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float4>, a, rows_per_item, n_cta)
+            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float2>, a, rows_per_item, n_cta);
+  return cuda_status(e);
+}
+
+}  // namespace ebd
