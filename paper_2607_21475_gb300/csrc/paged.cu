@@ -2,9 +2,9 @@
 // that the paged entry points share.
 //
 // The gather reads and writes every kept row once (4 d * elem bytes per row of
-// K and V together), so HBM bounds it.  A thread moves 16-byte chunks, four in
-// flight: the chain index -> page number -> row is three dependent loads, and
-// neighbouring lanes share the first two.
+// K and V together), so HBM bounds it, if enough rows are in flight: the chain
+// index -> page number -> row is three dependent loads, which a warp goes
+// through for 8 rows at once.
 #include <cuda_runtime.h>
 
 #include "common.cuh"
@@ -14,7 +14,8 @@
 namespace ebd {
 
 constexpr int kPagedGatherThreads = 256;
-constexpr int kPagedGatherUnroll = 4;
+constexpr int kGatherFlight = 4;
+constexpr int kGatherRows = 8;
 
 ebd_status check_paged(const ebd_paged_cache* c) {
   if (!c || !c->K_pages || !c->V_pages || !c->block_table || !c->seq_len) return EBD_ERR_INVALID;
@@ -38,53 +39,54 @@ bool paged_aligned16(const ebd_paged_cache* c) {
          c->head_stride % wide == 0 && c->row_stride % wide == 0 && c->head_dim % wide == 0;
 }
 
-// cpr: 16-byte chunks per row; the view's strides are in chunks too.
+// One warp takes 8 kept rows of a unit: lane i < 8 finds row i's place (index,
+// page), then the warp copies the rows' chunks, `cpr` of 16 bytes each, with
+// kGatherFlight chunks of K and of V in flight per lane.  The view's strides are
+// in chunks.
 __global__ void __launch_bounds__(kPagedGatherThreads)
     paged_gather_kernel(const uint4* __restrict__ K, const uint4* __restrict__ V, PagedView v,
                         const int32_t* __restrict__ idx_c, const int32_t* __restrict__ n_kept,
                         int cap, int cpr, uint4* __restrict__ Kc, uint4* __restrict__ Vc,
                         int32_t* dev_status) {
   const int unit = blockIdx.y, b = unit / v.n_kv_heads, h = unit - b * v.n_kv_heads;
-  const int len = v.seq_len[b];
-  const long long items = (long long)min(max(n_kept[unit], 0), cap) * cpr;
-  const long long stride = (long long)gridDim.x * kPagedGatherThreads;
-  const int32_t* idx = idx_c + (size_t)unit * cap;
-  const size_t dst_base = (size_t)unit * cap * cpr;
-  bool bad = false;
-  for (long long it0 = (long long)blockIdx.x * kPagedGatherThreads + threadIdx.x; it0 < items;
-       it0 += stride * kPagedGatherUnroll) {
-    uint4 kv[kPagedGatherUnroll], vv[kPagedGatherUnroll];
-    long long src[kPagedGatherUnroll];
+  const int lane = threadIdx.x & 31;
+  const int p0 = (blockIdx.x * (kPagedGatherThreads / 32) + (threadIdx.x >> 5)) * kGatherRows;
+  if (p0 >= cap) return;
+  // the three loads do not wait for one another; a row past n_kept is dropped below
+  const int kept = n_kept[unit], len = v.seq_len[b];
+  const int r = lane < kGatherRows && p0 + lane < cap ? idx_c[(size_t)unit * cap + p0 + lane] : -1;
+  const int n = min(min(max(kept, 0), cap) - p0, kGatherRows);
+  if (n <= 0) return;
+  long long src = -1;
+  if (lane < n && (unsigned)r < (unsigned)max(len, 0)) {
+    const int page = page_of(v, b, r);
+    if (page >= 0) src = slot_offset(v, page, h, r);
+    else raise_status(dev_status, EBD_DEV_RANGE);
+  }
+  __syncwarp();
+  const size_t dst = ((size_t)unit * cap + p0) * cpr;
+  const int total = n * cpr;
+  for (int i0 = lane; i0 < total + lane; i0 += 32 * kGatherFlight) {
+    uint4 kv[kGatherFlight], vv[kGatherFlight];
+    bool ok[kGatherFlight];
 #pragma unroll
-    for (int u = 0; u < kPagedGatherUnroll; ++u) {
-      const long long it = it0 + u * stride;
-      src[u] = -1;
-      if (it < items) {
-        const int p = (int)(it / cpr);
-        const int r = idx[p];
-        if ((unsigned)r < (unsigned)max(len, 0)) {
-          const int page = page_of(v, b, r);
-          if (page >= 0) src[u] = slot_offset(v, page, h, r) + (it - (long long)p * cpr);
-          else bad = true;
-        }
+    for (int f = 0; f < kGatherFlight; ++f) {
+      const int i = i0 + 32 * f, row = i / cpr;
+      const long long at = __shfl_sync(0xffffffffu, src, row & (kGatherRows - 1));
+      ok[f] = i < total && at >= 0;
+      if (ok[f]) {
+        kv[f] = __ldg(K + at + (i - row * cpr));
+        vv[f] = __ldg(V + at + (i - row * cpr));
       }
     }
 #pragma unroll
-    for (int u = 0; u < kPagedGatherUnroll; ++u) {
-      if (src[u] >= 0) {
-        kv[u] = __ldg(K + src[u]);
-        vv[u] = __ldg(V + src[u]);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kPagedGatherUnroll; ++u) {
-      if (src[u] >= 0) {
-        Kc[dst_base + it0 + u * stride] = kv[u];
-        Vc[dst_base + it0 + u * stride] = vv[u];
+    for (int f = 0; f < kGatherFlight; ++f) {
+      if (ok[f]) {
+        Kc[dst + i0 + 32 * f] = kv[f];
+        Vc[dst + i0 + 32 * f] = vv[f];
       }
     }
   }
-  if (bad) raise_status(dev_status, EBD_DEV_RANGE);
 }
 
 }  // namespace ebd
@@ -107,10 +109,8 @@ extern "C" ebd_status ebd_paged_gather(const ebd_paged_cache* cache, const int32
   v.page_stride /= wide;
   v.head_stride /= wide;
   v.row_stride /= wide;
-  const long long per_block = (long long)kPagedGatherThreads * kPagedGatherUnroll;
-  long long bx = ((long long)capacity * cpr + per_block - 1) / per_block;
-  const long long most = ((long long)sm_count() * 8 + units - 1) / units;
-  if (bx > most) bx = most;
+  const int per_block = kPagedGatherThreads / 32 * kGatherRows;
+  const int bx = (capacity + per_block - 1) / per_block;
   paged_gather_kernel<<<dim3((unsigned)bx, (unsigned)units), kPagedGatherThreads, 0,
                         (cudaStream_t)stream>>>((const uint4*)cache->K_pages,
                                                 (const uint4*)cache->V_pages, v, idx_c, n_kept,

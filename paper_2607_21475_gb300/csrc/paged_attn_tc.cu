@@ -42,7 +42,7 @@ namespace ebd {
 
 constexpr int kTcBM = kTcAttnRows;
 constexpr int kTcBN = 128;
-constexpr int kTcAttnThreads = 384;
+constexpr int kTcAttnThreads = 640;  // 16 softmax warps, MMA, TMA, 2 for queries
 
 template <int D>
 struct PagedTcLayout {
@@ -52,8 +52,9 @@ struct PagedTcLayout {
   static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kQ = 0;  // two tiles
   static constexpr int kKV = 2 * kTile;
-  static constexpr int kBar = kKV + kStages * kTile;
-  static constexpr int kBytes = kBar + 512 + 1024;  // + alignment slack
+  static constexpr int kMax = kKV + kStages * kTile;  // [X][half][row] f32
+  static constexpr int kBar = kMax + 2 * 2 * 128 * 4;
+  static constexpr int kBytes = kBar + 512;
 };
 
 struct TcBars {
@@ -61,23 +62,55 @@ struct TcBars {
   uint64_t s_full[2], p_full[2], o_full[2];
   uint64_t fixed, done;
   uint64_t kv_full[10], kv_empty[10];
+  uint64_t pair[8];  // the two warps that share 32 rows of one X
+  WorkStart start;
+  uint32_t tmem;
 };
+static_assert(sizeof(TcBars) <= 512, "barriers");
 
-// Recomputes 16-channel groups of one row's output whose products came out
-// NaN: a weight of 0 times a hidden value that is NaN or infinite, or a value
-// that the row does see.  Reads only positions [k_lo, k_hi), which it sees, with
-// the row's reference and sum of the fast path; writes mean of the weighted
-// values (bf16 to y, or float32 to a partial result).
+// max(a, b, c) in one instruction.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// Mends one row's output where a value that the row does not see made it NaN:
+// such a value has weight 0 in the tile's product, and 0 times NaN or infinity
+// is NaN.  For each 16-channel group with a NaN: the channels in which a hidden
+// value of the piece's tiles (at most a few hundred positions at either end) is
+// not finite are recomputed from the positions that the row sees; a NaN in any
+// other channel is the row's own.  The sum stops once every such channel has met
+// a NaN of its own.
 template <int D>
-__device__ __noinline__ void redo_groups(const PagedAttnArgs& a, int b, int h, int token, int g,
-                                         int k_lo, int k_hi, float base, float inv,
-                                         uint32_t groups, __nv_bfloat16* y, float* part) {
+__device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int h, int token, int g,
+                                      int tile_lo, int lo, int hi, int tile_hi, float base,
+                                      float inv, uint32_t groups, __nv_bfloat16* y, float* part) {
   const uint4* q = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + token * a.q_ts +
                                                   (h * a.group + g) * a.q_hs);
+  const int k_lo = max(lo, tile_lo), k_hi = min(hi, tile_hi);  // seen
   for (int c = 0; c < D; c += 16) {
     if (!(groups >> (c / 16) & 1)) continue;
+    uint32_t mend = 0;
+    for (int pos = tile_lo; pos < tile_hi; ++pos) {
+      if (pos == k_lo && k_lo < k_hi) pos = k_hi;
+      const int page = pos < tile_hi ? page_of(a.pv, b, pos) : -1;
+      if (page < 0) continue;
+      const __nv_bfloat16* v =
+          (const __nv_bfloat16*)a.V_pages + slot_offset(a.pv, page, h, pos) + c;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(fabsf(to_f32(v[i])) < INFINITY)) mend |= 1u << i;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float o = y ? to_f32(y[c + i]) : part[c + i];
+      if (o == o) mend &= ~(1u << i);
+    }
+    if (!mend) continue;
     float acc[16] = {};
-    for (int pos = k_lo; pos < k_hi; ++pos) {
+    uint32_t open = mend;  // channels without a NaN of their own so far
+    for (int pos = k_hi - 1; open && pos >= k_lo; --pos) {
       const int page = page_of(a.pv, b, pos);
       if (page < 0) continue;
       const long long off = slot_offset(a.pv, page, h, pos);
@@ -93,10 +126,14 @@ __device__ __noinline__ void redo_groups(const PagedAttnArgs& a, int b, int h, i
       const float p = exp2f(fmaf(s, a.scale2, -base));
       const __nv_bfloat16* v = (const __nv_bfloat16*)a.V_pages + off + c;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
+      for (int i = 0; i < 16; ++i) {
+        acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
+        if (acc[i] != acc[i]) open &= ~(1u << i);
+      }
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
+      if (!(mend >> i & 1)) continue;
       if (y) y[c + i] = __float2bfloat16_rn(acc[i] * inv);
       else part[c + i] = acc[i] * inv;
     }
@@ -109,26 +146,24 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
                          const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs a) {
   using L = PagedTcLayout<D>;
   constexpr int KS = L::kStages;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char* smem = (unsigned char*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  extern __shared__ __align__(1024) unsigned char smem[];
   TcBars* bar = reinterpret_cast<TcBars*>(smem + L::kBar);
-  __shared__ WorkStart start_s;
-  __shared__ uint32_t tmem_s;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int cta = blockIdx.x;
-  if (warp == 8) {
-    tmem_alloc(&tmem_s, 512);
+  if (warp == 16) {
+    tmem_alloc(&bar->tmem, 512);
     tmem_relinquish();
-  } else if (warp == 9) {
+  } else if (warp == 17) {
     if (lane == 0) {
       mbar_init(&bar->q_full, 64);
       mbar_init(&bar->q_empty, 1);
       for (int x = 0; x < 2; ++x) {
         mbar_init(&bar->s_full[x], 1);
-        mbar_init(&bar->p_full[x], 128);
+        mbar_init(&bar->p_full[x], 8);
         mbar_init(&bar->o_full[x], 1);
       }
+      for (int i = 0; i < 8; ++i) mbar_init(&bar->pair[i], 2);
       mbar_init(&bar->fixed, 64);
       mbar_init(&bar->done, 1);
       for (int s = 0; s < KS; ++s) {
@@ -139,25 +174,32 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     }
   } else if (warp == 0) {
     const WorkStart w = find_work<kTcBM, kTcBN>(a, cta, gridDim.x, lane);
-    if (lane == 0) start_s = w;
+    if (lane == 0) bar->start = w;
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_s;
-  const uint32_t tO[2] = {tmem, tmem + 128}, tS[2] = {tmem + 256, tmem + 384};
-  PieceWalk<kTcBM, kTcBN> w(a, start_s);
+  const uint32_t tmem = bar->tmem;
+  const WorkStart start = bar->start;
+  PieceWalk<kTcBM, kTcBN> w(a, start);
   bool ok = true;
 
-  // 384 x 168 registers at launch: 64512 = 256 x 208 + 128 x 88
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    // ---------------- softmax and epilogue: one row per thread
-    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
+  if (warp < 16) {
+    // ---------------- softmax and epilogue: half a row per thread
+    const int x = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
+    uint64_t* pair = &bar->pair[x * 4 + (warp & 3)];
+    uint32_t pairs = 0;
+    auto pair_sync = [&]() {  // bounded, unlike a named barrier
+      __syncwarp();
+      if (lane == 0) mbar_arrive(pair);
+      return mbar_wait_warp(pair, pairs++ & 1);
+    };
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t sS = tS[x] + lane_base, sO = tO[x] + lane_base;
+    const uint32_t sS = tmem + 256 + x * 128 + lane_base;
+    const uint32_t sO = tmem + x * 128 + lane_base + half * (D / 2);
+    float* mx = reinterpret_cast<float*>(smem + L::kMax) + x * 256 + row;
     uint32_t it = 0;  // tiles of X so far: barrier phases
-    if (threadIdx.x == 0) write_record<kTcBM, kTcBN>(a, start_s, cta);  // while the first tile loads
+    if (threadIdx.x == 0) write_record<kTcBM, kTcBN>(a, start, cta);  // while the first tile loads
     __syncwarp();
     for (; ok && w.live(); w.next(a)) {
       const int rows = w.rows(a);
@@ -168,29 +210,40 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
       float m = -INFINITY, l = 0.f;
       for (int j = w.cur; j < w.end; ++j, ++it) {
-        const int k0 = j * kTcBN;
+        const int k0 = j * kTcBN + half * 64;
         if (!mbar_wait_warp(&bar->s_full[x], it & 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
-        uint32_t s[2][64];
-        tmem_ld64(sS, s[0]);
-        tmem_ld64(sS + 64, s[1]);
+        uint32_t s[64];
+        tmem_ld64(sS + half * 64, s);
         tmem_ld_wait();
-        if (__any_sync(0xffffffffu, hi - k0 < kTcBN || lo > k0)) {
+        if (__any_sync(0xffffffffu, hi - k0 < 64 || lo > k0)) {
           const int chi = hi - k0, clo = lo - k0;
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (i >= chi || i < clo) s[i >> 6][i & 63] = __float_as_uint(-INFINITY);
+          for (int i = 0; i < 64; ++i)
+            if (i >= chi || i < clo) s[i] = __float_as_uint(-INFINITY);
         }
         float t4[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) t4[i] = __uint_as_float(s[0][i]);
+        for (int i = 0; i < 4; ++i) t4[i] = __uint_as_float(s[i]);
 #pragma unroll
-        for (int i = 4; i < 128; ++i)
-          t4[i & 3] = fmaxf(t4[i & 3], __uint_as_float(s[i >> 6][i & 63]));
-        const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+        for (int i = 4; i < 60; i += 8)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            t4[e] = max3(t4[e], __uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1]));
+        float top = fmaxf(max3(t4[0], t4[1], t4[2]),
+                          max3(t4[3], __uint_as_float(s[60]), __uint_as_float(s[61])));
+        top = max3(top, __uint_as_float(s[62]), __uint_as_float(s[63]));
+        mx[half * 128] = top;
+        tc_fence_before();  // P overwrites columns that the other warp has read
+        if (!pair_sync()) {
+          ok = false;
+          break;
+        }
+        tc_fence_after();
+        top = fmaxf(top, mx[(half ^ 1) * 128]);
         const bool grow = m > -INFINITY && (top - m) * a.scale2 > kRescaleLog2;
         if (__any_sync(0xffffffffu, grow)) {
           // O_X holds the tiles before this one: wait for their product
@@ -203,9 +256,9 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           const float f = m > -INFINITY ? exp2f((m - m1) * a.scale2) : 1.f;
           l *= f;
           m = m1;
-          // 16 columns at a time: the 128 logits stay in registers meanwhile
+          // 16 columns at a time: the logits stay in registers meanwhile
 #pragma unroll 1
-          for (int c = 0; c < D; c += 16) {
+          for (int c = 0; c < D / 2; c += 16) {
             uint32_t o[16];
             tmem_ld16(sO + c, o);
             tmem_ld_wait();
@@ -218,29 +271,38 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         }
         const float base = m == -INFINITY ? 0.f : m * a.scale2;
         const float2 sc2 = make_float2(a.scale2, a.scale2), nb = make_float2(-base, -base);
-        float2 sum = make_float2(0.f, 0.f);
+        float2 sum0 = make_float2(0.f, 0.f), sum1 = sum0;
+        uint32_t p[32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t p[32];
-#pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            float2 e = __ffma2_rn(make_float2(__uint_as_float(s[c][2 * i]),
-                                              __uint_as_float(s[c][2 * i + 1])),
-                                  sc2, nb);
-            e.x = exp2f(e.x);
-            e.y = exp2f(e.y);
-            sum = __fadd2_rn(sum, e);
-            p[i] = pack_bf16(e.x, e.y);
-          }
-          tmem_st32(sS + c * 32, p);
+        for (int i = 0; i < 32; i += 2) {
+          float2 e = __ffma2_rn(
+              make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc2, nb);
+          float2 f = __ffma2_rn(
+              make_float2(__uint_as_float(s[2 * i + 2]), __uint_as_float(s[2 * i + 3])), sc2, nb);
+          e.x = exp2f(e.x);
+          e.y = exp2f(e.y);
+          f.x = exp2f(f.x);
+          f.y = exp2f(f.y);
+          sum0 = __fadd2_rn(sum0, e);
+          sum1 = __fadd2_rn(sum1, f);
+          p[i] = pack_bf16(e.x, e.y);
+          p[i + 1] = pack_bf16(f.x, f.y);
         }
-        l += sum.x + sum.y;
+        tmem_st32(sS + half * 32, p);
+        l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&bar->p_full[x]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bar->p_full[x]);
       }
       if (!ok) break;
-      if (!mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
+      // the row's sum from its two halves
+      ok = pair_sync();  // the other warp has read the last maxima
+      mx[half * 128] = l;
+      ok = ok && pair_sync();
+      l = half ? mx[0] + l : l + mx[128];
+      ok = ok && pair_sync();  // both have read the sums: the next item's maxima may come
+      if (!ok || !mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
         ok = false;
         break;
       }
@@ -252,9 +314,10 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const long long out = (long long)(w.sp.t0 + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
       const size_t prow = (size_t)slot * kTcBM + x * 128 + row;
+      const int c0 = half * (D / 2);
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
-      for (int c = 0; c < D; c += 32) {
+      for (int c = 0; c < D / 2; c += 32) {
         uint32_t o[32];
         __syncwarp();
         tmem_ld32(sO + c, o);
@@ -265,17 +328,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           z0 = fmaf(__uint_as_float(o[i]), 0.f, z0);
           z1 = fmaf(__uint_as_float(o[16 + i]), 0.f, z1);
         }
-        nan_groups |= (z0 != z0 ? 1u : 0u) << (c / 16) | (z1 != z1 ? 2u : 0u) << (c / 16);
+        nan_groups |= ((z0 != z0 ? 1u : 0u) | (z1 != z1 ? 2u : 0u)) << ((c0 + c) / 16);
         if (!mine) {
         } else if (slot >= 0) {
-          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
+          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c0 + c);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             dst[i] = make_float4(
                 __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
                 __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
         } else {
-          uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.y + out * D + c);
+          uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.y + out * D + c0 + c);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t q[4];
@@ -288,117 +351,129 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         }
       }
       if (mine) {
-        if (slot >= 0) a.part_lse[prow] = lse2;
-        else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
+        if (half == 0) {
+          if (slot >= 0) a.part_lse[prow] = lse2;
+          else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
+        }
         if (nan_groups)
-          redo_groups<D>(a, w.b, w.h, w.sp.t0 + tok, g, max(lo, w.cur * kTcBN),
-                         min(hi, w.end * kTcBN), m == -INFINITY ? 0.f : m * a.scale2, inv,
-                         nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
+          mend_row<D>(a, w.b, w.h, w.sp.t0 + tok, g, w.cur * kTcBN, lo, hi,
+                      min(w.end * kTcBN, w.sp.len), m == -INFINITY ? 0.f : m * a.scale2, inv,
+                      nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
                          slot < 0 ? nullptr : a.part_o + prow * D);
       }
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
-  } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-  }
-  if (warp == 8) {
-    // ---------------- MMA issue
-    if (lane == 0) {
-      const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
-      const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
-      const uint32_t qb = smem_u32(smem + L::kQ), kvb = smem_u32(smem + L::kKV);
-      uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
-      uint32_t it[2] = {0, 0}, items = 0, fixes = 0;
-      auto s_mma = [&](int x, uint32_t kslot) {
+  } else if (warp == 16) {
+    // ---------------- MMA issue: the warp stays converged, one lane issues
+    const uint32_t leader = lane == 0;
+    const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
+    const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
+    // descriptors once; a step along them is an addition to the start address
+    const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ));
+    const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kKV));
+    const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kKV), L::kBox);
+    uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
+    uint32_t it0 = 0, it1 = 0, items = 0, fixes = 0;
+    auto s_mma = [&](int x, uint32_t kslot) {
+      const uint64_t ad = qd + (uint32_t)(x * (L::kTile >> 4));
+      const uint64_t bd = kd + kslot * (L::kTile >> 4);
+      const uint32_t d = tmem + 256 + x * 128;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (uint32_t)((kk >> 2) * L::kBox + (kk & 3) * 32);
-          umma_bf16(tS[x], umma_desc_k_sw128(qb + x * L::kTile + off),
-                    umma_desc_k_sw128(kvb + kslot * L::kTile + off), idesc_s, kk > 0);
-        }
-        umma_commit(&bar->s_full[x]);
-      };
-      auto o_mma = [&](int x, uint32_t vslot, bool acc) {
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t off = (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4);
+        umma_bf16_if(leader, d, ad + off, bd + off, idesc_s, kk > 0);
+      }
+      umma_commit_if(leader, &bar->s_full[x]);
+    };
+    auto o_mma = [&](int x, uint32_t vslot, bool acc) {
+      const uint64_t bd = vd + vslot * (L::kTile >> 4);
+      const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128;
 #pragma unroll
-        for (int kk = 0; kk < kTcBN / 16; ++kk)
-          umma_bf16_ta(tO[x], tS[x] + kk * 8,
-                       umma_desc_mn_sw128(kvb + vslot * L::kTile + kk * 2048, L::kBox), idesc_o,
-                       acc || kk > 0);
-        umma_commit(&bar->o_full[x]);
-      };
-      auto step = [&]() {
-        if (++slot == KS) {
-          slot = 0;
-          ph ^= 1;
-        }
-      };
-      for (; ok && w.live(); w.next(a), ++items) {
-        const int nx = w.rows(a) > 128 ? 2 : 1;
-        const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
-        ok = mbar_wait_bounded(&bar->q_full, items & 1) &&
-             mbar_wait_bounded(&bar->kv_full[slot], ph);
+      for (int kk = 0; kk < kTcBN / 16; ++kk)
+        umma_bf16_ta_if(leader, d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o,
+                        acc || kk > 0);
+      umma_commit_if(leader, &bar->o_full[x]);
+    };
+    auto step = [&]() {
+      if (++slot == KS) {
+        slot = 0;
+        ph ^= 1;
+      }
+    };
+    for (; ok && w.live(); w.next(a), ++items) {
+      const int nx = w.rows(a) > 128 ? 2 : 1;
+      const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
+      ok = mbar_wait_warp(&bar->q_full, items & 1) && mbar_wait_warp(&bar->kv_full[slot], ph);
+      // S_X overwrites the last item's P_X: its product has to be done
+      if (ok && it0 > 0) ok = mbar_wait_warp(&bar->o_full[0], (it0 - 1) & 1);
+      if (ok && nx == 2 && it1 > 0) ok = mbar_wait_warp(&bar->o_full[1], (it1 - 1) & 1);
+      if (!ok) break;
+      tc_fence_after();
+      s_mma(0, slot);
+      if (nx == 2) s_mma(1, slot);
+      umma_commit_if(leader, &bar->kv_empty[slot]);
+      if (w.end - w.cur == 1) umma_commit_if(leader, &bar->q_empty);
+      step();
+      for (int j = w.cur; j < w.end; ++j) {
+        const uint32_t vslot = slot;
+        ok = mbar_wait_warp(&bar->kv_full[slot], ph);
+        if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_warp(&bar->fixed, fixes++ & 1);
         if (!ok) break;
-        tc_fence_after();
-        for (int x = 0; ok && x < nx; ++x) {
-          // S_X overwrites the last item's P_X: its product has to be done
-          if (it[x] > 0) ok = mbar_wait_bounded(&bar->o_full[x], (it[x] - 1) & 1);
-          if (ok) s_mma(x, slot);
-        }
-        if (!ok) break;
-        umma_commit(&bar->kv_empty[slot]);
-        if (w.end - w.cur == 1) umma_commit(&bar->q_empty);
         step();
-        for (int j = w.cur; ok && j < w.end; ++j) {
-          const uint32_t vslot = slot;
-          ok = mbar_wait_bounded(&bar->kv_full[slot], ph);
-          if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
+        const bool more = j + 1 < w.end;
+        const uint32_t kslot = slot;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (x == 1 && nx == 1) break;
+          const uint32_t it = x == 0 ? it0 : it1;
+          ok = mbar_wait_warp(&bar->p_full[x], it & 1);
           if (!ok) break;
-          step();
-          const bool more = j + 1 < w.end;
-          const uint32_t kslot = slot;
-          for (int x = 0; ok && x < nx; ++x) {
-            ok = mbar_wait_bounded(&bar->p_full[x], it[x] & 1);
+          tc_fence_after();
+          o_mma(x, vslot, j > w.cur);
+          if (x + 1 == nx) umma_commit_if(leader, &bar->kv_empty[vslot]);
+          if (more) {
+            if (x == 0) ok = mbar_wait_warp(&bar->kv_full[kslot], ph);
+            // S_X overwrites P_X: its product has to be done
+            ok = ok && mbar_wait_warp(&bar->o_full[x], it & 1);
             if (!ok) break;
             tc_fence_after();
-            o_mma(x, vslot, j > w.cur);
-            if (x + 1 == nx) umma_commit(&bar->kv_empty[vslot]);
-            if (more) {
-              if (x == 0) ok = mbar_wait_bounded(&bar->kv_full[kslot], ph);
-              // S_X overwrites P_X: its product has to be done
-              ok = ok && mbar_wait_bounded(&bar->o_full[x], it[x] & 1);
-              if (!ok) break;
-              tc_fence_after();
-              s_mma(x, kslot);
-              if (x + 1 == nx) umma_commit(&bar->kv_empty[kslot]);
-              if (x + 1 == nx && j + 2 == w.end) umma_commit(&bar->q_empty);
+            s_mma(x, kslot);
+            if (x + 1 == nx) {
+              umma_commit_if(leader, &bar->kv_empty[kslot]);
+              if (j + 2 == w.end) umma_commit_if(leader, &bar->q_empty);
             }
-            ++it[x];
           }
-          if (ok && more) step();
+          if (x == 0) ++it0;
+          else ++it1;
         }
+        if (!ok) break;
+        if (more) step();
       }
-      umma_commit(&bar->done);
-      mbar_wait_bounded(&bar->done, 0);
     }
     __syncwarp();
-  } else if (warp == 9) {
+    umma_commit_if(leader, &bar->done);
+    mbar_wait_warp(&bar->done, 0);
+  } else if (warp == 17) {
     // ---------------- K and V copies
     uint32_t slot = 0, ph = 0, issued = 0;
     const int page = 1 << a.pv.page_shift;
     const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
     bool bad = false;
     for (; ok && w.live(); w.next(a)) {
+      // lane i: one box of a tile (keys bx * box .., channels half * 64 ..); its
+      // page is looked up a tile ahead, past the pool where there is none
+      const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
+      auto page_at = [&](int pos) {
+        if (bx >= boxes || pos >= w.sp.len) return a.pv.n_pages;
+        const int p = page_of(a.pv, w.b, pos);
+        if (p < 0) bad = true;
+        return p < 0 ? a.pv.n_pages : p;
+      };
+      int next_pg = page_at(w.cur * kTcBN + bx * box);
       for (int j = w.cur; ok && j < w.end; ++j) {
-        // lane i: one box of the tile (keys bx * box .., channels half * 64 ..)
-        const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
-        const int pos = j * kTcBN + bx * box;
-        int pg = a.pv.n_pages;  // past the pool where there is none
-        if (bx < boxes && pos < w.sp.len) {
-          const int p = page_of(a.pv, w.b, pos);
-          if (p >= 0) pg = p;
-          else bad = true;
-        }
+        const int pos = j * kTcBN + bx * box, pg = next_pg;
+        if (j + 1 < w.end) next_pg = page_at(pos + kTcBN);
         for (int kv = 0; ok && kv < 2; ++kv) {
           if (issued >= KS && !mbar_wait_warp(&bar->kv_empty[slot], ph ^ 1)) {
             ok = false;
@@ -423,9 +498,9 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     // every copy has landed before the block may end
     for (uint32_t i = issued > KS ? issued - KS : 0; i < issued; ++i)
       mbar_wait_bounded(&bar->kv_full[i % KS], (i / KS) & 1);
-  } else if (warp > 9) {
+  } else {
     // ---------------- query rows; value rows past the end
-    const int tid = threadIdx.x - 320;
+    const int tid = threadIdx.x - 576;
     constexpr int CH = D / 8;  // 16-byte chunks per row
     uint32_t items = 0, tile0 = 0;  // tiles before this piece: ring position 2 tile
     for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
@@ -476,7 +551,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   if (!ok) raise_status(a.dev_status, EBD_DEV_TIMEOUT);
   tc_fence_before();
   __syncthreads();
-  if (warp == 8) {
+  if (warp == 16) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }

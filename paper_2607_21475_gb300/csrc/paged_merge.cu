@@ -102,7 +102,8 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
                               int n_cta, cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
   cudaLaunchConfig_t cfg = {};
-  int by = (rows_per_item + kMergeWarps - 1) / kMergeWarps;
+  const long long most = min((long long)a.max_new * a.group, (long long)rows_per_item);
+  const int by = (int)((most + kMergeWarps - 1) / kMergeWarps);
   cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
   cfg.blockDim = dim3(kMergeWarps * 32);
   cfg.stream = s;

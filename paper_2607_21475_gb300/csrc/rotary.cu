@@ -72,6 +72,7 @@ struct RotaryArgs {
   int rot;
   int parts;                 // warps per token
   float sin_sign;            // -1: inverse
+  bool wide_table;           // two pairs of the table per 16-byte access
   int32_t* dev_status;
 };
 
@@ -97,12 +98,14 @@ __device__ __forceinline__ void unit_channels(const RotaryArgs& a, int u, int& c
   }
 }
 
-template <typename T, int VEC, bool PAIRS, bool APPEND>
-__global__ void __launch_bounds__(kRotWarps * 32) rotary_kernel(const RotaryArgs a) {
-  constexpr int kRows = 4;  // rows in flight per lane
+// STEADY: 32 * parts is a multiple of the units, so that a lane keeps its unit
+// (and its angles) from head to head.
+template <typename T, int VEC, bool PAIRS, bool APPEND, bool STEADY>
+__global__ void __launch_bounds__(kRotWarps * 32, 4) rotary_kernel(const RotaryArgs a) {
+  constexpr int kRows = 2;  // rows in flight per lane
   const int lane = threadIdx.x & 31;
   const long long w = (long long)blockIdx.x * kRotWarps + (threadIdx.x >> 5);
-  const int t = (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
+  const int t = a.parts == 1 ? (int)w : (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
   if (t >= a.n_tokens) return;
 
   int pos, b = 0, page = -1;
@@ -126,11 +129,22 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotary_kernel(const RotaryArgs
   auto load_angles = [&](int u) {
     if (u >= a.rot_units) return;
     const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * kFreq;
+    if (kFreq % 2 == 0 && a.wide_table) {
 #pragma unroll
-    for (int i = 0; i < kFreq; ++i) {
-      const float2 f = __ldg(row + i);
-      cs[i] = f.x;
-      sn[i] = f.y * a.sin_sign;
+      for (int i = 0; i + 1 < kFreq; i += 2) {
+        const float4 f = __ldg(reinterpret_cast<const float4*>(row + i));
+        cs[i] = f.x;
+        sn[i] = f.y * a.sin_sign;
+        cs[i + 1] = f.z;
+        sn[i + 1] = f.w * a.sin_sign;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kFreq; ++i) {
+        const float2 f = __ldg(row + i);
+        cs[i] = f.x;
+        sn[i] = f.y * a.sin_sign;
+      }
     }
   };
   auto turn = [&](Piece<T, VEC, PAIRS>& r) {
@@ -152,21 +166,22 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotary_kernel(const RotaryArgs
   };
 
   const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
-  const int total = heads * a.units, stride = 32 * a.parts;
-  const bool fixed = stride % a.units == 0;  // the lane keeps its unit from head to head
-  int i0 = part * 32 + lane;
-  if (fixed && i0 < total) load_angles(i0 % a.units);
-  for (; i0 < total; i0 += kRows * stride) {
+  const int stride = 32 * a.parts, step = stride / a.units, rest = stride - step * a.units;
+  int h = (part * 32 + lane) / a.units, u = part * 32 + lane - h * a.units;
+  int c1, c2;
+  unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
+  if (STEADY && h < heads && (a.table || !APPEND)) load_angles(u);
+  while (h < heads) {
     Piece<T, VEC, PAIRS> r[kRows];
     T* dst[kRows];
+    int us[kRows], hs[kRows];
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      const int i = i0 + k * stride;
       dst[k] = nullptr;
-      if (i < total) {
-        const int h = i / a.units, u = i - h * a.units;
-        int c1, c2;
-        unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
+      us[k] = u;
+      hs[k] = h;
+      if (h < heads) {
+        if (!STEADY) unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
         const T* src;
         if (!APPEND || h < a.n_x) {
           src = (const T*)a.x.p + t * a.x.ts + h * a.x.hs;
@@ -174,26 +189,29 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotary_kernel(const RotaryArgs
         } else {
           const bool is_v = h >= a.n_x + a.n_kv;
           const int kh = h - a.n_x - (is_v ? a.n_kv : 0);
-          const Rows& s = is_v ? a.v : a.k;
-          src = (const T*)s.p + t * s.ts + kh * s.hs;
+          src = is_v ? (const T*)a.v.p + t * a.v.ts + kh * a.v.hs
+                     : (const T*)a.k.p + t * a.k.ts + kh * a.k.hs;
           if (page >= 0)
             dst[k] = (T*)(is_v ? a.V_pages : a.K_pages) + slot_offset(a.pv, page, kh, pos);
         }
-        if (dst[k]) {
-          r[k].a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
-          if (c2 >= 0) r[k].b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
+        r[k].a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
+        if (c2 >= 0) r[k].b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
+      }
+      h += step;
+      if (!STEADY) {
+        u += rest;
+        if (u >= a.units) {
+          u -= a.units;
+          ++h;
         }
       }
     }
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
       if (!dst[k]) continue;
-      const int i = i0 + k * stride;
-      const int h = i / a.units, u = i - h * a.units;
-      int c1, c2;
-      unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
-      if (u < a.rot_units && !(APPEND && h >= a.n_x + a.n_kv)) {
-        if (!fixed) load_angles(u);
+      if (!STEADY) unit_channels<T, VEC, PAIRS>(a, us[k], c1, c2);
+      if (us[k] < a.rot_units && !(APPEND && hs[k] >= a.n_x + a.n_kv)) {
+        if (!STEADY) load_angles(us[k]);
         turn(r[k]);
       }
       *reinterpret_cast<Chunk<T, VEC>*>(dst[k] + c1) = r[k].a;
@@ -214,14 +232,20 @@ static ebd_status launch_rotary_v(RotaryArgs a, int head_dim, cudaStream_t s) {
   a.half_off = rot / 2;
   a.rot_units = PAIRS ? rot / VEC : rot / 2 / VEC;
   a.units = a.rot_units + (head_dim - rot) / VEC;
+  a.wide_table = rot % 4 == 0 && (uintptr_t)a.table % 16 == 0;
   const int chunks = (a.n_x + (APPEND ? 2 * a.n_kv : 0)) * a.units;
   // one chunk pair per lane while the call has fewer warps than the GPU holds
-  // (latency), four rows per lane beyond that
-  const int few = (chunks + 127) / 128, many = (chunks + 31) / 32;
+  // (latency), up to eight rows per lane beyond that
+  const int few = (chunks + 255) / 256, many = (chunks + 31) / 32;
   a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
   const long long blocks = ((long long)a.n_tokens * a.parts + kRotWarps - 1) / kRotWarps;
   if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
-  rotary_kernel<T, VEC, PAIRS, APPEND><<<(unsigned)blocks, kRotWarps * 32, 0, s>>>(a);
+  if (32 * a.parts % a.units == 0)
+    rotary_kernel<T, VEC, PAIRS, APPEND, true>
+        <<<(unsigned)blocks, kRotWarps * 32, 0, s>>>(a);
+  else
+    rotary_kernel<T, VEC, PAIRS, APPEND, false>
+        <<<(unsigned)blocks, kRotWarps * 32, 0, s>>>(a);
   return launch_status();
 }
 
