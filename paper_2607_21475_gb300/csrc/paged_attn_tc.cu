@@ -365,95 +365,91 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
   } else if (warp == 16) {
-    // ---------------- MMA issue: the warp stays converged, one lane issues
-    const uint32_t leader = lane == 0;
-    const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
-    const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
-    // descriptors once; a step along them is an addition to the start address
-    const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ));
-    const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kKV));
-    const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kKV), L::kBox);
-    uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
-    uint32_t it0 = 0, it1 = 0, items = 0, fixes = 0;
-    auto s_mma = [&](int x, uint32_t kslot) {
-      const uint64_t ad = qd + (uint32_t)(x * (L::kTile >> 4));
-      const uint64_t bd = kd + kslot * (L::kTile >> 4);
-      const uint32_t d = tmem + 256 + x * 128;
+    // ---------------- MMA issue
+    if (elect_one()) {
+      const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
+      const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
+      // descriptors once; a step along them is an addition to the start address
+      const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ));
+      const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kKV));
+      const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kKV), L::kBox);
+      uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
+      uint32_t it0 = 0, it1 = 0, items = 0, fixes = 0;
+      auto s_mma = [&](int x, uint32_t kslot) {
+        const uint64_t ad = qd + (uint32_t)(x * (L::kTile >> 4));
+        const uint64_t bd = kd + kslot * (L::kTile >> 4);
+        const uint32_t d = tmem + 256 + x * 128;
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        const uint32_t off = (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4);
-        umma_bf16_if(leader, d, ad + off, bd + off, idesc_s, kk > 0);
-      }
-      umma_commit_if(leader, &bar->s_full[x]);
-    };
-    auto o_mma = [&](int x, uint32_t vslot, bool acc) {
-      const uint64_t bd = vd + vslot * (L::kTile >> 4);
-      const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128;
+        for (int kk = 0; kk < D / 16; ++kk) {
+          const uint32_t off = (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4);
+          umma_bf16(d, ad + off, bd + off, idesc_s, kk > 0);
+        }
+        umma_commit(&bar->s_full[x]);
+      };
+      auto o_mma = [&](int x, uint32_t vslot, bool acc) {
+        const uint64_t bd = vd + vslot * (L::kTile >> 4);
+        const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128;
 #pragma unroll
-      for (int kk = 0; kk < kTcBN / 16; ++kk)
-        umma_bf16_ta_if(leader, d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o,
-                        acc || kk > 0);
-      umma_commit_if(leader, &bar->o_full[x]);
-    };
-    auto step = [&]() {
-      if (++slot == KS) {
-        slot = 0;
-        ph ^= 1;
-      }
-    };
-    for (; ok && w.live(); w.next(a), ++items) {
-      const int nx = w.rows(a) > 128 ? 2 : 1;
-      const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
-      ok = mbar_wait_warp(&bar->q_full, items & 1) && mbar_wait_warp(&bar->kv_full[slot], ph);
-      // S_X overwrites the last item's P_X: its product has to be done
-      if (ok && it0 > 0) ok = mbar_wait_warp(&bar->o_full[0], (it0 - 1) & 1);
-      if (ok && nx == 2 && it1 > 0) ok = mbar_wait_warp(&bar->o_full[1], (it1 - 1) & 1);
-      if (!ok) break;
-      tc_fence_after();
-      s_mma(0, slot);
-      if (nx == 2) s_mma(1, slot);
-      umma_commit_if(leader, &bar->kv_empty[slot]);
-      if (w.end - w.cur == 1) umma_commit_if(leader, &bar->q_empty);
-      step();
-      for (int j = w.cur; j < w.end; ++j) {
-        const uint32_t vslot = slot;
-        ok = mbar_wait_warp(&bar->kv_full[slot], ph);
-        if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_warp(&bar->fixed, fixes++ & 1);
+        for (int kk = 0; kk < kTcBN / 16; ++kk)
+          umma_bf16_ta(d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o, acc || kk > 0);
+        umma_commit(&bar->o_full[x]);
+      };
+      auto step = [&]() {
+        if (++slot == KS) {
+          slot = 0;
+          ph ^= 1;
+        }
+      };
+      for (; ok && w.live(); w.next(a), ++items) {
+        const int nx = w.rows(a) > 128 ? 2 : 1;
+        const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
+        ok = mbar_wait_bounded(&bar->q_full, items & 1) &&
+             mbar_wait_bounded(&bar->kv_full[slot], ph);
+        // S_X overwrites the last item's P_X: its product has to be done
+        if (ok && it0 > 0) ok = mbar_wait_bounded(&bar->o_full[0], (it0 - 1) & 1);
+        if (ok && nx == 2 && it1 > 0) ok = mbar_wait_bounded(&bar->o_full[1], (it1 - 1) & 1);
         if (!ok) break;
+        tc_fence_after();
+        s_mma(0, slot);
+        if (nx == 2) s_mma(1, slot);
+        umma_commit(&bar->kv_empty[slot]);
+        if (w.end - w.cur == 1) umma_commit(&bar->q_empty);
         step();
-        const bool more = j + 1 < w.end;
-        const uint32_t kslot = slot;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (x == 1 && nx == 1) break;
-          const uint32_t it = x == 0 ? it0 : it1;
-          ok = mbar_wait_warp(&bar->p_full[x], it & 1);
+        for (int j = w.cur; j < w.end; ++j) {
+          const uint32_t vslot = slot;
+          ok = mbar_wait_bounded(&bar->kv_full[slot], ph);
+          if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
           if (!ok) break;
-          tc_fence_after();
-          o_mma(x, vslot, j > w.cur);
-          if (x + 1 == nx) umma_commit_if(leader, &bar->kv_empty[vslot]);
-          if (more) {
-            if (x == 0) ok = mbar_wait_warp(&bar->kv_full[kslot], ph);
+          step();
+          const bool more = j + 1 < w.end;
+          const uint32_t kslot = slot;
+          auto products = [&](int x, uint32_t it) {  // O of tile j, then S of tile j + 1
+            if (!mbar_wait_bounded(&bar->p_full[x], it & 1)) return false;
+            tc_fence_after();
+            o_mma(x, vslot, j > w.cur);
+            if (x + 1 == nx) umma_commit(&bar->kv_empty[vslot]);
+            if (!more) return true;
+            if (x == 0 && !mbar_wait_bounded(&bar->kv_full[kslot], ph)) return false;
             // S_X overwrites P_X: its product has to be done
-            ok = ok && mbar_wait_warp(&bar->o_full[x], it & 1);
-            if (!ok) break;
+            if (!mbar_wait_bounded(&bar->o_full[x], it & 1)) return false;
             tc_fence_after();
             s_mma(x, kslot);
             if (x + 1 == nx) {
-              umma_commit_if(leader, &bar->kv_empty[kslot]);
-              if (j + 2 == w.end) umma_commit_if(leader, &bar->q_empty);
+              umma_commit(&bar->kv_empty[kslot]);
+              if (j + 2 == w.end) umma_commit(&bar->q_empty);
             }
-          }
-          if (x == 0) ++it0;
-          else ++it1;
+            return true;
+          };
+          ok = products(0, it0++);
+          if (ok && nx == 2) ok = products(1, it1++);
+          if (!ok) break;
+          if (more) step();
         }
-        if (!ok) break;
-        if (more) step();
       }
+      umma_commit(&bar->done);
+      mbar_wait_bounded(&bar->done, 0);
     }
-    __syncwarp();
-    umma_commit_if(leader, &bar->done);
-    mbar_wait_warp(&bar->done, 0);
+    ok = __all_sync(0xffffffffu, ok);
   } else if (warp == 17) {
     // ---------------- K and V copies
     uint32_t slot = 0, ph = 0, issued = 0;

@@ -238,6 +238,12 @@ static ebd_status launch_rotary_v(RotaryArgs a, int head_dim, cudaStream_t s) {
   // (latency), up to eight rows per lane beyond that
   const int few = (chunks + 255) / 256, many = (chunks + 31) / 32;
   a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
+  // a few warps more per token, where that lets every lane keep its unit
+  for (int p = a.parts; p < a.parts + 4; ++p)
+    if (32 * p % a.units == 0) {
+      a.parts = p;
+      break;
+    }
   const long long blocks = ((long long)a.n_tokens * a.parts + kRotWarps - 1) / kRotWarps;
   if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
   if (32 * a.parts % a.units == 0)

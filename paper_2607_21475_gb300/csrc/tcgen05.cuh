@@ -109,38 +109,17 @@ __device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, u
       : "memory");
 }
 
-// The same instructions for a converged warp of which `leader` (one lane) issues:
-// control flow and operands stay uniform, so that descriptors live in uniform
-// registers.  A one-lane branch around the plain forms instead makes each MMA
-// wait for its operands to be moved there (about 100 cycles per instruction).
-__device__ __forceinline__ void umma_bf16_if(uint32_t leader, uint32_t d_tmem, uint64_t adesc,
-                                             uint64_t bdesc, uint32_t idesc, bool accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate), "r"(leader)
-      : "memory");
-}
-__device__ __forceinline__ void umma_bf16_ta_if(uint32_t leader, uint32_t d_tmem, uint32_t a_tmem,
-                                                uint64_t bdesc, uint32_t idesc, bool accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "setp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"((uint32_t)accumulate), "r"(leader)
-      : "memory");
-}
-__device__ __forceinline__ void umma_commit_if(uint32_t leader, uint64_t* bar) {
+// True in one lane of a converged warp.  MMA issue loops run under it: the
+// compiler then keeps the operands in uniform registers, where the MMA wants
+// them (under a plain lane test it may move each one there, MMA by MMA).
+__device__ __forceinline__ bool elect_one() {
+  uint32_t p;
   asm volatile(
       "{\n\t.reg .pred q;\n\t"
-      "setp.ne.b32 q, %1, 0;\n\t"
-      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(
-          smem_u32(bar)),
-      "r"(leader)
-      : "memory");
+      "elect.sync _|q, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(p));
+  return p != 0u;
 }
 
 // Arrive once on `bar` when every tcgen05.mma this thread issued so far has
