@@ -249,6 +249,6 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
                                   : launch_paged_simt<float, 64>(a, s);
   const int n_cta = sm_count();
   paged_split_layout(a, workspace, n_cta, kTcAttnRows);
-  a.min_share = 2;
+  a.min_share = 4;
   return launch_paged_tc(a, *cache, n_cta, s);
 }

@@ -1,13 +1,17 @@
-// Paged attention on the 5th-generation tensor cores: bf16, head_dim 64 / 128,
-// more than a few rows per (sequence, KV head).
+// Paged attention on the 5th-generation tensor cores: bf16, head_dim 64 / 128.
 //
 // An item is 256 rows as two MMA tiles X = A, B of 128 rows; keys come in tiles
-// of 128.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
+// of 64.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
 // the softmax warps turn S_X into weights P_X, and O_X += P_X V with P_X read
-// from tensor memory.  While the softmax of one X runs, the tensor cores work
-// for the other.  Tensor memory (512 columns): O_A, O_B (128 columns each, D
-// used), S_A, S_B (128 columns each); P_X (bf16) overwrites the first 64
-// columns of S_X.
+// from tensor memory.  Tensor memory (512 columns): O_A, O_B (128 columns each,
+// D used) and two buffers of 64 columns of S_A and of S_B; P_X (bf16) overwrites
+// the first 32 columns of its S_X buffer.  With two buffers the product S of the
+// next tile is ready when the softmax of this one ends, so neither the softmax
+// nor the tensor cores wait for the other's latency; 128-key tiles fit only one
+// buffer each, and that chain (S product, softmax, O product, S product) took
+// 3490 cycles per 128 keys of two X against 2050 of MMA work.  The price is
+// the S product's rate: at N = 64 it reads Q again for half the keys, and shared
+// memory holds it to 2/3 of the MMA rate.
 //
 // The softmax keeps one row per thread.  Its reference m moves only when a
 // tile's maximum exceeds it by more than 2^8 (in the weight), so that O_X is
@@ -41,28 +45,29 @@
 namespace ebd {
 
 constexpr int kTcBM = kTcAttnRows;
-constexpr int kTcBN = 128;
-constexpr int kTcAttnThreads = 640;  // 16 softmax warps, MMA, TMA, 2 for queries
+constexpr int kTcBN = 64;
+constexpr int kTcAttnThreads = 384;
 
 template <int D>
 struct PagedTcLayout {
   static constexpr int kHalves = D / 64;
-  static constexpr int kBox = 128 * 128;  // 128 rows x 64 bf16
+  static constexpr int kQBox = 128 * 128;      // 128 rows x 64 bf16
+  static constexpr int kQTile = kHalves * kQBox;
+  static constexpr int kBox = kTcBN * 128;     // 64 rows x 64 bf16
   static constexpr int kTile = kHalves * kBox;
-  static constexpr int kStages = D == 128 ? 5 : 10;
-  static constexpr int kQ = 0;  // two tiles
-  static constexpr int kKV = 2 * kTile;
-  static constexpr int kMax = kKV + kStages * kTile;  // [X][half][row] f32
-  static constexpr int kBar = kMax + 2 * 2 * 128 * 4;
+  static constexpr int kStages = D == 128 ? 5 : 8;  // of K, and of V
+  static constexpr int kQ = 0;                 // two tiles
+  static constexpr int kK = 2 * kQTile;
+  static constexpr int kV = kK + kStages * kTile;
+  static constexpr int kBar = kV + kStages * kTile;
   static constexpr int kBytes = kBar + 512;
 };
 
 struct TcBars {
   uint64_t q_full, q_empty;
-  uint64_t s_full[2], p_full[2], o_full[2];
+  uint64_t s_full[2][2], p_full[2][2], o_full[2][2];  // [X][S buffer]
   uint64_t fixed, done;
-  uint64_t kv_full[10], kv_empty[10];
-  uint64_t pair[8];  // the two warps that share 32 rows of one X
+  uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8];
   WorkStart start;
   uint32_t tmem;
 };
@@ -151,24 +156,27 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int cta = blockIdx.x;
-  if (warp == 16) {
+  if (warp == 8) {
     tmem_alloc(&bar->tmem, 512);
     tmem_relinquish();
-  } else if (warp == 17) {
+  } else if (warp == 9) {
     if (lane == 0) {
       mbar_init(&bar->q_full, 64);
       mbar_init(&bar->q_empty, 1);
       for (int x = 0; x < 2; ++x) {
-        mbar_init(&bar->s_full[x], 1);
-        mbar_init(&bar->p_full[x], 8);
-        mbar_init(&bar->o_full[x], 1);
+        for (int b = 0; b < 2; ++b) {
+          mbar_init(&bar->s_full[x][b], 1);
+          mbar_init(&bar->p_full[x][b], 4);
+          mbar_init(&bar->o_full[x][b], 1);
+        }
       }
-      for (int i = 0; i < 8; ++i) mbar_init(&bar->pair[i], 2);
       mbar_init(&bar->fixed, 64);
       mbar_init(&bar->done, 1);
       for (int s = 0; s < KS; ++s) {
-        mbar_init(&bar->kv_full[s], 1);
-        mbar_init(&bar->kv_empty[s], 1);
+        mbar_init(&bar->k_full[s], 1);
+        mbar_init(&bar->k_empty[s], 1);
+        mbar_init(&bar->v_full[s], 1);
+        mbar_init(&bar->v_empty[s], 1);
       }
       fence_barrier_init();
     }
@@ -184,21 +192,13 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   PieceWalk<kTcBM, kTcBN> w(a, start);
   bool ok = true;
 
-  if (warp < 16) {
-    // ---------------- softmax and epilogue: half a row per thread
-    const int x = warp >> 3, half = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
-    uint64_t* pair = &bar->pair[x * 4 + (warp & 3)];
-    uint32_t pairs = 0;
-    auto pair_sync = [&]() {  // bounded, unlike a named barrier
-      __syncwarp();
-      if (lane == 0) mbar_arrive(pair);
-      return mbar_wait_warp(pair, pairs++ & 1);
-    };
+  if (warp < 8) {
+    // ---------------- softmax and epilogue: one row per thread
+    const int x = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t sS = tmem + 256 + x * 128 + lane_base;
-    const uint32_t sO = tmem + x * 128 + lane_base + half * (D / 2);
-    float* mx = reinterpret_cast<float*>(smem + L::kMax) + x * 256 + row;
-    uint32_t it = 0;  // tiles of X so far: barrier phases
+    const uint32_t sO = tmem + x * 128 + lane_base;
+    uint32_t it = 0;  // tiles of X so far: S buffer it & 1
     if (threadIdx.x == 0) write_record<kTcBM, kTcBN>(a, start, cta);  // while the first tile loads
     __syncwarp();
     for (; ok && w.live(); w.next(a)) {
@@ -210,16 +210,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
       float m = -INFINITY, l = 0.f;
       for (int j = w.cur; j < w.end; ++j, ++it) {
-        const int k0 = j * kTcBN + half * 64;
-        if (!mbar_wait_warp(&bar->s_full[x], it & 1)) {
+        const int k0 = j * kTcBN;
+        const uint32_t buf = sS + (it & 1) * 64;
+        if (!mbar_wait_warp(&bar->s_full[x][it & 1], (it >> 1) & 1)) {
           ok = false;
           break;
         }
         tc_fence_after();
         uint32_t s[64];
-        tmem_ld64(sS + half * 64, s);
+        tmem_ld64(buf, s);
         tmem_ld_wait();
-        if (__any_sync(0xffffffffu, hi - k0 < 64 || lo > k0)) {
+        if (__any_sync(0xffffffffu, hi - k0 < kTcBN || lo > k0)) {
           const int chi = hi - k0, clo = lo - k0;
 #pragma unroll
           for (int i = 0; i < 64; ++i)
@@ -236,18 +237,10 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         float top = fmaxf(max3(t4[0], t4[1], t4[2]),
                           max3(t4[3], __uint_as_float(s[60]), __uint_as_float(s[61])));
         top = max3(top, __uint_as_float(s[62]), __uint_as_float(s[63]));
-        mx[half * 128] = top;
-        tc_fence_before();  // P overwrites columns that the other warp has read
-        if (!pair_sync()) {
-          ok = false;
-          break;
-        }
-        tc_fence_after();
-        top = fmaxf(top, mx[(half ^ 1) * 128]);
         const bool grow = m > -INFINITY && (top - m) * a.scale2 > kRescaleLog2;
         if (__any_sync(0xffffffffu, grow)) {
           // O_X holds the tiles before this one: wait for their product
-          if (!mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
+          if (!mbar_wait_warp(&bar->o_full[x][(it - 1) & 1], ((it - 1) >> 1) & 1)) {
             ok = false;
             break;
           }
@@ -258,7 +251,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           m = m1;
           // 16 columns at a time: the logits stay in registers meanwhile
 #pragma unroll 1
-          for (int c = 0; c < D / 2; c += 16) {
+          for (int c = 0; c < D; c += 16) {
             uint32_t o[16];
             tmem_ld16(sO + c, o);
             tmem_ld_wait();
@@ -288,21 +281,15 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           p[i] = pack_bf16(e.x, e.y);
           p[i + 1] = pack_bf16(f.x, f.y);
         }
-        tmem_st32(sS + half * 32, p);
+        tmem_st32(buf, p);
         l += (sum0.x + sum0.y) + (sum1.x + sum1.y);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bar->p_full[x]);
+        if (lane == 0) mbar_arrive(&bar->p_full[x][it & 1]);
       }
       if (!ok) break;
-      // the row's sum from its two halves
-      ok = pair_sync();  // the other warp has read the last maxima
-      mx[half * 128] = l;
-      ok = ok && pair_sync();
-      l = half ? mx[0] + l : l + mx[128];
-      ok = ok && pair_sync();  // both have read the sums: the next item's maxima may come
-      if (!ok || !mbar_wait_warp(&bar->o_full[x], (it - 1) & 1)) {
+      if (!mbar_wait_warp(&bar->o_full[x][(it - 1) & 1], ((it - 1) >> 1) & 1)) {
         ok = false;
         break;
       }
@@ -314,10 +301,9 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const long long out = (long long)(w.sp.t0 + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
       const size_t prow = (size_t)slot * kTcBM + x * 128 + row;
-      const int c0 = half * (D / 2);
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
-      for (int c = 0; c < D / 2; c += 32) {
+      for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
         __syncwarp();
         tmem_ld32(sO + c, o);
@@ -328,17 +314,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           z0 = fmaf(__uint_as_float(o[i]), 0.f, z0);
           z1 = fmaf(__uint_as_float(o[16 + i]), 0.f, z1);
         }
-        nan_groups |= ((z0 != z0 ? 1u : 0u) | (z1 != z1 ? 2u : 0u)) << ((c0 + c) / 16);
+        nan_groups |= ((z0 != z0 ? 1u : 0u) | (z1 != z1 ? 2u : 0u)) << (c / 16);
         if (!mine) {
         } else if (slot >= 0) {
-          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c0 + c);
+          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             dst[i] = make_float4(
                 __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
                 __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
         } else {
-          uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.y + out * D + c0 + c);
+          uint4* dst = reinterpret_cast<uint4*>((__nv_bfloat16*)a.y + out * D + c);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             uint32_t q[4];
@@ -351,108 +337,127 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         }
       }
       if (mine) {
-        if (half == 0) {
-          if (slot >= 0) a.part_lse[prow] = lse2;
-          else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
-        }
+        if (slot >= 0) a.part_lse[prow] = lse2;
+        else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
         if (nan_groups)
           mend_row<D>(a, w.b, w.h, w.sp.t0 + tok, g, w.cur * kTcBN, lo, hi,
                       min(w.end * kTcBN, w.sp.len), m == -INFINITY ? 0.f : m * a.scale2, inv,
                       nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
-                         slot < 0 ? nullptr : a.part_o + prow * D);
+                      slot < 0 ? nullptr : a.part_o + prow * D);
       }
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
-  } else if (warp == 16) {
+  } else if (warp == 8) {
     // ---------------- MMA issue
     if (elect_one()) {
       const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
       const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
       // descriptors once; a step along them is an addition to the start address
       const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ));
-      const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kKV));
-      const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kKV), L::kBox);
-      uint32_t slot = 0, ph = 0;  // ring position of the next K or V tile, and its phase
-      uint32_t it0 = 0, it1 = 0, items = 0, fixes = 0;
-      auto s_mma = [&](int x, uint32_t kslot) {
-        const uint64_t ad = qd + (uint32_t)(x * (L::kTile >> 4));
-        const uint64_t bd = kd + kslot * (L::kTile >> 4);
-        const uint32_t d = tmem + 256 + x * 128;
+      const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kK));
+      const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kV), L::kBox);
+      uint32_t tile0 = 0;                // tiles before this piece
+      uint32_t it0 = 0, it1 = 0;         // products O of A and B issued so far
+      uint32_t items = 0, fixes = 0;
+      // S of the piece's tile t, the X's tile number n
+      auto s_mma = [&](int x, int t, uint32_t n) {
+        const uint32_t at = tile0 + t, slot = at % KS;
+        const uint64_t ad = qd + (uint32_t)(x * (L::kQTile >> 4));
+        const uint64_t bd = kd + slot * (L::kTile >> 4);
+        const uint32_t d = tmem + 256 + x * 128 + (n & 1) * 64;
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) {
-          const uint32_t off = (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4);
-          umma_bf16(d, ad + off, bd + off, idesc_s, kk > 0);
-        }
-        umma_commit(&bar->s_full[x]);
+        for (int kk = 0; kk < D / 16; ++kk)
+          umma_bf16(d, ad + (uint32_t)(((kk >> 2) * L::kQBox + (kk & 3) * 32) >> 4),
+                    bd + (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
+        umma_commit(&bar->s_full[x][n & 1]);
       };
-      auto o_mma = [&](int x, uint32_t vslot, bool acc) {
-        const uint64_t bd = vd + vslot * (L::kTile >> 4);
-        const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128;
+      auto k_wait = [&](int t) {
+        const uint32_t at = tile0 + t;
+        return mbar_wait_bounded(&bar->k_full[at % KS], (at / KS) & 1);
+      };
+      auto v_wait = [&](int t) {
+        const uint32_t at = tile0 + t;
+        return mbar_wait_bounded(&bar->v_full[at % KS], (at / KS) & 1);
+      };
+      // O of the X's tile number n is done
+      auto o_wait = [&](int x, uint32_t n) {
+        return mbar_wait_bounded(&bar->o_full[x][n & 1], (n >> 1) & 1);
+      };
+      auto k_done = [&](int t) { umma_commit(&bar->k_empty[(tile0 + t) % KS]); };
+      // O of the piece's tile t, the X's tile number n
+      auto o_mma = [&](int x, int t, uint32_t n) {
+        if (!mbar_wait_bounded(&bar->p_full[x][n & 1], (n >> 1) & 1)) return false;
+        tc_fence_after();
+        const uint64_t bd = vd + ((tile0 + t) % KS) * (L::kTile >> 4);
+        const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128 + (n & 1) * 64;
 #pragma unroll
         for (int kk = 0; kk < kTcBN / 16; ++kk)
-          umma_bf16_ta(d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o, acc || kk > 0);
-        umma_commit(&bar->o_full[x]);
+          umma_bf16_ta(d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o, t > 0 || kk > 0);
+        umma_commit(&bar->o_full[x][n & 1]);
+        return true;
       };
-      auto step = [&]() {
-        if (++slot == KS) {
-          slot = 0;
-          ph ^= 1;
-        }
-      };
-      for (; ok && w.live(); w.next(a), ++items) {
-        const int nx = w.rows(a) > 128 ? 2 : 1;
+      for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
+        const bool two = w.rows(a) > 128;
+        const int n = w.end - w.cur;
         const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
-        ok = mbar_wait_bounded(&bar->q_full, items & 1) &&
-             mbar_wait_bounded(&bar->kv_full[slot], ph);
-        // S_X overwrites the last item's P_X: its product has to be done
-        if (ok && it0 > 0) ok = mbar_wait_bounded(&bar->o_full[0], (it0 - 1) & 1);
-        if (ok && nx == 2 && it1 > 0) ok = mbar_wait_bounded(&bar->o_full[1], (it1 - 1) & 1);
+        ok = mbar_wait_bounded(&bar->q_full, items & 1) && k_wait(0);
+        // S_X overwrites the last item's P_X: its products have to be done
+        if (ok && it0 > 0) ok = o_wait(0, it0 - 1);
+        if (ok && two && it1 > 0) ok = o_wait(1, it1 - 1);
         if (!ok) break;
         tc_fence_after();
-        s_mma(0, slot);
-        if (nx == 2) s_mma(1, slot);
-        umma_commit(&bar->kv_empty[slot]);
-        if (w.end - w.cur == 1) umma_commit(&bar->q_empty);
-        step();
-        for (int j = w.cur; j < w.end; ++j) {
-          const uint32_t vslot = slot;
-          ok = mbar_wait_bounded(&bar->kv_full[slot], ph);
-          if (ok && ragged_end && j + 1 == w.end) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
+        s_mma(0, 0, it0);
+        if (two) s_mma(1, 0, it1);
+        k_done(0);
+        if (n > 1) {
+          ok = k_wait(1);
           if (!ok) break;
-          step();
-          const bool more = j + 1 < w.end;
-          const uint32_t kslot = slot;
-          auto products = [&](int x, uint32_t it) {  // O of tile j, then S of tile j + 1
-            if (!mbar_wait_bounded(&bar->p_full[x], it & 1)) return false;
-            tc_fence_after();
-            o_mma(x, vslot, j > w.cur);
-            if (x + 1 == nx) umma_commit(&bar->kv_empty[vslot]);
-            if (!more) return true;
-            if (x == 0 && !mbar_wait_bounded(&bar->kv_full[kslot], ph)) return false;
-            // S_X overwrites P_X: its product has to be done
-            if (!mbar_wait_bounded(&bar->o_full[x], it & 1)) return false;
-            tc_fence_after();
-            s_mma(x, kslot);
-            if (x + 1 == nx) {
-              umma_commit(&bar->kv_empty[kslot]);
-              if (j + 2 == w.end) umma_commit(&bar->q_empty);
+          tc_fence_after();
+          s_mma(0, 1, it0 + 1);
+          if (!two) k_done(1);
+        } else {
+          umma_commit(&bar->q_empty);
+        }
+        // per tile: O_A, the next S_B, O_B, the next S_A but one; each S writes a
+        // buffer whose weights went into the O product before the last issued
+        for (int t = 0; ok && t < n; ++t) {
+          ok = v_wait(t);
+          if (ok && ragged_end && t + 1 == n) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
+          ok = ok && o_mma(0, t, it0);
+          if (!ok) break;
+          ++it0;
+          if (two) {
+            if (t + 1 < n) {
+              if (t > 0) ok = o_wait(1, it1 - 1);
+              if (!ok) break;
+              tc_fence_after();
+              s_mma(1, t + 1, it1 + 1);
+              k_done(t + 1);
+              if (t + 2 == n) umma_commit(&bar->q_empty);
             }
-            return true;
-          };
-          ok = products(0, it0++);
-          if (ok && nx == 2) ok = products(1, it1++);
-          if (!ok) break;
-          if (more) step();
+            ok = o_mma(1, t, it1);
+            if (!ok) break;
+            ++it1;
+          }
+          umma_commit(&bar->v_empty[(tile0 + t) % KS]);
+          if (t + 2 < n) {
+            ok = k_wait(t + 2) && o_wait(0, it0 - 1);
+            if (!ok) break;
+            tc_fence_after();
+            s_mma(0, t + 2, it0 + 1);
+            if (!two) k_done(t + 2);
+          }
+          if (!two && t + 2 == (n > 2 ? n - 1 : n)) umma_commit(&bar->q_empty);
         }
       }
       umma_commit(&bar->done);
       mbar_wait_bounded(&bar->done, 0);
     }
     ok = __all_sync(0xffffffffu, ok);
-  } else if (warp == 17) {
-    // ---------------- K and V copies
-    uint32_t slot = 0, ph = 0, issued = 0;
+  } else if (warp == 9) {
+    // ---------------- K and V copies, in the order K0 K1 V0 K2 V1 ... of the MMAs
+    uint32_t nk = 0, nv = 0;  // tiles issued
     const int page = 1 << a.pv.page_shift;
     const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
     bool bad = false;
@@ -460,45 +465,53 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       // lane i: one box of a tile (keys bx * box .., channels half * 64 ..); its
       // page is looked up a tile ahead, past the pool where there is none
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
-      auto page_at = [&](int pos) {
+      auto page_at = [&](int j) {
+        const int pos = j * kTcBN + bx * box;
         if (bx >= boxes || pos >= w.sp.len) return a.pv.n_pages;
         const int p = page_of(a.pv, w.b, pos);
         if (p < 0) bad = true;
         return p < 0 ? a.pv.n_pages : p;
       };
-      int next_pg = page_at(w.cur * kTcBN + bx * box);
+      auto copy = [&](const CUtensorMap* tm, int base, uint64_t* full, uint64_t* empty,
+                      uint32_t n, int j, int pg) {
+        const uint32_t slot = n % KS;
+        if (n >= KS && !mbar_wait_warp(&empty[slot], (n / KS - 1) & 1)) return false;
+        if (lane == 0) mbar_arrive_expect_tx(&full[slot], L::kTile);
+        __syncwarp();
+        if (bx < boxes)
+          tma_load_4d(smem + base + slot * L::kTile + half * L::kBox + bx * box * 128, tm,
+                      half * 64, (j * kTcBN + bx * box) & (page - 1), w.h, pg, &full[slot]);
+        __syncwarp();
+        return true;
+      };
+      int pg = page_at(w.cur), next_pg = w.cur + 1 < w.end ? page_at(w.cur + 1) : 0;
+      ok = copy(&tmK, L::kK, bar->k_full, bar->k_empty, nk, w.cur, pg);
+      if (ok) ++nk;
       for (int j = w.cur; ok && j < w.end; ++j) {
-        const int pos = j * kTcBN + bx * box, pg = next_pg;
-        if (j + 1 < w.end) next_pg = page_at(pos + kTcBN);
-        for (int kv = 0; ok && kv < 2; ++kv) {
-          if (issued >= KS && !mbar_wait_warp(&bar->kv_empty[slot], ph ^ 1)) {
-            ok = false;
-            break;
-          }
-          if (lane == 0) mbar_arrive_expect_tx(&bar->kv_full[slot], L::kTile);
-          __syncwarp();
-          if (bx < boxes)
-            tma_load_4d(smem + L::kKV + slot * L::kTile + half * L::kBox + bx * box * 128,
-                        kv ? &tmV : &tmK, half * 64, pos & (page - 1), w.h, pg,
-                        &bar->kv_full[slot]);
-          __syncwarp();
-          ++issued;
-          if (++slot == KS) {
-            slot = 0;
-            ph ^= 1;
-          }
+        const int ahead = j + 2 < w.end ? page_at(j + 2) : 0;
+        if (j + 1 < w.end) {
+          ok = copy(&tmK, L::kK, bar->k_full, bar->k_empty, nk, j + 1, next_pg);
+          if (!ok) break;
+          ++nk;
         }
+        ok = copy(&tmV, L::kV, bar->v_full, bar->v_empty, nv, j, pg);
+        if (!ok) break;
+        ++nv;
+        pg = next_pg;
+        next_pg = ahead;
       }
     }
     if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
     // every copy has landed before the block may end
-    for (uint32_t i = issued > KS ? issued - KS : 0; i < issued; ++i)
-      mbar_wait_bounded(&bar->kv_full[i % KS], (i / KS) & 1);
+    for (uint32_t i = nk > KS ? nk - KS : 0; i < nk; ++i)
+      mbar_wait_bounded(&bar->k_full[i % KS], (i / KS) & 1);
+    for (uint32_t i = nv > KS ? nv - KS : 0; i < nv; ++i)
+      mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
     // ---------------- query rows; value rows past the end
-    const int tid = threadIdx.x - 576;
+    const int tid = threadIdx.x - 320;
     constexpr int CH = D / 8;  // 16-byte chunks per row
-    uint32_t items = 0, tile0 = 0;  // tiles before this piece: ring position 2 tile
+    uint32_t items = 0, tile0 = 0;  // tiles before this piece
     for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
       if (items > 0 && !mbar_wait_bounded(&bar->q_empty, (items - 1) & 1)) {
         ok = false;
@@ -509,7 +522,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (long long)w.sp.t0 * a.q_ts +
                                (long long)(w.h * a.group) * a.q_hs + c * 8;
       for (int r = tid / CH; r < padded; r += 64 / CH) {
-        unsigned char* dst = smem + L::kQ + (r >> 7) * L::kTile + (c >> 3) * L::kBox +
+        unsigned char* dst = smem + L::kQ + (r >> 7) * L::kQTile + (c >> 3) * L::kQBox +
                              (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
         if (r < rows) {
           const int tok = (w.m * kTcBM + r) / a.group, g = w.m * kTcBM + r - tok * a.group;
@@ -523,18 +536,18 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       fence_proxy_async_smem();
       mbar_arrive(&bar->q_full);
       if (w.sp.len < w.end * kTcBN) {
-        // the piece's last value tile: ring position 2 (tile0 + tiles) - 1.  Its
-        // stage's phase is certain only once the piece's last S product is done
-        // (q_empty): every earlier copy has landed by then, and no later one
-        // can take the stage before the rows are cleared.
-        const uint32_t at = 2 * (tile0 + (w.end - w.cur)) - 1;
+        // The piece's last value tile.  Its stage's phase is certain only once the
+        // piece's last S product is done (q_empty): the stage's earlier tile
+        // has landed by then, and no later one can take the stage before the
+        // rows are cleared.
+        const uint32_t at = tile0 + (w.end - w.cur) - 1;
         if (!mbar_wait_bounded(&bar->q_empty, items & 1) ||
-            !mbar_wait_bounded(&bar->kv_full[at % KS], (at / KS) & 1)) {
+            !mbar_wait_bounded(&bar->v_full[at % KS], (at / KS) & 1)) {
           ok = false;
           break;
         }
         const int first = w.sp.len - (w.end - 1) * kTcBN;  // rows from here on are cleared
-        unsigned char* v = smem + L::kKV + (at % KS) * L::kTile;
+        unsigned char* v = smem + L::kV + (at % KS) * L::kTile;
         for (int i = max(first, 0) * 8 + tid; i < kTcBN * 8; i += 64)
 #pragma unroll
           for (int h = 0; h < L::kHalves; ++h)
@@ -547,7 +560,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   if (!ok) raise_status(a.dev_status, EBD_DEV_TIMEOUT);
   tc_fence_before();
   __syncthreads();
-  if (warp == 16) {
+  if (warp == 8) {
     tc_fence_after();
     tmem_dealloc(tmem, 512);
   }
