@@ -20,10 +20,10 @@
 // of the unrounded ones), which costs at most 2^-8 of the largest value, as
 // the result's own rounding does.
 //
-// Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warp 8 issues the
-// MMAs, warp 9 the TMA copies of K and V (one box per page and 64 channels;
-// pages past the sequence's end are read past the pool's end, which fills
-// zeros), warps 10-11 bring the query rows into the swizzled layout and clear
+// Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warps 8 / 9 issue the
+// MMAs of A / B, warp 10 the TMA copies of K and V (one box per page and 64
+// channels; pages past the sequence's end are read past the pool's end, which
+// fills zeros), warp 11 brings the query rows into the swizzled layout and clears
 // the value rows of a tile past the sequence's end (weight 0 times whatever a
 // page holds there must stay 0).
 //
@@ -66,7 +66,7 @@ struct PagedTcLayout {
 struct TcBars {
   uint64_t q_full, q_empty;
   uint64_t s_full[2][2], p_full[2][2], o_full[2][2];  // [X][S buffer]
-  uint64_t fixed, done;
+  uint64_t fixed, done[2];
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8];
   WorkStart start;
   uint32_t tmem;
@@ -161,22 +161,22 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     tmem_relinquish();
   } else if (warp == 9) {
     if (lane == 0) {
-      mbar_init(&bar->q_full, 64);
-      mbar_init(&bar->q_empty, 1);
+      mbar_init(&bar->q_full, 32);
+      mbar_init(&bar->q_empty, 2);
       for (int x = 0; x < 2; ++x) {
+        mbar_init(&bar->done[x], 1);
         for (int b = 0; b < 2; ++b) {
           mbar_init(&bar->s_full[x][b], 1);
           mbar_init(&bar->p_full[x][b], 4);
           mbar_init(&bar->o_full[x][b], 1);
         }
       }
-      mbar_init(&bar->fixed, 64);
-      mbar_init(&bar->done, 1);
+      mbar_init(&bar->fixed, 32);
       for (int s = 0; s < KS; ++s) {
         mbar_init(&bar->k_full[s], 1);
-        mbar_init(&bar->k_empty[s], 1);
+        mbar_init(&bar->k_empty[s], 2);
         mbar_init(&bar->v_full[s], 1);
-        mbar_init(&bar->v_empty[s], 1);
+        mbar_init(&bar->v_empty[s], 2);
       }
       fence_barrier_init();
     }
@@ -348,114 +348,90 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
-  } else if (warp == 8) {
-    // ---------------- MMA issue
+  } else if (warp < 10) {
+    // ---------------- MMA issue: a warp per X (one thread's instructions between
+    // the MMAs of both would take longer than the MMAs)
+    const int x = warp - 8;
     if (elect_one()) {
       const uint32_t idesc_s = umma_idesc_bf16_f32(128, kTcBN);
       const uint32_t idesc_o = umma_idesc_bf16_f32_bt(128, D);
       // descriptors once; a step along them is an addition to the start address
-      const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ));
+      const uint64_t qd = umma_desc_k_sw128(smem_u32(smem + L::kQ + x * L::kQTile));
       const uint64_t kd = umma_desc_k_sw128(smem_u32(smem + L::kK));
       const uint64_t vd = umma_desc_mn_sw128(smem_u32(smem + L::kV), L::kBox);
-      uint32_t tile0 = 0;                // tiles before this piece
-      uint32_t it0 = 0, it1 = 0;         // products O of A and B issued so far
+      const uint32_t tS = tmem + 256 + x * 128, tO = tmem + x * 128;
+      uint32_t ks = 0, kph = 0, vs = 0, vph = 0;  // ring positions and phases
+      uint32_t n_s = 0, n_o = 0;                  // products issued so far
       uint32_t items = 0, fixes = 0;
-      // S of the piece's tile t, the X's tile number n
-      auto s_mma = [&](int x, int t, uint32_t n) {
-        const uint32_t at = tile0 + t, slot = at % KS;
-        const uint64_t ad = qd + (uint32_t)(x * (L::kQTile >> 4));
-        const uint64_t bd = kd + slot * (L::kTile >> 4);
-        const uint32_t d = tmem + 256 + x * 128 + (n & 1) * 64;
+      auto s_mma = [&](bool last) {
+        if (!mbar_wait_bounded(&bar->k_full[ks], kph)) return false;
+        // S overwrites the weights of two tiles ago: their product has to be done
+        const uint32_t b = n_s & 1;
+        if (n_s >= 2 && !mbar_wait_bounded(&bar->o_full[x][b], ((n_s >> 1) - 1) & 1)) return false;
+        tc_fence_after();
+        const uint64_t bd = kd + ks * (L::kTile >> 4);
+        const uint32_t d = tS + b * 64;
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
-          umma_bf16(d, ad + (uint32_t)(((kk >> 2) * L::kQBox + (kk & 3) * 32) >> 4),
+          umma_bf16(d, qd + (uint32_t)(((kk >> 2) * L::kQBox + (kk & 3) * 32) >> 4),
                     bd + (uint32_t)(((kk >> 2) * L::kBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
-        umma_commit(&bar->s_full[x][n & 1]);
-      };
-      auto k_wait = [&](int t) {
-        const uint32_t at = tile0 + t;
-        return mbar_wait_bounded(&bar->k_full[at % KS], (at / KS) & 1);
-      };
-      auto v_wait = [&](int t) {
-        const uint32_t at = tile0 + t;
-        return mbar_wait_bounded(&bar->v_full[at % KS], (at / KS) & 1);
-      };
-      // O of the X's tile number n is done
-      auto o_wait = [&](int x, uint32_t n) {
-        return mbar_wait_bounded(&bar->o_full[x][n & 1], (n >> 1) & 1);
-      };
-      auto k_done = [&](int t) { umma_commit(&bar->k_empty[(tile0 + t) % KS]); };
-      // O of the piece's tile t, the X's tile number n
-      auto o_mma = [&](int x, int t, uint32_t n) {
-        if (!mbar_wait_bounded(&bar->p_full[x][n & 1], (n >> 1) & 1)) return false;
-        tc_fence_after();
-        const uint64_t bd = vd + ((tile0 + t) % KS) * (L::kTile >> 4);
-        const uint32_t d = tmem + x * 128, p = tmem + 256 + x * 128 + (n & 1) * 64;
-#pragma unroll
-        for (int kk = 0; kk < kTcBN / 16; ++kk)
-          umma_bf16_ta(d, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o, t > 0 || kk > 0);
-        umma_commit(&bar->o_full[x][n & 1]);
+        umma_commit(&bar->s_full[x][b]);
+        umma_commit(&bar->k_empty[ks]);
+        if (last) umma_commit(&bar->q_empty);
+        ++n_s;
+        if (++ks == KS) ks = 0, kph ^= 1;
         return true;
       };
-      for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
+      auto o_mma = [&](bool first, bool fix) {
+        const uint32_t b = n_o & 1;
+        if (!mbar_wait_bounded(&bar->v_full[vs], vph)) return false;
+        if (fix && !mbar_wait_bounded(&bar->fixed, fixes++ & 1)) return false;
+        if (!mbar_wait_bounded(&bar->p_full[x][b], (n_o >> 1) & 1)) return false;
+        tc_fence_after();
+        const uint64_t bd = vd + vs * (L::kTile >> 4);
+        const uint32_t p = tS + b * 64;
+#pragma unroll
+        for (int kk = 0; kk < kTcBN / 16; ++kk)
+          umma_bf16_ta(tO, p + kk * 8, bd + (uint32_t)(kk * (2048 >> 4)), idesc_o, !first || kk > 0);
+        umma_commit(&bar->o_full[x][b]);
+        umma_commit(&bar->v_empty[vs]);
+        ++n_o;
+        if (++vs == KS) vs = 0, vph ^= 1;
+        return true;
+      };
+      for (; ok && w.live(); w.next(a), ++items) {
         const bool two = w.rows(a) > 128;
         const int n = w.end - w.cur;
         const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
-        ok = mbar_wait_bounded(&bar->q_full, items & 1) && k_wait(0);
-        // S_X overwrites the last item's P_X: its products have to be done
-        if (ok && it0 > 0) ok = o_wait(0, it0 - 1);
-        if (ok && two && it1 > 0) ok = o_wait(1, it1 - 1);
-        if (!ok) break;
-        tc_fence_after();
-        s_mma(0, 0, it0);
-        if (two) s_mma(1, 0, it1);
-        k_done(0);
-        if (n > 1) {
-          ok = k_wait(1);
-          if (!ok) break;
-          tc_fence_after();
-          s_mma(0, 1, it0 + 1);
-          if (!two) k_done(1);
-        } else {
-          umma_commit(&bar->q_empty);
+        ok = mbar_wait_bounded(&bar->q_full, items & 1);
+        if (x == 1 && !two) {
+          // A does the item alone.  B still follows every stage and gives its
+          // consent to each reuse: no barrier's phase can pass it by.
+          // (the last value tile is cleared only after q_empty: before its wait)
+          if (ok && n == 1) mbar_arrive(&bar->q_empty);
+          for (int t = 0; ok && t < n; ++t) {
+            ok = mbar_wait_bounded(&bar->k_full[ks], kph) &&
+                 mbar_wait_bounded(&bar->v_full[vs], vph) &&
+                 (!ragged_end || t + 1 < n || mbar_wait_bounded(&bar->fixed, fixes++ & 1));
+            mbar_arrive(&bar->k_empty[ks]);
+            mbar_arrive(&bar->v_empty[vs]);
+            if (++ks == KS) ks = 0, kph ^= 1;
+            if (++vs == KS) vs = 0, vph ^= 1;
+            if (t + 2 == n) mbar_arrive(&bar->q_empty);
+          }
+          continue;
         }
-        // per tile: O_A, the next S_B, O_B, the next S_A but one; each S writes a
-        // buffer whose weights went into the O product before the last issued
+        ok = ok && s_mma(n == 1) && (n == 1 || s_mma(n == 2));
         for (int t = 0; ok && t < n; ++t) {
-          ok = v_wait(t);
-          if (ok && ragged_end && t + 1 == n) ok = mbar_wait_bounded(&bar->fixed, fixes++ & 1);
-          ok = ok && o_mma(0, t, it0);
-          if (!ok) break;
-          ++it0;
-          if (two) {
-            if (t + 1 < n) {
-              if (t > 0) ok = o_wait(1, it1 - 1);
-              if (!ok) break;
-              tc_fence_after();
-              s_mma(1, t + 1, it1 + 1);
-              k_done(t + 1);
-              if (t + 2 == n) umma_commit(&bar->q_empty);
-            }
-            ok = o_mma(1, t, it1);
-            if (!ok) break;
-            ++it1;
-          }
-          umma_commit(&bar->v_empty[(tile0 + t) % KS]);
-          if (t + 2 < n) {
-            ok = k_wait(t + 2) && o_wait(0, it0 - 1);
-            if (!ok) break;
-            tc_fence_after();
-            s_mma(0, t + 2, it0 + 1);
-            if (!two) k_done(t + 2);
-          }
-          if (!two && t + 2 == (n > 2 ? n - 1 : n)) umma_commit(&bar->q_empty);
+          ok = o_mma(t == 0, ragged_end && t + 1 == n);
+          if (ok && t + 2 < n) ok = s_mma(t + 3 == n);
         }
       }
-      umma_commit(&bar->done);
-      mbar_wait_bounded(&bar->done, 0);
+      umma_commit(&bar->done[x]);
+      mbar_wait_bounded(&bar->done[x], 0);
     }
     ok = __all_sync(0xffffffffu, ok);
-  } else if (warp == 9) {
+  } else if (warp == 10) {
     // ---------------- K and V copies, in the order K0 K1 V0 K2 V1 ... of the MMAs
     uint32_t nk = 0, nv = 0;  // tiles issued
     const int page = 1 << a.pv.page_shift;
@@ -509,26 +485,32 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
     // ---------------- query rows; value rows past the end
-    const int tid = threadIdx.x - 320;
     constexpr int CH = D / 8;  // 16-byte chunks per row
     uint32_t items = 0, tile0 = 0;  // tiles before this piece
     for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
-      if (items > 0 && !mbar_wait_bounded(&bar->q_empty, (items - 1) & 1)) {
+      if (items > 0 && !mbar_wait_warp(&bar->q_empty, (items - 1) & 1)) {
         ok = false;
         break;
       }
-      const int rows = w.rows(a);
-      const int c = tid % CH, padded = rows > 128 ? 256 : 128;
-      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (long long)w.sp.t0 * a.q_ts +
-                               (long long)(w.h * a.group) * a.q_hs + c * 8;
-      for (int r = tid / CH; r < padded; r += 64 / CH) {
-        unsigned char* dst = smem + L::kQ + (r >> 7) * L::kQTile + (c >> 3) * L::kQBox +
-                             (r & 127) * 128 + (((c & 7) ^ (r & 7)) << 4);
-        if (r < rows) {
-          const int tok = (w.m * kTcBM + r) / a.group, g = w.m * kTcBM + r - tok * a.group;
-          cp_async16(dst, q + tok * a.q_ts + g * a.q_hs);
-        } else {
-          *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+      const int rows = w.rows(a), padded = rows > 128 ? 256 : 128;
+      // the lane's chunk of rows lane / CH, + 32 / CH, ..., as (token, head of the group)
+      const int c = lane % CH;
+      int tok = (w.m * kTcBM + lane / CH) / a.group;
+      int g = w.m * kTcBM + lane / CH - tok * a.group;
+      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (long long)(w.sp.t0 + tok) * a.q_ts +
+                               (long long)(w.h * a.group + g) * a.q_hs + c * 8;
+      unsigned char* dst0 = smem + L::kQ + (c >> 3) * L::kQBox;
+#pragma unroll 4
+      for (int r = lane / CH; r < padded; r += 32 / CH) {
+        unsigned char* dst = dst0 + (r >> 7) * L::kQTile + (r & 127) * 128 +
+                             (((c & 7) ^ (r & 7)) << 4);
+        if (r < rows) cp_async16(dst, q);
+        else *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
+        g += 32 / CH;
+        q += (32 / CH) * a.q_hs;
+        while (g >= a.group) {
+          g -= a.group;
+          q += a.q_ts - a.group * a.q_hs;
         }
       }
       cp_async_commit();
@@ -541,14 +523,14 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         // has landed by then, and no later one can take the stage before the
         // rows are cleared.
         const uint32_t at = tile0 + (w.end - w.cur) - 1;
-        if (!mbar_wait_bounded(&bar->q_empty, items & 1) ||
-            !mbar_wait_bounded(&bar->v_full[at % KS], (at / KS) & 1)) {
+        if (!mbar_wait_warp(&bar->q_empty, items & 1) ||
+            !mbar_wait_warp(&bar->v_full[at % KS], (at / KS) & 1)) {
           ok = false;
           break;
         }
         const int first = w.sp.len - (w.end - 1) * kTcBN;  // rows from here on are cleared
         unsigned char* v = smem + L::kV + (at % KS) * L::kTile;
-        for (int i = max(first, 0) * 8 + tid; i < kTcBN * 8; i += 64)
+        for (int i = max(first, 0) * 8 + lane; i < kTcBN * 8; i += 32)
 #pragma unroll
           for (int h = 0; h < L::kHalves; ++h)
             *reinterpret_cast<uint4*>(v + h * L::kBox + i * 16) = make_uint4(0, 0, 0, 0);
