@@ -13,6 +13,7 @@
 namespace ebd {
 
 constexpr int kMergeWarps = 8;
+constexpr int kMergeFlight = 4;  // pieces in flight per warp
 
 __device__ __forceinline__ void store_row(float* p, int lane, float4 v) {
   reinterpret_cast<float4*>(p)[lane] = v;
@@ -53,28 +54,55 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   if (r.b < 0) return;
   const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
   const int rows = min(bm, sp.n * a.group - r.m * bm);
-  // the item goes on through the first pieces of the following CTAs
+  // the item goes on through the first pieces of the following CTAs: up to the
+  // first that does not just continue it (32 records at a time)
   int c1 = c0 + 1;
-  while (c1 + 1 < n_cta && a.rec[c1].cont == 1) ++c1;
+  for (;; c1 += 32) {
+    const bool on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
+    const uint32_t off = ~__ballot_sync(0xffffffffu, on);
+    if (off) {
+      c1 += __ffs(off) - 1;
+      break;
+    }
+  }
   constexpr int D = 32 * (int)(sizeof(VT) / 4);
   const int hq = a.pv.n_kv_heads * a.group;
   for (int row = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); row < rows;
        row += gridDim.y * kMergeWarps) {
-    float M = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32)
-      M = fmaxf(M, a.part_lse[(size_t)(2 * c + (c == c0)) * bm + row]);
+    // lane i keeps the weight of piece i of 32; the rows' loads do not wait for it
+    const int n = c1 - c0 + 1;
+    float s0 = lane < n ? a.part_lse[(size_t)(2 * (c0 + lane) + (lane == 0)) * bm + row]
+                        : -INFINITY;
+    float M = s0;
+    for (int i = 32 + lane; i < n; i += 32)
+      M = fmaxf(M, a.part_lse[(size_t)(2 * (c0 + i)) * bm + row]);
     M = warp_max(M);
     const float base = M == -INFINITY ? 0.f : M;
     float sum = 0.f;
     VT o = {};
-#pragma unroll 4
-    for (int c = c0; c <= c1; ++c) {
-      const size_t slot = (size_t)(2 * c + (c == c0)) * bm + row;
-      const VT v = reinterpret_cast<const VT*>(a.part_o + slot * D)[lane];
-      const float f = exp2f(a.part_lse[slot] - base);
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      if (i0 > 0)
+        s0 = i0 + lane < n ? a.part_lse[(size_t)(2 * (c0 + i0 + lane)) * bm + row] : -INFINITY;
+      const float f = exp2f(s0 - base);
       sum += f;
-      add_scaled(o, f, v);
+      const int k = min(32, n - i0);
+      for (int j = 0; j < k; j += kMergeFlight) {
+        VT v[kMergeFlight];
+#pragma unroll
+        for (int e = 0; e < kMergeFlight; ++e) {
+          const int c = c0 + i0 + j + e;
+          if (j + e < k)
+            v[e] = reinterpret_cast<const VT*>(
+                a.part_o + ((size_t)(2 * c + (c == c0)) * bm + row) * D)[lane];
+        }
+#pragma unroll
+        for (int e = 0; e < kMergeFlight; ++e) {
+          const float fe = __shfl_sync(0xffffffffu, f, (j + e) & 31);
+          if (j + e < k) add_scaled(o, fe, v[e]);
+        }
+      }
     }
+    sum = warp_sum(sum);
     const int t = (r.m * bm + row) / a.group, g = (r.m * bm + row) - t * a.group;
     const long long out = (long long)(sp.t0 + t) * hq + r.h * a.group + g;
     store_row((T*)a.y + out * D, lane, scaled(o, sum == 0.f ? 0.f : 1.f / sum));
