@@ -200,7 +200,7 @@ extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cac
                                                       int32_t n_q_heads, int32_t max_new) {
   if (check_paged(cache) != EBD_OK || n_q_heads < 1 || max_new < 1) return 0;
   if (cache->dtype != EBD_BF16) return 0;
-  return paged_split_bytes(sm_count(), kTcAttnRows, cache->head_dim);
+  return paged_split_bytes(sm_count(), kTcSlotRows, cache->head_dim);
 }
 
 extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens,
@@ -221,8 +221,8 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   if (n_tokens == 0 || max_new == 0) return EBD_OK;
   if (!cu_new || !q || !y || !dev_status) return EBD_ERR_INVALID;
   const int wide = cache->dtype == EBD_F32 ? 4 : 8;
-  if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride % wide != 0 ||
-      q_head_stride % wide != 0)
+  if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride < 0 ||
+      q_head_stride < 0 || q_token_stride % wide != 0 || q_head_stride % wide != 0)
     return EBD_ERR_INVALID;
   const size_t need = ebd_paged_attention_workspace_bytes(cache, n_q_heads, max_new);
   if (ws_bytes < need) return EBD_ERR_CAPACITY;
@@ -248,7 +248,7 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
     return cache->head_dim == 128 ? launch_paged_simt<float, 128>(a, s)
                                   : launch_paged_simt<float, 64>(a, s);
   const int n_cta = sm_count();
-  paged_split_layout(a, workspace, n_cta, kTcAttnRows);
+  paged_split_layout(a, workspace, n_cta, kTcSlotRows);
   a.min_share = 4;
   return launch_paged_tc(a, *cache, n_cta, s);
 }

@@ -1,8 +1,8 @@
 // Work split and partial results shared by the paged-attention kernels.
 //
-// An item is one (sequence, KV head, m-tile): up to BM rows (row = new token x
-// query head of the group, token-major) over the key tiles of BN positions
-// that at least one row sees.  Items in order of (sequence, head, m-tile) form
+// An item is one (sequence, KV head, m-tile): `tokens` new tokens with the G query
+// heads of the group (row = token x head, token-major) over the key tiles of
+// BN positions that at least one row sees.  Items in order of (sequence, head, m-tile) form
 // one line of key tiles, and CTA c of n takes the tiles
 // [c share, (c + 1) share), whatever items they belong to: every CTA gets the
 // same number of tiles however ragged the batch is.  A CTA's range is cut at
@@ -43,23 +43,24 @@ struct PagedAttnArgs {
   // split results: slot 2 c of CTA c for a piece that continues an item, slot
   // 2 c + 1 for one that begins an item without ending it
   PieceRecord* rec;  // [n_cta]
-  float* part_lse;   // [2 n_cta][BM], log2 units
-  float* part_o;     // [2 n_cta][BM][D]
+  float* part_lse;   // [2 n_cta][slot rows], log2 units
+  float* part_o;     // [2 n_cta][slot rows][D]
+  int tokens;        // new tokens per item
+  int half_tokens;   // of those, how many the slot's first 128 rows hold
   int min_share;     // fewest key tiles per CTA
 };
 
-// Key tiles [kb, ke) of m-tile m; a tile with nothing to see keeps one (fully
+// Key tiles [kb, ke) of m-tile m; an item with nothing to see keeps one (fully
 // masked) tile, so that its rows get written.
-template <int BM, int BN>
-__device__ __forceinline__ void item_range(const PagedAttnArgs& a, const SeqSpan& sp, int m,
-                                           int& kb, int& ke) {
-  const int row0 = m * BM, last = min(sp.n * a.group, row0 + BM) - 1;
-  const int p0 = sp.len - sp.n;
-  const int k_end = p0 + last / a.group + 1;  // <= len
+template <int BN>
+__device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int len, int m, int& kb,
+                                           int& ke) {
+  const int first = m * a.tokens, last = min(n, first + a.tokens) - 1, p0 = len - n;
+  const int k_end = p0 + last + 1;  // <= len
   kb = 0;
   ke = 1;
   if (k_end > 0) {
-    if (a.window > 0) kb = max(0, p0 + row0 / a.group - a.window + 1) / BN;
+    if (a.window > 0) kb = max(0, p0 + first - a.window + 1) / BN;
     ke = (k_end + BN - 1) / BN;
   }
 }
@@ -79,7 +80,7 @@ __device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
 }
 
 // Key tiles of one head of the sequences base + lane (lane = 0..31).
-template <int BM, int BN>
+template <int BN>
 __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int base, int lane,
                                                     bool report) {
   const int b = base + lane;
@@ -88,24 +89,22 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
     if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
   }
-  const int mt = (sp.n * a.group + BM - 1) / BM;
+  const int mt = (sp.n + a.tokens - 1) / a.tokens;
   long long c = 0;
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
-    item_range<BM, BN>(a, sp, m, kb, ke);
+    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
     c += ke - kb;
   }
   // long chunks: the warp walks the remaining m-tiles of one sequence together
   for (uint32_t left = __ballot_sync(0xffffffffu, mt > 4); left; left &= left - 1) {
     const int src = __ffs(left) - 1;
-    SeqSpan s;
-    s.n = __shfl_sync(0xffffffffu, sp.n, src);
-    s.len = __shfl_sync(0xffffffffu, sp.len, src);
-    const int k = (s.n * a.group + BM - 1) / BM;
+    const int n = __shfl_sync(0xffffffffu, sp.n, src), len = __shfl_sync(0xffffffffu, sp.len, src);
+    const int k = __shfl_sync(0xffffffffu, mt, src);
     long long sum = 0;
     for (int m = 4 + lane; m < k; m += 32) {
       int kb, ke;
-      item_range<BM, BN>(a, s, m, kb, ke);
+      item_range<BN>(a, n, len, m, kb, ke);
       sum += ke - kb;
     }
 #pragma unroll
@@ -115,24 +114,29 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
   return c;
 }
 
+__device__ __forceinline__ long long divide(long long x, long long y) {
+  return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // The first tile and the number of tiles of CTA `cta`; one whole warp.
-template <int BM, int BN>
+template <int BN>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
   const int H = a.pv.n_kv_heads;
-  long long total = 0;
-  for (int base = 0; base < a.pv.batch; base += 32)
-    total += H * sequence_tiles<BM, BN>(a, base, lane, cta == 0);
+  long long total = 0, c = 0;
+  for (int base = 0; base < a.pv.batch; base += 32) {
+    c = sequence_tiles<BN>(a, base, lane, cta == 0);
+    total += H * c;
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  const long long share = max((long long)a.min_share, (total + n_cta - 1) / n_cta);
+  const long long share = max((long long)a.min_share, divide(total + n_cta - 1, n_cta));
   long long at = cta * share;
   WorkStart w = {0, 0, 0, 0, 0};
   if (at >= total) return w;
   w.count = min(share, total - at);
-  long long c = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
-    c = sequence_tiles<BM, BN>(a, base, lane, false);
+    if (a.pv.batch > 32) c = sequence_tiles<BN>(a, base, lane, false);
     const long long upto = warp_scan_add(c * H, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
@@ -144,13 +148,19 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
     }
     at -= __shfl_sync(0xffffffffu, upto, 31);
   }
-  w.h = (int)(at / c);
+  w.h = (int)divide(at, c);
   at -= w.h * c;
   const SeqSpan sp = seq_span(a.pv, a.cu, w.b, a.n_tokens, a.max_new);
-  const int mt = (sp.n * a.group + BM - 1) / BM;
+  const int mt = (sp.n + a.tokens - 1) / a.tokens;
+  if (mt == 1) {
+    int kb, ke;
+    item_range<BN>(a, sp.n, sp.len, 0, kb, ke);
+    w.cur = kb + (int)at;
+    return w;
+  }
   for (int base = 0; base < mt; base += 32) {
     int kb = 0, ke = 0;
-    if (base + lane < mt) item_range<BM, BN>(a, sp, base + lane, kb, ke);
+    if (base + lane < mt) item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
     const long long upto = warp_scan_add(ke - kb, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
@@ -166,7 +176,7 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
 }
 
 // Walks a CTA's pieces; every role of the CTA walks the same ones.
-template <int BM, int BN>
+template <int BN>
 struct PieceWalk {
   int b, h, m, mt;
   SeqSpan sp;
@@ -183,13 +193,15 @@ struct PieceWalk {
   }
   __device__ __forceinline__ void load(const PagedAttnArgs& a) {
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
-    mt = (sp.n * a.group + BM - 1) / BM;
-    item_range<BM, BN>(a, sp, m, kb, ke);
+    mt = (sp.n + a.tokens - 1) / a.tokens;
+    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
   }
   __device__ __forceinline__ bool live() const { return left > 0; }
-  __device__ __forceinline__ int rows(const PagedAttnArgs& a) const {
-    return min(BM, sp.n * a.group - m * BM);
+  // New tokens of the item, and the first one's number in the sequence.
+  __device__ __forceinline__ int tokens(const PagedAttnArgs& a) const {
+    return min(a.tokens, sp.n - m * a.tokens);
   }
+  __device__ __forceinline__ int first(const PagedAttnArgs& a) const { return m * a.tokens; }
   // Slot of this piece's partial result; -1: the piece is a whole item.
   __device__ __forceinline__ int slot(int cta) const {
     return cur > kb ? 2 * cta : (end < ke ? 2 * cta + 1 : -1);
@@ -198,7 +210,7 @@ struct PieceWalk {
     left -= end - cur;
     if (left <= 0) return;
     if (++m < mt) {
-      item_range<BM, BN>(a, sp, m, kb, ke);
+      item_range<BN>(a, sp.n, sp.len, m, kb, ke);
     } else {
       m = 0;
       if (++h == a.pv.n_kv_heads) {
@@ -211,7 +223,7 @@ struct PieceWalk {
           load(a);
         } while (mt == 0);
       } else {
-        item_range<BM, BN>(a, sp, m, kb, ke);
+        item_range<BN>(a, sp.n, sp.len, m, kb, ke);
       }
     }
     cur = kb;
@@ -220,10 +232,10 @@ struct PieceWalk {
 };
 
 // One thread of each CTA writes its record (before the merge kernel's wait).
-template <int BM, int BN>
+template <int BN>
 __device__ __forceinline__ void write_record(const PagedAttnArgs& a, const WorkStart& w, int cta) {
   PieceRecord r = {0, -1, 0, 0};
-  PieceWalk<BM, BN> p(a, w);
+  PieceWalk<BN> p(a, w);
   bool first = true;
   for (; p.live(); p.next(a)) {
     if (first && p.cur > p.kb) r.cont = p.end < p.ke ? 1 : 2;
@@ -237,17 +249,17 @@ __device__ __forceinline__ void write_record(const PagedAttnArgs& a, const WorkS
   a.rec[cta] = r;
 }
 
-// Joins the pieces of split items.  `a` as the attention kernel had it, rows_per_item = its BM.
-ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int rows_per_item,
+// Joins the pieces of split items.  `a` as the attention kernel had it.
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int slot_rows,
                               int n_cta, cudaStream_t s);
 
 // Bytes of the split results of n_cta CTAs.
-size_t paged_split_bytes(int n_cta, int rows_per_item, int head_dim);
+size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim);
 // Points a's split arrays into the workspace.
-void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int rows_per_item);
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int slot_rows);
 
-ebd_status launch_paged_tc(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
+ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
                            cudaStream_t s);
-constexpr int kTcAttnRows = 256;
+constexpr int kTcSlotRows = 256;  // rows of a partial result
 
 }  // namespace ebd

@@ -1,7 +1,7 @@
 // Paged attention on the 5th-generation tensor cores: bf16, head_dim 64 / 128.
 //
-// An item is 256 rows as two MMA tiles X = A, B of 128 rows; keys come in tiles
-// of 64.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
+// An item is two MMA tiles X = A, B of 128 rows, whole tokens with all heads of the
+// group each; keys come in tiles of 64.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
 // the softmax warps turn S_X into weights P_X, and O_X += P_X V with P_X read
 // from tensor memory.  Tensor memory (512 columns): O_A, O_B (128 columns each,
 // D used) and two buffers of 64 columns of S_A and of S_B; P_X (bf16) overwrites
@@ -23,7 +23,7 @@
 // Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warps 8 / 9 issue the
 // MMAs of A / B, warp 10 the TMA copies of K and V (one box per page and 64
 // channels; pages past the sequence's end are read past the pool's end, which
-// fills zeros), warp 11 brings the query rows into the swizzled layout and clears
+// fills zeros), warp 11 copies the query rows and clears
 // the value rows of a tile past the sequence's end (weight 0 times whatever a
 // page holds there must stay 0).
 //
@@ -44,7 +44,6 @@
 
 namespace ebd {
 
-constexpr int kTcBM = kTcAttnRows;
 constexpr int kTcBN = 64;
 constexpr int kTcAttnThreads = 384;
 
@@ -147,7 +146,8 @@ __device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int h, int 
 
 template <int D>
 __global__ void __launch_bounds__(kTcAttnThreads, 1)
-    paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmK,
+    paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
+                         const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV, const PagedAttnArgs a) {
   using L = PagedTcLayout<D>;
   constexpr int KS = L::kStages;
@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     tmem_relinquish();
   } else if (warp == 9) {
     if (lane == 0) {
-      mbar_init(&bar->q_full, 32);
+      mbar_init(&bar->q_full, 1);
       mbar_init(&bar->q_empty, 2);
       for (int x = 0; x < 2; ++x) {
         mbar_init(&bar->done[x], 1);
@@ -181,15 +181,21 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       fence_barrier_init();
     }
   } else if (warp == 0) {
-    const WorkStart w = find_work<kTcBM, kTcBN>(a, cta, gridDim.x, lane);
+    const WorkStart w = find_work<kTcBN>(a, cta, gridDim.x, lane);
     if (lane == 0) bar->start = w;
+  }
+  if (warp > 0) {
+    // the rows past an X's last query row are never loaded: numbers, once
+    for (int i = threadIdx.x - 32; i < 2 * L::kQTile / 16; i += kTcAttnThreads - 32)
+      *reinterpret_cast<uint4*>(smem + L::kQ + i * 16) = make_uint4(0, 0, 0, 0);
+    fence_proxy_async_smem();
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar->tmem;
   const WorkStart start = bar->start;
-  PieceWalk<kTcBM, kTcBN> w(a, start);
+  PieceWalk<kTcBN> w(a, start);
   bool ok = true;
 
   if (warp < 8) {
@@ -199,13 +205,14 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const uint32_t sS = tmem + 256 + x * 128 + lane_base;
     const uint32_t sO = tmem + x * 128 + lane_base;
     uint32_t it = 0;  // tiles of X so far: S buffer it & 1
-    if (threadIdx.x == 0) write_record<kTcBM, kTcBN>(a, start, cta);  // while the first tile loads
+    if (threadIdx.x == 0) write_record<kTcBN>(a, start, cta);  // while the first tile loads
     __syncwarp();
     for (; ok && w.live(); w.next(a)) {
-      const int rows = w.rows(a);
-      if (x * 128 >= rows) continue;  // no row of this X
-      const int r = min(x * 128 + row, rows - 1);  // rows past the end repeat the last one
-      const int tok = (w.m * kTcBM + r) / a.group, g = w.m * kTcBM + r - tok * a.group;
+      // the X's tokens [x0, x0 + tokens); rows past the last repeat its last token
+      const int x0 = x * a.half_tokens, tokens = min(w.tokens(a) - x0, a.half_tokens);
+      if (tokens <= 0) continue;
+      const int rt = row / a.group, g = row - rt * a.group;
+      const int tok = w.first(a) + x0 + min(rt, tokens - 1);
       const int pos = w.sp.len - w.sp.n + tok;
       const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
       float m = -INFINITY, l = 0.f;
@@ -296,11 +303,11 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       tc_fence_after();
       const int slot = w.slot(cta);
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      const bool mine = x * 128 + row < rows;
+      const bool mine = rt < tokens;
       const float lse2 = l == 0.f ? -INFINITY : m * a.scale2 + log2f(l);
       const long long out = (long long)(w.sp.t0 + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
-      const size_t prow = (size_t)slot * kTcBM + x * 128 + row;
+      const size_t prow = (size_t)slot * kTcSlotRows + x * 128 + row;
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
@@ -400,7 +407,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         return true;
       };
       for (; ok && w.live(); w.next(a), ++items) {
-        const bool two = w.rows(a) > 128;
+        const bool two = w.tokens(a) > a.half_tokens;
         const int n = w.end - w.cur;
         const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
         ok = mbar_wait_bounded(&bar->q_full, items & 1);
@@ -485,38 +492,22 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
     // ---------------- query rows; value rows past the end
-    constexpr int CH = D / 8;  // 16-byte chunks per row
     uint32_t items = 0, tile0 = 0;  // tiles before this piece
     for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
       if (items > 0 && !mbar_wait_warp(&bar->q_empty, (items - 1) & 1)) {
         ok = false;
         break;
       }
-      const int rows = w.rows(a), padded = rows > 128 ? 256 : 128;
-      // the lane's chunk of rows lane / CH, + 32 / CH, ..., as (token, head of the group)
-      const int c = lane % CH;
-      int tok = (w.m * kTcBM + lane / CH) / a.group;
-      int g = w.m * kTcBM + lane / CH - tok * a.group;
-      const __nv_bfloat16* q = (const __nv_bfloat16*)a.q + (long long)(w.sp.t0 + tok) * a.q_ts +
-                               (long long)(w.h * a.group + g) * a.q_hs + c * 8;
-      unsigned char* dst0 = smem + L::kQ + (c >> 3) * L::kQBox;
-#pragma unroll 4
-      for (int r = lane / CH; r < padded; r += 32 / CH) {
-        unsigned char* dst = dst0 + (r >> 7) * L::kQTile + (r & 127) * 128 +
-                             (((c & 7) ^ (r & 7)) << 4);
-        if (r < rows) cp_async16(dst, q);
-        else *reinterpret_cast<uint4*>(dst) = make_uint4(0, 0, 0, 0);
-        g += 32 / CH;
-        q += (32 / CH) * a.q_hs;
-        while (g >= a.group) {
-          g -= a.group;
-          q += a.q_ts - a.group * a.q_hs;
-        }
+      if (lane == 0) {
+        const int nx = w.tokens(a) > a.half_tokens ? 2 : 1;
+        mbar_arrive_expect_tx(&bar->q_full, nx * L::kHalves * a.half_tokens * a.group * 128);
+        for (int x = 0; x < nx; ++x)
+#pragma unroll
+          for (int h = 0; h < L::kHalves; ++h)
+            tma_load_3d(smem + L::kQ + x * L::kQTile + h * L::kQBox, &tmQ, h * 64, w.h * a.group,
+                        w.sp.t0 + w.first(a) + x * a.half_tokens, &bar->q_full);
       }
-      cp_async_commit();
-      cp_async_wait<0>();
-      fence_proxy_async_smem();
-      mbar_arrive(&bar->q_full);
+      __syncwarp();
       if (w.sp.len < w.end * kTcBN) {
         // The piece's last value tile.  Its stage's phase is certain only once the
         // piece's last S product is done (q_empty): the stage's earlier tile
@@ -580,27 +571,46 @@ static bool encode_pool(CUtensorMap* map, const ebd_paged_cache& c, const void* 
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Queries [token, head, channel]; box: 64 channels x the group's heads x the tokens
+// of one X.
+static bool encode_queries(CUtensorMap* map, const PagedAttnArgs& a, int head_dim) {
+  auto enc = paged_encoder();
+  if (!enc) return false;
+  const int hq = a.pv.n_kv_heads * a.group;
+  const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)hq, (cuuint64_t)a.n_tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)(hq > 1 ? a.q_hs * 2 : head_dim * 2),
+                                 (cuuint64_t)(a.n_tokens > 1 ? a.q_ts * 2 : head_dim * 2)};
+  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)a.half_tokens};
+  const cuuint32_t one[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.q), dims, strides, box,
+             one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D>
 static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
                               cudaStream_t s) {
-  CUtensorMap tmK, tmV;
+  CUtensorMap tmQ, tmK, tmV;
   const int box = c.page_size < kTcBN ? c.page_size : kTcBN;
-  if (!encode_pool(&tmK, c, c.K_pages, box) || !encode_pool(&tmV, c, c.V_pages, box))
+  if (!encode_queries(&tmQ, a, D) || !encode_pool(&tmK, c, c.K_pages, box) || !encode_pool(&tmV, c, c.V_pages, box))
     return EBD_ERR_CUDA;
   constexpr int smem = PagedTcLayout<D>::kBytes;
   if (cudaFuncSetAttribute(paged_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  paged_attn_tc_kernel<D><<<n_cta, kTcAttnThreads, smem, s>>>(tmK, tmV, a);
+  paged_attn_tc_kernel<D><<<n_cta, kTcAttnThreads, smem, s>>>(tmQ, tmK, tmV, a);
   return launch_status();
 }
 
-ebd_status launch_paged_tc(const PagedAttnArgs& a, const ebd_paged_cache& c, int n_cta,
+ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
                            cudaStream_t s) {
+  // whole tokens in each X of 128 rows (126 of them used at G = 7): one TMA box
+  a.half_tokens = 128 / a.group;
+  a.tokens = 2 * a.half_tokens;
   const ebd_status st =
       c.head_dim == 128 ? launch_tc_t<128>(a, c, n_cta, s) : launch_tc_t<64>(a, c, n_cta, s);
   if (st != EBD_OK) return st;
-  return launch_paged_merge(a, true, c.head_dim, kTcAttnRows, n_cta, s);
+  return launch_paged_merge(a, true, c.head_dim, kTcSlotRows, n_cta, s);
 }
 
 }  // namespace ebd

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const PieceRecord r = a.rec[c0];
   if (r.b < 0) return;
   const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
-  const int rows = min(bm, sp.n * a.group - r.m * bm);
+  const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.group;
   // the item goes on through the first pieces of the following CTAs: up to the
   // first that does not just continue it (32 records at a time)
   int c1 = c0 + 1;
@@ -67,8 +67,11 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   }
   constexpr int D = 32 * (int)(sizeof(VT) / 4);
   const int hq = a.pv.n_kv_heads * a.group;
-  for (int row = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); row < rows;
-       row += gridDim.y * kMergeWarps) {
+  for (int i = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); i < rows;
+       i += gridDim.y * kMergeWarps) {
+    // row i of the item is token t, head g; the slot's second half starts at row 128
+    const int t = i / a.group, g = i - t * a.group;
+    const int row = t < a.half_tokens ? i : 128 + i - a.half_tokens * a.group;
     // lane i keeps the weight of piece i of 32; the rows' loads do not wait for it
     const int n = c1 - c0 + 1;
     float s0 = lane < n ? a.part_lse[(size_t)(2 * (c0 + lane) + (lane == 0)) * bm + row]
@@ -103,35 +106,34 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
       }
     }
     sum = warp_sum(sum);
-    const int t = (r.m * bm + row) / a.group, g = (r.m * bm + row) - t * a.group;
-    const long long out = (long long)(sp.t0 + t) * hq + r.h * a.group + g;
+    const long long out = (long long)(sp.t0 + r.m * a.tokens + t) * hq + r.h * a.group + g;
     store_row((T*)a.y + out * D, lane, scaled(o, sum == 0.f ? 0.f : 1.f / sum));
     if (a.lse && lane == 0)
       a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
   }
 }
 
-size_t paged_split_bytes(int n_cta, int rows_per_item, int head_dim) {
-  const size_t rows = (size_t)2 * n_cta * rows_per_item;
+size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim) {
+  const size_t rows = (size_t)2 * n_cta * slot_rows;
   return align_up(n_cta * sizeof(PieceRecord), 256) + align_up(rows * 4, 256) +
          rows * head_dim * 4;
 }
 
-void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int rows_per_item) {
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int slot_rows) {
   char* p = (char*)ws;
   a.rec = (PieceRecord*)p;
   p += align_up(n_cta * sizeof(PieceRecord), 256);
   a.part_lse = (float*)p;
-  p += align_up((size_t)2 * n_cta * rows_per_item * 4, 256);
+  p += align_up((size_t)2 * n_cta * slot_rows * 4, 256);
   a.part_o = (float*)p;
 }
 
-ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int rows_per_item,
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int slot_rows,
                               int n_cta, cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
   cudaLaunchConfig_t cfg = {};
-  const long long most = min((long long)a.max_new * a.group, (long long)rows_per_item);
-  const int by = (int)((most + kMergeWarps - 1) / kMergeWarps);
+  const int most = min(a.max_new, a.tokens) * a.group;
+  const int by = (most + kMergeWarps - 1) / kMergeWarps;
   cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
   cfg.blockDim = dim3(kMergeWarps * 32);
   cfg.stream = s;
@@ -143,14 +145,14 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
   cudaError_t e;
   if (bf16)
     e = head_dim == 128
-            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float4>, a, rows_per_item,
+            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float4>, a, slot_rows,
                                  n_cta)
-            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float2>, a, rows_per_item,
+            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float2>, a, slot_rows,
                                  n_cta);
   else
     e = head_dim == 128
-            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float4>, a, rows_per_item, n_cta)
-            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float2>, a, rows_per_item, n_cta);
+            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float4>, a, slot_rows, n_cta)
+            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float2>, a, slot_rows, n_cta);
   return cuda_status(e);
 }
 
