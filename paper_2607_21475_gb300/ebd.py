@@ -199,15 +199,22 @@ def _ptr(t, dtype=None, shape=None, name="tensor", host_ok=False):
         raise ValueError(f"{name} must be contiguous")
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
+
+
+# torch.cuda.current_stream() builds a Stream object (microseconds per call);
+# the raw handle of the same stream is enough here
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _stream(stream):
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None and torch.cuda.is_initialized():
+        return _raw_stream(torch._C._cuda_getDevice())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _check(name, code):
@@ -222,7 +229,7 @@ def _workspace(nbytes, device, ws):
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
     if ws.numel() * ws.element_size() < nbytes:
         raise ValueError(f"workspace too small: {ws.numel() * ws.element_size()} < {nbytes}")
-    return ctypes.c_void_p(ws.data_ptr()), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 # ---------------------------------------------------------------- entry points
@@ -564,25 +571,27 @@ def alloc_paged(batch, n_kv_heads, n_pages, page_size, head_dim, max_blocks, dty
 
 def _paged(pc: PagedCache) -> EbdPagedCache:
     K, V, bt, n = pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len
-    if K.dim() != 4 or K.shape != V.shape or K.stride() != V.stride():
+    shape, stride = K.shape, K.stride()
+    if len(shape) != 4 or V.shape != shape or V.stride() != stride:
         raise ValueError("K_pages and V_pages must be [n_pages, Hkv, page_size, d] tensors of "
                          "equal shapes and strides")
     if not (K.is_cuda and V.is_cuda and bt.is_cuda and n.is_cuda):
         raise ValueError("a paged cache's tensors must be CUDA tensors")
-    if V.dtype != K.dtype:
-        raise TypeError(f"V_pages has dtype {V.dtype}, expected {K.dtype}")
+    dt = K.dtype
+    if V.dtype != dt:
+        raise TypeError(f"V_pages has dtype {V.dtype}, expected {dt}")
     if bt.dtype != torch.int32 or n.dtype != torch.int32:
         raise TypeError("block_table and seq_len must be int32")
-    B = n.shape[0]
-    if bt.dim() != 2 or n.dim() != 1 or bt.shape[0] != B or not (
+    if bt.dim() != 2 or n.dim() != 1 or bt.shape[0] != n.shape[0] or not (
             bt.is_contiguous() and n.is_contiguous()):
         raise ValueError("block_table must be a contiguous [B, max_blocks] and seq_len a "
                          "contiguous [B] tensor")
-    n_pages, H, page, d = K.shape
-    ps, hs, rs, cs = K.stride()
+    B, blocks = bt.shape
+    n_pages, H, page, d = shape
+    ps, hs, rs, cs = stride
     if cs != 1:
         raise ValueError("the last dimension of K_pages and V_pages must be contiguous")
-    return EbdPagedCache(_dtype_code(K), B, H, d, page, n_pages, bt.shape[1], 0, ps, hs, rs,
+    return EbdPagedCache(_dtype_code(K), B, H, d, page, n_pages, blocks, 0, ps, hs, rs,
                          K.data_ptr(), V.data_ptr(), bt.data_ptr(), n.data_ptr())
 
 
@@ -595,7 +604,7 @@ def _rows(t, dtype, n_tokens, n_heads, head_dim, name):
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if tuple(t.shape) != (n_tokens, n_heads, head_dim):
+    if t.shape != (n_tokens, n_heads, head_dim):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected "
                          f"{(n_tokens, n_heads, head_dim)}")
     ts, hs, cs = t.stride()
