@@ -1,33 +1,37 @@
 // Attention of each sequence's new tokens over its paged cache,
 //   y_i = sum_j softmax_j(scale q_i . k_j) v_j,  max(0, p_i - window + 1) <= j <= p_i,
-// and its log-sum-exp, with an online softmax: running maximum m, sum l and
-// output o in float32, rescaled by e^(m - m') when a tile raises the maximum.
+// and its log-sum-exp: the entry point, and the float32 kernel (the bf16 one is
+// in paged_attn_tc.cu).
 //
-// A CTA takes 32 rows of one (sequence, KV head): the G query heads of the
-// group times the new tokens, token-major, so that all heads of the group read
-// each key and value once.  Keys come in tiles of 64, converted to float32 in
-// shared memory.  128 threads as 8 x 16: thread (ty, tx) owns rows 4 ty .. + 3,
-// keys tx + 16 j of a tile's logits and channels 4 tx + 64 j of the output.
+// Online softmax: running maximum m, sum l and output o in float32, rescaled by
+// e^(m - m') when a tile raises the maximum.  An item is 32 rows, keys come in
+// tiles of 64 (32 at 128 channels, so that two CTAs fit an SM), the next tile
+// copied by cp.async while this one is worked on.  128 threads as 8 x 16: thread
+// (ty, tx) owns rows 4 ty .. + 3, keys tx + 16 j of a tile's logits and channels
+// 4 tx + 64 j of the output, so a 16-byte shared-memory load feeds 8 FMAs and
+// the FMA units are the bound.
 #include <cuda_runtime.h>
 #include <math.h>
 
 #include "common.cuh"
 #include "internal.h"
 #include "paged_attn.cuh"
+#include "ptx.cuh"
 
 namespace ebd {
 
 constexpr int kAttnRows = 32;
-constexpr int kAttnKeys = 64;
 constexpr int kAttnThreads = 128;
 
 template <int D>
 struct SimtLayout {
+  static constexpr int kKeys = D == 128 ? 32 : 64;
   static constexpr int kQ = 0;  // [rows][D + 4]
-  static constexpr int kK = kQ + kAttnRows * (D + 4);
-  static constexpr int kV = kK + kAttnKeys * (D + 4);
-  static constexpr int kP = kV + kAttnKeys * D;  // [rows][keys + 4]
-  static constexpr int kFloats = kP + kAttnRows * (kAttnKeys + 4);
+  static constexpr int kK = kQ + kAttnRows * (D + 4);      // [2][keys][D + 4]
+  static constexpr int kV = kK + 2 * kKeys * (D + 4);      // [2][keys][D]
+  static constexpr int kP = kV + 2 * kKeys * D;            // [rows][keys + 4]
+  static constexpr int kStart = kP + kAttnRows * (kKeys + 4);
+  static constexpr int kFloats = kStart + 8;
 };
 
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
@@ -37,159 +41,208 @@ __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
 __device__ __forceinline__ void store4(float* p, const float (&x)[4]) {
   *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
 }
-template <typename T, int D>
-__global__ void __launch_bounds__(kAttnThreads) paged_attn_simt_kernel(const PagedAttnArgs a) {
-  using L = SimtLayout<D>;
-  extern __shared__ float4 smem4[];
-  float* sm = reinterpret_cast<float*>(smem4);
-  float *Qs = sm + L::kQ, *Ks = sm + L::kK, *Vs = sm + L::kV, *Ps = sm + L::kP;
-  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-  const int b = blockIdx.z, h = blockIdx.y, row0 = blockIdx.x * kAttnRows;
-  const SeqSpan sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
-  if (sp.bad && threadIdx.x == 0 && h == 0 && row0 == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
-  const int rows = min(sp.n * a.group - row0, kAttnRows);
-  if (rows <= 0) return;
-  const int hq = a.pv.n_kv_heads * a.group;
-  const int p0 = sp.len - sp.n;  // position of the first new token
-
-  for (int i = threadIdx.x; i < kAttnRows * (D / 4); i += kAttnThreads) {
-    const int r = i / (D / 4), c = i % (D / 4) * 4;
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < rows) {
-      const int t = (row0 + r) / a.group, g = (row0 + r) - t * a.group;
-      load4((const T*)a.q + (sp.t0 + t) * a.q_ts + (h * a.group + g) * a.q_hs + c, x);
-    }
-    store4(Qs + r * (D + 4) + c, x);
-  }
-  int hi[4], lo[4];  // keys that this thread's rows see
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i, p = p0 + (row0 + min(r, rows - 1)) / a.group;
-    hi[i] = min(p + 1, sp.len);
-    lo[i] = a.window > 0 ? max(0, p - a.window + 1) : 0;
-  }
-  const int p_first = p0 + row0 / a.group, p_last = p0 + (row0 + rows - 1) / a.group;
-  const int k_end = min(p_last + 1, sp.len);
-  const int k_begin = (a.window > 0 ? max(0, p_first - a.window + 1) : 0) / kAttnKeys * kAttnKeys;
-
-  float m[4], l[4], o[4][D / 16];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
-  }
-  for (int k0 = k_begin; k0 < k_end; k0 += kAttnKeys) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < kAttnKeys * (D / 4); i += kAttnThreads) {
-      const int r = i / (D / 4), c = i % (D / 4) * 4, pos = k0 + r;
-      float kx[4] = {0.f, 0.f, 0.f, 0.f}, vx[4] = {0.f, 0.f, 0.f, 0.f};
-      if (pos < k_end) {  // what lies past the last key seen is never read
-        const int page = page_of(a.pv, b, pos);
-        if (page >= 0) {
-          const long long off = slot_offset(a.pv, page, h, pos) + c;
-          load4((const T*)a.K_pages + off, kx);
-          load4((const T*)a.V_pages + off, vx);
-        } else {
-          raise_status(a.dev_status, EBD_DEV_RANGE);
-        }
-      }
-      store4(Ks + r * (D + 4) + c, kx);
-      store4(Vs + r * D + c, vx);
-    }
-    __syncthreads();
-    float s[4][4] = {};
-#pragma unroll 4
-    for (int c = 0; c < D; c += 4) {
-      float q[4][4], k[4][4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) load4(Ks + (tx + 16 * j) * (D + 4) + c, k[j]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[i][j] = fmaf(q[i][e], k[j][e], s[i][j]);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float top = m[i];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int pos = k0 + tx + 16 * j;
-        s[i][j] = pos >= lo[i] && pos < hi[i] ? s[i][j] * a.scale2 : -INFINITY;
-        top = fmaxf(top, s[i][j]);
-      }
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-      const float base = top == -INFINITY ? 0.f : top;  // nothing seen yet: every weight is 0
-      const float f = exp2f(m[i] - base);
-      m[i] = top;
-      float sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float p = exp2f(s[i][j] - base);
-        sum += p;
-        Ps[(ty * 4 + i) * (kAttnKeys + 4) + tx + 16 * j] = p;
-      }
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-      l[i] = l[i] * f + sum;
-#pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
-    }
-    __syncwarp();
-    const int nk = min(kAttnKeys, k_end - k0);
-    for (int k = 0; k < nk; ++k) {
-      float p[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) p[i] = Ps[(ty * 4 + i) * (kAttnKeys + 4) + k];
-#pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        float v[4];
-        load4(Vs + k * D + c * 64 + tx * 4, v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          // a key that the row does not see adds nothing, whatever its value holds
-          if (k0 + k >= lo[i] && k0 + k < hi[i]) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][c * 4 + e] = fmaf(p[i], v[e], o[i][c * 4 + e]);
-          }
-      }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i;
-    if (r >= rows) continue;
-    const int t = (row0 + r) / a.group, g = (row0 + r) - t * a.group;
-    const long long out = (long long)(sp.t0 + t) * hq + h * a.group + g;
-    const float inv = l[i] > 0.f ? 1.f / l[i] : (l[i] == 0.f ? 0.f : l[i]);  // NaN stays
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = o[i][c * 4 + e] * inv;
-      store4((T*)a.y + out * D + c * 64 + tx * 4, x);
-    }
-    if (a.lse && tx == 0) a.lse[out] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
-  }
+// 16 bytes global -> shared; zeros when `ok` is false (nothing is read then).
+__device__ __forceinline__ void cp_async16_or_zero(void* dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src),
+               "r"(ok ? 16 : 0)
+               : "memory");
 }
 
-template <typename T, int D>
-static ebd_status launch_paged_simt(const PagedAttnArgs& a, cudaStream_t s) {
+template <int D>
+__global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const PagedAttnArgs a) {
+  using L = SimtLayout<D>;
+  constexpr int BN = L::kKeys, NK = BN / 16;  // keys per thread
+  extern __shared__ float4 smem4[];
+  float* sm = reinterpret_cast<float*>(smem4);
+  float *Qs = sm + L::kQ, *Ps = sm + L::kP;
+  const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+  WorkStart* start_s = reinterpret_cast<WorkStart*>(sm + L::kStart);
+  if (threadIdx.x < 32) {
+    const WorkStart w = find_work<BN>(a, blockIdx.x, gridDim.x, threadIdx.x);
+    if (threadIdx.x == 0) {
+      *start_s = w;
+      write_record<BN>(a, w, blockIdx.x);
+    }
+  }
+  __syncthreads();
+  bool bad = false;
+  for (PieceWalk<BN> w(a, *start_s); w.live(); w.next(a)) {
+    const HeadSlice hs = head_slice(a, w.h);
+    const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);
+    const int p0 = w.sp.len - w.sp.n + w.first(a);  // position of the item's first token
+    auto copy = [&](int j) {  // key tile j into stage j & 1
+      float *Ks = sm + L::kK + (j & 1) * BN * (D + 4), *Vs = sm + L::kV + (j & 1) * BN * D;
+#pragma unroll 4
+      for (int i = threadIdx.x; i < BN * (D / 4); i += kAttnThreads) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4, pos = j * BN + r;
+        // what lies past the sequence's end is never read
+        const int page = pos < w.sp.len ? page_of(a.pv, w.b, pos) : -1;
+        bad |= page < 0 && pos < w.sp.len;
+        const long long off = page < 0 ? 0 : slot_offset(a.pv, page, hs.kvh, pos) + c;
+        cp_async16_or_zero(Ks + r * (D + 4) + c, (const float*)a.K_pages + off, page >= 0);
+        cp_async16_or_zero(Vs + r * D + c, (const float*)a.V_pages + off, page >= 0);
+      }
+      cp_async_commit();
+    };
+    __syncthreads();  // the last piece's readers are done
+    copy(w.cur);
+    for (int i = threadIdx.x; i < kAttnRows * (D / 4); i += kAttnThreads) {
+      const int r = i / (D / 4), c = i % (D / 4) * 4, t = r / a.slice, g = r - t * a.slice;
+      float x[4] = {0.f, 0.f, 0.f, 0.f};
+      if (t < tokens && g < hs.n)
+        load4((const float*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs + c, x);
+      store4(Qs + r * (D + 4) + c, x);
+    }
+    int hi[4], lo[4];  // keys that this thread's rows see
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int p = p0 + min((ty * 4 + i) / a.slice, tokens - 1);
+      hi[i] = p + 1;
+      lo[i] = a.window > 0 ? max(0, p - a.window + 1) : 0;
+    }
+    float m[4], l[4], o[4][D / 16];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
+    }
+    for (int j = w.cur; j < w.end; ++j) {
+      const int k0 = j * BN;
+      const float *Ks = sm + L::kK + (j & 1) * BN * (D + 4), *Vs = sm + L::kV + (j & 1) * BN * D;
+      cp_async_wait<0>();
+      __syncthreads();  // tile j is there for all, and stage j + 1 is read no more
+      if (j + 1 < w.end) copy(j + 1);
+      float s[4][NK] = {};
+#pragma unroll 4
+      for (int c = 0; c < D; c += 4) {
+        float q[4][4], k[NK][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
+#pragma unroll
+        for (int e = 0; e < NK; ++e) load4(Ks + (tx + 16 * e) * (D + 4) + c, k[e]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < NK; ++e)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) s[i][e] = fmaf(q[i][z], k[e][z], s[i][e]);
+      }
+      bool all = true;  // every row of the warp sees every key of the tile
+#pragma unroll
+      for (int i = 0; i < 4; ++i) all = all && lo[i] <= k0 && hi[i] >= k0 + BN;
+      all = __all_sync(0xffffffffu, all);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float top = m[i];
+#pragma unroll
+        for (int e = 0; e < NK; ++e) {
+          const int pos = k0 + tx + 16 * e;
+          s[i][e] = all || (pos >= lo[i] && pos < hi[i]) ? s[i][e] * a.scale2 : -INFINITY;
+          top = fmaxf(top, s[i][e]);
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+        const float base = top == -INFINITY ? 0.f : top;  // nothing seen yet: every weight is 0
+        const float f = exp2f(m[i] - base);
+        m[i] = top;
+        float sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < NK; ++e) {
+          const float p = exp2f(s[i][e] - base);
+          sum += p;
+          Ps[(ty * 4 + i) * (BN + 4) + tx + 16 * e] = p;
+        }
+#pragma unroll
+        for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+        l[i] = l[i] * f + sum;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+      }
+      __syncwarp();  // a warp reads the weights of its own rows only
+      if (all) {
+#pragma unroll 2
+        for (int k = 0; k < BN; k += 4) {
+          float p[4][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load4(Ps + (ty * 4 + i) * (BN + 4) + k, p[i]);
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              float v[4];
+              load4(Vs + (k + z) * D + c * 64 + tx * 4, v);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  o[i][c * 4 + e] = fmaf(p[i][z], v[e], o[i][c * 4 + e]);
+            }
+        }
+      } else {
+        for (int k = 0; k < BN; ++k) {
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = Ps[(ty * 4 + i) * (BN + 4) + k];
+#pragma unroll
+          for (int c = 0; c < D / 64; ++c) {
+            float v[4];
+            load4(Vs + k * D + c * 64 + tx * 4, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              // a key that the row does not see adds nothing, whatever its value holds
+              if (k0 + k >= lo[i] && k0 + k < hi[i]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[i][c * 4 + e] = fmaf(p[i], v[e], o[i][c * 4 + e]);
+              }
+          }
+        }
+      }
+      __syncwarp();  // before the next tile's weights
+    }
+    const int slot = w.slot(blockIdx.x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
+      if (t >= tokens || g >= hs.n) continue;
+      const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+      const size_t prow = (size_t)slot * kAttnRows + r;
+      float* dst = slot < 0 ? (float*)a.y + out * D : a.part_o + prow * D;
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+      for (int c = 0; c < D / 64; ++c) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = o[i][c * 4 + e] * inv;
+        store4(dst + c * 64 + tx * 4, x);
+      }
+      const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
+      if (tx == 0 && slot >= 0) a.part_lse[prow] = lse2;
+      if (tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
+    }
+  }
+  if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
+}
+
+constexpr int kAttnCtasPerSm = 2;
+
+template <int D>
+static ebd_status launch_paged_f32(PagedAttnArgs a, cudaStream_t s) {
   const int smem = SimtLayout<D>::kFloats * 4;
-  auto kern = paged_attn_simt_kernel<T, D>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) !=
-      cudaSuccess)
+  if (cudaFuncSetAttribute(paged_attn_f32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  const long long mt = ((long long)a.max_new * a.group + kAttnRows - 1) / kAttnRows;
-  if (mt > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
-  kern<<<dim3((unsigned)mt, a.pv.n_kv_heads, a.pv.batch), kAttnThreads, smem, s>>>(a);
-  return launch_status();
+  a.slices = (a.group + kAttnRows - 1) / kAttnRows;
+  a.slice = (a.group + a.slices - 1) / a.slices;
+  a.heads = a.pv.n_kv_heads * a.slices;
+  a.tokens = a.half_tokens = kAttnRows / a.slice;
+  a.min_share = 2;
+  const int n_cta = sm_count() * kAttnCtasPerSm;
+  paged_attn_f32_kernel<D><<<n_cta, kAttnThreads, smem, s>>>(a);
+  const ebd_status st = launch_status();
+  if (st != EBD_OK) return st;
+  return launch_paged_merge(a, false, D, kAttnRows, n_cta, s);
 }
 
 }  // namespace ebd
@@ -199,7 +252,8 @@ using namespace ebd;
 extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cache,
                                                       int32_t n_q_heads, int32_t max_new) {
   if (check_paged(cache) != EBD_OK || n_q_heads < 1 || max_new < 1) return 0;
-  if (cache->dtype != EBD_BF16) return 0;
+  if (cache->dtype == EBD_F32)
+    return paged_split_bytes(sm_count() * kAttnCtasPerSm, kAttnRows, cache->head_dim);
   return paged_split_bytes(sm_count(), kTcSlotRows, cache->head_dim);
 }
 
@@ -244,9 +298,10 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   a.scale2 = scale * kLog2e;
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
-  if (cache->dtype == EBD_F32)
-    return cache->head_dim == 128 ? launch_paged_simt<float, 128>(a, s)
-                                  : launch_paged_simt<float, 64>(a, s);
+  if (cache->dtype == EBD_F32) {
+    paged_split_layout(a, workspace, sm_count() * kAttnCtasPerSm, kAttnRows);
+    return cache->head_dim == 128 ? launch_paged_f32<128>(a, s) : launch_paged_f32<64>(a, s);
+  }
   const int n_cta = sm_count();
   paged_split_layout(a, workspace, n_cta, kTcSlotRows);
   a.min_share = 4;

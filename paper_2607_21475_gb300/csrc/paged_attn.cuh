@@ -1,6 +1,6 @@
 // Work split and partial results shared by the paged-attention kernels.
 //
-// An item is one (sequence, KV head, m-tile): `tokens` new tokens with the G query
+// An item is one (sequence, KV head, m-tile): `tokens` new tokens with the query
 // heads of the group (row = token x head, token-major) over the key tiles of
 // BN positions that at least one row sees.  Items in order of (sequence, head, m-tile) form
 // one line of key tiles, and CTA c of n takes the tiles
@@ -45,10 +45,27 @@ struct PagedAttnArgs {
   PieceRecord* rec;  // [n_cta]
   float* part_lse;   // [2 n_cta][slot rows], log2 units
   float* part_o;     // [2 n_cta][slot rows][D]
+  // A kernel with few rows per item cuts a large group into slices of at most
+  // `slice` query heads; each slice is a head of its own on the line of items.
+  int heads;         // KV heads x slices
+  int slices, slice;
   int tokens;        // new tokens per item
   int half_tokens;   // of those, how many the slot's first 128 rows hold
   int min_share;     // fewest key tiles per CTA
 };
+
+// KV head, first query head and number of query heads of (sliced) head h.
+struct HeadSlice {
+  int kvh, q0, n;
+};
+__device__ __forceinline__ HeadSlice head_slice(const PagedAttnArgs& a, int h) {
+  HeadSlice s;
+  s.kvh = a.slices == 1 ? h : h / a.slices;
+  const int g0 = (h - s.kvh * a.slices) * a.slice;
+  s.q0 = s.kvh * a.group + g0;
+  s.n = min(a.slice, a.group - g0);
+  return s;
+}
 
 // Key tiles [kb, ke) of m-tile m; an item with nothing to see keeps one (fully
 // masked) tile, so that its rows get written.
@@ -122,7 +139,7 @@ __device__ __forceinline__ long long divide(long long x, long long y) {
 template <int BN>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
-  const int H = a.pv.n_kv_heads;
+  const int H = a.heads;
   long long total = 0, c = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
     c = sequence_tiles<BN>(a, base, lane, cta == 0);
@@ -213,7 +230,7 @@ struct PieceWalk {
       item_range<BN>(a, sp.n, sp.len, m, kb, ke);
     } else {
       m = 0;
-      if (++h == a.pv.n_kv_heads) {
+      if (++h == a.heads) {
         h = 0;
         do {
           if (++b >= a.pv.batch) {  // the arrays changed under the call: stop

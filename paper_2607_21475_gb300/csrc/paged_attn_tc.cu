@@ -605,6 +605,9 @@ static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, 
 ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
                            cudaStream_t s) {
   // whole tokens in each X of 128 rows (126 of them used at G = 7): one TMA box
+  a.heads = a.pv.n_kv_heads;
+  a.slices = 1;
+  a.slice = a.group;
   a.half_tokens = 128 / a.group;
   a.tokens = 2 * a.half_tokens;
   const ebd_status st =

@@ -53,7 +53,8 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const PieceRecord r = a.rec[c0];
   if (r.b < 0) return;
   const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
-  const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.group;
+  const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.slice;
+  const HeadSlice hs = head_slice(a, r.h);
   // the item goes on through the first pieces of the following CTAs: up to the
   // first that does not just continue it (32 records at a time)
   int c1 = c0 + 1;
@@ -70,8 +71,9 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   for (int i = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); i < rows;
        i += gridDim.y * kMergeWarps) {
     // row i of the item is token t, head g; the slot's second half starts at row 128
-    const int t = i / a.group, g = i - t * a.group;
-    const int row = t < a.half_tokens ? i : 128 + i - a.half_tokens * a.group;
+    const int t = i / a.slice, g = i - t * a.slice;
+    if (g >= hs.n) continue;
+    const int row = t < a.half_tokens ? i : 128 + i - a.half_tokens * a.slice;
     // lane i keeps the weight of piece i of 32; the rows' loads do not wait for it
     const int n = c1 - c0 + 1;
     float s0 = lane < n ? a.part_lse[(size_t)(2 * (c0 + lane) + (lane == 0)) * bm + row]
@@ -106,7 +108,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
       }
     }
     sum = warp_sum(sum);
-    const long long out = (long long)(sp.t0 + r.m * a.tokens + t) * hq + r.h * a.group + g;
+    const long long out = (long long)(sp.t0 + r.m * a.tokens + t) * hq + hs.q0 + g;
     store_row((T*)a.y + out * D, lane, scaled(o, sum == 0.f ? 0.f : 1.f / sum));
     if (a.lse && lane == 0)
       a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
@@ -132,7 +134,7 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
                               int n_cta, cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
   cudaLaunchConfig_t cfg = {};
-  const int most = min(a.max_new, a.tokens) * a.group;
+  const int most = min(a.max_new, a.tokens) * a.slice;
   const int by = (most + kMergeWarps - 1) / kMergeWarps;
   cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
   cfg.blockDim = dim3(kMergeWarps * 32);
