@@ -135,7 +135,8 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
   if (n_cta <= 1) return EBD_OK;
   cudaLaunchConfig_t cfg = {};
   const int most = min(a.max_new, a.tokens) * a.slice;
-  const int by = (most + kMergeWarps - 1) / kMergeWarps;
+  // four rows per warp: a block's chain of loads up to the first row is as long as a row
+  const int by = (most + 4 * kMergeWarps - 1) / (4 * kMergeWarps);
   cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
   cfg.blockDim = dim3(kMergeWarps * 32);
   cfg.stream = s;

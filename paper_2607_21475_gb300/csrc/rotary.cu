@@ -27,6 +27,7 @@
 namespace ebd {
 
 constexpr int kRotWarps = 8;
+constexpr int kRotBlocks = 4;  // resident blocks of 256 threads: 64 registers per thread
 
 __global__ void rotary_table_kernel(const double* __restrict__ inv_freq, int n_freq,
                                     long long total, double mscale, float2* __restrict__ table) {
@@ -66,8 +67,9 @@ struct RotaryArgs {
   const float2* table;       // [n_pos, rot / 2]; null: no rotation
   int n_pos;
   int n_tokens, n_x, n_kv;   // heads of x; kv heads (0: rotary)
-  int units;                 // chunk pairs (half) or chunks (pairs) of a row
-  int rot_units;             // how many of them are rotated
+  int head_dim;
+  int units;                 // pairs of chunks of a row
+  int rot_units;             // how many of them are rotated (pairs: in part or whole)
   int half_off;              // half layout: rot / 2
   int rot;
   int parts;                 // warps per token
@@ -76,37 +78,68 @@ struct RotaryArgs {
   int32_t* dev_status;
 };
 
-// A lane's share of one row: chunk c1, and in the half layout c2.
-template <typename T, int VEC, bool PAIRS>
+// A lane's share of one row: two chunks.
+template <typename T, int VEC>
 struct Piece {
   Chunk<T, VEC> a, b;
 };
 
-// HALF layout: unit u < rot_units is the chunk pair (u VEC, rot / 2 + u VEC);
-// later units are the chunk pairs of the copied channels, in order.
-template <typename T, int VEC, bool PAIRS>
+// Channels of unit u's chunks (c2 < 0: the row has no second one).  Half layout:
+// units below rot_units are the chunk pairs (u VEC, rot / 2 + u VEC) that turn
+// together, later ones neighbouring chunks of the copied channels.  Pairs layout:
+// neighbouring chunks, turned where they lie below rot.
+template <int VEC, bool PAIRS>
 __device__ __forceinline__ void unit_channels(const RotaryArgs& a, int u, int& c1, int& c2) {
-  if (PAIRS) {
+  if (!PAIRS && u < a.rot_units) {
     c1 = u * VEC;
-    c2 = -1;
-  } else if (u < a.rot_units) {
-    c1 = u * VEC;
-    c2 = a.half_off + u * VEC;
+    c2 = a.half_off + c1;
   } else {
-    c1 = a.rot + (u - a.rot_units) * VEC;
-    c2 = -1;
+    c1 = PAIRS ? 2 * u * VEC : a.rot + 2 * (u - a.rot_units) * VEC;
+    c2 = c1 + VEC < a.head_dim ? c1 + VEC : -1;
   }
 }
 
 // STEADY: 32 * parts is a multiple of the units, so that a lane keeps its unit
-// (and its angles) from head to head.
+// (and its angles) from head to head.  Rows are loaded one step ahead: the first
+// ones before the token's place is known, the next ones before these are stored.
 template <typename T, int VEC, bool PAIRS, bool APPEND, bool STEADY>
-__global__ void __launch_bounds__(kRotWarps * 32, 4) rotary_kernel(const RotaryArgs a) {
-  constexpr int kRows = 2;  // rows in flight per lane
+__global__ void __launch_bounds__(kRotWarps * 32, kRotBlocks) rotary_kernel(const RotaryArgs a) {
   const int lane = threadIdx.x & 31;
   const long long w = (long long)blockIdx.x * kRotWarps + (threadIdx.x >> 5);
   const int t = a.parts == 1 ? (int)w : (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
   if (t >= a.n_tokens) return;
+
+  const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
+  const int stride = 32 * a.parts, step = stride / a.units, rest = stride - step * a.units;
+  int h = (part * 32 + lane) / a.units, u = part * 32 + lane - h * a.units;
+  const T* xp = (const T*)a.x.p + t * a.x.ts;
+  const T* kp = (const T*)a.k.p + t * a.k.ts;
+  const T* vp = (const T*)a.v.p + t * a.v.ts;
+  auto load = [&](int h, int u, Piece<T, VEC>& r) {
+    if (h >= heads) return;
+    int c1, c2;
+    unit_channels<VEC, PAIRS>(a, u, c1, c2);
+    const T* src = !APPEND || h < a.n_x  ? xp + h * a.x.hs
+                   : h < a.n_x + a.n_kv ? kp + (h - a.n_x) * a.k.hs
+                                        : vp + (h - a.n_x - a.n_kv) * a.v.hs;
+    r.a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
+    if (c2 >= 0) r.b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
+  };
+  auto next = [&](int& h, int& u) {
+    h += step;
+    if (!STEADY) {
+      u += rest;
+      if (u >= a.units) {
+        u -= a.units;
+        ++h;
+      }
+    }
+  };
+  Piece<T, VEC> r0, r1;
+  int h1 = h, u1 = u;
+  next(h1, u1);
+  load(h, u, r0);
+  load(h1, u1, r1);
 
   int pos, b = 0, page = -1;
   if (APPEND) {
@@ -117,21 +150,20 @@ __global__ void __launch_bounds__(kRotWarps * 32, 4) rotary_kernel(const RotaryA
     }
     pos = a.pv.seq_len[b] - (a.cu[b + 1] - t);
     page = page_of(a.pv, b, pos);
-    if (page < 0 && lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
   } else {
     pos = a.positions[t];
   }
   const int tpos = min(max(pos, 0), a.n_pos - 1);
-  if (a.table && tpos != pos && lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
 
-  constexpr int kFreq = PAIRS ? VEC / 2 : VEC;
-  float cs[kFreq], sn[kFreq];
+  float cs[VEC], sn[VEC];  // the pairs of a unit
   auto load_angles = [&](int u) {
     if (u >= a.rot_units) return;
-    const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * kFreq;
-    if (kFreq % 2 == 0 && a.wide_table) {
+    const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * VEC;
+    const int n = PAIRS ? min(VEC, a.rot / 2 - u * VEC) : VEC;
+    if (VEC % 2 == 0 && a.wide_table) {
 #pragma unroll
-      for (int i = 0; i + 1 < kFreq; i += 2) {
+      for (int i = 0; i + 1 < VEC; i += 2) {
+        if (PAIRS && i >= n) break;
         const float4 f = __ldg(reinterpret_cast<const float4*>(row + i));
         cs[i] = f.x;
         sn[i] = f.y * a.sin_sign;
@@ -140,83 +172,68 @@ __global__ void __launch_bounds__(kRotWarps * 32, 4) rotary_kernel(const RotaryA
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kFreq; ++i) {
+      for (int i = 0; i < VEC; ++i) {
+        if (PAIRS && i >= n) break;
         const float2 f = __ldg(row + i);
         cs[i] = f.x;
         sn[i] = f.y * a.sin_sign;
       }
     }
   };
-  auto turn = [&](Piece<T, VEC, PAIRS>& r) {
-    if (PAIRS) {
+  if (STEADY) load_angles(u);
+  if (lane == 0 && ((APPEND && page < 0) || (a.table && tpos != pos)))
+    raise_status(a.dev_status, EBD_DEV_RANGE);
+  T* yp = (T*)a.y.p + t * a.y.ts;
+  const long long slot = page >= 0 ? slot_offset(a.pv, page, 0, pos) : -1;
+  // turns and stores one row's piece
+  auto store = [&](int h, int u, Piece<T, VEC>& r) {
+    if (h >= heads) return;
+    int c1, c2;
+    unit_channels<VEC, PAIRS>(a, u, c1, c2);
+    const bool is_v = APPEND && h >= a.n_x + a.n_kv;
+    if (u < a.rot_units && !is_v) {
+      if (!STEADY) load_angles(u);
+      auto turn = [&](T& e0, T& e1, int i) {
+        const float p = to_f32(e0), q = to_f32(e1);
+        from_f32(p * cs[i] - q * sn[i], e0);
+        from_f32(q * cs[i] + p * sn[i], e1);
+      };
+      if (PAIRS) {
 #pragma unroll
-      for (int i = 0; i < kFreq; ++i) {
-        const float p = to_f32(r.a.e[2 * i]), q = to_f32(r.a.e[2 * i + 1]);
-        from_f32(p * cs[i] - q * sn[i], r.a.e[2 * i]);
-        from_f32(q * cs[i] + p * sn[i], r.a.e[2 * i + 1]);
+        for (int i = 0; i < VEC / 2; ++i) turn(r.a.e[2 * i], r.a.e[2 * i + 1], i);
+        if (c2 >= 0 && c2 < a.rot) {
+#pragma unroll
+          for (int i = 0; i < VEC / 2; ++i)
+            turn(r.b.e[2 * i], r.b.e[2 * i + 1], VEC / 2 + i);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) turn(r.a.e[i], r.b.e[i], i);
       }
+    }
+    T* dst;
+    if (!APPEND || h < a.n_x) {
+      dst = yp + h * a.y.hs;
     } else {
-#pragma unroll
-      for (int i = 0; i < kFreq; ++i) {
-        const float p = to_f32(r.a.e[i]), q = to_f32(r.b.e[i]);
-        from_f32(p * cs[i] - q * sn[i], r.a.e[i]);
-        from_f32(q * cs[i] + p * sn[i], r.b.e[i]);
-      }
+      if (slot < 0) return;
+      const int kh = h - a.n_x - (is_v ? a.n_kv : 0);
+      dst = (T*)(is_v ? a.V_pages : a.K_pages) + slot + kh * a.pv.head_stride;
     }
+    *reinterpret_cast<Chunk<T, VEC>*>(dst + c1) = r.a;
+    if (c2 >= 0) *reinterpret_cast<Chunk<T, VEC>*>(dst + c2) = r.b;
   };
-
-  const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
-  const int stride = 32 * a.parts, step = stride / a.units, rest = stride - step * a.units;
-  int h = (part * 32 + lane) / a.units, u = part * 32 + lane - h * a.units;
-  int c1, c2;
-  unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
-  if (STEADY && h < heads && (a.table || !APPEND)) load_angles(u);
   while (h < heads) {
-    Piece<T, VEC, PAIRS> r[kRows];
-    T* dst[kRows];
-    int us[kRows], hs[kRows];
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      dst[k] = nullptr;
-      us[k] = u;
-      hs[k] = h;
-      if (h < heads) {
-        if (!STEADY) unit_channels<T, VEC, PAIRS>(a, u, c1, c2);
-        const T* src;
-        if (!APPEND || h < a.n_x) {
-          src = (const T*)a.x.p + t * a.x.ts + h * a.x.hs;
-          dst[k] = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
-        } else {
-          const bool is_v = h >= a.n_x + a.n_kv;
-          const int kh = h - a.n_x - (is_v ? a.n_kv : 0);
-          src = is_v ? (const T*)a.v.p + t * a.v.ts + kh * a.v.hs
-                     : (const T*)a.k.p + t * a.k.ts + kh * a.k.hs;
-          if (page >= 0)
-            dst[k] = (T*)(is_v ? a.V_pages : a.K_pages) + slot_offset(a.pv, page, kh, pos);
-        }
-        r[k].a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
-        if (c2 >= 0) r[k].b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
-      }
-      h += step;
-      if (!STEADY) {
-        u += rest;
-        if (u >= a.units) {
-          u -= a.units;
-          ++h;
-        }
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < kRows; ++k) {
-      if (!dst[k]) continue;
-      if (!STEADY) unit_channels<T, VEC, PAIRS>(a, us[k], c1, c2);
-      if (us[k] < a.rot_units && !(APPEND && hs[k] >= a.n_x + a.n_kv)) {
-        if (!STEADY) load_angles(us[k]);
-        turn(r[k]);
-      }
-      *reinterpret_cast<Chunk<T, VEC>*>(dst[k] + c1) = r[k].a;
-      if (c2 >= 0) *reinterpret_cast<Chunk<T, VEC>*>(dst[k] + c2) = r[k].b;
-    }
+    store(h, u, r0);
+    h = h1;
+    u = u1;
+    next(h, u);
+    load(h, u, r0);
+    if (h1 >= heads) break;
+    store(h1, u1, r1);
+    h1 = h;
+    u1 = u;
+    next(h1, u1);
+    load(h1, u1, r1);
   }
 }
 
@@ -230,8 +247,11 @@ static ebd_status launch_rotary_v(RotaryArgs a, int head_dim, cudaStream_t s) {
   const int rot = a.table ? a.rot : 0;
   a.rot = rot;
   a.half_off = rot / 2;
-  a.rot_units = PAIRS ? rot / VEC : rot / 2 / VEC;
-  a.units = a.rot_units + (head_dim - rot) / VEC;
+  a.head_dim = head_dim;
+  const int chunks_of_rot = rot / VEC, chunks_of_row = head_dim / VEC;
+  a.rot_units = PAIRS ? (chunks_of_rot + 1) / 2 : chunks_of_rot / 2;
+  a.units = PAIRS ? (chunks_of_row + 1) / 2
+                  : a.rot_units + (chunks_of_row - chunks_of_rot + 1) / 2;
   a.wide_table = rot % 4 == 0 && (uintptr_t)a.table % 16 == 0;
   const int chunks = (a.n_x + (APPEND ? 2 * a.n_kv : 0)) * a.units;
   // one chunk pair per lane while the call has fewer warps than the GPU holds
