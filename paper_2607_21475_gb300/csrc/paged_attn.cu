@@ -14,6 +14,7 @@
 #include <math.h>
 
 #include "common.cuh"
+#include "decode_tile.cuh"
 #include "internal.h"
 #include "paged_attn.cuh"
 #include "ptx.cuh"
@@ -57,16 +58,17 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const P
   float *Qs = sm + L::kQ, *Ps = sm + L::kP;
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   WorkStart* start_s = reinterpret_cast<WorkStart*>(sm + L::kStart);
+  grid_dependency_wait();
   if (threadIdx.x < 32) {
     const WorkStart w = find_work<BN>(a, blockIdx.x, gridDim.x, threadIdx.x);
-    if (threadIdx.x == 0) {
-      *start_s = w;
-      write_record<BN>(a, w, blockIdx.x);
-    }
+    if (threadIdx.x == 0) *start_s = w;
   }
   __syncthreads();
-  bool bad = false;
+  bool bad = false, first = true;
+  PieceRecord record = {0, -1, 0, 0};
   for (PieceWalk<BN> w(a, *start_s); w.live(); w.next(a)) {
+    record_piece(record, w, first);
+    first = false;
     const HeadSlice hs = head_slice(a, w.h);
     const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);
     const int p0 = w.sp.len - w.sp.n + w.first(a);  // position of the item's first token
@@ -222,6 +224,7 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const P
       if (tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
     }
   }
+  if (threadIdx.x == 0) a.rec[blockIdx.x] = record;
   if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
 }
 
@@ -238,9 +241,10 @@ static ebd_status launch_paged_f32(PagedAttnArgs a, cudaStream_t s) {
   a.heads = a.pv.n_kv_heads * a.slices;
   a.tokens = a.half_tokens = kAttnRows / a.slice;
   a.min_share = 2;
+  a.item_cost = 0;
   const int n_cta = sm_count() * kAttnCtasPerSm;
-  paged_attn_f32_kernel<D><<<n_cta, kAttnThreads, smem, s>>>(a);
-  const ebd_status st = launch_status();
+  const ebd_status st =
+      launch_dependent(paged_attn_f32_kernel<D>, dim3(n_cta), kAttnThreads, smem, s, a);
   if (st != EBD_OK) return st;
   return launch_paged_merge(a, false, D, kAttnRows, n_cta, s);
 }
@@ -305,5 +309,6 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   const int n_cta = sm_count();
   paged_split_layout(a, workspace, n_cta, kTcSlotRows);
   a.min_share = 4;
+  a.item_cost = 4;
   return launch_paged_tc(a, *cache, n_cta, s);
 }

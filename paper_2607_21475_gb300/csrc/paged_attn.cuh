@@ -3,9 +3,10 @@
 // An item is one (sequence, KV head, m-tile): `tokens` new tokens with the query
 // heads of the group (row = token x head, token-major) over the key tiles of
 // BN positions that at least one row sees.  Items in order of (sequence, head, m-tile) form
-// one line of key tiles, and CTA c of n takes the tiles
-// [c share, (c + 1) share), whatever items they belong to: every CTA gets the
-// same number of tiles however ragged the batch is.  A CTA's range is cut at
+// one line of work, each as long as its key tiles and `item_cost` tiles more (the
+// time that beginning and ending an item takes), and CTA c of n takes
+// [c share, (c + 1) share) of it, whatever items that belongs to: every CTA gets
+// the same work however ragged the batch is.  A CTA's range is cut at
 // item boundaries into pieces; the pieces of an item that more than one CTA
 // holds leave (o / l, log2-sum) in the workspace and a merge kernel joins them
 // in CTA order, so results do not depend on timing.  The lengths are on the
@@ -51,7 +52,8 @@ struct PagedAttnArgs {
   int slices, slice;
   int tokens;        // new tokens per item
   int half_tokens;   // of those, how many the slot's first 128 rows hold
-  int min_share;     // fewest key tiles per CTA
+  int min_share;     // least work per CTA, in key tiles
+  int item_cost;     // work of an item beside its key tiles, in key tiles
 };
 
 // KV head, first query head and number of query heads of (sliced) head h.
@@ -83,8 +85,9 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
 }
 
 struct WorkStart {
-  int b, h, m, cur;
-  long long count;  // key tiles of this CTA
+  int b, h, m;
+  int off;          // work of the item that earlier CTAs have
+  long long count;  // work of this CTA
 };
 
 __device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
@@ -96,7 +99,7 @@ __device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
   return v;
 }
 
-// Key tiles of one head of the sequences base + lane (lane = 0..31).
+// Work of one head of the sequences base + lane (lane = 0..31).
 template <int BN>
 __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int base, int lane,
                                                     bool report) {
@@ -111,7 +114,7 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
-    c += ke - kb;
+    c += ke - kb + a.item_cost;
   }
   // long chunks: the warp walks the remaining m-tiles of one sequence together
   for (uint32_t left = __ballot_sync(0xffffffffu, mt > 4); left; left &= left - 1) {
@@ -122,7 +125,7 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
     for (int m = 4 + lane; m < k; m += 32) {
       int kb, ke;
       item_range<BN>(a, n, len, m, kb, ke);
-      sum += ke - kb;
+      sum += ke - kb + a.item_cost;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -135,7 +138,7 @@ __device__ __forceinline__ long long divide(long long x, long long y) {
   return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
-// The first tile and the number of tiles of CTA `cta`; one whole warp.
+// Where CTA `cta` begins on the line, and how much of it is its own; one whole warp.
 template <int BN>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
@@ -170,21 +173,18 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
   const SeqSpan sp = seq_span(a.pv, a.cu, w.b, a.n_tokens, a.max_new);
   const int mt = (sp.n + a.tokens - 1) / a.tokens;
   if (mt == 1) {
-    int kb, ke;
-    item_range<BN>(a, sp.n, sp.len, 0, kb, ke);
-    w.cur = kb + (int)at;
+    w.off = (int)at;
     return w;
   }
   for (int base = 0; base < mt; base += 32) {
-    int kb = 0, ke = 0;
+    int kb = 0, ke = -a.item_cost;
     if (base + lane < mt) item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
-    const long long upto = warp_scan_add(ke - kb, lane);
+    const long long work = ke - kb + a.item_cost, upto = warp_scan_add(work, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
       const int src = __ffs(past) - 1;
-      at -= __shfl_sync(0xffffffffu, upto - (ke - kb), src);
       w.m = base + src;
-      w.cur = __shfl_sync(0xffffffffu, kb, src) + (int)at;
+      w.off = (int)(at - __shfl_sync(0xffffffffu, upto - work, src));
       break;
     }
     at -= __shfl_sync(0xffffffffu, upto, 31);
@@ -199,21 +199,32 @@ struct PieceWalk {
   SeqSpan sp;
   int kb, ke;    // the item's tiles
   int cur, end;  // this piece's
-  long long left;
+  long long left;  // work after this piece; -1: no piece
 
   __device__ __forceinline__ PieceWalk(const PagedAttnArgs& a, const WorkStart& w)
       : b(w.b), h(w.h), m(w.m), left(w.count) {
-    if (left <= 0) return;
+    if (left <= 0) {
+      left = -1;
+      return;
+    }
     load(a);
-    cur = w.cur;
-    end = (int)min((long long)ke, cur + left);
+    take(a, w.off);
+    if (cur == end) next(a);
   }
   __device__ __forceinline__ void load(const PagedAttnArgs& a) {
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
     mt = (sp.n + a.tokens - 1) / a.tokens;
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
   }
-  __device__ __forceinline__ bool live() const { return left > 0; }
+  // This CTA's tiles of the item, of which earlier CTAs have `off`: an item's own
+  // cost comes first, so a share that ends within it has no tile.
+  __device__ __forceinline__ void take(const PagedAttnArgs& a, int off) {
+    const int most = ke - kb + a.item_cost - off, mine = (int)min((long long)most, left);
+    cur = kb + max(0, off - a.item_cost);
+    end = kb + max(0, off + mine - a.item_cost);
+    left -= mine;
+  }
+  __device__ __forceinline__ bool live() const { return left >= 0; }
   // New tokens of the item, and the first one's number in the sequence.
   __device__ __forceinline__ int tokens(const PagedAttnArgs& a) const {
     return min(a.tokens, sp.n - m * a.tokens);
@@ -224,46 +235,62 @@ struct PieceWalk {
     return cur > kb ? 2 * cta : (end < ke ? 2 * cta + 1 : -1);
   }
   __device__ __forceinline__ void next(const PagedAttnArgs& a) {
-    left -= end - cur;
-    if (left <= 0) return;
-    if (++m < mt) {
-      item_range<BN>(a, sp.n, sp.len, m, kb, ke);
-    } else {
-      m = 0;
-      if (++h == a.heads) {
-        h = 0;
-        do {
-          if (++b >= a.pv.batch) {  // the arrays changed under the call: stop
-            left = 0;
-            return;
-          }
-          load(a);
-        } while (mt == 0);
-      } else {
-        item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+    do {
+      if (left <= 0) {
+        left = -1;
+        return;
       }
-    }
-    cur = kb;
-    end = (int)min((long long)ke, cur + left);
+      if (++m < mt) {
+        item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+      } else {
+        m = 0;
+        if (++h == a.heads) {
+          h = 0;
+          do {
+            if (++b >= a.pv.batch) {  // the arrays changed under the call: stop
+              left = -1;
+              return;
+            }
+            load(a);
+          } while (mt == 0);
+        } else {
+          item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+        }
+      }
+      take(a, 0);
+    } while (cur == end);
   }
 };
 
-// One thread of each CTA writes its record (before the merge kernel's wait).
+// Enters a piece into the CTA's record.
 template <int BN>
-__device__ __forceinline__ void write_record(const PagedAttnArgs& a, const WorkStart& w, int cta) {
-  PieceRecord r = {0, -1, 0, 0};
-  PieceWalk<BN> p(a, w);
-  bool first = true;
-  for (; p.live(); p.next(a)) {
-    if (first && p.cur > p.kb) r.cont = p.end < p.ke ? 1 : 2;
-    else if (p.end < p.ke) {
-      r.b = p.b;
-      r.h = p.h;
-      r.m = p.m;
-    }
-    first = false;
+__device__ __forceinline__ void record_piece(PieceRecord& r, const PieceWalk<BN>& p, bool first) {
+  if (first && p.cur > p.kb) {
+    r.cont = p.end < p.ke ? 1 : 2;
+  } else if (p.end < p.ke) {
+    r.b = p.b;
+    r.h = p.h;
+    r.m = p.m;
   }
-  a.rec[cta] = r;
+}
+
+// Launches a kernel as a programmatic dependent of whatever precedes it in the
+// stream: its prologue overlaps that kernel's tail (it waits before it reads or
+// writes memory).
+template <typename... Params, typename... Args>
+inline ebd_status launch_dependent(void (*kern)(Params...), dim3 grid, int threads, int smem,
+                                   cudaStream_t s, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cuda_status(cudaLaunchKernelEx(&cfg, kern, args...));
 }
 
 // Joins the pieces of split items.  `a` as the attention kernel had it.

@@ -23,7 +23,7 @@
 // Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warps 8 / 9 issue the
 // MMAs of A / B, warp 10 the TMA copies of K and V (one box per page and 64
 // channels; pages past the sequence's end are read past the pool's end, which
-// fills zeros), warp 11 copies the query rows and clears
+// fills zeros), warp 11 walks the CTA's pieces, copies the query rows and clears
 // the value rows of a tile past the sequence's end (weight 0 times whatever a
 // page holds there must stay 0).
 //
@@ -59,18 +59,31 @@ struct PagedTcLayout {
   static constexpr int kK = 2 * kQTile;
   static constexpr int kV = kK + kStages * kTile;
   static constexpr int kBar = kV + kStages * kTile;
-  static constexpr int kBytes = kBar + 512;
+  static constexpr int kBytes = kBar + 1024;
 };
+
+// One piece of the CTA's work, as the roles see it.
+struct Piece {
+  int cur, end;     // key tiles; equal: no piece, the work is done
+  int b, h, len;    // sequence, KV head, keys in the cache
+  int token;        // packed number of the first token
+  int pos;          // its position
+  int tokens;
+  int slot;         // partial result, -1: the output itself
+};
+constexpr int kPieceSlots = 4;
+constexpr int kPieceReaders = 11;  // warps that read a piece
 
 struct TcBars {
   uint64_t q_full, q_empty;
   uint64_t s_full[2][2], p_full[2][2], o_full[2][2];  // [X][S buffer]
   uint64_t fixed, done[2];
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8];
-  WorkStart start;
+  uint64_t piece_full[kPieceSlots], piece_empty[kPieceSlots];
+  Piece piece[kPieceSlots];
   uint32_t tmem;
 };
-static_assert(sizeof(TcBars) <= 512, "barriers");
+static_assert(sizeof(TcBars) <= 1024, "barriers");
 
 // max(a, b, c) in one instruction.
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -172,6 +185,10 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         }
       }
       mbar_init(&bar->fixed, 32);
+      for (int i = 0; i < kPieceSlots; ++i) {
+        mbar_init(&bar->piece_full[i], 1);
+        mbar_init(&bar->piece_empty[i], kPieceReaders);
+      }
       for (int s = 0; s < KS; ++s) {
         mbar_init(&bar->k_full[s], 1);
         mbar_init(&bar->k_empty[s], 2);
@@ -180,23 +197,30 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       }
       fence_barrier_init();
     }
-  } else if (warp == 0) {
-    const WorkStart w = find_work<kTcBN>(a, cta, gridDim.x, lane);
-    if (lane == 0) bar->start = w;
   }
-  if (warp > 0) {
-    // the rows past an X's last query row are never loaded: numbers, once
-    for (int i = threadIdx.x - 32; i < 2 * L::kQTile / 16; i += kTcAttnThreads - 32)
-      *reinterpret_cast<uint4*>(smem + L::kQ + i * 16) = make_uint4(0, 0, 0, 0);
-    fence_proxy_async_smem();
-  }
+  // the rows past an X's last query row are never loaded: numbers, once
+  for (int i = threadIdx.x; i < 2 * L::kQTile / 16; i += kTcAttnThreads)
+    *reinterpret_cast<uint4*>(smem + L::kQ + i * 16) = make_uint4(0, 0, 0, 0);
+  fence_proxy_async_smem();
+  grid_dependency_wait();  // nothing of the caller's was read or written so far
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bar->tmem;
-  const WorkStart start = bar->start;
-  PieceWalk<kTcBN> w(a, start);
   bool ok = true;
+  // The i-th piece; a reading warp takes it with read_piece and hands its place
+  // back with drop_piece.
+  auto read_piece = [&](uint32_t i, Piece& w) {
+    if (!mbar_wait_warp(&bar->piece_full[i % kPieceSlots], (i / kPieceSlots) & 1))
+      return ok = false;
+    w = bar->piece[i % kPieceSlots];
+    return w.cur < w.end;
+  };
+  auto drop_piece = [&](uint32_t i) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&bar->piece_empty[i % kPieceSlots]);
+  };
+  Piece w;
 
   if (warp < 8) {
     // ---------------- softmax and epilogue: one row per thread
@@ -205,15 +229,13 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const uint32_t sS = tmem + 256 + x * 128 + lane_base;
     const uint32_t sO = tmem + x * 128 + lane_base;
     uint32_t it = 0;  // tiles of X so far: S buffer it & 1
-    if (threadIdx.x == 0) write_record<kTcBN>(a, start, cta);  // while the first tile loads
-    __syncwarp();
-    for (; ok && w.live(); w.next(a)) {
+    const int rt = row / a.group, g = row - rt * a.group;
+    for (uint32_t i = 0; read_piece(i, w); drop_piece(i++)) {
       // the X's tokens [x0, x0 + tokens); rows past the last repeat its last token
-      const int x0 = x * a.half_tokens, tokens = min(w.tokens(a) - x0, a.half_tokens);
+      const int x0 = x * a.half_tokens, tokens = min(w.tokens - x0, a.half_tokens);
       if (tokens <= 0) continue;
-      const int rt = row / a.group, g = row - rt * a.group;
-      const int tok = w.first(a) + x0 + min(rt, tokens - 1);
-      const int pos = w.sp.len - w.sp.n + tok;
+      const int tok = x0 + min(rt, tokens - 1);
+      const int pos = w.pos + tok;
       const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
       float m = -INFINITY, l = 0.f;
       for (int j = w.cur; j < w.end; ++j, ++it) {
@@ -301,11 +323,11 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         break;
       }
       tc_fence_after();
-      const int slot = w.slot(cta);
+      const int slot = w.slot;
       const float inv = l == 0.f ? 0.f : 1.f / l;
       const bool mine = rt < tokens;
       const float lse2 = l == 0.f ? -INFINITY : m * a.scale2 + log2f(l);
-      const long long out = (long long)(w.sp.t0 + tok) * (a.pv.n_kv_heads * a.group) +
+      const long long out = (long long)(w.token + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
       const size_t prow = (size_t)slot * kTcSlotRows + x * 128 + row;
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
@@ -347,8 +369,8 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         if (slot >= 0) a.part_lse[prow] = lse2;
         else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
         if (nan_groups)
-          mend_row<D>(a, w.b, w.h, w.sp.t0 + tok, g, w.cur * kTcBN, lo, hi,
-                      min(w.end * kTcBN, w.sp.len), m == -INFINITY ? 0.f : m * a.scale2, inv,
+          mend_row<D>(a, w.b, w.h, w.token + tok, g, w.cur * kTcBN, lo, hi,
+                      min(w.end * kTcBN, w.len), m == -INFINITY ? 0.f : m * a.scale2, inv,
                       nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
                       slot < 0 ? nullptr : a.part_o + prow * D);
       }
@@ -406,10 +428,16 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         if (++vs == KS) vs = 0, vph ^= 1;
         return true;
       };
-      for (; ok && w.live(); w.next(a), ++items) {
-        const bool two = w.tokens(a) > a.half_tokens;
-        const int n = w.end - w.cur;
-        const bool ragged_end = w.sp.len < w.end * kTcBN;  // value rows to be cleared first
+      for (; ok; ++items) {
+        const uint32_t at = items % kPieceSlots;
+        ok = mbar_wait_bounded(&bar->piece_full[at], (items / kPieceSlots) & 1);
+        if (!ok) break;
+        const int n = bar->piece[at].end - bar->piece[at].cur;
+        const bool two = bar->piece[at].tokens > a.half_tokens;
+        // value rows to be cleared first
+        const bool ragged_end = bar->piece[at].len < bar->piece[at].end * kTcBN;
+        mbar_arrive(&bar->piece_empty[at]);
+        if (n <= 0) break;
         ok = mbar_wait_bounded(&bar->q_full, items & 1);
         if (x == 1 && !two) {
           // A does the item alone.  B still follows every stage and gives its
@@ -444,13 +472,13 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const int page = 1 << a.pv.page_shift;
     const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
     bool bad = false;
-    for (; ok && w.live(); w.next(a)) {
+    for (uint32_t i = 0; ok && read_piece(i, w); drop_piece(i++)) {
       // lane i: one box of a tile (keys bx * box .., channels half * 64 ..); its
       // page is looked up a tile ahead, past the pool where there is none
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
       auto page_at = [&](int j) {
         const int pos = j * kTcBN + bx * box;
-        if (bx >= boxes || pos >= w.sp.len) return a.pv.n_pages;
+        if (bx >= boxes || pos >= w.len) return a.pv.n_pages;
         const int p = page_of(a.pv, w.b, pos);
         if (p < 0) bad = true;
         return p < 0 ? a.pv.n_pages : p;
@@ -491,24 +519,61 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     for (uint32_t i = nv > KS ? nv - KS : 0; i < nv; ++i)
       mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
-    // ---------------- query rows; value rows past the end
-    uint32_t items = 0, tile0 = 0;  // tiles before this piece
-    for (; ok && w.live(); tile0 += w.end - w.cur, w.next(a), ++items) {
+    // ---------------- the CTA's pieces; query rows; value rows past the end
+    const WorkStart start = find_work<kTcBN>(a, cta, gridDim.x, lane);
+    PieceWalk<kTcBN> walk(a, start);
+    uint32_t items = 0, pushed = 0, tile0 = 0;  // tile0: tiles before this piece
+    bool all = false;  // the end of the work was told
+    PieceRecord record = {0, -1, 0, 0};
+    for (;; tile0 += w.end - w.cur, ++items) {
+      // two pieces ahead: the one two before this must have been dropped by then
+      for (; !all && pushed < items + 3; ++pushed) {
+        const uint32_t at = pushed % kPieceSlots;
+        if (pushed >= kPieceSlots &&
+            !mbar_wait_warp(&bar->piece_empty[at], (pushed / kPieceSlots - 1) & 1)) {
+          ok = false;
+          break;
+        }
+        Piece p = {};
+        all = !walk.live();
+        if (!all) {
+          p.cur = walk.cur;
+          p.end = walk.end;
+          p.b = walk.b;
+          p.h = walk.h;
+          p.len = walk.sp.len;
+          p.token = walk.sp.t0 + walk.first(a);
+          p.pos = walk.sp.len - walk.sp.n + walk.first(a);
+          p.tokens = walk.tokens(a);
+          p.slot = walk.slot(cta);
+          record_piece(record, walk, pushed == 0);
+          walk.next(a);
+        } else if (lane == 0) {
+          a.rec[cta] = record;
+        }
+        if (lane == 0) {
+          bar->piece[at] = p;
+          mbar_arrive(&bar->piece_full[at]);
+        }
+        __syncwarp();
+      }
+      if (!ok || items + 1 >= pushed) break;  // the last one pushed says that there are no more
+      w = bar->piece[items % kPieceSlots];
       if (items > 0 && !mbar_wait_warp(&bar->q_empty, (items - 1) & 1)) {
         ok = false;
         break;
       }
       if (lane == 0) {
-        const int nx = w.tokens(a) > a.half_tokens ? 2 : 1;
+        const int nx = w.tokens > a.half_tokens ? 2 : 1;
         mbar_arrive_expect_tx(&bar->q_full, nx * L::kHalves * a.half_tokens * a.group * 128);
         for (int x = 0; x < nx; ++x)
 #pragma unroll
           for (int h = 0; h < L::kHalves; ++h)
             tma_load_3d(smem + L::kQ + x * L::kQTile + h * L::kQBox, &tmQ, h * 64, w.h * a.group,
-                        w.sp.t0 + w.first(a) + x * a.half_tokens, &bar->q_full);
+                        w.token + x * a.half_tokens, &bar->q_full);
       }
       __syncwarp();
-      if (w.sp.len < w.end * kTcBN) {
+      if (w.len < w.end * kTcBN) {
         // The piece's last value tile.  Its stage's phase is certain only once the
         // piece's last S product is done (q_empty): the stage's earlier tile
         // has landed by then, and no later one can take the stage before the
@@ -519,7 +584,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           ok = false;
           break;
         }
-        const int first = w.sp.len - (w.end - 1) * kTcBN;  // rows from here on are cleared
+        const int first = w.len - (w.end - 1) * kTcBN;  // rows from here on are cleared
         unsigned char* v = smem + L::kV + (at % KS) * L::kTile;
         for (int i = max(first, 0) * 8 + lane; i < kTcBN * 8; i += 32)
 #pragma unroll
@@ -598,8 +663,8 @@ static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, 
   if (cudaFuncSetAttribute(paged_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  paged_attn_tc_kernel<D><<<n_cta, kTcAttnThreads, smem, s>>>(tmQ, tmK, tmV, a);
-  return launch_status();
+  return launch_dependent(paged_attn_tc_kernel<D>, dim3(n_cta), kTcAttnThreads, smem, s, tmQ, tmK,
+                          tmV, a);
 }
 
 ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,

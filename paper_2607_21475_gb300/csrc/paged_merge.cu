@@ -133,30 +133,20 @@ void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int slot_rows) {
 ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int slot_rows,
                               int n_cta, cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
-  cudaLaunchConfig_t cfg = {};
   const int most = min(a.max_new, a.tokens) * a.slice;
-  // four rows per warp: a block's chain of loads up to the first row is as long as a row
-  const int by = (most + 4 * kMergeWarps - 1) / (4 * kMergeWarps);
-  cfg.gridDim = dim3((unsigned)(n_cta - 1), (unsigned)by);
-  cfg.blockDim = dim3(kMergeWarps * 32);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  cudaError_t e;
+  const dim3 grid(n_cta - 1, (most + kMergeWarps - 1) / kMergeWarps);
+  const int threads = kMergeWarps * 32;
+  if (bf16 && head_dim == 128)
+    return launch_dependent(paged_merge_kernel<__nv_bfloat16, float4>, grid, threads, 0, s, a,
+                            slot_rows, n_cta);
   if (bf16)
-    e = head_dim == 128
-            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float4>, a, slot_rows,
-                                 n_cta)
-            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<__nv_bfloat16, float2>, a, slot_rows,
-                                 n_cta);
-  else
-    e = head_dim == 128
-            ? cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float4>, a, slot_rows, n_cta)
-            : cudaLaunchKernelEx(&cfg, paged_merge_kernel<float, float2>, a, slot_rows, n_cta);
-  return cuda_status(e);
+    return launch_dependent(paged_merge_kernel<__nv_bfloat16, float2>, grid, threads, 0, s, a,
+                            slot_rows, n_cta);
+  if (head_dim == 128)
+    return launch_dependent(paged_merge_kernel<float, float4>, grid, threads, 0, s, a, slot_rows,
+                            n_cta);
+  return launch_dependent(paged_merge_kernel<float, float2>, grid, threads, 0, s, a, slot_rows,
+                          n_cta);
 }
 
 }  // namespace ebd
