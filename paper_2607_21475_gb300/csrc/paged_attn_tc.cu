@@ -473,15 +473,27 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
     bool bad = false;
     for (uint32_t i = 0; ok && read_piece(i, w); drop_piece(i++)) {
-      // lane i: one box of a tile (keys bx * box .., channels half * 64 ..); its
-      // page is looked up a tile ahead, past the pool where there is none
+      // lane i: one box of a tile (keys bx * box .., channels half * 64 ..).  The
+      // lanes look up 32 pages at a time (a lookup per tile would hold up the
+      // copies by its latency); past the pool where there is none.
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
+      int block0 = 0, entry = 0, held = 0;  // pages of blocks block0 .. + held - 1
       auto page_at = [&](int j) {
-        const int pos = j * kTcBN + bx * box;
-        if (bx >= boxes || pos >= w.len) return a.pv.n_pages;
-        const int p = page_of(a.pv, w.b, pos);
-        if (p < 0) bad = true;
-        return p < 0 ? a.pv.n_pages : p;
+        const int first = (j * kTcBN) >> a.pv.page_shift;
+        const int last = (j * kTcBN + kTcBN - 1) >> a.pv.page_shift;
+        if (last >= block0 + held) {
+          block0 = first;
+          held = 32;
+          const int blk = block0 + lane, pos = blk << a.pv.page_shift;
+          entry = a.pv.n_pages;
+          if (blk < a.pv.max_blocks && pos < w.len) {
+            const int p = page_of(a.pv, w.b, pos);
+            if (p >= 0) entry = p;
+            else bad = true;
+          }
+        }
+        return __shfl_sync(0xffffffffu, entry,
+                           (((j * kTcBN + bx * box) >> a.pv.page_shift) - block0) & 31);
       };
       auto copy = [&](const CUtensorMap* tm, int base, uint64_t* full, uint64_t* empty,
                       uint32_t n, int j, int pg) {
@@ -495,12 +507,12 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         __syncwarp();
         return true;
       };
-      int pg = page_at(w.cur), next_pg = w.cur + 1 < w.end ? page_at(w.cur + 1) : 0;
+      int pg = page_at(w.cur), next_pg = 0;
       ok = copy(&tmK, L::kK, bar->k_full, bar->k_empty, nk, w.cur, pg);
       if (ok) ++nk;
       for (int j = w.cur; ok && j < w.end; ++j) {
-        const int ahead = j + 2 < w.end ? page_at(j + 2) : 0;
         if (j + 1 < w.end) {
+          next_pg = page_at(j + 1);
           ok = copy(&tmK, L::kK, bar->k_full, bar->k_empty, nk, j + 1, next_pg);
           if (!ok) break;
           ++nk;
@@ -509,7 +521,6 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         if (!ok) break;
         ++nv;
         pg = next_pg;
-        next_pg = ahead;
       }
     }
     if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
