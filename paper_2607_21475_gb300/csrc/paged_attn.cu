@@ -26,12 +26,14 @@ constexpr int kAttnThreads = 128;
 
 template <int D>
 struct SimtLayout {
-  static constexpr int kKeys = D == 128 ? 32 : 64;
+  static constexpr int kKeys = 32;
+  static constexpr int kCtasPerSm = D == 128 ? 2 : 4;
   static constexpr int kQ = 0;  // [rows][D + 4]
   static constexpr int kK = kQ + kAttnRows * (D + 4);      // [2][keys][D + 4]
   static constexpr int kV = kK + 2 * kKeys * (D + 4);      // [2][keys][D]
   static constexpr int kP = kV + 2 * kKeys * D;            // [rows][keys + 4]
-  static constexpr int kStart = kP + kAttnRows * (kKeys + 4);
+  static constexpr int kOff = kP + kAttnRows * (kKeys + 4);  // [2][keys] row offsets, 64 bits
+  static constexpr int kStart = kOff + 4 * kKeys;
   static constexpr int kFloats = kStart + 8;
 };
 
@@ -50,12 +52,14 @@ __device__ __forceinline__ void cp_async16_or_zero(void* dst, const void* src, b
 }
 
 template <int D>
-__global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const PagedAttnArgs a) {
+__global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
+    paged_attn_f32_kernel(const PagedAttnArgs a) {
   using L = SimtLayout<D>;
   constexpr int BN = L::kKeys, NK = BN / 16;  // keys per thread
   extern __shared__ float4 smem4[];
   float* sm = reinterpret_cast<float*>(smem4);
   float *Qs = sm + L::kQ, *Ps = sm + L::kP;
+  long long* offs = reinterpret_cast<long long*>(sm + L::kOff);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   WorkStart* start_s = reinterpret_cast<WorkStart*>(sm + L::kStart);
   grid_dependency_wait();
@@ -72,21 +76,33 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const P
     const HeadSlice hs = head_slice(a, w.h);
     const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);
     const int p0 = w.sp.len - w.sp.n + w.first(a);  // position of the item's first token
+    // Row threadIdx.x of key tile j: its offset in the pools; -1 past the sequence's
+    // end, where nothing is read
+    auto find_row = [&](int j) {
+      const int pos = j * BN + threadIdx.x;
+      if (pos >= w.sp.len) return -1ll;
+      const int page = page_of(a.pv, w.b, pos);
+      bad |= page < 0;
+      return page < 0 ? -1ll : slot_offset(a.pv, page, hs.kvh, pos);
+    };
     auto copy = [&](int j) {  // key tile j into stage j & 1
       float *Ks = sm + L::kK + (j & 1) * BN * (D + 4), *Vs = sm + L::kV + (j & 1) * BN * D;
-#pragma unroll 4
+      const long long* off = offs + (j & 1) * BN;
+#pragma unroll
       for (int i = threadIdx.x; i < BN * (D / 4); i += kAttnThreads) {
-        const int r = i / (D / 4), c = i % (D / 4) * 4, pos = j * BN + r;
-        // what lies past the sequence's end is never read
-        const int page = pos < w.sp.len ? page_of(a.pv, w.b, pos) : -1;
-        bad |= page < 0 && pos < w.sp.len;
-        const long long off = page < 0 ? 0 : slot_offset(a.pv, page, hs.kvh, pos) + c;
-        cp_async16_or_zero(Ks + r * (D + 4) + c, (const float*)a.K_pages + off, page >= 0);
-        cp_async16_or_zero(Vs + r * D + c, (const float*)a.V_pages + off, page >= 0);
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        const long long o = off[r];
+        cp_async16_or_zero(Ks + r * (D + 4) + c, (const float*)a.K_pages + max(o, 0ll) + c, o >= 0);
+        cp_async16_or_zero(Vs + r * D + c, (const float*)a.V_pages + max(o, 0ll) + c, o >= 0);
       }
       cp_async_commit();
     };
     __syncthreads();  // the last piece's readers are done
+    if (threadIdx.x < BN) {
+      offs[(w.cur & 1) * BN + threadIdx.x] = find_row(w.cur);
+      if (w.cur + 1 < w.end) offs[(w.cur + 1 & 1) * BN + threadIdx.x] = find_row(w.cur + 1);
+    }
+    __syncthreads();
     copy(w.cur);
     for (int i = threadIdx.x; i < kAttnRows * (D / 4); i += kAttnThreads) {
       const int r = i / (D / 4), c = i % (D / 4) * 4, t = r / a.slice, g = r - t * a.slice;
@@ -116,6 +132,9 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const P
       cp_async_wait<0>();
       __syncthreads();  // tile j is there for all, and stage j + 1 is read no more
       if (j + 1 < w.end) copy(j + 1);
+      // the rows of the tile after it: found while this one is worked on
+      long long row = -1;
+      if (j + 2 < w.end && threadIdx.x < BN) row = find_row(j + 2);
       float s[4][NK] = {};
 #pragma unroll 4
       for (int c = 0; c < D; c += 4) {
@@ -156,79 +175,94 @@ __global__ void __launch_bounds__(kAttnThreads, 2) paged_attn_f32_kernel(const P
           sum += p;
           Ps[(ty * 4 + i) * (BN + 4) + tx + 16 * e] = p;
         }
-#pragma unroll
-        for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
-        l[i] = l[i] * f + sum;
+        l[i] = l[i] * f + sum;  // this thread's share
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
       }
       __syncwarp();  // a warp reads the weights of its own rows only
-      if (all) {
+      // hidden keys have weight 0; a hidden value that is not finite is mended below
 #pragma unroll 2
-        for (int k = 0; k < BN; k += 4) {
-          float p[4][4];
+      for (int k = 0; k < BN; k += 4) {
+        float p[4][4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) load4(Ps + (ty * 4 + i) * (BN + 4) + k, p[i]);
+        for (int i = 0; i < 4; ++i) load4(Ps + (ty * 4 + i) * (BN + 4) + k, p[i]);
 #pragma unroll
-          for (int z = 0; z < 4; ++z)
-#pragma unroll
-            for (int c = 0; c < D / 64; ++c) {
-              float v[4];
-              load4(Vs + (k + z) * D + c * 64 + tx * 4, v);
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  o[i][c * 4 + e] = fmaf(p[i][z], v[e], o[i][c * 4 + e]);
-            }
-        }
-      } else {
-        for (int k = 0; k < BN; ++k) {
-          float p[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = Ps[(ty * 4 + i) * (BN + 4) + k];
+        for (int z = 0; z < 4; ++z)
 #pragma unroll
           for (int c = 0; c < D / 64; ++c) {
             float v[4];
-            load4(Vs + k * D + c * 64 + tx * 4, v);
+            load4(Vs + (k + z) * D + c * 64 + tx * 4, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              // a key that the row does not see adds nothing, whatever its value holds
-              if (k0 + k >= lo[i] && k0 + k < hi[i]) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) o[i][c * 4 + e] = fmaf(p[i], v[e], o[i][c * 4 + e]);
-              }
+              for (int e = 0; e < 4; ++e)
+                o[i][c * 4 + e] = fmaf(p[i][z], v[e], o[i][c * 4 + e]);
           }
-        }
       }
+      // (stage j & 1's offsets were read before this tile's barrier)
+      if (j + 2 < w.end && threadIdx.x < BN) offs[(j & 1) * BN + threadIdx.x] = row;
       __syncwarp();  // before the next tile's weights
     }
     const int slot = w.slot(blockIdx.x);
+    uint32_t nan_groups[4];  // 16-channel groups of the rows with a NaN
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], x);
       const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
-      if (t >= tokens || g >= hs.n) continue;
+      const bool mine = t < tokens && g < hs.n;
       const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
       const size_t prow = (size_t)slot * kAttnRows + r;
       float* dst = slot < 0 ? (float*)a.y + out * D : a.part_o + prow * D;
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+      nan_groups[i] = 0;
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         float x[4];
+        bool nan = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = o[i][c * 4 + e] * inv;
-        store4(dst + c * 64 + tx * 4, x);
+        for (int e = 0; e < 4; ++e) {
+          x[e] = o[i][c * 4 + e] * inv;
+          nan = nan || x[e] != x[e];
+        }
+        if (mine) store4(dst + c * 64 + tx * 4, x);
+        if (mine && nan) nan_groups[i] |= 1u << (4 * c + tx / 4);
       }
       const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
-      if (tx == 0 && slot >= 0) a.part_lse[prow] = lse2;
-      if (tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
+      if (mine && tx == 0 && slot >= 0) a.part_lse[prow] = lse2;
+      if (mine && tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
+    }
+    bool mend = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+      for (int x = 8; x > 0; x >>= 1)
+        nan_groups[i] |= __shfl_xor_sync(0xffffffffu, nan_groups[i], x);
+      mend = mend || nan_groups[i];
+    }
+    __syncwarp();  // the rows' values, before one thread looks at them again
+    if (mend && tx == 0) {
+#pragma unroll 1
+      for (int i = 0; i < 4; ++i) {
+        if (!nan_groups[i]) continue;
+        const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
+        const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+        mend_row<float, D>(
+            a, w.b, hs.kvh, (const float*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs,
+            w.cur * BN, lo[i], hi[i], min(w.end * BN, w.sp.len), m[i] == -INFINITY ? 0.f : m[i],
+            l[i] == 0.f ? 0.f : 1.f / l[i], nan_groups[i],
+            slot < 0 ? (float*)a.y + out * D : nullptr,
+            slot < 0 ? nullptr : a.part_o + ((size_t)slot * kAttnRows + r) * D);
+      }
     }
   }
   if (threadIdx.x == 0) a.rec[blockIdx.x] = record;
   if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
 }
 
-constexpr int kAttnCtasPerSm = 2;
+static int f32_ctas(int head_dim) {
+  return sm_count() * (head_dim == 128 ? SimtLayout<128>::kCtasPerSm : SimtLayout<64>::kCtasPerSm);
+}
 
 template <int D>
 static ebd_status launch_paged_f32(PagedAttnArgs a, cudaStream_t s) {
@@ -242,7 +276,8 @@ static ebd_status launch_paged_f32(PagedAttnArgs a, cudaStream_t s) {
   a.tokens = a.half_tokens = kAttnRows / a.slice;
   a.min_share = 2;
   a.item_cost = 0;
-  const int n_cta = sm_count() * kAttnCtasPerSm;
+  if (!line_fits(a, SimtLayout<D>::kKeys)) return EBD_ERR_UNSUPPORTED;
+  const int n_cta = f32_ctas(D);
   const ebd_status st =
       launch_dependent(paged_attn_f32_kernel<D>, dim3(n_cta), kAttnThreads, smem, s, a);
   if (st != EBD_OK) return st;
@@ -257,7 +292,7 @@ extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cac
                                                       int32_t n_q_heads, int32_t max_new) {
   if (check_paged(cache) != EBD_OK || n_q_heads < 1 || max_new < 1) return 0;
   if (cache->dtype == EBD_F32)
-    return paged_split_bytes(sm_count() * kAttnCtasPerSm, kAttnRows, cache->head_dim);
+    return paged_split_bytes(f32_ctas(cache->head_dim), kAttnRows, cache->head_dim);
   return paged_split_bytes(sm_count(), kTcSlotRows, cache->head_dim);
 }
 
@@ -303,7 +338,7 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
   if (cache->dtype == EBD_F32) {
-    paged_split_layout(a, workspace, sm_count() * kAttnCtasPerSm, kAttnRows);
+    paged_split_layout(a, workspace, f32_ctas(cache->head_dim), kAttnRows);
     return cache->head_dim == 128 ? launch_paged_f32<128>(a, s) : launch_paged_f32<64>(a, s);
   }
   const int n_cta = sm_count();

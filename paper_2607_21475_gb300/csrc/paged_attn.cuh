@@ -10,7 +10,8 @@
 // item boundaries into pieces; the pieces of an item that more than one CTA
 // holds leave (o / l, log2-sum) in the workspace and a merge kernel joins them
 // in CTA order, so results do not depend on timing.  The lengths are on the
-// device only, so one warp of each CTA finds the CTA's place on that line.
+// device only, so one warp of each CTA finds the CTA's place on that line (32-bit
+// arithmetic: the entry point refuses what could be longer).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -87,13 +88,13 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
 struct WorkStart {
   int b, h, m;
   int off;          // work of the item that earlier CTAs have
-  long long count;  // work of this CTA
+  int count;      // work of this CTA
 };
 
-__device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
+__device__ __forceinline__ int warp_scan_add(int v, int lane) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long u = __shfl_up_sync(0xffffffffu, v, o);
+    const int u = __shfl_up_sync(0xffffffffu, v, o);
     if (lane >= o) v += u;
   }
   return v;
@@ -101,7 +102,7 @@ __device__ __forceinline__ long long warp_scan_add(long long v, int lane) {
 
 // Work of one head of the sequences base + lane (lane = 0..31).
 template <int BN>
-__device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int base, int lane,
+__device__ __forceinline__ int sequence_tiles(const PagedAttnArgs& a, int base, int lane,
                                                     bool report) {
   const int b = base + lane;
   SeqSpan sp = {};
@@ -110,7 +111,7 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
     if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
   }
   const int mt = (sp.n + a.tokens - 1) / a.tokens;
-  long long c = 0;
+  int c = 0;
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
@@ -121,7 +122,7 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
     const int src = __ffs(left) - 1;
     const int n = __shfl_sync(0xffffffffu, sp.n, src), len = __shfl_sync(0xffffffffu, sp.len, src);
     const int k = __shfl_sync(0xffffffffu, mt, src);
-    long long sum = 0;
+    int sum = 0;
     for (int m = 4 + lane; m < k; m += 32) {
       int kb, ke;
       item_range<BN>(a, n, len, m, kb, ke);
@@ -134,30 +135,26 @@ __device__ __forceinline__ long long sequence_tiles(const PagedAttnArgs& a, int 
   return c;
 }
 
-__device__ __forceinline__ long long divide(long long x, long long y) {
-  return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
-}
-
 // Where CTA `cta` begins on the line, and how much of it is its own; one whole warp.
 template <int BN>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
   const int H = a.heads;
-  long long total = 0, c = 0;
+  int total = 0, c = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
     c = sequence_tiles<BN>(a, base, lane, cta == 0);
     total += H * c;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  const long long share = max((long long)a.min_share, divide(total + n_cta - 1, n_cta));
-  long long at = cta * share;
+  const int share = max(a.min_share, (int)((uint32_t)(total + n_cta - 1) / (uint32_t)n_cta));
+  int at = cta * share;
   WorkStart w = {0, 0, 0, 0, 0};
   if (at >= total) return w;
   w.count = min(share, total - at);
   for (int base = 0; base < a.pv.batch; base += 32) {
     if (a.pv.batch > 32) c = sequence_tiles<BN>(a, base, lane, false);
-    const long long upto = warp_scan_add(c * H, lane);
+    const int upto = warp_scan_add(c * H, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
       const int src = __ffs(past) - 1;
@@ -168,23 +165,23 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
     }
     at -= __shfl_sync(0xffffffffu, upto, 31);
   }
-  w.h = (int)divide(at, c);
+  w.h = (int)((uint32_t)at / (uint32_t)c);
   at -= w.h * c;
   const SeqSpan sp = seq_span(a.pv, a.cu, w.b, a.n_tokens, a.max_new);
   const int mt = (sp.n + a.tokens - 1) / a.tokens;
   if (mt == 1) {
-    w.off = (int)at;
+    w.off = at;
     return w;
   }
   for (int base = 0; base < mt; base += 32) {
     int kb = 0, ke = -a.item_cost;
     if (base + lane < mt) item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
-    const long long work = ke - kb + a.item_cost, upto = warp_scan_add(work, lane);
+    const int work = ke - kb + a.item_cost, upto = warp_scan_add(work, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
       const int src = __ffs(past) - 1;
       w.m = base + src;
-      w.off = (int)(at - __shfl_sync(0xffffffffu, upto - work, src));
+      w.off = at - __shfl_sync(0xffffffffu, upto - work, src);
       break;
     }
     at -= __shfl_sync(0xffffffffu, upto, 31);
@@ -199,7 +196,7 @@ struct PieceWalk {
   SeqSpan sp;
   int kb, ke;    // the item's tiles
   int cur, end;  // this piece's
-  long long left;  // work after this piece; -1: no piece
+  int left;      // work after this piece; -1: no piece
 
   __device__ __forceinline__ PieceWalk(const PagedAttnArgs& a, const WorkStart& w)
       : b(w.b), h(w.h), m(w.m), left(w.count) {
@@ -219,7 +216,7 @@ struct PieceWalk {
   // This CTA's tiles of the item, of which earlier CTAs have `off`: an item's own
   // cost comes first, so a share that ends within it has no tile.
   __device__ __forceinline__ void take(const PagedAttnArgs& a, int off) {
-    const int most = ke - kb + a.item_cost - off, mine = (int)min((long long)most, left);
+    const int most = ke - kb + a.item_cost - off, mine = min(most, left);
     cur = kb + max(0, off - a.item_cost);
     end = kb + max(0, off + mine - a.item_cost);
     left -= mine;
@@ -272,6 +269,74 @@ __device__ __forceinline__ void record_piece(PieceRecord& r, const PieceWalk<BN>
     r.h = p.h;
     r.m = p.m;
   }
+}
+
+__device__ __forceinline__ void round_to(float x, float& y) { y = x; }
+__device__ __forceinline__ void round_to(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
+
+// Mends one row's output where a value that the row does not see made it NaN:
+// such a value has weight 0 in the tile's product, and 0 times NaN or infinity
+// is NaN.  For each 16-channel group with a NaN (`groups`): the channels in which
+// a hidden value of the piece's positions [tile_lo, tile_hi) (at most a few
+// hundred at either end are hidden) is not finite are recomputed from those that
+// the row sees, [lo, hi) of them; a NaN in any other channel is the row's own.  The
+// sum stops once every such channel has met a NaN of its own.  q: the row's
+// query; base, inv: reference (log2) and reciprocal sum of its weights; y or part:
+// the output, as written.
+template <typename T, int D>
+__device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
+                                      int tile_lo, int lo, int hi, int tile_hi, float base,
+                                      float inv, uint32_t groups, T* y, float* part) {
+  const int k_lo = max(lo, tile_lo), k_hi = min(hi, tile_hi);  // seen
+  for (int c = 0; c < D; c += 16) {
+    if (!(groups >> (c / 16) & 1)) continue;
+    uint32_t mend = 0;
+    for (int pos = tile_lo; pos < tile_hi; ++pos) {
+      if (pos == k_lo && k_lo < k_hi) pos = k_hi;
+      const int page = pos < tile_hi ? page_of(a.pv, b, pos) : -1;
+      if (page < 0) continue;
+      const T* v = (const T*)a.V_pages + slot_offset(a.pv, page, kvh, pos) + c;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(fabsf(to_f32(v[i])) < INFINITY)) mend |= 1u << i;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float o = y ? to_f32(y[c + i]) : part[c + i];
+      if (o == o) mend &= ~(1u << i);
+    }
+    if (!mend) continue;
+    float acc[16] = {};
+    uint32_t open = mend;  // channels without a NaN of their own so far
+    for (int pos = k_hi - 1; open && pos >= k_lo; --pos) {
+      const int page = page_of(a.pv, b, pos);
+      if (page < 0) continue;
+      const long long off = slot_offset(a.pv, page, kvh, pos);
+      const T *k = (const T*)a.K_pages + off, *v = (const T*)a.V_pages + off + c;
+      float s = 0.f;
+#pragma unroll 8
+      for (int i = 0; i < D; ++i) s = fmaf(to_f32(q[i]), to_f32(k[i]), s);
+      const float p = exp2f(fmaf(s, a.scale2, -base));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
+        if (acc[i] != acc[i]) open &= ~(1u << i);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (!(mend >> i & 1)) continue;
+      if (y) round_to(acc[i] * inv, y[c + i]);
+      else part[c + i] = acc[i] * inv;
+    }
+  }
+}
+
+// Whether the line of work of any lengths within the call's bounds fits 31 bits.
+inline bool line_fits(const PagedAttnArgs& a, int keys_per_tile) {
+  const double tiles = (double)a.pv.max_blocks * (1 << a.pv.page_shift) / keys_per_tile + 1;
+  const double items = (double)a.n_tokens / a.tokens + a.pv.batch;
+  return items * a.heads * (tiles + a.item_cost) < 2.0e9;
 }
 
 // Launches a kernel as a programmatic dependent of whatever precedes it in the

@@ -92,71 +92,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// Mends one row's output where a value that the row does not see made it NaN:
-// such a value has weight 0 in the tile's product, and 0 times NaN or infinity
-// is NaN.  For each 16-channel group with a NaN: the channels in which a hidden
-// value of the piece's tiles (at most a few hundred positions at either end) is
-// not finite are recomputed from the positions that the row sees; a NaN in any
-// other channel is the row's own.  The sum stops once every such channel has met
-// a NaN of its own.
-template <int D>
-__device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int h, int token, int g,
-                                      int tile_lo, int lo, int hi, int tile_hi, float base,
-                                      float inv, uint32_t groups, __nv_bfloat16* y, float* part) {
-  const uint4* q = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.q + token * a.q_ts +
-                                                  (h * a.group + g) * a.q_hs);
-  const int k_lo = max(lo, tile_lo), k_hi = min(hi, tile_hi);  // seen
-  for (int c = 0; c < D; c += 16) {
-    if (!(groups >> (c / 16) & 1)) continue;
-    uint32_t mend = 0;
-    for (int pos = tile_lo; pos < tile_hi; ++pos) {
-      if (pos == k_lo && k_lo < k_hi) pos = k_hi;
-      const int page = pos < tile_hi ? page_of(a.pv, b, pos) : -1;
-      if (page < 0) continue;
-      const __nv_bfloat16* v =
-          (const __nv_bfloat16*)a.V_pages + slot_offset(a.pv, page, h, pos) + c;
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!(fabsf(to_f32(v[i])) < INFINITY)) mend |= 1u << i;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float o = y ? to_f32(y[c + i]) : part[c + i];
-      if (o == o) mend &= ~(1u << i);
-    }
-    if (!mend) continue;
-    float acc[16] = {};
-    uint32_t open = mend;  // channels without a NaN of their own so far
-    for (int pos = k_hi - 1; open && pos >= k_lo; --pos) {
-      const int page = page_of(a.pv, b, pos);
-      if (page < 0) continue;
-      const long long off = slot_offset(a.pv, page, h, pos);
-      const uint4* k = reinterpret_cast<const uint4*>((const __nv_bfloat16*)a.K_pages + off);
-      float s = 0.f;
-      for (int i = 0; i < D / 8; ++i) {
-        const uint4 x = q[i], z = k[i];
-        s = fmaf(bf16_lo(x.x), bf16_lo(z.x), fmaf(bf16_hi(x.x), bf16_hi(z.x), s));
-        s = fmaf(bf16_lo(x.y), bf16_lo(z.y), fmaf(bf16_hi(x.y), bf16_hi(z.y), s));
-        s = fmaf(bf16_lo(x.z), bf16_lo(z.z), fmaf(bf16_hi(x.z), bf16_hi(z.z), s));
-        s = fmaf(bf16_lo(x.w), bf16_lo(z.w), fmaf(bf16_hi(x.w), bf16_hi(z.w), s));
-      }
-      const float p = exp2f(fmaf(s, a.scale2, -base));
-      const __nv_bfloat16* v = (const __nv_bfloat16*)a.V_pages + off + c;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
-        if (acc[i] != acc[i]) open &= ~(1u << i);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (!(mend >> i & 1)) continue;
-      if (y) y[c + i] = __float2bfloat16_rn(acc[i] * inv);
-      else part[c + i] = acc[i] * inv;
-    }
-  }
-}
-
 template <int D>
 __global__ void __launch_bounds__(kTcAttnThreads, 1)
     paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
@@ -369,10 +304,14 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         if (slot >= 0) a.part_lse[prow] = lse2;
         else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
         if (nan_groups)
-          mend_row<D>(a, w.b, w.h, w.token + tok, g, w.cur * kTcBN, lo, hi,
-                      min(w.end * kTcBN, w.len), m == -INFINITY ? 0.f : m * a.scale2, inv,
-                      nan_groups, slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
-                      slot < 0 ? nullptr : a.part_o + prow * D);
+          mend_row<__nv_bfloat16, D>(
+              a, w.b, w.h,
+              (const __nv_bfloat16*)a.q + (w.token + tok) * a.q_ts +
+                  (w.h * a.group + g) * a.q_hs,
+              w.cur * kTcBN, lo, hi, min(w.end * kTcBN, w.len),
+              m == -INFINITY ? 0.f : m * a.scale2, inv, nan_groups,
+              slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
+              slot < 0 ? nullptr : a.part_o + prow * D);
       }
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
@@ -686,6 +625,7 @@ ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
   a.slice = a.group;
   a.half_tokens = 128 / a.group;
   a.tokens = 2 * a.half_tokens;
+  if (!line_fits(a, kTcBN)) return EBD_ERR_UNSUPPORTED;
   const ebd_status st =
       c.head_dim == 128 ? launch_tc_t<128>(a, c, n_cta, s) : launch_tc_t<64>(a, c, n_cta, s);
   if (st != EBD_OK) return st;
