@@ -448,7 +448,8 @@ typedef struct {
   int32_t head_dim;    /* d                                                      */
   int32_t page_size;   /* positions per page: a power of two, 8 .. 1024          */
   int32_t n_pages;     /* pages in the pool                                      */
-  int32_t max_blocks;  /* row length of block_table                              */
+  int32_t max_blocks;  /* row length of block_table; max_blocks * page_size stays
+                          below 2^31 - 2^20                                       */
   int32_t reserved;    /* 0                                                      */
   int64_t page_stride; /* elements                                               */
   int64_t head_stride;
@@ -529,8 +530,17 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  *   lse        device [n_tokens, Hq] float32 out, nullable
  *   dev_status device int32, required
  * Supports d in {64, 128}, G = Hq / Hkv <= 128; q, y and every cached row on
- * 16-byte boundaries (EBD_ERR_INVALID otherwise).  Products accumulate in
- * float32; softmax statistics and partial outputs are float32.
+ * 16-byte boundaries (EBD_ERR_INVALID otherwise); EBD_ERR_UNSUPPORTED when the
+ * bounds allow more work than 31 bits count (a million new tokens over a million
+ * positions).  Products accumulate in float32; softmax statistics and partial
+ * outputs are float32; bf16 rounds the softmax weights once (2^-8 relative)
+ * before they multiply the values.  A NaN or infinite key or value reaches only
+ * the tokens that see it.  Needs workspace of
+ * ebd_paged_attention_workspace_bytes(...) bytes.  Results are reproducible bit for
+ * bit for a batch on a given GPU; how a sequence's keys are split (and so the
+ * last bits) depends on the rest of the batch.  Both of its kernels are
+ * programmatic dependents of what precedes them on the stream and read and
+ * write the caller's memory only after that has completed.
  */
 size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cache, int32_t n_q_heads,
                                            int32_t max_new);

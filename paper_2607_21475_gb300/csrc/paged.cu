@@ -27,8 +27,8 @@ ebd_status check_paged(const ebd_paged_cache* c) {
     return EBD_ERR_UNSUPPORTED;
   if (c->page_stride < 0 || c->head_stride < 0 || c->row_stride < c->head_dim)
     return EBD_ERR_INVALID;
-  // positions are int32
-  if ((long long)c->max_blocks * c->page_size > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
+  // positions are int32, and so is a tile's end past the last one
+  if ((long long)c->max_blocks * c->page_size > 0x7ff00000LL) return EBD_ERR_UNSUPPORTED;
   return EBD_OK;
 }
 

@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     for (int i = 0; i < 4; ++i) {
       const int p = p0 + min((ty * 4 + i) / a.slice, tokens - 1);
       hi[i] = p + 1;
-      lo[i] = a.window > 0 ? max(0, p - a.window + 1) : 0;
+      lo[i] = first_seen(a, p);
     }
     float m[4], l[4], o[4][D / 16];
 #pragma unroll
@@ -305,13 +305,13 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
                                           void* stream) {
   const ebd_status st = check_paged(cache);
   if (st != EBD_OK) return st;
-  if (n_tokens < 0 || max_new < 0 || n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0)
+  if (n_tokens < 0 || max_new < (n_tokens > 0) || n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0)
     return EBD_ERR_INVALID;
   if (!(scale > 0.f) || !(scale < INFINITY) || window < 0) return EBD_ERR_INVALID;
   if (cache->head_dim != 64 && cache->head_dim != 128) return EBD_ERR_UNSUPPORTED;
   const int group = n_q_heads / cache->n_kv_heads;
   if (group > 128 || cache->batch > 65535 || cache->n_kv_heads > 65535) return EBD_ERR_UNSUPPORTED;
-  if (n_tokens == 0 || max_new == 0) return EBD_OK;
+  if (n_tokens == 0) return EBD_OK;
   if (!cu_new || !q || !y || !dev_status) return EBD_ERR_INVALID;
   const int wide = cache->dtype == EBD_F32 ? 4 : 8;
   if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride < 0 ||

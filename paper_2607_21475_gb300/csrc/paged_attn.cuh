@@ -70,6 +70,11 @@ __device__ __forceinline__ HeadSlice head_slice(const PagedAttnArgs& a, int h) {
   return s;
 }
 
+// The first position that a token at position p sees.
+__device__ __forceinline__ int first_seen(const PagedAttnArgs& a, int p) {
+  return a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
+}
+
 // Key tiles [kb, ke) of m-tile m; an item with nothing to see keeps one (fully
 // masked) tile, so that its rows get written.
 template <int BN>
@@ -80,7 +85,7 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
   kb = 0;
   ke = 1;
   if (k_end > 0) {
-    if (a.window > 0) kb = max(0, p0 + first - a.window + 1) / BN;
+    kb = first_seen(a, p0 + first) / BN;
     ke = (k_end + BN - 1) / BN;
   }
 }

@@ -133,9 +133,14 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       fence_barrier_init();
     }
   }
-  // the rows past an X's last query row are never loaded: numbers, once
-  for (int i = threadIdx.x; i < 2 * L::kQTile / 16; i += kTcAttnThreads)
-    *reinterpret_cast<uint4*>(smem + L::kQ + i * 16) = make_uint4(0, 0, 0, 0);
+  // the rows past an X's last query row (none where the group divides 128) are
+  // never loaded: numbers, once
+  const int used = a.half_tokens * a.group;
+  for (int i = threadIdx.x; i < (128 - used) * 8 * 2 * L::kHalves; i += kTcAttnThreads) {
+    const int box = i / ((128 - used) * 8), at = i - box * ((128 - used) * 8);
+    *reinterpret_cast<uint4*>(smem + L::kQ + box * L::kQBox + used * 128 + at * 16) =
+        make_uint4(0, 0, 0, 0);
+  }
   fence_proxy_async_smem();
   grid_dependency_wait();  // nothing of the caller's was read or written so far
   tc_fence_before();
@@ -171,7 +176,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       if (tokens <= 0) continue;
       const int tok = x0 + min(rt, tokens - 1);
       const int pos = w.pos + tok;
-      const int hi = pos + 1, lo = a.window > 0 ? max(0, pos - a.window + 1) : 0;
+      const int hi = pos + 1, lo = first_seen(a, pos);
       float m = -INFINITY, l = 0.f;
       for (int j = w.cur; j < w.end; ++j, ++it) {
         const int k0 = j * kTcBN;

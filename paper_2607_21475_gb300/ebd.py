@@ -222,11 +222,13 @@ def _check(name, code):
         raise EbdError(name, code, ebd_status_string(code))
 
 
-def _workspace(nbytes, device, ws):
+def _workspace(nbytes, device, ws, stream=None):
     if nbytes == 0:
         return None, 0
     if ws is None:
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream is not None:  # the buffer goes back to the allocator before the work is done
+            ws.record_stream(stream)
     if ws.numel() * ws.element_size() < nbytes:
         raise ValueError(f"workspace too small: {ws.numel() * ws.element_size()} < {nbytes}")
     return ws.data_ptr(), ws.numel() * ws.element_size()
@@ -266,7 +268,7 @@ def ebd_score(q_obs: torch.Tensor, K: torch.Tensor, scores: torch.Tensor, worksp
     B, H, N, d = K.shape
     R = q_obs.shape[2]
     dt = _dtype_code(K)
-    ws, wsb = _workspace(ebd_score_workspace_bytes(B, H, R), K.device, workspace)
+    ws, wsb = _workspace(ebd_score_workspace_bytes(B, H, R), K.device, workspace, stream)
     _check("ebd_score", lib().ebd_score(
         dt, B, H, d, N, R, _ptr(q_obs, K.dtype, (B, H, R, d), "q_obs"), _ptr(K, name="K"),
         _ptr(scores, torch.float32, (B, H, N), "scores"), ws, wsb, _stream(stream)))
@@ -335,7 +337,8 @@ def ebd_evict(design: EbdDesign, K: torch.Tensor, V: torch.Tensor, scores, q_obs
         raise ValueError("ebd_evict needs scores or q_obs")
     ws, wsb = (None, 0)
     if scores is None:
-        ws, wsb = _workspace(ebd_evict_workspace_bytes(design, n_obs), K.device, workspace)
+        ws, wsb = _workspace(ebd_evict_workspace_bytes(design, n_obs), K.device, workspace,
+                             stream)
     host_ok = scores is not None  # K, V, scores may stay in page-locked host memory
     _check("ebd_evict", lib().ebd_evict(
         ctypes.byref(design), dt, _ptr(K, K.dtype, (B, H, N, d), "K", host_ok),
@@ -395,7 +398,8 @@ def ebd_certified_decode(Q: torch.Tensor, K_c: torch.Tensor, V_c: torch.Tensor,
         raise ValueError("query heads must be a multiple of KV heads")
     G = Hq // H
     dt = _dtype_code(K_c)
-    ws, wsb = _workspace(ebd_decode_workspace_bytes(dt, B, H, G, d, cap), K_c.device, workspace)
+    ws, wsb = _workspace(ebd_decode_workspace_bytes(dt, B, H, G, d, cap), K_c.device, workspace,
+                         stream)
     f = torch.float32
     _check("ebd_certified_decode", lib().ebd_certified_decode(
         dt, B, H, G, d, _ptr(Q, K_c.dtype, (B, Hq, d), "Q"), _ptr(K_c, name="K_c"),
@@ -744,7 +748,7 @@ def ebd_paged_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, m
     L = lib()
     ref = ctypes.byref(c)
     ws, wsb = _workspace(L.ebd_paged_attention_workspace_bytes(ref, hq, int(max_new)), q.device,
-                         workspace)
+                         workspace, stream)
     _check("ebd_paged_attention", L.ebd_paged_attention(
         ref, T, int(max_new), hq, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"), qp, qt, qh,
         d ** -0.5 if scale is None else float(scale), int(window), _ptr(y, dt, (T, hq, d), "y"),

@@ -333,6 +333,23 @@ def test_attention_does_not_depend_on_the_launch(E, dtype, new):
     assert torch.equal(y0, y1) and torch.equal(l0, l1)
 
 
+def test_workspace_of_a_call_on_another_stream_is_not_reused(E):
+    """The binding's own workspace stays out of the allocator's hands while a call
+    on a stream other than the current one still works with it."""
+    s = R.make([40] * 4, [3000, 2500, 40, 999], 8, 2, 128, 32, torch.bfloat16, 72)
+    ref, _ = E.ebd_paged_attention(s["q"], cache(E, s), s["cu"], 40)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    ys = []
+    for _ in range(30):
+        y, _ = E.ebd_paged_attention(s["q"], cache(E, s), s["cu"], 40, stream=side)
+        ys.append(y)
+        for n in (1 << 20, 30 << 20, 40 << 20):  # what the allocator would hand out again
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, ref) for y in ys)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_captured_graph_follows_the_lengths(E, dtype):
     """Append and attention captured once, replayed as the sequences grow."""

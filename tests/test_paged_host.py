@@ -87,7 +87,7 @@ def test_bad_arguments_are_refused(E):
                      (dict(hq=-1), 1), (dict(layout=1, kt=129), 4)]:
         assert append(E, c, **kw) == code, kw
     assert append(E, c, n=0) == 0
-    for kw, code in [(dict(n=-1), 1), (dict(max_new=-1), 1), (dict(hq=3), 1), (dict(hq=0), 1),
+    for kw, code in [(dict(n=-1), 1), (dict(max_new=-1), 1), (dict(max_new=0), 1), (dict(hq=3), 1), (dict(hq=0), 1),
                      (dict(cu=None), 1), (dict(q=None), 1), (dict(y=None), 1), (dict(st=None), 1),
                      (dict(scale=0.0), 1), (dict(scale=math.nan), 1), (dict(scale=math.inf), 1),
                      (dict(window=-1), 1), (dict(q=FAKE + 8), 1), (dict(qt=129), 1),
@@ -95,6 +95,8 @@ def test_bad_arguments_are_refused(E):
         assert attention(E, c, **kw) == code, kw
     assert attention(E, c, n=0) == 0
     assert attention(E, good_cache(E, head_dim=96, row_stride=96)) == 4
+    huge = good_cache(E, batch=60000, max_blocks=1 << 20)  # 16 M positions each
+    assert attention(E, huge, n=60000) == 4
     assert attention(E, good_cache(E, row_stride=68)) == 1
     assert attention(E, good_cache(E, K_pages=FAKE + 8)) == 1
     for kw, code in [(dict(idx=None), 1), (dict(n=None), 1), (dict(cap=0), 1), (dict(k=None), 1),
