@@ -49,6 +49,25 @@ struct alignas(VEC * sizeof(T)) Chunk {
   T e[VEC];
 };
 
+// A chunk's load and store, marked for early eviction from L2 where it is 16 bytes:
+// each is used once here, and a long prompt's otherwise push each other's
+// unwritten lines out in the middle of the stream (16k-token prompt 47.7 us with
+// plain accesses, 38.9 us with the stores marked, 38.1 us with both).
+template <typename T, int VEC>
+__device__ __forceinline__ void load_chunk(const T* p, Chunk<T, VEC>& c) {
+  if constexpr (VEC * sizeof(T) == 16)
+    *reinterpret_cast<uint4*>(&c) = __ldcs(reinterpret_cast<const uint4*>(p));
+  else
+    c = *reinterpret_cast<const Chunk<T, VEC>*>(p);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_chunk(T* p, const Chunk<T, VEC>& c) {
+  if constexpr (VEC * sizeof(T) == 16)
+    __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&c));
+  else
+    *reinterpret_cast<Chunk<T, VEC>*>(p) = c;
+}
+
 __device__ __forceinline__ void from_f32(float x, float& y) { y = x; }
 __device__ __forceinline__ void from_f32(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
 
@@ -125,8 +144,8 @@ __global__ void __launch_bounds__(kRotWarps * 32, APPEND ? kAppendBlocks : kRotB
     const T* src = !APPEND || h < a.n_x  ? xp + h * a.x.hs
                    : h < a.n_x + a.n_kv ? kp + (h - a.n_x) * a.k.hs
                                         : vp + (h - a.n_x - a.n_kv) * a.v.hs;
-    r.a = *reinterpret_cast<const Chunk<T, VEC>*>(src + c1);
-    if (c2 >= 0) r.b = *reinterpret_cast<const Chunk<T, VEC>*>(src + c2);
+    load_chunk<T, VEC>(src + c1, r.a);
+    if (c2 >= 0) load_chunk<T, VEC>(src + c2, r.b);
   };
   auto next = [&](int& h, int& u) {
     h += step;
@@ -222,8 +241,8 @@ __global__ void __launch_bounds__(kRotWarps * 32, APPEND ? kAppendBlocks : kRotB
       const int kh = h - a.n_x - (is_v ? a.n_kv : 0);
       dst = (T*)(is_v ? a.V_pages : a.K_pages) + slot + kh * a.pv.head_stride;
     }
-    *reinterpret_cast<Chunk<T, VEC>*>(dst + c1) = r.a;
-    if (c2 >= 0) *reinterpret_cast<Chunk<T, VEC>*>(dst + c2) = r.b;
+    store_chunk<T, VEC>(dst + c1, r.a);
+    if (c2 >= 0) store_chunk<T, VEC>(dst + c2, r.b);
   };
   while (h < heads) {
     store(h, u, r0);
