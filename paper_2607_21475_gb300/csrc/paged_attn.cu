@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
       const bool mine = t < tokens && g < hs.n;
       const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
-      const size_t prow = (size_t)slot * kAttnRows + r;
+      const size_t prow = (size_t)slot * a.slot_rows + r;
       float* dst = slot < 0 ? (float*)a.y + out * D : a.part_o + prow * D;
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
       nan_groups[i] = 0;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
             w.cur * BN, lo[i], hi[i], min(w.end * BN, w.sp.len), m[i] == -INFINITY ? 0.f : m[i],
             l[i] == 0.f ? 0.f : 1.f / l[i], nan_groups[i],
             slot < 0 ? (float*)a.y + out * D : nullptr,
-            slot < 0 ? nullptr : a.part_o + ((size_t)slot * kAttnRows + r) * D);
+            slot < 0 ? nullptr : a.part_o + ((size_t)slot * a.slot_rows + r) * D);
       }
     }
   }
@@ -260,40 +260,64 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
 }
 
+// Query heads per slice of a group: equal slices of at most kAttnRows heads.
+static int f32_slice(int group) {
+  const int slices = (group + kAttnRows - 1) / kAttnRows;
+  return (group + slices - 1) / slices;
+}
+
 static int f32_ctas(int head_dim) {
   return sm_count() * (head_dim == 128 ? SimtLayout<128>::kCtasPerSm : SimtLayout<64>::kCtasPerSm);
 }
 
 template <int D>
-static ebd_status launch_paged_f32(PagedAttnArgs a, cudaStream_t s) {
+static ebd_status launch_paged_f32(PagedAttnArgs a, int n_cta, cudaStream_t s) {
   const int smem = SimtLayout<D>::kFloats * 4;
   if (cudaFuncSetAttribute(paged_attn_f32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  a.slices = (a.group + kAttnRows - 1) / kAttnRows;
-  a.slice = (a.group + a.slices - 1) / a.slices;
+  const int slice = f32_slice(a.group);
+  a.slices = (a.group + slice - 1) / slice;
+  a.slice = slice;
   a.heads = a.pv.n_kv_heads * a.slices;
   a.tokens = a.half_tokens = kAttnRows / a.slice;
   a.min_share = 2;
   a.item_cost = 0;
   if (!line_fits(a, SimtLayout<D>::kKeys)) return EBD_ERR_UNSUPPORTED;
-  const int n_cta = f32_ctas(D);
   const ebd_status st =
       launch_dependent(paged_attn_f32_kernel<D>, dim3(n_cta), kAttnThreads, smem, s, a);
   if (st != EBD_OK) return st;
-  return launch_paged_merge(a, false, D, kAttnRows, n_cta, s);
+  return launch_paged_merge(a, false, D, n_cta, s);
 }
 
 }  // namespace ebd
 
 using namespace ebd;
 
+namespace ebd {
+
+static int attention_ctas(const ebd_paged_cache& c) {
+  return c.dtype == EBD_F32 ? f32_ctas(c.head_dim) : sm_count();
+}
+
+static int attention_slot_rows(const ebd_paged_cache& c, int group, int max_new) {
+  if (c.dtype == EBD_F32) {
+    const int slice = f32_slice(group);
+    return paged_slot_rows(max_new, kAttnRows / slice, slice, kAttnRows);
+  }
+  return paged_slot_rows(max_new, 128 / group, group, kTcRows);
+}
+
+}  // namespace ebd
+
 extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cache,
                                                       int32_t n_q_heads, int32_t max_new) {
   if (check_paged(cache) != EBD_OK || n_q_heads < 1 || max_new < 1) return 0;
-  if (cache->dtype == EBD_F32)
-    return paged_split_bytes(f32_ctas(cache->head_dim), kAttnRows, cache->head_dim);
-  return paged_split_bytes(sm_count(), kTcSlotRows, cache->head_dim);
+  if (n_q_heads % cache->n_kv_heads != 0) return 0;
+  const int group = n_q_heads / cache->n_kv_heads;
+  if (group > 128) return 0;
+  return paged_split_bytes(attention_ctas(*cache), attention_slot_rows(*cache, group, max_new),
+                           cache->head_dim);
 }
 
 extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens,
@@ -337,12 +361,12 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   a.scale2 = scale * kLog2e;
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
-  if (cache->dtype == EBD_F32) {
-    paged_split_layout(a, workspace, f32_ctas(cache->head_dim), kAttnRows);
-    return cache->head_dim == 128 ? launch_paged_f32<128>(a, s) : launch_paged_f32<64>(a, s);
-  }
-  const int n_cta = sm_count();
-  paged_split_layout(a, workspace, n_cta, kTcSlotRows);
+  const int n_cta = attention_ctas(*cache);
+  a.slot_rows = attention_slot_rows(*cache, group, max_new);
+  paged_split_layout(a, workspace, n_cta);
+  if (cache->dtype == EBD_F32)
+    return cache->head_dim == 128 ? launch_paged_f32<128>(a, n_cta, s)
+                                  : launch_paged_f32<64>(a, n_cta, s);
   a.min_share = 4;
   a.item_cost = 4;
   return launch_paged_tc(a, *cache, n_cta, s);

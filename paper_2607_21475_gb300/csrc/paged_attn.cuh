@@ -53,6 +53,7 @@ struct PagedAttnArgs {
   int slices, slice;
   int tokens;        // new tokens per item
   int half_tokens;   // of those, how many the slot's first 128 rows hold
+  int slot_rows;     // rows of a partial result
   int min_share;     // least work per CTA, in key tiles
   int item_cost;     // work of an item beside its key tiles, in key tiles
 };
@@ -364,16 +365,21 @@ inline ebd_status launch_dependent(void (*kern)(Params...), dim3 grid, int threa
 }
 
 // Joins the pieces of split items.  `a` as the attention kernel had it.
-ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int slot_rows,
-                              int n_cta, cudaStream_t s);
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int n_cta,
+                              cudaStream_t s);
+
+// Rows that a partial result needs: those of the largest item the call can have.
+inline int paged_slot_rows(int max_new, int half_tokens, int slice, int most) {
+  return max_new > half_tokens ? most : (max_new * slice + 7) / 8 * 8;
+}
 
 // Bytes of the split results of n_cta CTAs.
 size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim);
 // Points a's split arrays into the workspace.
-void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int slot_rows);
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta);
 
 ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
                            cudaStream_t s);
-constexpr int kTcSlotRows = 256;  // rows of a partial result
+constexpr int kTcRows = 256;  // rows of an item at most
 
 }  // namespace ebd

@@ -269,7 +269,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const float lse2 = l == 0.f ? -INFINITY : m * a.scale2 + log2f(l);
       const long long out = (long long)(w.token + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
-      const size_t prow = (size_t)slot * kTcSlotRows + x * 128 + row;
+      const size_t prow = (size_t)slot * a.slot_rows + x * 128 + row;
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
@@ -634,7 +634,7 @@ ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
   const ebd_status st =
       c.head_dim == 128 ? launch_tc_t<128>(a, c, n_cta, s) : launch_tc_t<64>(a, c, n_cta, s);
   if (st != EBD_OK) return st;
-  return launch_paged_merge(a, true, c.head_dim, kTcSlotRows, n_cta, s);
+  return launch_paged_merge(a, true, c.head_dim, n_cta, s);
 }
 
 }  // namespace ebd

@@ -47,7 +47,7 @@ __device__ __forceinline__ float2 scaled(const float2& v, float f) {
 // VT: the float vector that a lane of a warp owns of a row (D / 32 floats).
 template <typename T, typename VT>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-    paged_merge_kernel(const PagedAttnArgs a, int bm, int n_cta) {
+    paged_merge_kernel(const PagedAttnArgs a, int n_cta) {
   grid_dependency_wait();
   const int c0 = blockIdx.x, lane = threadIdx.x & 31;
   const PieceRecord r = a.rec[c0];
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const int n = c1 - c0 + 1;
   // piece k of row `row` in part_lse, and (times D) in part_o
   const auto place = [&](int k, int row) {
-    return (size_t)(2 * (c0 + k) + (k == 0)) * bm + row;
+    return (size_t)(2 * (c0 + k) + (k == 0)) * a.slot_rows + row;
   };
   // row i of the item is token t, head g; the slot's second half starts at row 128
   const auto row_of = [&](int i) {
@@ -161,17 +161,17 @@ size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim) {
          rows * head_dim * 4;
 }
 
-void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta, int slot_rows) {
+void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta) {
   char* p = (char*)ws;
   a.rec = (PieceRecord*)p;
   p += align_up(n_cta * sizeof(PieceRecord), 256);
   a.part_lse = (float*)p;
-  p += align_up((size_t)2 * n_cta * slot_rows * 4, 256);
+  p += align_up((size_t)2 * n_cta * a.slot_rows * 4, 256);
   a.part_o = (float*)p;
 }
 
-ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int slot_rows,
-                              int n_cta, cudaStream_t s) {
+ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int n_cta,
+                              cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
   // large items are joined four rows per warp (256 rows of 2 pieces: 13.4 us for 151
   // items, a row per warp 18.2), small ones, often of many pieces, a row per warp
@@ -181,15 +181,13 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
   const int threads = kMergeWarps * 32;
   if (bf16 && head_dim == 128)
     return launch_dependent(paged_merge_kernel<__nv_bfloat16, float4>, grid, threads, 0, s, a,
-                            slot_rows, n_cta);
+                            n_cta);
   if (bf16)
     return launch_dependent(paged_merge_kernel<__nv_bfloat16, float2>, grid, threads, 0, s, a,
-                            slot_rows, n_cta);
-  if (head_dim == 128)
-    return launch_dependent(paged_merge_kernel<float, float4>, grid, threads, 0, s, a, slot_rows,
                             n_cta);
-  return launch_dependent(paged_merge_kernel<float, float2>, grid, threads, 0, s, a, slot_rows,
-                          n_cta);
+  if (head_dim == 128)
+    return launch_dependent(paged_merge_kernel<float, float4>, grid, threads, 0, s, a, n_cta);
+  return launch_dependent(paged_merge_kernel<float, float2>, grid, threads, 0, s, a, n_cta);
 }
 
 }  // namespace ebd

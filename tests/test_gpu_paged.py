@@ -437,6 +437,25 @@ def test_attention_reports_bad_pages_and_offsets(E, dtype, new):
     assert pc.dev_status.item() == E.EBD_DEV_RANGE
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("most", [1, 7, 31])
+def test_attention_more_new_tokens_than_the_bound(E, dtype, most):
+    """A sequence with more new tokens than max_new: a status bit, its tokens past
+    the bound are left as they were, nothing else is touched."""
+    s = R.make([most, 40, 1], [900, 800, 300], 8, 2, 128, 32, dtype, 96)
+    pc = cache(E, s)
+    y = torch.full((s["T"], 8, 128), 7.0, dtype=dtype, device="cuda")
+    need = E.ebd_paged_attention_workspace_bytes(pc, 8, most)
+    ws = torch.full((need + 4096,), 9, dtype=torch.uint8, device="cuda")
+    E.ebd_paged_attention(s["q"], pc, s["cu"], most, y=y, workspace=ws[:need])
+    assert pc.dev_status.item() == E.EBD_DEV_RANGE
+    assert (ws[need:] == 9).all()
+    assert (y[2 * most:most + 40] == 7).all()
+    keep = list(range(most)) + [most + 40]
+    ry, _ = R.attention(s["q"], s["K"], s["V"], s["bt"], s["seq_len"], s["cu"], 128 ** -0.5, 0)
+    assert (y.double() - ry)[keep].abs().max().item() <= 2e-5 * 5.5 + 2 * unit(dtype) * 5.5
+
+
 # ---------------------------------------------------------------- gather
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["head", "row"])
