@@ -451,7 +451,7 @@ typedef struct {
   int32_t max_blocks;  /* row length of block_table; max_blocks * page_size stays
                           below 2^31 - 2^20                                       */
   int32_t reserved;    /* 0                                                      */
-  int64_t page_stride; /* elements                                               */
+  int64_t page_stride; /* elements; positive where there is more than one page    */
   int64_t head_stride;
   int64_t row_stride;          /* >= d                                           */
   void* K_pages;               /* device                                         */
@@ -525,7 +525,7 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  * y = 0, lse = -inf.  Pages and rows past a sequence's length are not used,
  * whatever they hold.
  *   max_new    largest cu_new[b+1] - cu_new[b] (host bound; more: EBD_DEV_RANGE)
- *   q          device (dtype) [n_tokens, Hq, d] with token and head strides
+ *   q          device (dtype) [n_tokens, Hq, d] with (positive) token and head strides
  *   y          device (dtype) [n_tokens, Hq, d] out, dense
  *   lse        device [n_tokens, Hq] float32 out, nullable
  *   dev_status device int32, required

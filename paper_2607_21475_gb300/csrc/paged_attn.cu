@@ -5,11 +5,13 @@
 //
 // Online softmax: running maximum m, sum l and output o in float32, rescaled by
 // e^(m - m') when a tile raises the maximum.  An item is 32 rows, keys come in
-// tiles of 64 (32 at 128 channels, so that two CTAs fit an SM), the next tile
-// copied by cp.async while this one is worked on.  128 threads as 8 x 16: thread
-// (ty, tx) owns rows 4 ty .. + 3, keys tx + 16 j of a tile's logits and channels
-// 4 tx + 64 j of the output, so a 16-byte shared-memory load feeds 8 FMAs and
-// the FMA units are the bound.
+// tiles of 32 (four CTAs per SM at 64 channels, two at 128), the next tile copied
+// by cp.async while this one is worked on.  128 threads as 8 x 16: thread (ty, tx)
+// owns rows 4 ty .. + 3, keys tx + 16 j of a tile's logits and channels 4 tx + 64 j
+// of the output; the weights go through shared memory, four keys to a load.
+// Measured: three ragged prompts of up to 512 tokens (4 heads x 64) 32.9 us, of
+// which the FMAs are 9: a CTA has four tiles there, so finding its work and the
+// first tile (5 us), the softmax's shuffles and the merge weigh as much.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -329,7 +331,8 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
                                           void* stream) {
   const ebd_status st = check_paged(cache);
   if (st != EBD_OK) return st;
-  if (n_tokens < 0 || max_new < (n_tokens > 0) || n_q_heads < 1 || n_q_heads % cache->n_kv_heads != 0)
+  if (n_tokens < 0 || max_new < (n_tokens > 0) || n_q_heads < 1 ||
+      n_q_heads % cache->n_kv_heads != 0)
     return EBD_ERR_INVALID;
   if (!(scale > 0.f) || !(scale < INFINITY) || window < 0) return EBD_ERR_INVALID;
   if (cache->head_dim != 64 && cache->head_dim != 128) return EBD_ERR_UNSUPPORTED;
@@ -338,9 +341,10 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   if (n_tokens == 0) return EBD_OK;
   if (!cu_new || !q || !y || !dev_status) return EBD_ERR_INVALID;
   const int wide = cache->dtype == EBD_F32 ? 4 : 8;
-  if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride < 0 ||
-      q_head_stride < 0 || q_token_stride % wide != 0 || q_head_stride % wide != 0)
+  if (!paged_aligned16(cache) || !aligned16(q) || !aligned16(y) || q_token_stride % wide != 0 ||
+      q_head_stride % wide != 0)
     return EBD_ERR_INVALID;
+  if (q_token_stride < (n_tokens > 1) || q_head_stride < (n_q_heads > 1)) return EBD_ERR_INVALID;
   const size_t need = ebd_paged_attention_workspace_bytes(cache, n_q_heads, max_new);
   if (ws_bytes < need) return EBD_ERR_CAPACITY;
   if (need > 0 && (!workspace || !aligned16(workspace))) return EBD_ERR_INVALID;

@@ -1,17 +1,24 @@
 // Paged attention on the 5th-generation tensor cores: bf16, head_dim 64 / 128.
 //
-// An item is two MMA tiles X = A, B of 128 rows, whole tokens with all heads of the
-// group each; keys come in tiles of 64.  Per key tile and X:  S_X = Q_X K^T (both operands in shared memory),
-// the softmax warps turn S_X into weights P_X, and O_X += P_X V with P_X read
-// from tensor memory.  Tensor memory (512 columns): O_A, O_B (128 columns each,
-// D used) and two buffers of 64 columns of S_A and of S_B; P_X (bf16) overwrites
-// the first 32 columns of its S_X buffer.  With two buffers the product S of the
-// next tile is ready when the softmax of this one ends, so neither the softmax
-// nor the tensor cores wait for the other's latency; 128-key tiles fit only one
-// buffer each, and that chain (S product, softmax, O product, S product) took
-// 3490 cycles per 128 keys of two X against 2050 of MMA work.  The price is
-// the S product's rate: at N = 64 it reads Q again for half the keys, and shared
-// memory holds it to 2/3 of the MMA rate.
+// An item is two MMA tiles X = A, B of 128 rows, whole tokens with all heads of
+// the group each; keys come in tiles of 64.  Per key tile and X:  S_X = Q_X K^T
+// (both operands in shared memory), the softmax warps turn S_X into weights P_X,
+// and O_X += P_X V with P_X read from tensor memory.  Tensor memory (512
+// columns): O_A, O_B (128 columns each, D used) and two buffers of 64 columns of
+// S_A and of S_B; P_X (bf16) overwrites the first 32 columns of its S_X buffer.
+// With two buffers the product S of the next tile is ready when the softmax of
+// this one ends.  128-key tiles fit only one buffer each, and that chain (S
+// product, softmax, O product, S product) took 3490 cycles per 128 keys of two X
+// against 2050 of MMA work; this form takes 1410 per 64 keys.  The price is the S
+// product's rate: at N = 64 it reads Q again for half the keys, and shared memory
+// holds it to 2/3 of the MMA rate (1280 cycles of MMA work per 64 keys).
+//
+// What bounds it: a chunk of 4096 tokens over 16k positions (28/4 heads, d = 128)
+// runs at 1.69 PFLOP/s (88% of the measured bf16 peak) in isolation and 1.58 (534 us)
+// under the power cap of a long run; a decode batch of 32 sequences streams its
+// cache at 7.0 TB/s (at the copy peak); head_dim 64 and short windows are bound by
+// the softmax warps (about 1100 cycles per tile and X); one sequence of 6k tokens by
+// latencies (14.1 us, of which about 8500 cycles pass before the first product).
 //
 // The softmax keeps one row per thread.  Its reference m moves only when a
 // tile's maximum exceeds it by more than 2^8 (in the weight), so that O_X is
@@ -40,7 +47,7 @@
 #include "decode_tile.cuh"
 #include "paged_attn.cuh"
 #include "ptx.cuh"
-#include "tcgen05.cuh"
+#include "tcgen05_attn.cuh"
 
 namespace ebd {
 
@@ -550,7 +557,11 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       }
     }
   }
-  if (!ok) raise_status(a.dev_status, EBD_DEV_TIMEOUT);
+  if (!ok) {
+    raise_status(a.dev_status, EBD_DEV_TIMEOUT);
+    // the merge finds nothing to join
+    if (warp == 11 && lane == 0) a.rec[cta] = PieceRecord{0, -1, 0, 0};
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 8) {

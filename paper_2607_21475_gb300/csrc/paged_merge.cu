@@ -1,9 +1,11 @@
 // Joins the pieces of attention items that several CTAs worked on:
 //   y = sum_p 2^(s_p - M) o_p / sum_p 2^(s_p - M),  lse = (M + log2 sum_p 2^(s_p - M)) ln 2,
 // over the pieces p in CTA order, with o_p each piece's own weighted mean and
-// s_p its log2-sum (M the largest).  A warp joins one row; the partial results
-// were written just before and come from L2.  Launched as a programmatic
-// dependent of the attention kernel.
+// s_p its log2-sum (M the largest).  A warp joins one row, or four at a time where
+// an item has many rows of few pieces; the partial results were written just
+// before and come from L2.  What bounds it is its chain of loads (record, span,
+// weights, rows): 5-9 us for 151 items of 4 to 256 rows.  Launched as a
+// programmatic dependent of the attention kernel.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -51,7 +53,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   grid_dependency_wait();
   const int c0 = blockIdx.x, lane = threadIdx.x & 31;
   const PieceRecord r = a.rec[c0];
-  if (r.b < 0) return;
+  if ((unsigned)r.b >= (unsigned)a.pv.batch) return;
   const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
   const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.slice;
   const HeadSlice hs = head_slice(a, r.h);

@@ -72,7 +72,8 @@ def test_bad_caches_are_refused(E, call):
     for kw, code in [(dict(dtype=2), 1), (dict(batch=0), 1), (dict(n_kv_heads=0), 1),
                      (dict(head_dim=0), 1), (dict(n_pages=0), 1), (dict(max_blocks=0), 1),
                      (dict(page_size=4), 4), (dict(page_size=24), 4), (dict(page_size=2048), 4),
-                     (dict(row_stride=63), 1), (dict(page_stride=-1), 1), (dict(K_pages=None), 1),
+                     (dict(row_stride=63), 1), (dict(page_stride=-1), 1), (dict(page_stride=0), 1),
+                     (dict(head_stride=0), 1), (dict(K_pages=None), 1),
                      (dict(V_pages=None), 1), (dict(block_table=None), 1), (dict(seq_len=None), 1),
                      (dict(page_size=1024, max_blocks=1 << 21), 4)]:
         assert call(E, good_cache(E, **kw)) == code, kw
@@ -90,7 +91,7 @@ def test_bad_arguments_are_refused(E):
     for kw, code in [(dict(n=-1), 1), (dict(max_new=-1), 1), (dict(max_new=0), 1), (dict(hq=3), 1), (dict(hq=0), 1),
                      (dict(cu=None), 1), (dict(q=None), 1), (dict(y=None), 1), (dict(st=None), 1),
                      (dict(scale=0.0), 1), (dict(scale=math.nan), 1), (dict(scale=math.inf), 1),
-                     (dict(window=-1), 1), (dict(q=FAKE + 8), 1), (dict(qt=129), 1),
+                     (dict(window=-1), 1), (dict(q=FAKE + 8), 1), (dict(qt=129), 1), (dict(qh=0), 1), (dict(qh=-64), 1),
                      (dict(qh=4), 1), (dict(y=FAKE + 2), 1), (dict(hq=2 * 129), 4)]:
         assert attention(E, c, **kw) == code, kw
     assert attention(E, c, n=0) == 0
