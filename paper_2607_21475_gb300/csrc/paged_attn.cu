@@ -214,8 +214,8 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
       const bool mine = t < tokens && g < hs.n;
       const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
-      const size_t prow = (size_t)slot * a.slot_rows + r;
-      float* dst = slot < 0 ? (float*)a.y + out * D : a.part_o + prow * D;
+      float* dst = slot < 0 ? (float*)a.y + out * D : part_row<D>(a, slot, r);
+      const int step = slot < 0 ? 4 : a.part_step;  // between 4-channel groups
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
       nan_groups[i] = 0;
 #pragma unroll
@@ -227,11 +227,11 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
           x[e] = o[i][c * 4 + e] * inv;
           nan = nan || x[e] != x[e];
         }
-        if (mine) store4(dst + c * 64 + tx * 4, x);
+        if (mine) store4(dst + (c * 16 + tx) * step, x);
         if (mine && nan) nan_groups[i] |= 1u << (4 * c + tx / 4);
       }
       const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
-      if (mine && tx == 0 && slot >= 0) a.part_lse[prow] = lse2;
+      if (mine && tx == 0 && slot >= 0) a.part_lse[(size_t)slot * a.slot_rows + r] = lse2;
       if (mine && tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
     }
     bool mend = false;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
             w.cur * BN, lo[i], hi[i], min(w.end * BN, w.sp.len), m[i] == -INFINITY ? 0.f : m[i],
             l[i] == 0.f ? 0.f : 1.f / l[i], nan_groups[i],
             slot < 0 ? (float*)a.y + out * D : nullptr,
-            slot < 0 ? nullptr : a.part_o + ((size_t)slot * a.slot_rows + r) * D);
+            slot < 0 ? nullptr : part_row<D>(a, slot, r));
       }
     }
   }
@@ -283,8 +283,9 @@ static ebd_status launch_paged_f32(PagedAttnArgs a, int n_cta, cudaStream_t s) {
   a.slice = slice;
   a.heads = a.pv.n_kv_heads * a.slices;
   a.tokens = a.half_tokens = kAttnRows / a.slice;
+  a.tile_work = a.full_work = 1;
   a.min_share = 2;
-  a.item_cost = 0;
+  a.item_cost = 1;
   if (!line_fits(a, SimtLayout<D>::kKeys)) return EBD_ERR_UNSUPPORTED;
   const ebd_status st =
       launch_dependent(paged_attn_f32_kernel<D>, dim3(n_cta), kAttnThreads, smem, s, a);
@@ -371,7 +372,5 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   if (cache->dtype == EBD_F32)
     return cache->head_dim == 128 ? launch_paged_f32<128>(a, n_cta, s)
                                   : launch_paged_f32<64>(a, n_cta, s);
-  a.min_share = 4;
-  a.item_cost = 4;
   return launch_paged_tc(a, *cache, n_cta, s);
 }

@@ -3,7 +3,7 @@
 // An item is one (sequence, KV head, m-tile): `tokens` new tokens with the query
 // heads of the group (row = token x head, token-major) over the key tiles of
 // BN positions that at least one row sees.  Items in order of (sequence, head, m-tile) form
-// one line of work, each as long as its key tiles and `item_cost` tiles more (the
+// one line of work, each as long as its key tiles' work and `item_cost` more (the
 // time that beginning and ending an item takes), and CTA c of n takes
 // [c share, (c + 1) share) of it, whatever items that belongs to: every CTA gets
 // the same work however ragged the batch is.  A CTA's range is cut at
@@ -46,16 +46,20 @@ struct PagedAttnArgs {
   // 2 c + 1 for one that begins an item without ending it
   PieceRecord* rec;  // [n_cta]
   float* part_lse;   // [2 n_cta][slot rows], log2 units
-  float* part_o;     // [2 n_cta][slot rows][D]
+  float* part_o;     // [2 n_cta][slot rows / 32][D / 4][32 rows][4]: a warp that has a
+                     // row per lane reads and writes whole lines
   // A kernel with few rows per item cuts a large group into slices of at most
   // `slice` query heads; each slice is a head of its own on the line of items.
   int heads;         // KV heads x slices
   int slices, slice;
   int tokens;        // new tokens per item
   int half_tokens;   // of those, how many the slot's first 128 rows hold
-  int slot_rows;     // rows of a partial result
-  int min_share;     // least work per CTA, in key tiles
-  int item_cost;     // work of an item beside its key tiles, in key tiles
+  int slot_rows;     // rows of a partial result: 8, 16 or a multiple of 32
+  int part_step;     // floats between 4-channel groups of a row in part_o
+  int tile_work;     // work of a key tile of an item of at most half_tokens tokens,
+  int full_work;     // and of a larger item
+  int min_share;     // least work per CTA
+  int item_cost;     // work of an item beside its key tiles
 };
 
 // KV head, first query head and number of query heads of (sliced) head h.
@@ -91,6 +95,18 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
   }
 }
 
+// Work of a key tile of m-tile m of n new tokens.
+__device__ __forceinline__ int tile_work(const PagedAttnArgs& a, int n, int m) {
+  return n - m * a.tokens > a.half_tokens ? a.full_work : a.tile_work;
+}
+
+// Channel 0 of row `row` of a partial result; channels 4 c .. + 3 are c part_step
+// floats further.
+template <int D>
+__device__ __forceinline__ float* part_row(const PagedAttnArgs& a, int slot, int row) {
+  return a.part_o + ((size_t)slot * a.slot_rows + (row & ~31)) * D + (row & 31) * 4;
+}
+
 struct WorkStart {
   int b, h, m;
   int off;          // work of the item that earlier CTAs have
@@ -121,7 +137,7 @@ __device__ __forceinline__ int sequence_tiles(const PagedAttnArgs& a, int base, 
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
-    c += ke - kb + a.item_cost;
+    c += (ke - kb) * tile_work(a, sp.n, m) + a.item_cost;
   }
   // long chunks: the warp walks the remaining m-tiles of one sequence together
   for (uint32_t left = __ballot_sync(0xffffffffu, mt > 4); left; left &= left - 1) {
@@ -132,7 +148,7 @@ __device__ __forceinline__ int sequence_tiles(const PagedAttnArgs& a, int base, 
     for (int m = 4 + lane; m < k; m += 32) {
       int kb, ke;
       item_range<BN>(a, n, len, m, kb, ke);
-      sum += ke - kb + a.item_cost;
+      sum += (ke - kb) * tile_work(a, n, m) + a.item_cost;
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -180,9 +196,13 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
     return w;
   }
   for (int base = 0; base < mt; base += 32) {
-    int kb = 0, ke = -a.item_cost;
-    if (base + lane < mt) item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
-    const int work = ke - kb + a.item_cost, upto = warp_scan_add(work, lane);
+    int work = 0;
+    if (base + lane < mt) {
+      int kb, ke;
+      item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
+      work = (ke - kb) * tile_work(a, sp.n, base + lane) + a.item_cost;
+    }
+    const int upto = warp_scan_add(work, lane);
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
       const int src = __ffs(past) - 1;
@@ -219,12 +239,14 @@ struct PieceWalk {
     mt = (sp.n + a.tokens - 1) / a.tokens;
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
   }
-  // This CTA's tiles of the item, of which earlier CTAs have `off`: an item's own
-  // cost comes first, so a share that ends within it has no tile.
+  // This CTA's tiles of the item, of which earlier CTAs have the first `off` of its
+  // work: an item's own cost comes first, so a share that ends within it has no
+  // tile; a tile cut in two is the later CTA's.
   __device__ __forceinline__ void take(const PagedAttnArgs& a, int off) {
-    const int most = ke - kb + a.item_cost - off, mine = min(most, left);
-    cur = kb + max(0, off - a.item_cost);
-    end = kb + max(0, off + mine - a.item_cost);
+    const uint32_t each = tile_work(a, sp.n, m);
+    const int most = (ke - kb) * (int)each + a.item_cost - off, mine = min(most, left);
+    cur = kb + (int)((uint32_t)max(0, off - a.item_cost) / each);
+    end = kb + (int)((uint32_t)max(0, off + mine - a.item_cost) / each);
     left -= mine;
   }
   __device__ __forceinline__ bool live() const { return left >= 0; }
@@ -287,8 +309,8 @@ __device__ __forceinline__ void round_to(float x, __nv_bfloat16& y) { y = __floa
 // hundred at either end are hidden) is not finite are recomputed from those that
 // the row sees, [lo, hi) of them; a NaN in any other channel is the row's own.  The
 // sum stops once every such channel has met a NaN of its own.  q: the row's
-// query; base, inv: reference (log2) and reciprocal sum of its weights; y or part:
-// the output, as written.
+// query; base, inv: reference (log2) and reciprocal sum of its weights; y or part
+// (part_row): the output, as written.
 template <typename T, int D>
 __device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
                                       int tile_lo, int lo, int hi, int tile_hi, float base,
@@ -308,7 +330,7 @@ __device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, co
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float o = y ? to_f32(y[c + i]) : part[c + i];
+      const float o = y ? to_f32(y[c + i]) : part[(c + i) / 4 * a.part_step + i % 4];
       if (o == o) mend &= ~(1u << i);
     }
     if (!mend) continue;
@@ -333,7 +355,7 @@ __device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, co
     for (int i = 0; i < 16; ++i) {
       if (!(mend >> i & 1)) continue;
       if (y) round_to(acc[i] * inv, y[c + i]);
-      else part[c + i] = acc[i] * inv;
+      else part[(c + i) / 4 * a.part_step + i % 4] = acc[i] * inv;
     }
   }
 }
@@ -342,7 +364,7 @@ __device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, co
 inline bool line_fits(const PagedAttnArgs& a, int keys_per_tile) {
   const double tiles = (double)a.pv.max_blocks * (1 << a.pv.page_shift) / keys_per_tile + 1;
   const double items = (double)a.n_tokens / a.tokens + a.pv.batch;
-  return items * a.heads * (tiles + a.item_cost) < 2.0e9;
+  return items * a.heads * (tiles * a.full_work + a.item_cost) < 2.0e9;
 }
 
 // Launches a kernel as a programmatic dependent of whatever precedes it in the
@@ -370,7 +392,9 @@ ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, i
 
 // Rows that a partial result needs: those of the largest item the call can have.
 inline int paged_slot_rows(int max_new, int half_tokens, int slice, int most) {
-  return max_new > half_tokens ? most : (max_new * slice + 7) / 8 * 8;
+  if (max_new > half_tokens) return most;
+  const int rows = max_new * slice;
+  return rows <= 8 ? 8 : rows <= 16 ? 16 : (rows + 31) / 32 * 32;
 }
 
 // Bytes of the split results of n_cta CTAs.

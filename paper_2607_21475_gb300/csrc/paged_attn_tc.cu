@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const float lse2 = l == 0.f ? -INFINITY : m * a.scale2 + log2f(l);
       const long long out = (long long)(w.token + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
-      const size_t prow = (size_t)slot * a.slot_rows + x * 128 + row;
+      float* part = part_row<D>(a, slot, x * 128 + row);  // when slot >= 0
       uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
@@ -293,10 +293,10 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         nan_groups |= ((z0 != z0 ? 1u : 0u) | (z1 != z1 ? 2u : 0u)) << (c / 16);
         if (!mine) {
         } else if (slot >= 0) {
-          float4* dst = reinterpret_cast<float4*>(a.part_o + prow * D + c);
+          float* dst = part + c / 4 * a.part_step;
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            dst[i] = make_float4(
+            *reinterpret_cast<float4*>(dst + i * a.part_step) = make_float4(
                 __uint_as_float(o[4 * i]) * inv, __uint_as_float(o[4 * i + 1]) * inv,
                 __uint_as_float(o[4 * i + 2]) * inv, __uint_as_float(o[4 * i + 3]) * inv);
         } else {
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         }
       }
       if (mine) {
-        if (slot >= 0) a.part_lse[prow] = lse2;
+        if (slot >= 0) a.part_lse[(size_t)slot * a.slot_rows + x * 128 + row] = lse2;
         else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
         if (nan_groups)
           mend_row<__nv_bfloat16, D>(
@@ -323,7 +323,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
               w.cur * kTcBN, lo, hi, min(w.end * kTcBN, w.len),
               m == -INFINITY ? 0.f : m * a.scale2, inv, nan_groups,
               slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
-              slot < 0 ? nullptr : a.part_o + prow * D);
+              slot < 0 ? nullptr : part);
       }
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
@@ -641,6 +641,10 @@ ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
   a.slice = a.group;
   a.half_tokens = 128 / a.group;
   a.tokens = 2 * a.half_tokens;
+  a.tile_work = 2;
+  a.full_work = 3;
+  a.min_share = 8;
+  a.item_cost = 8;
   if (!line_fits(a, kTcBN)) return EBD_ERR_UNSUPPORTED;
   const ebd_status st =
       c.head_dim == 128 ? launch_tc_t<128>(a, c, n_cta, s) : launch_tc_t<64>(a, c, n_cta, s);

@@ -1,11 +1,11 @@
 // Joins the pieces of attention items that several CTAs worked on:
 //   y = sum_p 2^(s_p - M) o_p / sum_p 2^(s_p - M),  lse = (M + log2 sum_p 2^(s_p - M)) ln 2,
-// over the pieces p in CTA order, with o_p each piece's own weighted mean and
-// s_p its log2-sum (M the largest).  A warp joins one row, or four at a time where
-// an item has many rows of few pieces; the partial results were written just
-// before and come from L2.  What bounds it is its chain of loads (record, span,
-// weights, rows): 5-9 us for 151 items of 4 to 256 rows.  Launched as a
-// programmatic dependent of the attention kernel.
+// over the pieces p, with o_p each piece's own weighted mean and s_p its log2-sum
+// (M the largest).  A warp joins 16 channels of up to 32 rows, a row per lane; where
+// an item has 8 or 16 rows at most, 4 or 2 lanes share a row's pieces and add
+// up in a fixed order.  The partial results were written just before and come
+// from L2.  What bounds it is its chain of loads (record, span, pieces).
+// Launched as a programmatic dependent of the attention kernel.
 #include <cuda_runtime.h>
 #include <math.h>
 
@@ -15,39 +15,24 @@
 namespace ebd {
 
 constexpr int kMergeWarps = 8;
-constexpr int kMergeFlight = 4;  // pieces in flight per warp
+constexpr int kMergeChannels = 16;
 
-__device__ __forceinline__ void store_row(float* p, int lane, float4 v) {
-  reinterpret_cast<float4*>(p)[lane] = v;
+__device__ __forceinline__ void store16(float* p, const float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    reinterpret_cast<float4*>(p)[i] =
+        make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
 }
-__device__ __forceinline__ void store_row(float* p, int lane, float2 v) {
-  reinterpret_cast<float2*>(p)[lane] = v;
-}
-__device__ __forceinline__ void store_row(__nv_bfloat16* p, int lane, float4 v) {
-  reinterpret_cast<uint2*>(p)[lane] = make_uint2(pack_bf16(v.x, v.y), pack_bf16(v.z, v.w));
-}
-__device__ __forceinline__ void store_row(__nv_bfloat16* p, int lane, float2 v) {
-  reinterpret_cast<uint32_t*>(p)[lane] = pack_bf16(v.x, v.y);
-}
-__device__ __forceinline__ void add_scaled(float4& o, float f, const float4& v) {
-  o.x = fmaf(f, v.x, o.x);
-  o.y = fmaf(f, v.y, o.y);
-  o.z = fmaf(f, v.z, o.z);
-  o.w = fmaf(f, v.w, o.w);
-}
-__device__ __forceinline__ void add_scaled(float2& o, float f, const float2& v) {
-  o.x = fmaf(f, v.x, o.x);
-  o.y = fmaf(f, v.y, o.y);
-}
-__device__ __forceinline__ float4 scaled(const float4& v, float f) {
-  return make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-}
-__device__ __forceinline__ float2 scaled(const float2& v, float f) {
-  return make_float2(v.x * f, v.y * f);
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const float (&v)[16]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    reinterpret_cast<uint4*>(p)[i] =
+        make_uint4(pack_bf16(v[8 * i], v[8 * i + 1]), pack_bf16(v[8 * i + 2], v[8 * i + 3]),
+                   pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
 }
 
-// VT: the float vector that a lane of a warp owns of a row (D / 32 floats).
-template <typename T, typename VT>
+// FLIGHT: pieces of a lane in flight.
+template <typename T, int D, int FLIGHT>
 __global__ void __launch_bounds__(kMergeWarps * 32)
     paged_merge_kernel(const PagedAttnArgs a, int n_cta) {
   grid_dependency_wait();
@@ -56,6 +41,12 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   if ((unsigned)r.b >= (unsigned)a.pv.batch) return;
   const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
   const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.slice;
+  // this warp's rows of the slot (its second half starts at row 128) and channels
+  constexpr int kParts = D / kMergeChannels;
+  const int task = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
+  const int part = task % kParts, row0 = task / kParts * 32;
+  const int half_rows = a.half_tokens * a.slice;
+  if (row0 >= (rows > half_rows ? 128 + rows - half_rows : rows)) return;
   const HeadSlice hs = head_slice(a, r.h);
   // the item goes on through the first pieces of the following CTAs: up to the
   // first that does not just continue it (32 records at a time)
@@ -68,93 +59,72 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
       break;
     }
   }
-  constexpr int D = 32 * (int)(sizeof(VT) / 4);
-  const int hq = a.pv.n_kv_heads * a.group;
   const int n = c1 - c0 + 1;
-  // piece k of row `row` in part_lse, and (times D) in part_o
-  const auto place = [&](int k, int row) {
-    return (size_t)(2 * (c0 + k) + (k == 0)) * a.slot_rows + row;
-  };
-  // row i of the item is token t, head g; the slot's second half starts at row 128
-  const auto row_of = [&](int i) {
-    return i < a.half_tokens * a.slice ? i : 128 + i - a.half_tokens * a.slice;
-  };
-  const auto write = [&](int i, const VT& o, float sum, float M) {
-    const int t = i / a.slice, g = i - t * a.slice;
-    if (g >= hs.n) return;
-    const long long out = (long long)(sp.t0 + r.m * a.tokens + t) * hq + hs.q0 + g;
-    store_row((T*)a.y + out * D, lane, scaled(o, sum == 0.f ? 0.f : 1.f / sum));
-    if (a.lse && lane == 0) a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
-  };
-  const int w0 = blockIdx.y * kMergeWarps + (threadIdx.x >> 5), ws = gridDim.y * kMergeWarps;
-  if (n <= 8 && rows > 64) {
-    // few pieces of many rows: four rows at a time, lane 8 e + k weighs piece k of row e
-    for (int i0 = w0 * 4; i0 < rows; i0 += ws * 4) {
-      VT v[4][2];  // the first two pieces' rows do not wait for the weights
+  // lanes: `wide` rows, 32 / wide lanes share a row's pieces
+  const int wide = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
+  const int row = row0 + (lane & (wide - 1)), k0 = lane / wide, by = 32 / wide;
+  const int i = row < 128 ? row : half_rows + row - 128;  // row of the item
+  const bool live = i < rows && (row >= 128 || i < half_rows);
+  float M = -INFINITY, sum = 0.f, o[kMergeChannels] = {};
+  for (int k = k0; k < n && live; k += by * FLIGHT) {
+    float s[FLIGHT];
+    float4 v[FLIGHT][kMergeChannels / 4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int row = row_of(min(i0 + e, rows - 1));
+    for (int e = 0; e < FLIGHT; ++e) {
+      const int p = k + e * by, slot = 2 * (c0 + p) + (p == 0);
+      s[e] = -INFINITY;
+      if (p < n) {
+        s[e] = a.part_lse[(size_t)slot * a.slot_rows + row];
+        const float* src = part_row<D>(a, slot, row) + part * (kMergeChannels / 4) * a.part_step;
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
-          v[e][k] = reinterpret_cast<const VT*>(a.part_o + place(k, row) * D)[lane];
-      }
-      const float s = (lane & 7) < n
-                          ? a.part_lse[place(lane & 7, row_of(min(i0 + (lane >> 3), rows - 1)))]
-                          : -INFINITY;
-      float M = s;
+        for (int c = 0; c < kMergeChannels / 4; ++c)
+          v[e][c] = *reinterpret_cast<const float4*>(src + c * a.part_step);
+      } else {
 #pragma unroll
-      for (int o = 1; o < 8; o <<= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-      const float f = exp2f(s - (M == -INFINITY ? 0.f : M));
-      float sum = f;
-#pragma unroll
-      for (int o = 1; o < 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        VT o = {};
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-          add_scaled(o, __shfl_sync(0xffffffffu, f, 8 * e + k), v[e][k]);
-        const int row = row_of(min(i0 + e, rows - 1));
-        for (int k = 2; k < n; ++k)
-          add_scaled(o, __shfl_sync(0xffffffffu, f, 8 * e + k),
-                     reinterpret_cast<const VT*>(a.part_o + place(k, row) * D)[lane]);
-        const float se = __shfl_sync(0xffffffffu, sum, 8 * e);
-        const float me = __shfl_sync(0xffffffffu, M, 8 * e);
-        if (i0 + e < rows) write(i0 + e, o, se, me);
+        for (int c = 0; c < kMergeChannels / 4; ++c) v[e][c] = make_float4(0.f, 0.f, 0.f, 0.f);
       }
     }
-    return;
-  }
-  for (int i = w0; i < rows; i += ws) {
-    const int row = row_of(i);
-    // lane k keeps the weight of piece k of 32; the rows' loads do not wait for it
-    float s0 = lane < n ? a.part_lse[place(lane, row)] : -INFINITY;
-    float M = s0;
-    for (int k = 32 + lane; k < n; k += 32) M = fmaxf(M, a.part_lse[place(k, row)]);
-    M = warp_max(M);
-    const float base = M == -INFINITY ? 0.f : M;
-    float sum = 0.f;
-    VT o = {};
-    for (int k0 = 0; k0 < n; k0 += 32) {
-      if (k0 > 0) s0 = k0 + lane < n ? a.part_lse[place(k0 + lane, row)] : -INFINITY;
-      const float f = exp2f(s0 - base);
-      sum += f;
-      const int k = min(32, n - k0);
-      for (int j = 0; j < k; j += kMergeFlight) {
-        VT v[kMergeFlight];
+    float top = M;
 #pragma unroll
-        for (int e = 0; e < kMergeFlight; ++e)
-          if (j + e < k)
-            v[e] = reinterpret_cast<const VT*>(a.part_o + place(k0 + j + e, row) * D)[lane];
+    for (int e = 0; e < FLIGHT; ++e) top = fmaxf(top, s[e]);
+    const float base = top == -INFINITY ? 0.f : top;
+    const float f = exp2f(M - base);
+    M = top;
+    sum *= f;
 #pragma unroll
-        for (int e = 0; e < kMergeFlight; ++e) {
-          const float fe = __shfl_sync(0xffffffffu, f, (j + e) & 31);
-          if (j + e < k) add_scaled(o, fe, v[e]);
-        }
+    for (int c = 0; c < kMergeChannels; ++c) o[c] *= f;
+#pragma unroll
+    for (int e = 0; e < FLIGHT; ++e) {
+      const float w = exp2f(s[e] - base);
+      sum += w;
+#pragma unroll
+      for (int c = 0; c < kMergeChannels / 4; ++c) {
+        o[4 * c] = fmaf(w, v[e][c].x, o[4 * c]);
+        o[4 * c + 1] = fmaf(w, v[e][c].y, o[4 * c + 1]);
+        o[4 * c + 2] = fmaf(w, v[e][c].z, o[4 * c + 2]);
+        o[4 * c + 3] = fmaf(w, v[e][c].w, o[4 * c + 3]);
       }
     }
-    write(i, o, warp_sum(sum), M);
   }
+  for (int x = wide; x < 32; x <<= 1) {
+    const float m1 = __shfl_xor_sync(0xffffffffu, M, x), s1 = __shfl_xor_sync(0xffffffffu, sum, x);
+    const float top = fmaxf(M, m1), base = top == -INFINITY ? 0.f : top;
+    const float f0 = exp2f(M - base), f1 = exp2f(m1 - base);
+    M = top;
+    sum = sum * f0 + s1 * f1;
+#pragma unroll
+    for (int c = 0; c < kMergeChannels; ++c)
+      o[c] = o[c] * f0 + __shfl_xor_sync(0xffffffffu, o[c], x) * f1;
+  }
+  const int t = i / a.slice, g = i - t * a.slice;
+  if (!live || k0 > 0 || g >= hs.n) return;
+  const long long out =
+      (long long)(sp.t0 + r.m * a.tokens + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int c = 0; c < kMergeChannels; ++c) o[c] *= inv;
+  store16((T*)a.y + out * D + part * kMergeChannels, o);
+  if (a.lse && part == 0) a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
 size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim) {
@@ -170,26 +140,28 @@ void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta) {
   a.part_lse = (float*)p;
   p += align_up((size_t)2 * n_cta * a.slot_rows * 4, 256);
   a.part_o = (float*)p;
+  a.part_step = 4 * (a.slot_rows < 32 ? a.slot_rows : 32);
+}
+
+template <typename T, int D>
+static ebd_status launch_merge_t(const PagedAttnArgs& a, int n_cta, cudaStream_t s) {
+  const int rows = a.slot_rows > 32 ? a.slot_rows : 32;
+  const int tasks = (rows + 31) / 32 * (D / kMergeChannels);
+  const dim3 grid(n_cta - 1, (tasks + kMergeWarps - 1) / kMergeWarps);
+  // items of few rows often have many pieces, and there are few warps then
+  if (a.slot_rows <= 32)
+    return launch_dependent(paged_merge_kernel<T, D, 4>, grid, kMergeWarps * 32, 0, s, a, n_cta);
+  return launch_dependent(paged_merge_kernel<T, D, 2>, grid, kMergeWarps * 32, 0, s, a, n_cta);
 }
 
 ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int n_cta,
                               cudaStream_t s) {
   if (n_cta <= 1) return EBD_OK;
-  // large items are joined four rows per warp (256 rows of 2 pieces: 13.4 us for 151
-  // items, a row per warp 18.2), small ones, often of many pieces, a row per warp
-  const int most = min(a.max_new, a.tokens) * a.slice;
-  const int per_block = most > 64 ? 4 * kMergeWarps : kMergeWarps;
-  const dim3 grid(n_cta - 1, (most + per_block - 1) / per_block);
-  const int threads = kMergeWarps * 32;
-  if (bf16 && head_dim == 128)
-    return launch_dependent(paged_merge_kernel<__nv_bfloat16, float4>, grid, threads, 0, s, a,
-                            n_cta);
   if (bf16)
-    return launch_dependent(paged_merge_kernel<__nv_bfloat16, float2>, grid, threads, 0, s, a,
-                            n_cta);
-  if (head_dim == 128)
-    return launch_dependent(paged_merge_kernel<float, float4>, grid, threads, 0, s, a, n_cta);
-  return launch_dependent(paged_merge_kernel<float, float2>, grid, threads, 0, s, a, n_cta);
+    return head_dim == 128 ? launch_merge_t<__nv_bfloat16, 128>(a, n_cta, s)
+                           : launch_merge_t<__nv_bfloat16, 64>(a, n_cta, s);
+  return head_dim == 128 ? launch_merge_t<float, 128>(a, n_cta, s)
+                         : launch_merge_t<float, 64>(a, n_cta, s);
 }
 
 }  // namespace ebd
