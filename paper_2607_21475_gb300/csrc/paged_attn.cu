@@ -36,7 +36,7 @@ struct SimtLayout {
   static constexpr int kP = kV + 2 * kKeys * D;            // [rows][keys + 4]
   static constexpr int kOff = kP + kAttnRows * (kKeys + 4);  // [2][keys] row offsets, 64 bits
   static constexpr int kStart = kOff + 4 * kKeys;
-  static constexpr int kFloats = kStart + 8;
+  static constexpr int kFloats = kStart + 12;
 };
 
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
@@ -64,6 +64,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   long long* offs = reinterpret_cast<long long*>(sm + L::kOff);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   WorkStart* start_s = reinterpret_cast<WorkStart*>(sm + L::kStart);
+  static_assert(sizeof(WorkStart) <= 12 * 4, "start");
   grid_dependency_wait();
   if (threadIdx.x < 32) {
     const WorkStart w = find_work<BN>(a, blockIdx.x, gridDim.x, threadIdx.x);

@@ -109,8 +109,10 @@ __device__ __forceinline__ float* part_row(const PagedAttnArgs& a, int slot, int
 
 struct WorkStart {
   int b, h, m;
-  int off;          // work of the item that earlier CTAs have
-  int count;      // work of this CTA
+  int off;     // work of the item that earlier CTAs have
+  int count;   // work of this CTA
+  int mt;      // m-tiles of the sequence
+  SeqSpan sp;  // and its span
 };
 
 __device__ __forceinline__ int warp_scan_add(int v, int lane) {
@@ -122,17 +124,17 @@ __device__ __forceinline__ int warp_scan_add(int v, int lane) {
   return v;
 }
 
-// Work of one head of the sequences base + lane (lane = 0..31).
+// Work of one head of the sequences base + lane (lane = 0..31), their spans and m-tiles.
 template <int BN>
-__device__ __forceinline__ int sequence_tiles(const PagedAttnArgs& a, int base, int lane,
-                                                    bool report) {
+__device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, int lane,
+                                             bool report, SeqSpan& sp, int& mt) {
   const int b = base + lane;
-  SeqSpan sp = {};
+  sp = SeqSpan{};
   if (b < a.pv.batch) {
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
     if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
   }
-  const int mt = (sp.n + a.tokens - 1) / a.tokens;
+  mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);
   int c = 0;
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
@@ -150,8 +152,7 @@ __device__ __forceinline__ int sequence_tiles(const PagedAttnArgs& a, int base, 
       item_range<BN>(a, n, len, m, kb, ke);
       sum += (ke - kb) * tile_work(a, n, m) + a.item_cost;
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    sum = __reduce_add_sync(0xffffffffu, sum);
     if (lane == src) c += sum;
   }
   return c;
@@ -162,55 +163,61 @@ template <int BN>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
   const int H = a.heads;
-  int total = 0, c = 0;
+  SeqSpan sp;
+  int total = 0, c = 0, upto = 0, mt = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
-    c = sequence_tiles<BN>(a, base, lane, cta == 0);
-    total += H * c;
+    c = sequence_work<BN>(a, base, lane, cta == 0, sp, mt);
+    upto = warp_scan_add(c * H, lane);
+    total += __shfl_sync(0xffffffffu, upto, 31);
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
   const int share = max(a.min_share, (int)((uint32_t)(total + n_cta - 1) / (uint32_t)n_cta));
   int at = cta * share;
-  WorkStart w = {0, 0, 0, 0, 0};
+  WorkStart w = {};
   if (at >= total) return w;
-  w.count = min(share, total - at);
+  const int count = min(share, total - at);
   for (int base = 0; base < a.pv.batch; base += 32) {
-    if (a.pv.batch > 32) c = sequence_tiles<BN>(a, base, lane, false);
-    const int upto = warp_scan_add(c * H, lane);
+    if (a.pv.batch > 32) {
+      c = sequence_work<BN>(a, base, lane, false, sp, mt);
+      upto = warp_scan_add(c * H, lane);
+    }
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
     if (past) {
       const int src = __ffs(past) - 1;
       at -= __shfl_sync(0xffffffffu, upto - c * H, src);
       c = __shfl_sync(0xffffffffu, c, src);
       w.b = base + src;
+      w.mt = __shfl_sync(0xffffffffu, mt, src);
+      w.sp.t0 = __shfl_sync(0xffffffffu, sp.t0, src);
+      w.sp.n = __shfl_sync(0xffffffffu, sp.n, src);
+      w.sp.len = __shfl_sync(0xffffffffu, sp.len, src);
+      w.count = count;
       break;
     }
     at -= __shfl_sync(0xffffffffu, upto, 31);
   }
+  if (w.count == 0) return w;  // the arrays changed under the call: no work
   w.h = (int)((uint32_t)at / (uint32_t)c);
   at -= w.h * c;
-  const SeqSpan sp = seq_span(a.pv, a.cu, w.b, a.n_tokens, a.max_new);
-  const int mt = (sp.n + a.tokens - 1) / a.tokens;
-  if (mt == 1) {
+  if (w.mt == 1) {
     w.off = at;
     return w;
   }
-  for (int base = 0; base < mt; base += 32) {
+  for (int base = 0; base < w.mt; base += 32) {
     int work = 0;
-    if (base + lane < mt) {
+    if (base + lane < w.mt) {
       int kb, ke;
-      item_range<BN>(a, sp.n, sp.len, base + lane, kb, ke);
-      work = (ke - kb) * tile_work(a, sp.n, base + lane) + a.item_cost;
+      item_range<BN>(a, w.sp.n, w.sp.len, base + lane, kb, ke);
+      work = (ke - kb) * tile_work(a, w.sp.n, base + lane) + a.item_cost;
     }
-    const int upto = warp_scan_add(work, lane);
-    const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
+    const int end = warp_scan_add(work, lane);
+    const uint32_t past = __ballot_sync(0xffffffffu, end > at);
     if (past) {
       const int src = __ffs(past) - 1;
       w.m = base + src;
-      w.off = at - __shfl_sync(0xffffffffu, upto - work, src);
+      w.off = at - __shfl_sync(0xffffffffu, end - work, src);
       break;
     }
-    at -= __shfl_sync(0xffffffffu, upto, 31);
+    at -= __shfl_sync(0xffffffffu, end, 31);
   }
   return w;
 }
@@ -225,18 +232,18 @@ struct PieceWalk {
   int left;      // work after this piece; -1: no piece
 
   __device__ __forceinline__ PieceWalk(const PagedAttnArgs& a, const WorkStart& w)
-      : b(w.b), h(w.h), m(w.m), left(w.count) {
+      : b(w.b), h(w.h), m(w.m), mt(w.mt), sp(w.sp), left(w.count) {
     if (left <= 0) {
       left = -1;
       return;
     }
-    load(a);
+    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
     take(a, w.off);
     if (cur == end) next(a);
   }
   __device__ __forceinline__ void load(const PagedAttnArgs& a) {
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
-    mt = (sp.n + a.tokens - 1) / a.tokens;
+    mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);
     item_range<BN>(a, sp.n, sp.len, m, kb, ke);
   }
   // This CTA's tiles of the item, of which earlier CTAs have the first `off` of its
@@ -245,8 +252,8 @@ struct PieceWalk {
   __device__ __forceinline__ void take(const PagedAttnArgs& a, int off) {
     const uint32_t each = tile_work(a, sp.n, m);
     const int most = (ke - kb) * (int)each + a.item_cost - off, mine = min(most, left);
-    cur = kb + (int)((uint32_t)max(0, off - a.item_cost) / each);
-    end = kb + (int)((uint32_t)max(0, off + mine - a.item_cost) / each);
+    cur = off <= a.item_cost ? kb : kb + (int)((uint32_t)(off - a.item_cost) / each);
+    end = mine == most ? ke : kb + (int)((uint32_t)max(0, off + mine - a.item_cost) / each);
     left -= mine;
   }
   __device__ __forceinline__ bool live() const { return left >= 0; }

@@ -150,6 +150,8 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   }
   fence_proxy_async_smem();
   grid_dependency_wait();  // nothing of the caller's was read or written so far
+  WorkStart start = {};
+  if (warp == 11) start = find_work<kTcBN>(a, cta, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -482,20 +484,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
     // ---------------- the CTA's pieces; query rows; value rows past the end
-    const WorkStart start = find_work<kTcBN>(a, cta, gridDim.x, lane);
     PieceWalk<kTcBN> walk(a, start);
     uint32_t items = 0, pushed = 0, tile0 = 0;  // tile0: tiles before this piece
     bool all = false;  // the end of the work was told
     PieceRecord record = {0, -1, 0, 0};
-    for (;; tile0 += w.end - w.cur, ++items) {
-      // two pieces ahead: the one two before this must have been dropped by then
-      for (; !all && pushed < items + 3; ++pushed) {
+    // Tells the roles pieces up to the limit-th.
+    auto push = [&](uint32_t limit) {
+      for (; !all && pushed < limit; ++pushed) {
         const uint32_t at = pushed % kPieceSlots;
         if (pushed >= kPieceSlots &&
-            !mbar_wait_warp(&bar->piece_empty[at], (pushed / kPieceSlots - 1) & 1)) {
-          ok = false;
-          break;
-        }
+            !mbar_wait_warp(&bar->piece_empty[at], (pushed / kPieceSlots - 1) & 1))
+          return false;
         Piece p = {};
         all = !walk.live();
         if (!all) {
@@ -509,7 +508,6 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           p.tokens = walk.tokens(a);
           p.slot = walk.slot(cta);
           record_piece(record, walk, pushed == 0);
-          walk.next(a);
         } else if (lane == 0) {
           a.rec[cta] = record;
         }
@@ -518,8 +516,16 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           mbar_arrive(&bar->piece_full[at]);
         }
         __syncwarp();
+        if (!all) walk.next(a);
       }
-      if (!ok || items + 1 >= pushed) break;  // the last one pushed says that there are no more
+      return true;
+    };
+    for (;; tile0 += w.end - w.cur, ++items) {
+      if (!push(items + 1)) {
+        ok = false;
+        break;
+      }
+      if (all && items + 1 >= pushed) break;  // the last one pushed says that there are no more
       w = bar->piece[items % kPieceSlots];
       if (items > 0 && !mbar_wait_warp(&bar->q_empty, (items - 1) & 1)) {
         ok = false;
@@ -535,6 +541,11 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
                         w.token + x * a.half_tokens, &bar->q_full);
       }
       __syncwarp();
+      // two pieces ahead: the one two before this must have been dropped by then
+      if (!push(items + 3)) {
+        ok = false;
+        break;
+      }
       if (w.len < w.end * kTcBN) {
         // The piece's last value tile.  Its stage's phase is certain only once the
         // piece's last S product is done (q_empty): the stage's earlier tile
