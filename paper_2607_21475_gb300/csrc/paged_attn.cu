@@ -129,6 +129,9 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
     }
+    // A warp whose 8 rows are all past the item's last leaves the arithmetic to the
+    // others, which are bound by shared-memory reads
+    const bool live = (threadIdx.x >> 5) * 8 < tokens * a.slice;
     for (int j = w.cur; j < w.end; ++j) {
       const int k0 = j * BN;
       const float *Ks = sm + L::kK + (j & 1) * BN * (D + 4), *Vs = sm + L::kV + (j & 1) * BN * D;
@@ -138,69 +141,71 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       // the rows of the tile after it: found while this one is worked on
       long long row = -1;
       if (j + 2 < w.end && threadIdx.x < BN) row = find_row(j + 2);
-      float s[4][NK] = {};
+      if (live) {
+        float s[4][NK] = {};
 #pragma unroll 4
-      for (int c = 0; c < D; c += 4) {
-        float q[4][4], k[NK][4];
+        for (int c = 0; c < D; c += 4) {
+          float q[4][4], k[NK][4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
+          for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
 #pragma unroll
-        for (int e = 0; e < NK; ++e) load4(Ks + (tx + 16 * e) * (D + 4) + c, k[e]);
+          for (int e = 0; e < NK; ++e) load4(Ks + (tx + 16 * e) * (D + 4) + c, k[e]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i)
 #pragma unroll
-          for (int e = 0; e < NK; ++e)
+            for (int e = 0; e < NK; ++e)
 #pragma unroll
-            for (int z = 0; z < 4; ++z) s[i][e] = fmaf(q[i][z], k[e][z], s[i][e]);
-      }
-      bool all = true;  // every row of the warp sees every key of the tile
-#pragma unroll
-      for (int i = 0; i < 4; ++i) all = all && lo[i] <= k0 && hi[i] >= k0 + BN;
-      all = __all_sync(0xffffffffu, all);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float top = m[i];
-#pragma unroll
-        for (int e = 0; e < NK; ++e) {
-          const int pos = k0 + tx + 16 * e;
-          s[i][e] = all || (pos >= lo[i] && pos < hi[i]) ? s[i][e] * a.scale2 : -INFINITY;
-          top = fmaxf(top, s[i][e]);
+              for (int z = 0; z < 4; ++z) s[i][e] = fmaf(q[i][z], k[e][z], s[i][e]);
         }
+        bool all = true;  // every row of the warp sees every key of the tile
 #pragma unroll
-        for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-        const float base = top == -INFINITY ? 0.f : top;  // nothing seen yet: every weight is 0
-        const float f = exp2f(m[i] - base);
-        m[i] = top;
-        float sum = 0.f;
+        for (int i = 0; i < 4; ++i) all = all && lo[i] <= k0 && hi[i] >= k0 + BN;
+        all = __all_sync(0xffffffffu, all);
 #pragma unroll
-        for (int e = 0; e < NK; ++e) {
-          const float p = exp2f(s[i][e] - base);
-          sum += p;
-          Ps[(ty * 4 + i) * (BN + 4) + tx + 16 * e] = p;
-        }
-        l[i] = l[i] * f + sum;  // this thread's share
+        for (int i = 0; i < 4; ++i) {
+          float top = m[i];
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
-      }
-      __syncwarp();  // a warp reads the weights of its own rows only
-      // hidden keys have weight 0; a hidden value that is not finite is mended below
-#pragma unroll 2
-      for (int k = 0; k < BN; k += 4) {
-        float p[4][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load4(Ps + (ty * 4 + i) * (BN + 4) + k, p[i]);
-#pragma unroll
-        for (int z = 0; z < 4; ++z)
-#pragma unroll
-          for (int c = 0; c < D / 64; ++c) {
-            float v[4];
-            load4(Vs + (k + z) * D + c * 64 + tx * 4, v);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                o[i][c * 4 + e] = fmaf(p[i][z], v[e], o[i][c * 4 + e]);
+          for (int e = 0; e < NK; ++e) {
+            const int pos = k0 + tx + 16 * e;
+            s[i][e] = all || (pos >= lo[i] && pos < hi[i]) ? s[i][e] * a.scale2 : -INFINITY;
+            top = fmaxf(top, s[i][e]);
           }
+#pragma unroll
+          for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+          const float base = top == -INFINITY ? 0.f : top;  // nothing seen yet: every weight is 0
+          const float f = exp2f(m[i] - base);
+          m[i] = top;
+          float sum = 0.f;
+#pragma unroll
+          for (int e = 0; e < NK; ++e) {
+            const float p = exp2f(s[i][e] - base);
+            sum += p;
+            Ps[(ty * 4 + i) * (BN + 4) + tx + 16 * e] = p;
+          }
+          l[i] = l[i] * f + sum;  // this thread's share
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+        }
+        __syncwarp();  // a warp reads the weights of its own rows only
+        // hidden keys have weight 0; a hidden value that is not finite is mended below
+#pragma unroll 2
+        for (int k = 0; k < BN; k += 4) {
+          float p[4][4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) load4(Ps + (ty * 4 + i) * (BN + 4) + k, p[i]);
+#pragma unroll
+          for (int z = 0; z < 4; ++z)
+#pragma unroll
+            for (int c = 0; c < D / 64; ++c) {
+              float v[4];
+              load4(Vs + (k + z) * D + c * 64 + tx * 4, v);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  o[i][c * 4 + e] = fmaf(p[i][z], v[e], o[i][c * 4 + e]);
+            }
+        }
       }
       // (stage j & 1's offsets were read before this tile's barrier)
       if (j + 2 < w.end && threadIdx.x < BN) offs[(j & 1) * BN + threadIdx.x] = row;
