@@ -72,9 +72,9 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   }
   __syncthreads();
   bool bad = false, first = true;
-  PieceRecord record = {0, -1, 0, 0};
+  PieceRecord record = {0, 0, 0, 0};
   for (PieceWalk<BN> w(a, *start_s); w.live(); w.next(a)) {
-    record_piece(record, w, first);
+    record_piece(a, record, w, first);
     first = false;
     const HeadSlice hs = head_slice(a, w.h);
     const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);

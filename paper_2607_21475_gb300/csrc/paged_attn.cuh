@@ -26,10 +26,11 @@ namespace ebd {
 
 // What a CTA leaves for the merge: whether its first piece continues an item
 // that an earlier CTA began (1: and does not end it, 2: and ends it), and the
-// item that its last piece begins without ending (b < 0: none).
+// item that its last piece begins without ending: its head, first packed token and
+// number of tokens (0: no such item).
 struct PieceRecord {
   int cont;
-  int b, h, m;
+  int h, token, tokens;
 };
 
 struct PagedAttnArgs {
@@ -296,13 +297,14 @@ struct PieceWalk {
 
 // Enters a piece into the CTA's record.
 template <int BN>
-__device__ __forceinline__ void record_piece(PieceRecord& r, const PieceWalk<BN>& p, bool first) {
+__device__ __forceinline__ void record_piece(const PagedAttnArgs& a, PieceRecord& r,
+                                             const PieceWalk<BN>& p, bool first) {
   if (first && p.cur > p.kb) {
     r.cont = p.end < p.ke ? 1 : 2;
   } else if (p.end < p.ke) {
-    r.b = p.b;
     r.h = p.h;
-    r.m = p.m;
+    r.token = p.sp.t0 + p.first(a);
+    r.tokens = p.tokens(a);
   }
 }
 

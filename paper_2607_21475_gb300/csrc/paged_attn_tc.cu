@@ -487,7 +487,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     PieceWalk<kTcBN> walk(a, start);
     uint32_t items = 0, pushed = 0, tile0 = 0;  // tile0: tiles before this piece
     bool all = false;  // the end of the work was told
-    PieceRecord record = {0, -1, 0, 0};
+    PieceRecord record = {0, 0, 0, 0};
     // Tells the roles pieces up to the limit-th.
     auto push = [&](uint32_t limit) {
       for (; !all && pushed < limit; ++pushed) {
@@ -507,7 +507,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           p.pos = walk.sp.len - walk.sp.n + walk.first(a);
           p.tokens = walk.tokens(a);
           p.slot = walk.slot(cta);
-          record_piece(record, walk, pushed == 0);
+          record_piece(a, record, walk, pushed == 0);
         } else if (lane == 0) {
           a.rec[cta] = record;
         }
@@ -571,7 +571,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   if (!ok) {
     raise_status(a.dev_status, EBD_DEV_TIMEOUT);
     // the merge finds nothing to join
-    if (warp == 11 && lane == 0) a.rec[cta] = PieceRecord{0, -1, 0, 0};
+    if (warp == 11 && lane == 0) a.rec[cta] = PieceRecord{0, 0, 0, 0};
   }
   tc_fence_before();
   __syncthreads();

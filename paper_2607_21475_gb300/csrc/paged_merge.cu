@@ -4,7 +4,7 @@
 // (M the largest).  A warp joins 16 channels of up to 32 rows, a row per lane; where
 // an item has 8 or 16 rows at most, 4 or 2 lanes share a row's pieces and add
 // up in a fixed order.  The partial results were written just before and come
-// from L2.  What bounds it is its chain of loads (record, span, pieces).
+// from L2.  What bounds it is its chain of loads (records, pieces).
 // Launched as a programmatic dependent of the attention kernel.
 #include <cuda_runtime.h>
 #include <math.h>
@@ -38,9 +38,14 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   grid_dependency_wait();
   const int c0 = blockIdx.x, lane = threadIdx.x & 31;
   const PieceRecord r = a.rec[c0];
-  if ((unsigned)r.b >= (unsigned)a.pv.batch) return;
-  const SeqSpan sp = seq_span(a.pv, a.cu, r.b, a.n_tokens, a.max_new);
-  const int rows = min(a.tokens, sp.n - r.m * a.tokens) * a.slice;
+  // the item goes on through the first pieces of the following CTAs: up to the
+  // first that does not just continue it (32 records at a time)
+  int c1 = c0 + 1;
+  bool on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
+  if (r.tokens < 1 || r.tokens > a.tokens || r.token < 0 || r.token > a.n_tokens - r.tokens ||
+      (unsigned)r.h >= (unsigned)a.heads)
+    return;  // none begun here
+  const int rows = r.tokens * a.slice;
   // this warp's rows of the slot (its second half starts at row 128) and channels
   constexpr int kParts = D / kMergeChannels;
   const int task = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
@@ -48,16 +53,14 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const int half_rows = a.half_tokens * a.slice;
   if (row0 >= (rows > half_rows ? 128 + rows - half_rows : rows)) return;
   const HeadSlice hs = head_slice(a, r.h);
-  // the item goes on through the first pieces of the following CTAs: up to the
-  // first that does not just continue it (32 records at a time)
-  int c1 = c0 + 1;
-  for (;; c1 += 32) {
-    const bool on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
+  for (;;) {
     const uint32_t off = ~__ballot_sync(0xffffffffu, on);
     if (off) {
       c1 += __ffs(off) - 1;
       break;
     }
+    c1 += 32;
+    on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
   }
   const int n = c1 - c0 + 1;
   // lanes: `wide` rows, 32 / wide lanes share a row's pieces
@@ -119,7 +122,7 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   const int t = i / a.slice, g = i - t * a.slice;
   if (!live || k0 > 0 || g >= hs.n) return;
   const long long out =
-      (long long)(sp.t0 + r.m * a.tokens + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+      (long long)(r.token + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
   for (int c = 0; c < kMergeChannels; ++c) o[c] *= inv;
