@@ -531,8 +531,8 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  *   dev_status device int32, required
  * Supports d in {64, 128}, G = Hq / Hkv <= 128; q, y and every cached row on
  * 16-byte boundaries (EBD_ERR_INVALID otherwise); EBD_ERR_UNSUPPORTED when the
- * bounds allow more work than 31 bits count (a million new tokens over a million
- * positions).  Products accumulate in float32; softmax statistics and partial
+ * bounds allow more work than 31 bits count (at 32 / 8 heads a million new tokens
+ * over 300 thousand positions).  Products accumulate in float32; softmax statistics and partial
  * outputs are float32; bf16 rounds the softmax weights once (2^-8 relative)
  * before they multiply the values.  A NaN or infinite key or value reaches only
  * the tokens that see it.  Needs workspace of

@@ -14,11 +14,12 @@
 // holds it to 2/3 of the MMA rate (1280 cycles of MMA work per 64 keys).
 //
 // What bounds it: a chunk of 4096 tokens over 16k positions (28/4 heads, d = 128)
-// runs at 1.69 PFLOP/s (88% of the measured bf16 peak) in isolation and 1.58 (534 us)
+// runs at 1.69 PFLOP/s (88% of the measured bf16 peak) in isolation and 1.59 (530 us)
 // under the power cap of a long run; a decode batch of 32 sequences streams its
 // cache at 7.0 TB/s (at the copy peak); head_dim 64 and short windows are bound by
-// the softmax warps (about 1100 cycles per tile and X); one sequence of 6k tokens by
-// latencies (14.1 us, of which about 8500 cycles pass before the first product).
+// the softmax warps (mixed batch with a window of 1024: 42 us, 1370 cycles per tile of
+// two X, 1070 of one); one sequence of 6k tokens by latencies (12.4 us, of which
+// about 8000 cycles pass before the first product).
 //
 // The softmax keeps one row per thread.  Its reference m moves only when a
 // tile's maximum exceeds it by more than 2^8 (in the weight), so that O_X is
@@ -652,9 +653,11 @@ ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
   a.slice = a.group;
   a.half_tokens = 128 / a.group;
   a.tokens = 2 * a.half_tokens;
+  // measured: 1070 cycles per tile of one X, 1370 of two (64 channels); equal weights
+  // left CTAs between 52k and 82k cycles of work in the mixed batch, these 64k to 77k
   a.tile_work = 2;
   a.full_work = 3;
-  a.min_share = 8;
+  a.min_share = 8;  // more than a tile: a CTA in the middle of an item has one at least
   a.item_cost = 8;
   if (!line_fits(a, kTcBN)) return EBD_ERR_UNSUPPORTED;
   const ebd_status st =
