@@ -258,6 +258,20 @@ def test_attention(E, dtype, d, case):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 7, 12, 16, 24, 32, 48, 128])
+@pytest.mark.parametrize("new,total", [([1], [5003]), ([2], [4100]), ([1, 150], [2900, 1300])])
+def test_items_split_over_many_ctas(E, dtype, d, group, new, total):
+    """Few rows over many keys: every CTA has a piece of an item, of 1 to 256 rows
+    in slots of 8 to 256; twice, with the same bits."""
+    s = R.make(new, total, group, 1, d, 32, dtype, 300 + group, stale=math.nan)
+    check_attention(E, s, dtype, None, 0)
+    y0, l0 = E.ebd_paged_attention(s["q"], cache(E, s), s["cu"], s["max_new"])
+    y1, l1 = E.ebd_paged_attention(s["q"], cache(E, s), s["cu"], s["max_new"])
+    assert torch.equal(y0, y1) and torch.equal(l0, l1)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["row", "side"])
 @pytest.mark.parametrize("new", [1, 70])
 def test_attention_over_other_pool_orders(E, dtype, order, new):
