@@ -655,8 +655,9 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "n
         # index at which a pair makes n turns over original_positions
         at = [rotary_dim / 2 * math.log(original_positions / (2 * math.pi * n)) / math.log(base)
               for n in (fast_turns, slow_turns)]
-        lo, hi = max(math.floor(at[0]), 0), min(math.ceil(at[1]), rotary_dim // 2 - 1)
-        slow = ((i / 2 - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        # either end may lie outside the pairs there are: the line between them stays
+        lo, hi = math.floor(at[0]), math.ceil(at[1])
+        slow = ((i / 2 - lo) / max(hi - lo, 1)).clamp(0, 1)
         return f * (1 - slow) + f / factor * slow, 0.1 * math.log(factor) + 1.0
     return f, 1.0
 

@@ -154,3 +154,33 @@ def test_frequency_scalings(E):
     assert torch.allclose(g[turns < 0.9], f[turns < 0.9] / 8, rtol=1e-12)
     mid = (turns < 30) & (turns > 1.2)
     assert (g[mid] < f[mid]).all() and (g[mid] > f[mid] / 8).all()
+
+
+@pytest.mark.parametrize("rot,base,factor,positions", [
+    (128, 1e4, 4.0, 131072),  # the ramp ends past the last pair
+    (64, 1e4, 8.0, 131072),
+    (64, 1e4, 8.0, 1 << 20),
+    (128, 1e4, 4.0, 100),     # the ramp begins before the first pair
+    (64, 1e4, 8.0, 4096),
+    (2, 1e4, 8.0, 4096),
+])
+def test_parts_scaling_follows_its_rule_at_both_ends(E, rot, base, factor, positions):
+    """A pair of at least fast_turns turns stays, one of at most slow_turns slows by the
+    factor, and every pair in between lies on one line from the last index that stays to
+    the first that slows in full, wherever these two lie.  Compared in float64 with
+    indices found by counting turns one by one."""
+    f, _ = E.rotary_frequencies(rot, base=base)
+    g, _ = E.rotary_frequencies(rot, base=base, scaling="parts", factor=factor,
+                                original_positions=positions)
+
+    def turns(i):
+        return base ** (-2.0 * i / rot) * positions / (2 * math.pi)
+
+    lo = next(i for i in range(4 * rot, -4 * rot, -1) if turns(i) >= 32.0)
+    hi = next(i for i in range(-4 * rot, 4 * rot) if turns(i) <= 1.0)
+    for i in range(rot // 2):
+        slow = min(max((i - lo) / (hi - lo), 0.0), 1.0)
+        want = f[i].item() * (1 - slow + slow / factor)
+        assert abs(g[i].item() - want) <= 1e-12 * f[i].item(), (i, turns(i))
+        assert turns(i) < 32.0 or g[i] == f[i]
+        assert turns(i) <= 1.0 or g[i] > f[i] / factor * (1 + 1e-9)
