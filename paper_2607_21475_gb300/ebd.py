@@ -222,13 +222,37 @@ def _check(name, code):
         raise EbdError(name, code, ebd_status_string(code))
 
 
+def _empty(shape, dtype, device, stream=None):
+    """A buffer for a call on `stream` (None: the current one), from that stream's
+    pool: the allocator hands out memory whose last use may still be queued on
+    the pool's own stream, and takes it back for later work there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _result(shape, dtype, device, stream=None):
+    """The same for a tensor that is returned: the current stream may read it too."""
+    t = _empty(shape, dtype, device, stream)
+    if stream is not None:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _on_device(t, device, stream=None):
+    """t on `device`; a copy is ordered, and lives, on `stream`."""
+    if stream is None:
+        return t.to(device)
+    with torch.cuda.stream(stream):
+        return t.to(device)
+
+
 def _workspace(nbytes, device, ws, stream=None):
     if nbytes == 0:
         return None, 0
     if ws is None:
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream is not None:  # the buffer goes back to the allocator before the work is done
-            ws.record_stream(stream)
+        ws = _empty(nbytes, torch.uint8, device, stream)
     if ws.numel() * ws.element_size() < nbytes:
         raise ValueError(f"workspace too small: {ws.numel() * ws.element_size()} < {nbytes}")
     return ws.data_ptr(), ws.numel() * ws.element_size()
@@ -501,7 +525,7 @@ def ebd_gather_queries(Q: torch.Tensor, positions: torch.Tensor, n_kv_heads: int
     G = Hq // n_kv_heads
     P = positions.shape[0]
     if q_obs is None:
-        q_obs = torch.empty((B, n_kv_heads, G * P, d), dtype=Q.dtype, device=Q.device)
+        q_obs = _result((B, n_kv_heads, G * P, d), Q.dtype, Q.device, stream)
     _check("ebd_gather_queries", lib().ebd_gather_queries(
         _dtype_code(Q), B, n_kv_heads, G, d, Nq, _ptr(Q, name="Q"),
         _ptr(positions, torch.int32, (P,), "positions"), P,
@@ -518,7 +542,7 @@ def ebd_variance_contributions(Q: torch.Tensor, K_c: torch.Tensor, V_c: torch.Te
     G = Hq // H
     f = torch.float32
     if contrib is None:
-        contrib = torch.empty((B, Hq, cap), dtype=f, device=K_c.device)
+        contrib = _result((B, Hq, cap), f, K_c.device, stream)
     _check("ebd_variance_contributions", lib().ebd_variance_contributions(
         _dtype_code(K_c), B, H, G, d, _ptr(Q, K_c.dtype, (B, Hq, d), "Q"), _ptr(K_c, name="K_c"),
         _ptr(V_c, K_c.dtype, (B, H, cap, d), "V_c"), _ptr(logw_c, f, (B, H, cap), "logw_c"),
@@ -534,7 +558,7 @@ def ebd_block_scores(contrib: torch.Tensor, idx_c: torch.Tensor, n_kept: torch.T
     Hq = contrib.shape[1]
     G = Hq // H
     if out is None:
-        out = torch.empty((B, H, n_blocks), dtype=torch.float32, device=idx_c.device)
+        out = _result((B, H, n_blocks), torch.float32, idx_c.device, stream)
     _check("ebd_block_scores", lib().ebd_block_scores(
         B, H, G, _ptr(contrib, torch.float32, (B, Hq, cap), "contrib"),
         _ptr(idx_c, torch.int32, (B, H, cap), "idx_c"), _ptr(n_kept, torch.int32, (B, H), "n_kept"),
@@ -670,8 +694,8 @@ def ebd_rotary_table(inv_freq: torch.Tensor, n_pos: int, mscale: float = 1.0, ta
         raise TypeError("inv_freq must be a one-dimensional float64 tensor")
     if table is None:
         dev = inv_freq.device if inv_freq.is_cuda else (device or "cuda")
-        table = torch.empty((n_pos, inv_freq.shape[0], 2), dtype=torch.float32, device=dev)
-    f = inv_freq.to(table.device)
+        table = _result((n_pos, inv_freq.shape[0], 2), torch.float32, dev, stream)
+    f = _on_device(inv_freq, table.device, stream)
     _check("ebd_rotary_table", lib().ebd_rotary_table(
         _ptr(f, name="inv_freq"), f.shape[0], int(n_pos), float(mscale),
         _ptr(table, torch.float32, (n_pos, f.shape[0], 2), "table"), _stream(stream)))
@@ -687,7 +711,7 @@ def ebd_rotary(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, ou
         raise ValueError("x must be [T, H, d]")
     T, H, d = x.shape
     if out is None:
-        out = torch.empty((T, H, d), dtype=x.dtype, device=x.device)
+        out = _result((T, H, d), x.dtype, x.device, stream)
     tab, n_pos, rot = _rotary_rows(table)
     xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
     yp, yt, yh = _rows(out, x.dtype, T, H, d, "out")
@@ -743,9 +767,9 @@ def ebd_paged_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, m
     T, hq, d = q.shape[0], q.shape[1], c.head_dim
     qp, qt, qh = _rows(q, dt, T, hq, d, "q")
     if y is None:
-        y = torch.empty((T, hq, d), dtype=dt, device=q.device)
+        y = _result((T, hq, d), dt, q.device, stream)
     if lse is None:
-        lse = torch.empty((T, hq), dtype=torch.float32, device=q.device)
+        lse = _result((T, hq), torch.float32, q.device, stream)
     L = lib()
     ref = ctypes.byref(c)
     ws, wsb = _workspace(L.ebd_paged_attention_workspace_bytes(ref, hq, int(max_new)), q.device,

@@ -364,6 +364,39 @@ def test_workspace_of_a_call_on_another_stream_is_not_reused(E):
     assert all(torch.equal(y, ref) for y in ys)
 
 
+def test_buffers_of_a_call_on_another_stream_are_its_own(E):
+    """Workspace, outputs and the frequencies' copy of a call on a side stream share no
+    memory with tensors freed on the current stream whose writes are still queued,
+    nor with tensors made there after a dropped output."""
+    s = R.make([40] * 4, [3000, 2500, 40, 999], 8, 2, 128, 32, torch.bfloat16, 73)
+    pc = cache(E, s)
+    y0, l0 = E.ebd_paged_attention(s["q"], pc, s["cu"], 40)
+    f, m = E.rotary_frequencies(128)
+    t0 = E.ebd_rotary_table(f, 3000, m)
+    pos = torch.arange(s["T"], device="cuda").int()
+    r0 = E.ebd_rotary(s["q"], pos, t0)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    sizes = [E.ebd_paged_attention_workspace_bytes(pc, 8, 40), t0.numel() * 4, y0.numel() * 2,
+             l0.numel() * 4, f.numel() * 8]
+    got = []
+    for _ in range(4):
+        freed = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes]
+        torch.cuda._sleep(20_000_000)  # about 10 ms: what follows here waits that long
+        for x in freed:
+            x.fill_(255)
+        del freed, x
+        tab = E.ebd_rotary_table(f, 3000, m, stream=side)
+        rot = E.ebd_rotary(s["q"], pos, tab, stream=side)
+        y, _ = E.ebd_paged_attention(s["q"], pc, s["cu"], 40, stream=side)  # lse dropped
+        got.append((y, rot, tab))
+        for n in sizes:
+            torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+    torch.cuda.synchronize()
+    for y, rot, tab in got:
+        assert torch.equal(y, y0) and torch.equal(rot, r0) and torch.equal(tab, t0)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_captured_graph_follows_the_lengths(E, dtype):
     """Append and attention captured once, replayed as the sequences grow."""

@@ -184,3 +184,57 @@ def test_parts_scaling_follows_its_rule_at_both_ends(E, rot, base, factor, posit
         assert abs(g[i].item() - want) <= 1e-12 * f[i].item(), (i, turns(i))
         assert turns(i) < 32.0 or g[i] == f[i]
         assert turns(i) <= 1.0 or g[i] > f[i] / factor * (1 + 1e-9)
+
+
+# ---------------------------------------------------------------- buffers of the binding
+def test_no_entry_point_allocates_outside_its_stream(E):
+    """A function that takes a stream makes its buffers and its tensors' copies through
+    the helpers that order them on that stream, never with the current stream's pool."""
+    import ast
+    with open(E.__file__) as fh:
+        tree = ast.parse(fh.read())
+    makers = {"empty", "zeros", "ones", "full", "empty_like", "zeros_like", "to", "contiguous",
+              "clone", "cuda", "float", "double"}
+    found = []
+    for fn in tree.body:
+        if not isinstance(fn, ast.FunctionDef) or fn.name.startswith("_"):
+            continue
+        if "stream" not in [a.arg for a in fn.args.args]:
+            continue
+        for node in ast.walk(fn):
+            if (isinstance(node, ast.Call) and isinstance(node.func, ast.Attribute)
+                    and node.func.attr in makers):
+                found.append((fn.name, node.func.attr))
+    assert found == []
+
+
+def test_workspace_is_taken_from_the_streams_pool(E, monkeypatch):
+    """Allocation happens while the call's stream is the current one; without a stream
+    the current one stays."""
+    entered, made = [], []
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            entered.append(self.stream)
+
+        def __exit__(self, *exc):
+            entered.pop()
+
+    def empty(*shape, **kw):
+        made.append(list(entered))
+        return real(*shape, **kw)
+
+    real = torch.empty
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch, "empty", empty)
+    _, n = E._workspace(256, "cpu", None, "side")
+    assert n == 256 and made == [["side"]]
+    E._workspace(256, "cpu", None, None)
+    assert made == [["side"], []]
+    ws = real(300, dtype=torch.uint8)
+    assert E._workspace(256, "cpu", ws, "side") == (ws.data_ptr(), 300) and len(made) == 2
+    with pytest.raises(ValueError, match="too small"):
+        E._workspace(301, "cpu", ws, "side")
