@@ -498,8 +498,9 @@ ebd_status ebd_rotary(ebd_dtype dtype, int32_t n_tokens, int32_t n_heads, int32_
 /*
  * Append of the new tokens' keys and values to the paged cache, keys turned to
  * their positions on the way; with n_q_heads > 0 the queries are turned by the
- * same launch.  Positions past the block table, or on a page outside the
- * pool, are dropped (EBD_DEV_RANGE).
+ * same launch.  Positions before 0, past the block table or on a page outside
+ * the pool are dropped (EBD_DEV_RANGE); so are, with their queries, tokens that
+ * cu_new gives to no sequence.
  *   k_new, v_new device (dtype) [n_tokens, Hkv, d] with token and head strides
  *   table        device [n_pos, rotary_dim / 2, 2] float32; NULL: keys go in
  *                as they are (rotary_dim, layout, n_pos unused, n_q_heads 0)

@@ -50,15 +50,22 @@ __device__ __forceinline__ long long slot_offset(const PagedView& v, int page, i
          (long long)(pos & ((1 << v.page_shift) - 1)) * v.row_stride;
 }
 
-// Sequence of packed token t: the number of sequences that end at or before
-// it (cu [batch + 1], non-decreasing).  Whole warp, one t.
-__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int t, int lane) {
+// Sequence of packed token t: the first whose tokens end after it (cu [batch + 1]).
+// odd: an offset steps back past t.  Whole warp, one t.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int batch, int t, int lane,
+                                           bool& odd) {
   int b = 0;
+  odd = false;
   for (int i = lane; i - lane < batch; i += 32) {
     const bool before = i < batch && cu[i + 1] <= t;
-    const int n = __popc(__ballot_sync(0xffffffffu, before));
-    b += n;
-    if (n < 32) break;
+    const uint32_t ended = __ballot_sync(0xffffffffu, before);
+    if (ended == 0xffffffffu) {
+      b += 32;
+      continue;
+    }
+    b += __ffs(~ended) - 1;
+    odd = (ended & (ended + 1)) != 0;
+    break;
   }
   return b;
 }

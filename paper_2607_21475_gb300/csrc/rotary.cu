@@ -168,12 +168,14 @@ __global__ void __launch_bounds__(kRotWarps * 32, APPEND ? kAppendBlocks : kRotB
 
   int pos, b = 0, page = -1;
   if (APPEND) {
-    b = sequence_of(a.cu, a.pv.batch, t, lane);
-    if (b >= a.pv.batch) {  // past the last sequence: no place for it
-      if (lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
-      return;
-    }
-    pos = a.pv.seq_len[b] - (a.cu[b + 1] - t);
+    bool odd;
+    b = sequence_of(a.cu, a.pv.batch, t, lane, odd);
+    // the offsets run from 0 to n_tokens; the first token's warp looks at both ends
+    if (t == 0) odd = odd || a.cu[0] != 0 || a.cu[a.pv.batch] != a.n_tokens;
+    const bool none = b >= a.pv.batch || t < a.cu[b];  // no sequence's token: no place for it
+    if (lane == 0 && (odd || none)) raise_status(a.dev_status, EBD_DEV_RANGE);
+    if (none) return;
+    pos = a.pv.seq_len[b] - (min(a.cu[b + 1], a.n_tokens) - t);
     page = page_of(a.pv, b, pos);
   } else {
     pos = a.positions[t];

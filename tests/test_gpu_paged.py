@@ -208,6 +208,35 @@ def test_append_drops_what_has_no_page(E):
     assert torch.equal(changed, want) and torch.equal((s["K"] != K0).any(-1).any(1), want)
 
 
+@pytest.mark.parametrize("cu", [[5, 8, 12], [0, 4, 9], [3, 3, 12], [0, 8, 6], [5, 8, 9], [-2, 6, 12]])
+def test_append_skips_tokens_of_no_sequence(E, cu):
+    """Packed tokens before the first offset, past the last one or under an offset
+    that steps back belong to no sequence: nothing is written for them, not even over
+    a sequence's earlier rows, and the status tells."""
+    s = R.make([6, 6], [40, 50], 4, 2, 64, 16, torch.bfloat16, 5)
+    K0, V0 = s["K"].clone(), s["V"].clone()
+    pc, tab = cache(E, s), table_of(E, 64, 64)
+    q_out = torch.full((12, 4, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    E.ebd_paged_append(pc, s["k"], s["v"], torch.tensor(cu, device="cuda").int(), table=tab,
+                       q=s["q"], q_out=q_out)
+    assert pc.dev_status.item() == E.EBD_DEV_RANGE
+    owned = [(b, t) for b in (0, 1) for t in range(max(cu[b], 0), cu[b + 1])]
+    changed = torch.zeros(K0.shape[:1] + K0.shape[2:3], dtype=torch.bool, device="cuda")
+    q_left = torch.ones(12, dtype=torch.bool)
+    for b, t in owned:
+        pos = int(s["seq_len"][b]) - (cu[b + 1] - t)
+        page, off = int(s["bt"][b, pos // 16]), pos % 16
+        changed[page, off] = True
+        q_left[t] = False
+        assert torch.equal(s["V"][page, :, off], s["v"][t])
+        cs = tab[pos][None]
+        check_rotated(s["K"][page, :, off][None], s["k"][t][None], cs, "half", False, torch.bfloat16)
+        check_rotated(q_out[t][None], s["q"][t][None], cs, "half", False, torch.bfloat16)
+    same = ~changed[:, None, :, None].expand_as(K0)
+    assert torch.equal(s["K"][same], K0[same]) and torch.equal(s["V"][same], V0[same])
+    assert (q_out[q_left] == 7).all()
+
+
 # ---------------------------------------------------------------- attention
 def check_attention(E, s, dtype, scale, window, q=None, stream=None):
     q = s["q"] if q is None else q
