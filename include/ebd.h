@@ -525,6 +525,8 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  * A token with no such position (a sequence shorter than its new tokens) gets
  * y = 0, lse = -inf.  Pages and rows past a sequence's length are not used,
  * whatever they hold.
+ * Tokens that cu_new gives to no sequence, or past max_new of their own, keep
+ * what y and lse held (EBD_DEV_RANGE).
  *   max_new    largest cu_new[b+1] - cu_new[b] (host bound; more: EBD_DEV_RANGE)
  *   q          device (dtype) [n_tokens, Hq, d] with (positive) token and head strides
  *   y          device (dtype) [n_tokens, Hq, d] out, dense

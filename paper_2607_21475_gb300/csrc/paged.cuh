@@ -89,7 +89,9 @@ __device__ __forceinline__ SeqSpan seq_span(const PagedView& v, const int32_t* c
   s.n = min(t1 - s.t0, max_new);
   const long long most = (long long)v.max_blocks << v.page_shift;
   s.len = (int)min((long long)max(l, 0), most);
-  s.bad = s.t0 != c0 || s.t0 + s.n != c1 || s.len != l;
+  // the offsets run from 0 to n_tokens: what lies before or after is no sequence's
+  s.bad = s.t0 != c0 || s.t0 + s.n != c1 || s.len != l || (b == 0 && c0 != 0) ||
+          (b == v.batch - 1 && c1 != n_tokens);
   return s;
 }
 

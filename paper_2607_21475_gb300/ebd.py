@@ -759,7 +759,8 @@ def ebd_paged_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, m
     """Causal attention of the packed new tokens q [T, Hq, d] over the paged
     cache that already holds their keys and values: y [T, Hq, d] in q's type and
     the log-sum-exp [T, Hq].  max_new: the most new tokens of any sequence;
-    scale defaults to d^-1/2; window 0 sees every earlier position."""
+    scale defaults to d^-1/2; window 0 sees every earlier position.  Tokens that cu_new
+    gives to no sequence (EBD_DEV_RANGE in dev_status) keep what y and lse held."""
     if q.dim() != 3:
         raise ValueError("q must be [T, Hq, d]")
     c = _paged(pc)

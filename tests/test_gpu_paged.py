@@ -532,6 +532,30 @@ def test_attention_more_new_tokens_than_the_bound(E, dtype, most):
     assert (y.double() - ry)[keep].abs().max().item() <= 2e-5 * 5.5 + 2 * unit(dtype) * 5.5
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cu", [[5, 8, 12], [0, 4, 9], [3, 3, 12], [0, 0, 11], [0, 12, 13]])
+def test_attention_reports_tokens_of_no_sequence(E, dtype, cu):
+    """Offsets that do not run from 0 to n_tokens: a status bit; the rows of tokens
+    of no sequence are left as they were, the others are right."""
+    s = R.make([6, 6], [40, 50], 4, 2, 64, 16, dtype, 97)
+    pc = cache(E, s)
+    y = torch.full((12, 4, 64), 7.0, dtype=dtype, device="cuda")
+    lse = torch.full((12, 4), 7.0, device="cuda")
+    off = torch.tensor(cu, device="cuda").int()
+    E.ebd_paged_attention(s["q"], pc, off, 12, y=y, lse=lse)
+    assert pc.dev_status.item() == E.EBD_DEV_RANGE
+    lo, hi = cu[0], min(cu[2], 12)
+    held = [min(c, 12) for c in cu]
+    ry, rl = R.attention(s["q"], s["K"], s["V"], s["bt"], s["seq_len"],
+                         torch.tensor(held, device="cuda").int(), 0.125, 0)
+    for t in range(12):
+        if lo <= t < hi:
+            assert (y[t].double() - ry[t]).abs().max().item() <= (2e-5 + 2 * unit(dtype)) * 5.5
+            assert (lse[t].double() - rl[t]).abs().max().item() <= 2e-5
+        else:
+            assert (y[t] == 7).all() and (lse[t] == 7).all()
+
+
 # ---------------------------------------------------------------- gather
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["head", "row"])
