@@ -523,8 +523,9 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  * kvh * G + g, over positions max(0, p - window + 1) <= j <= p (window 0: all),
  *   y = sum_j softmax_j(scale * q . k_j) v_j,   lse = log sum_j e^(scale q . k_j).
  * A token with no such position (a sequence shorter than its new tokens) gets
- * y = 0, lse = -inf.  Pages and rows past a sequence's length are not used,
- * whatever they hold.
+ * y = 0, lse = -inf.  Pages and rows past a sequence's length, and blocks that
+ * end before the first position that a new token sees, are not used, whatever
+ * they hold and whatever the block table says of them.
  * Tokens that cu_new gives to no sequence, or past max_new of their own, keep
  * what y and lse held (EBD_DEV_RANGE).
  *   max_new    largest cu_new[b+1] - cu_new[b] (host bound; more: EBD_DEV_RANGE)

@@ -79,13 +79,14 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     const HeadSlice hs = head_slice(a, w.h);
     const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);
     const int p0 = w.sp.len - w.sp.n + w.first(a);  // position of the item's first token
+    const int seen = first_seen(a, p0);  // pages before it may have been released
     // Row threadIdx.x of key tile j: its offset in the pools; -1 past the sequence's
     // end, where nothing is read
     auto find_row = [&](int j) {
       const int pos = j * BN + threadIdx.x;
       if (pos >= w.sp.len) return -1ll;
       const int page = page_of(a.pv, w.b, pos);
-      bad |= page < 0;
+      bad |= page < 0 && pos >= seen;
       return page < 0 ? -1ll : slot_offset(a.pv, page, hs.kvh, pos);
     };
     auto copy = [&](int j) {  // key tile j into stage j & 1

@@ -432,6 +432,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       // copies by its latency); past the pool where there is none.
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
       int block0 = 0, entry = 0, held = 0;  // pages of blocks block0 .. + held - 1
+      const int seen = first_seen(a, w.pos);  // pages before it may have been released
       auto page_at = [&](int j) {
         const int first = (j * kTcBN) >> a.pv.page_shift;
         const int last = (j * kTcBN + kTcBN - 1) >> a.pv.page_shift;
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           if (blk < a.pv.max_blocks && pos < w.len) {
             const int p = page_of(a.pv, w.b, pos);
             if (p >= 0) entry = p;
-            else bad = true;
+            else if (pos + page > seen) bad = true;
           }
         }
         return __shfl_sync(0xffffffffu, entry,

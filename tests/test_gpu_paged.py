@@ -556,6 +556,30 @@ def test_attention_reports_tokens_of_no_sequence(E, dtype, cu):
             assert (y[t] == 7).all() and (lse[t] == 7).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("page", [8, 16, 32])
+@pytest.mark.parametrize("new,window", [(1, 50), (1, 1), (40, 50), (300, 129), (7, 1000)])
+def test_pages_behind_the_window_may_be_released(E, dtype, page, new, window):
+    """Blocks that end before the first position that a new token sees may hold any
+    number: no status, the same bits.  The block of that position may not."""
+    total = [new + 211, new + 1500, new]
+    s = R.make([new] * 3, total, 4, 2, 64, page, dtype, 98, stale=math.nan)
+    y0, l0 = E.ebd_paged_attention(s["q"], cache(E, s), s["cu"], new, window=window)
+    first = [max(0, n - new - window + 1) for n in total]
+    for fill in (-1, 1 << 30):
+        bt = s["bt"].clone()
+        for b in range(3):
+            bt[b, :first[b] // page] = fill
+        pc = cache(E, dict(s, bt=bt))
+        y, lse = E.ebd_paged_attention(s["q"], pc, s["cu"], new, window=window)
+        assert pc.dev_status.item() == 0
+        assert torch.equal(y, y0) and torch.equal(lse, l0)
+        bt[1, first[1] // page] = fill
+        pc = cache(E, dict(s, bt=bt))
+        E.ebd_paged_attention(s["q"], pc, s["cu"], new, window=window)
+        assert pc.dev_status.item() == E.EBD_DEV_RANGE
+
+
 # ---------------------------------------------------------------- gather
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["head", "row"])
