@@ -526,6 +526,7 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  * y = 0, lse = -inf.  Pages and rows past a sequence's length, and blocks that
  * end before the first position that a new token sees, are not used, whatever
  * they hold and whatever the block table says of them.
+ * Positions on a page outside the pool take no part (EBD_DEV_RANGE).
  * Tokens that cu_new gives to no sequence, or past max_new of their own, keep
  * what y and lse held (EBD_DEV_RANGE).
  *   max_new    largest cu_new[b+1] - cu_new[b] (host bound; more: EBD_DEV_RANGE)

@@ -36,7 +36,8 @@ struct SimtLayout {
   static constexpr int kP = kV + 2 * kKeys * D;            // [rows][keys + 4]
   static constexpr int kOff = kP + kAttnRows * (kKeys + 4);  // [2][keys] row offsets, 64 bits
   static constexpr int kStart = kOff + 4 * kKeys;
-  static constexpr int kFloats = kStart + 12;
+  static constexpr int kAbsent = kStart + 12;  // [4] keys of a tile without a row, by tile number
+  static constexpr int kFloats = kAbsent + 4;
 };
 
 __device__ __forceinline__ void load4(const float* p, float (&x)[4]) {
@@ -62,6 +63,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   float* sm = reinterpret_cast<float*>(smem4);
   float *Qs = sm + L::kQ, *Ps = sm + L::kP;
   long long* offs = reinterpret_cast<long long*>(sm + L::kOff);
+  uint32_t* absent_s = reinterpret_cast<uint32_t*>(sm + L::kAbsent);
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   WorkStart* start_s = reinterpret_cast<WorkStart*>(sm + L::kStart);
   static_assert(sizeof(WorkStart) <= 12 * 4, "start");
@@ -101,10 +103,18 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       }
       cp_async_commit();
     };
+    // Enters the rows that the first warp found.  A tile's absent keys are read while
+    // it is worked on, when the warp may be two tiles ahead: four places.
+    auto put_row = [&](int j, long long row) {
+      static_assert(BN == 32, "a lane per key");
+      offs[(j & 1) * BN + threadIdx.x] = row;
+      const uint32_t absent = __ballot_sync(0xffffffffu, row < 0);
+      if (threadIdx.x == 0) absent_s[j & 3] = absent;
+    };
     __syncthreads();  // the last piece's readers are done
     if (threadIdx.x < BN) {
-      offs[(w.cur & 1) * BN + threadIdx.x] = find_row(w.cur);
-      if (w.cur + 1 < w.end) offs[(w.cur + 1 & 1) * BN + threadIdx.x] = find_row(w.cur + 1);
+      put_row(w.cur, find_row(w.cur));
+      if (w.cur + 1 < w.end) put_row(w.cur + 1, find_row(w.cur + 1));
     }
     __syncthreads();
     copy(w.cur);
@@ -158,7 +168,8 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
 #pragma unroll
               for (int z = 0; z < 4; ++z) s[i][e] = fmaf(q[i][z], k[e][z], s[i][e]);
         }
-        bool all = true;  // every row of the warp sees every key of the tile
+        const uint32_t absent = absent_s[j & 3];
+        bool all = absent == 0;  // every row of the warp sees every key of the tile
 #pragma unroll
         for (int i = 0; i < 4; ++i) all = all && lo[i] <= k0 && hi[i] >= k0 + BN;
         all = __all_sync(0xffffffffu, all);
@@ -168,7 +179,9 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
 #pragma unroll
           for (int e = 0; e < NK; ++e) {
             const int pos = k0 + tx + 16 * e;
-            s[i][e] = all || (pos >= lo[i] && pos < hi[i]) ? s[i][e] * a.scale2 : -INFINITY;
+            s[i][e] = all || (pos >= lo[i] && pos < hi[i] && !(absent >> (tx + 16 * e) & 1))
+                          ? s[i][e] * a.scale2
+                          : -INFINITY;
             top = fmaxf(top, s[i][e]);
           }
 #pragma unroll
@@ -209,7 +222,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
         }
       }
       // (stage j & 1's offsets were read before this tile's barrier)
-      if (j + 2 < w.end && threadIdx.x < BN) offs[(j & 1) * BN + threadIdx.x] = row;
+      if (j + 2 < w.end && threadIdx.x < BN) put_row(j + 2, row);
       __syncwarp();  // before the next tile's weights
     }
     const int slot = w.slot(blockIdx.x);

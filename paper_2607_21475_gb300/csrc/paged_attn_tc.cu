@@ -30,8 +30,9 @@
 //
 // Roles: warps 0-3 / 4-7 softmax and epilogue of A / B, warps 8 / 9 issue the
 // MMAs of A / B, warp 10 the TMA copies of K and V (one box per page and 64
-// channels; pages past the sequence's end are read past the pool's end, which
-// fills zeros), warp 11 walks the CTA's pieces, copies the query rows and clears
+// channels; pages past the sequence's end are read past the pool's end, and
+// keys of pages outside the pool, which the softmax hides, before its beginning:
+// both fill zeros), warp 11 walks the CTA's pieces, copies the query rows and clears
 // the value rows of a tile past the sequence's end (weight 0 times whatever a
 // page holds there must stay 0).
 //
@@ -78,9 +79,17 @@ struct Piece {
   int pos;          // its position
   int tokens;
   int slot;         // partial result, -1: the output itself
+  int absent;       // a key that it sees has no page; told with q_full, so that the softmax
+                    // asks once a piece (once a tile: mixed batch 41.5 -> 42.9 us,
+                    // 4096-token chunk 490 -> 503 us at the full clock)
 };
 constexpr int kPieceSlots = 4;
 constexpr int kPieceReaders = 11;  // warps that read a piece
+// Keys of a tile (bit i: key i) whose page is outside the pool, by the CTA's tile
+// number.  A tile's entry is written before its K copy is announced and read before
+// its P is, and tile t + stages is copied after S of t, which follows P of t - 2: more
+// than stages + 2 entries are never in use.
+constexpr int kAbsentSlots = 16;
 
 struct TcBars {
   uint64_t q_full, q_empty;
@@ -88,10 +97,14 @@ struct TcBars {
   uint64_t fixed, done[2];
   uint64_t k_full[8], k_empty[8], v_full[8], v_empty[8];
   uint64_t piece_full[kPieceSlots], piece_empty[kPieceSlots];
+  uint64_t absent[kAbsentSlots];
   Piece piece[kPieceSlots];
   uint32_t tmem;
 };
 static_assert(sizeof(TcBars) <= 1024, "barriers");
+static_assert(PagedTcLayout<64>::kStages + 2 <= kAbsentSlots &&
+                  PagedTcLayout<128>::kStages + 2 <= kAbsentSlots,
+              "absent keys");
 
 // max(a, b, c) in one instruction.
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -116,8 +129,9 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     tmem_alloc(&bar->tmem, 512);
     tmem_relinquish();
   } else if (warp == 9) {
+    if (lane < kAbsentSlots) bar->absent[lane] = 0;
     if (lane == 0) {
-      mbar_init(&bar->q_full, 1);
+      mbar_init(&bar->q_full, 2);
       mbar_init(&bar->q_empty, 2);
       for (int x = 0; x < 2; ++x) {
         mbar_init(&bar->done[x], 1);
@@ -178,15 +192,23 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t sS = tmem + 256 + x * 128 + lane_base;
     const uint32_t sO = tmem + x * 128 + lane_base;
-    uint32_t it = 0;  // tiles of X so far: S buffer it & 1
+    uint32_t it = 0;     // tiles of X so far: S buffer it & 1
+    uint32_t tile0 = 0;  // tiles of the CTA before this piece
     const int rt = row / a.group, g = row - rt * a.group;
-    for (uint32_t i = 0; read_piece(i, w); drop_piece(i++)) {
+    for (uint32_t i = 0; read_piece(i, w); tile0 += w.end - w.cur, drop_piece(i++)) {
       // the X's tokens [x0, x0 + tokens); rows past the last repeat its last token
       const int x0 = x * a.half_tokens, tokens = min(w.tokens - x0, a.half_tokens);
       if (tokens <= 0) continue;
       const int tok = x0 + min(rt, tokens - 1);
       const int pos = w.pos + tok;
       const int hi = pos + 1, lo = first_seen(a, pos);
+      // (whether keys are absent is known by the first product)
+      if (!mbar_wait_warp(&bar->s_full[x][it & 1], (it >> 1) & 1)) {
+        ok = false;
+        break;
+      }
+      const bool absent_keys = bar->piece[i % kPieceSlots].absent;
+      const int edge = absent_keys ? 0x7fffffff : lo;  // every tile is looked at then
       float m = -INFINITY, l = 0.f;
       for (int j = w.cur; j < w.end; ++j, ++it) {
         const int k0 = j * kTcBN;
@@ -199,11 +221,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         uint32_t s[64];
         tmem_ld64(buf, s);
         tmem_ld_wait();
-        if (__any_sync(0xffffffffu, hi - k0 < kTcBN || lo > k0)) {
+        if (__any_sync(0xffffffffu, hi - k0 < kTcBN || edge > k0)) {
           const int chi = hi - k0, clo = lo - k0;
 #pragma unroll
           for (int i = 0; i < 64; ++i)
             if (i >= chi || i < clo) s[i] = __float_as_uint(-INFINITY);
+          if (absent_keys) {
+            const uint64_t absent = bar->absent[(tile0 + (j - w.cur)) % kAbsentSlots];
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (absent >> i & 1) s[i] = __float_as_uint(-INFINITY);
+          }
         }
         float t4[4];
 #pragma unroll
@@ -425,11 +453,12 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     uint32_t nk = 0, nv = 0;  // tiles issued
     const int page = 1 << a.pv.page_shift;
     const int box = min(page, kTcBN), boxes = kTcBN / box;  // boxes of keys per tile
-    bool bad = false;
+    bool any_absent = false;
     for (uint32_t i = 0; ok && read_piece(i, w); drop_piece(i++)) {
       // lane i: one box of a tile (keys bx * box .., channels half * 64 ..).  The
       // lanes look up 32 pages at a time (a lookup per tile would hold up the
-      // copies by its latency); past the pool where there is none.
+      // copies by its latency); past the pool where there is none, before it (-1)
+      // where the table names a page outside.
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
       int block0 = 0, entry = 0, held = 0;  // pages of blocks block0 .. + held - 1
       const int seen = first_seen(a, w.pos);  // pages before it may have been released
@@ -443,17 +472,27 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           entry = a.pv.n_pages;
           if (blk < a.pv.max_blocks && pos < w.len) {
             const int p = page_of(a.pv, w.b, pos);
-            if (p >= 0) entry = p;
-            else if (pos + page > seen) bad = true;
+            if (p >= 0 || pos + page > seen) entry = p;
           }
+          any_absent = any_absent || __any_sync(0xffffffffu, entry < 0);  // (the entries begin as zeros)
         }
         return __shfl_sync(0xffffffffu, entry,
                            (((j * kTcBN + bx * box) >> a.pv.page_shift) - block0) & 31);
+      };
+      // Tells the softmax which keys of K tile nk are absent.
+      auto tell_absent = [&](int pg) {
+        uint64_t absent = 0;
+        uint32_t out = __ballot_sync(0xffffffffu, pg < 0 && half == 0 && bx < boxes);
+        for (; out; out &= out - 1)
+          absent |= (box == 64 ? ~0ull : (1ull << box) - 1)
+                    << ((__ffs(out) - 1) / L::kHalves * box);
+        if (lane == 0) bar->absent[nk % kAbsentSlots] = absent;
       };
       auto copy = [&](const CUtensorMap* tm, int base, uint64_t* full, uint64_t* empty,
                       uint32_t n, int j, int pg) {
         const uint32_t slot = n % KS;
         if (n >= KS && !mbar_wait_warp(&empty[slot], (n / KS - 1) & 1)) return false;
+        if (base == L::kK && any_absent) tell_absent(pg);
         if (lane == 0) mbar_arrive_expect_tx(&full[slot], L::kTile);
         __syncwarp();
         if (bx < boxes)
@@ -478,7 +517,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         pg = next_pg;
       }
     }
-    if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
+    if (any_absent && lane == 0) raise_status(a.dev_status, EBD_DEV_RANGE);
     // every copy has landed before the block may end
     for (uint32_t i = nk > KS ? nk - KS : 0; i < nk; ++i)
       mbar_wait_bounded(&bar->k_full[i % KS], (i / KS) & 1);
@@ -543,11 +582,29 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
                         w.token + x * a.half_tokens, &bar->q_full);
       }
       __syncwarp();
-      // two pieces ahead: the one two before this must have been dropped by then
-      if (!push(items + 3)) {
-        ok = false;
-        break;
+      // The second arrival on q_full says that the piece's pages were looked up: the
+      // first one's now, the others' a piece ahead.
+      if (items > 0 && lane == 0) mbar_arrive(&bar->q_full);
+      for (int turn = items > 0; ok && turn < 2; ++turn) {
+        // two pieces ahead: the one two before this must have been dropped by then
+        if (turn == 1 && !push(items + 3)) ok = false;
+        const uint32_t at = items + turn;
+        if (!ok || at + all >= pushed) break;
+        const Piece& p = bar->piece[at % kPieceSlots];
+        const int first = max(p.cur * kTcBN, first_seen(a, p.pos)) >> a.pv.page_shift;
+        const int past = min(p.end * kTcBN, p.len);
+        bool out = false;
+#pragma unroll 4
+        for (int blk = first + lane; blk << a.pv.page_shift < past; blk += 32)
+          out |= page_of(a.pv, p.b, blk << a.pv.page_shift) < 0;
+        out = __any_sync(0xffffffffu, out);
+        if (lane == 0) {
+          bar->piece[at % kPieceSlots].absent = out;
+          if (at == 0) mbar_arrive(&bar->q_full);
+        }
+        __syncwarp();
       }
+      if (!ok) break;
       if (w.len < w.end * kTcBN) {
         // The piece's last value tile.  Its stage's phase is certain only once the
         // piece's last S product is done (q_empty): the stage's earlier tile

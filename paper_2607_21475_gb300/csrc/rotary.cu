@@ -168,14 +168,18 @@ __global__ void __launch_bounds__(kRotWarps * 32, APPEND ? kAppendBlocks : kRotB
 
   int pos, b = 0, page = -1;
   if (APPEND) {
+    // the offsets run from 0 to n_tokens; the first token's warp looks at both ends
+    const int c_first = t == 0 ? a.cu[0] : 0, c_last = t == 0 ? a.cu[a.pv.batch] : a.n_tokens;
     bool odd;
     b = sequence_of(a.cu, a.pv.batch, t, lane, odd);
-    // the offsets run from 0 to n_tokens; the first token's warp looks at both ends
-    if (t == 0) odd = odd || a.cu[0] != 0 || a.cu[a.pv.batch] != a.n_tokens;
-    const bool none = b >= a.pv.batch || t < a.cu[b];  // no sequence's token: no place for it
-    if (lane == 0 && (odd || none)) raise_status(a.dev_status, EBD_DEV_RANGE);
+    bool none = b >= a.pv.batch;  // no sequence's token: no place for it
+    int c0 = 0, c1 = 0, len = 0;
+    if (!none) c0 = a.cu[b], c1 = a.cu[b + 1], len = a.pv.seq_len[b];
+    none |= t < c0;
+    odd |= none | (c_first != 0) | (c_last != a.n_tokens);
+    if (lane == 0 && odd) raise_status(a.dev_status, EBD_DEV_RANGE);
     if (none) return;
-    pos = a.pv.seq_len[b] - (min(a.cu[b + 1], a.n_tokens) - t);
+    pos = len - (min(c1, a.n_tokens) - t);
     page = page_of(a.pv, b, pos);
   } else {
     pos = a.positions[t];

@@ -68,6 +68,43 @@ def attention(q, K, V, block_table, seq_len, cu, scale, window):
     return y, lse
 
 
+def attention_detail(q, K, V, block_table, seq_len, cu, scale, window, absent=()):
+    """attention() and, for the size of its rounding errors, sum_j p_j |v_j| and
+    (sum_j p_j^2 v_j^2)^1/2 of every output, p the softmax weights.  absent: (sequence,
+    block) pairs whose positions no token sees.  Finite inputs."""
+    T, hq, d = q.shape
+    hkv = K.shape[1]
+    page, g = K.shape[2], hq // hkv
+    y, mean, root = (torch.zeros((T, hq, d), dtype=torch.float64, device=q.device)
+                     for _ in range(3))
+    lse = torch.full((T, hq), -math.inf, dtype=torch.float64, device=q.device)
+    for b, n in enumerate(seq_len.tolist()):
+        lo, hi = int(cu[b]), int(cu[b + 1])
+        if hi == lo or n == 0:
+            continue
+        at = torch.arange(n - (hi - lo), n, device=q.device)[:, None]
+        keys = torch.arange(n, device=q.device)
+        seen = keys <= at
+        if window:
+            seen &= keys > at - window
+        bt = block_table[b:b + 1].clone()
+        for i, block in absent:
+            if i == b:
+                seen[:, block * page:(block + 1) * page] = False
+                bt[0, block] = 0
+        for h in range(hkv):
+            k, v = rows(K, bt, 0, h, n), rows(V, bt, 0, h, n)
+            s = torch.einsum("tgd,nd->tgn", q[lo:hi, h * g:h * g + g].double(), k) * scale
+            s.masked_fill_(~seen[:, None], -math.inf)
+            z = torch.logsumexp(s, -1)
+            p = torch.where(seen[:, None], (s - z[..., None]).exp(), torch.zeros_like(s))
+            lse[lo:hi, h * g:h * g + g] = z
+            y[lo:hi, h * g:h * g + g] = p @ v
+            mean[lo:hi, h * g:h * g + g] = p @ v.abs()
+            root[lo:hi, h * g:h * g + g] = ((p * p) @ (v * v)).sqrt()
+    return y, lse, mean, root
+
+
 def make(new, total, hq, hkv, d, page, dtype, seed, order="head", spare=3, stale=0.0,
          max_blocks=None):
     """Inputs of one call.  new / total: new tokens and lengths per sequence.

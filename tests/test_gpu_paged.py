@@ -580,6 +580,32 @@ def test_pages_behind_the_window_may_be_released(E, dtype, page, new, window):
         assert pc.dev_status.item() == E.EBD_DEV_RANGE
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [8, 16, 64, 128])
+@pytest.mark.parametrize("new", [1, 30, 200])
+def test_attention_leaves_out_keys_on_bad_pages(E, dtype, d, page, new):
+    """The positions of a block outside the pool take no part in any row, over long
+    runs of tiles and in the last one; a row that sees nothing else is empty."""
+    total = [new + 700, new + 1400, new]
+    s = R.make([new] * 3, total, 4, 2, d, page, dtype, 99, stale=math.nan)
+    absent = [(0, 0), (0, 3), (0, (total[0] - 1) // page), (1, 600 // page), (1, 700 // page),
+              (2, 0)]
+    bt = s["bt"].clone()
+    for i, (b, block) in enumerate(absent):
+        bt[b, block] = -1 if i % 2 else s["K"].shape[0] + i
+    pc = cache(E, dict(s, bt=bt))
+    y, lse = E.ebd_paged_attention(s["q"], pc, s["cu"], new)
+    assert pc.dev_status.item() == E.EBD_DEV_RANGE
+    ry, rl, _, _ = R.attention_detail(s["q"], s["K"].nan_to_num(0.0), s["V"].nan_to_num(0.0),
+                                      s["bt"], s["seq_len"], s["cu"], d ** -0.5, 0, absent)
+    empty = rl == -math.inf
+    assert torch.equal(lse == -math.inf, empty) and (y[empty] == 0).all()
+    assert empty.any() and not empty.all()
+    assert (y.double() - ry).abs().max().item() <= (2e-5 + 2 * unit(dtype)) * 5.5
+    assert (lse.double() - rl)[~empty].abs().max().item() <= 2e-5
+
+
 # ---------------------------------------------------------------- gather
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["head", "row"])
