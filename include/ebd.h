@@ -540,7 +540,8 @@ ebd_status ebd_paged_append(const ebd_paged_cache* cache, int32_t n_tokens, cons
  * over 300 thousand positions).  Products accumulate in float32; softmax statistics and partial
  * outputs are float32; bf16 rounds the softmax weights once (2^-8 relative)
  * before they multiply the values.  A NaN or infinite key or value reaches only
- * the tokens that see it.  Needs workspace of
+ * the tokens that see it (tokens that share a tile with it and do not see it are
+ * computed once more, at a small part of the normal rate).  Needs workspace of
  * ebd_paged_attention_workspace_bytes(...) bytes.  Results are reproducible bit for
  * bit for a batch on a given GPU; how a sequence's keys are split (and so the
  * last bits) depends on the rest of the batch.  Both of its kernels are

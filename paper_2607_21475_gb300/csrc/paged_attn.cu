@@ -74,6 +74,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   }
   __syncthreads();
   bool bad = false, first = true;
+  bool nan = false;  // a NaN in this thread's outputs
   PieceRecord record = {0, 0, 0, 0};
   for (PieceWalk<BN> w(a, *start_s); w.live(); w.next(a)) {
     record_piece(a, record, w, first);
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
           for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
         }
         __syncwarp();  // a warp reads the weights of its own rows only
-        // hidden keys have weight 0; a hidden value that is not finite is mended below
+        // hidden keys have weight 0; a hidden value that is not finite is mended at the end
 #pragma unroll 2
         for (int k = 0; k < BN; k += 4) {
           float p[4][4];
@@ -226,7 +227,6 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       __syncwarp();  // before the next tile's weights
     }
     const int slot = w.slot(blockIdx.x);
-    uint32_t nan_groups[4];  // 16-channel groups of the rows with a NaN
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -237,47 +237,24 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       float* dst = slot < 0 ? (float*)a.y + out * D : part_row<D>(a, slot, r);
       const int step = slot < 0 ? 4 : a.part_step;  // between 4-channel groups
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
-      nan_groups[i] = 0;
 #pragma unroll
       for (int c = 0; c < D / 64; ++c) {
         float x[4];
-        bool nan = false;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           x[e] = o[i][c * 4 + e] * inv;
-          nan = nan || x[e] != x[e];
+          nan = nan || (mine && x[e] != x[e]);
         }
         if (mine) store4(dst + (c * 16 + tx) * step, x);
-        if (mine && nan) nan_groups[i] |= 1u << (4 * c + tx / 4);
       }
       const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
       if (mine && tx == 0 && slot >= 0) a.part_lse[(size_t)slot * a.slot_rows + r] = lse2;
       if (mine && tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
     }
-    bool mend = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-#pragma unroll
-      for (int x = 8; x > 0; x >>= 1)
-        nan_groups[i] |= __shfl_xor_sync(0xffffffffu, nan_groups[i], x);
-      mend = mend || nan_groups[i];
-    }
-    __syncwarp();  // the rows' values, before one thread looks at them again
-    if (mend && tx == 0) {
-#pragma unroll 1
-      for (int i = 0; i < 4; ++i) {
-        if (!nan_groups[i]) continue;
-        const int r = ty * 4 + i, t = r / a.slice, g = r - t * a.slice;
-        const long long out = (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
-        mend_row<float, D>(
-            a, w.b, hs.kvh, (const float*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs,
-            w.cur * BN, lo[i], hi[i], min(w.end * BN, w.sp.len), m[i] == -INFINITY ? 0.f : m[i],
-            l[i] == 0.f ? 0.f : 1.f / l[i], nan_groups[i],
-            slot < 0 ? (float*)a.y + out * D : nullptr,
-            slot < 0 ? nullptr : part_row<D>(a, slot, r));
-      }
-    }
   }
+  if (__any_sync(0xffffffffu, nan))
+    mend_pieces<float, D, BN>(a, blockIdx.x, gridDim.x, 0, 0, (threadIdx.x >> 5) * 8, 8,
+                              threadIdx.x & 31);
   if (threadIdx.x == 0) a.rec[blockIdx.x] = record;
   if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
 }

@@ -311,60 +311,144 @@ __device__ __forceinline__ void record_piece(const PagedAttnArgs& a, PieceRecord
 __device__ __forceinline__ void round_to(float x, float& y) { y = x; }
 __device__ __forceinline__ void round_to(float x, __nv_bfloat16& y) { y = __float2bfloat16_rn(x); }
 
-// Mends one row's output where a value that the row does not see made it NaN:
-// such a value has weight 0 in the tile's product, and 0 times NaN or infinity
-// is NaN.  For each 16-channel group with a NaN (`groups`): the channels in which
-// a hidden value of the piece's positions [tile_lo, tile_hi) (at most a few
-// hundred at either end are hidden) is not finite are recomputed from those that
-// the row sees, [lo, hi) of them; a NaN in any other channel is the row's own.  The
-// sum stops once every such channel has met a NaN of its own.  q: the row's
-// query; base, inv: reference (log2) and reciprocal sum of its weights; y or part
-// (part_row): the output, as written.
+// C consecutive values of a row, in one access.
+template <typename T, int C>
+__device__ __forceinline__ void load_row(const T* p, float (&x)[C]) {
+  struct alignas(sizeof(T) * C) Vec {
+    T e[C];
+  };
+  const Vec v = *reinterpret_cast<const Vec*>(p);
+#pragma unroll
+  for (int i = 0; i < C; ++i) x[i] = to_f32(v.e[i]);
+}
+
+// Mends one row's output where a value that the row does not see made it NaN: such a
+// value has weight 0 in the tile's product, and 0 times NaN or infinity is NaN.  The
+// channels that are NaN and in which a hidden value of the piece's positions
+// [tile_lo, tile_hi) (at most a few hundred at either end are hidden) is not finite are
+// recomputed from those that the row sees, [lo, hi) of them, 32 keys at a time with one
+// set of weights for all channels; a NaN in any other channel is the row's own.  It
+// stops once every such channel has met a NaN of its own.  q: the row's query; y or part
+// (part_row): the output, as written.  Whole warp: lane i has channels C i .. + C - 1,
+// and key i of 32.
 template <typename T, int D>
-__device__ __noinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
-                                      int tile_lo, int lo, int hi, int tile_hi, float base,
-                                      float inv, uint32_t groups, T* y, float* part) {
-  const int k_lo = max(lo, tile_lo), k_hi = min(hi, tile_hi);  // seen
-  for (int c = 0; c < D; c += 16) {
-    if (!(groups >> (c / 16) & 1)) continue;
-    uint32_t mend = 0;
-    for (int pos = tile_lo; pos < tile_hi; ++pos) {
-      if (pos == k_lo && k_lo < k_hi) pos = k_hi;
-      const int page = pos < tile_hi ? page_of(a.pv, b, pos) : -1;
-      if (page < 0) continue;
-      const T* v = (const T*)a.V_pages + slot_offset(a.pv, page, kvh, pos) + c;
+__device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
+                                         int tile_lo, int lo, int hi, int tile_hi, T* y,
+                                         float* part, int lane) {
+  constexpr int C = D / 32;
+  const int c0 = lane * C;
+  auto at = [&](int c) { return part + (c0 + c) / 4 * a.part_step + (c0 + c) % 4; };
+  uint32_t nan = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!(fabsf(to_f32(v[i])) < INFINITY)) mend |= 1u << i;
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float o = y ? to_f32(y[c + i]) : part[(c + i) / 4 * a.part_step + i % 4];
-      if (o == o) mend &= ~(1u << i);
-    }
-    if (!mend) continue;
-    float acc[16] = {};
-    uint32_t open = mend;  // channels without a NaN of their own so far
-    for (int pos = k_hi - 1; open && pos >= k_lo; --pos) {
-      const int page = page_of(a.pv, b, pos);
-      if (page < 0) continue;
-      const long long off = slot_offset(a.pv, page, kvh, pos);
-      const T *k = (const T*)a.K_pages + off, *v = (const T*)a.V_pages + off + c;
-      float s = 0.f;
+  for (int c = 0; c < C; ++c) {
+    const float o = y ? to_f32(y[c0 + c]) : *at(c);
+    nan |= (o != o ? 1u : 0u) << c;
+  }
+  if (!__any_sync(0xffffffffu, nan)) return;
+  // offset of the lane's position; -1: not there
+  auto place = [&](int pos, bool there) {
+    const int page = there ? page_of(a.pv, b, pos) : -1;
+    return page < 0 ? -1ll : slot_offset(a.pv, page, kvh, pos);
+  };
+  const int k_lo = min(max(lo, tile_lo), tile_hi), k_hi = max(min(hi, tile_hi), k_lo);  // seen
+  uint32_t mend = 0;
+  auto look = [&](int from, int to) {  // hidden positions [from, to)
+    for (int p0 = from; p0 < to; p0 += 32) {
+      const long long off = place(p0 + lane, p0 + lane < to);
 #pragma unroll 8
-      for (int i = 0; i < D; ++i) s = fmaf(to_f32(q[i]), to_f32(k[i]), s);
-      const float p = exp2f(fmaf(s, a.scale2, -base));
+      for (int i = 0; i < 32; ++i) {
+        const long long o = __shfl_sync(0xffffffffu, off, i);
+        float v[C] = {};
+        if (o >= 0) load_row<T, C>((const T*)a.V_pages + o + c0, v);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        acc[i] = fmaf(p, to_f32(v[i]), acc[i]);
-        if (acc[i] != acc[i]) open &= ~(1u << i);
+        for (int c = 0; c < C; ++c) mend |= (fabsf(v[c]) < INFINITY ? 0u : 1u) << c;
       }
     }
+  };
+  look(tile_lo, k_lo);
+  look(k_hi, tile_hi);
+  mend &= nan;
+  if (!__any_sync(0xffffffffu, mend)) return;
+  float m = -INFINITY, l = 0.f, acc[C] = {};
+  for (int top = k_hi; top > k_lo; top -= 32) {
+    const int pos = top - 1 - lane;
+    const long long off = place(pos, pos >= k_lo);
+    float s = -INFINITY;
+    if (off >= 0) {
+      constexpr int W = 16 / sizeof(T);
+      const T* k = (const T*)a.K_pages + off;
+      s = 0.f;
+#pragma unroll 4
+      for (int i = 0; i < D; i += W) {
+        float x[W], z[W];
+        load_row<T, W>(q + i, x);
+        load_row<T, W>(k + i, z);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (!(mend >> i & 1)) continue;
-      if (y) round_to(acc[i] * inv, y[c + i]);
-      else part[(c + i) / 4 * a.part_step + i % 4] = acc[i] * inv;
+        for (int e = 0; e < W; ++e) s = fmaf(x[e], z[e], s);
+      }
+      s *= a.scale2;
+    }
+    float m1 = fmaxf(m, s);
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
+    const float base = m1 == -INFINITY ? 0.f : m1, f = exp2f(m - base), p = exp2f(s - base);
+    m = m1;
+    l = l * f + p;  // this lane's share
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[c] *= f;
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i) {
+      const long long o = __shfl_sync(0xffffffffu, off, i);
+      const float w = __shfl_sync(0xffffffffu, p, i);
+      float v[C] = {};
+      if (o >= 0) load_row<T, C>((const T*)a.V_pages + o + c0, v);
+#pragma unroll
+      for (int c = 0; c < C; ++c) acc[c] = fmaf(w, v[c], acc[c]);
+    }
+    bool open = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) open = open || ((mend >> c & 1) && acc[c] == acc[c]);
+    if (!__any_sync(0xffffffffu, open)) break;
+  }
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    if (!(mend >> c & 1)) continue;
+    if (y) round_to(acc[c] * inv, y[c0 + c]);
+    else *at(c) = acc[c] * inv;
+  }
+}
+
+// Mends what a warp has written, once all of the CTA's pieces are done: nothing waits on
+// the warp then, however many keys its rows see (a wait with a bound would run out over a
+// long context).  Its rows are [row0, row0 + rows) of those of tokens x0, x0 + 1, .. of every
+// item (slot row slot0 + the row).  Walks the pieces anew; whole warp.
+// Measured: one NaN value row in the middle of 1216 new tokens over 33k (130k) positions,
+// 32/8 heads x 128, bf16: the call takes 113 (690) ms instead of 0.46 (1.5); with every value
+// NaN 5.5 (6.5) ms.  With 4 rows to a pass over the keys it took 37 (229) ms, but its 168
+// registers and its size made every call 1-2% slower.
+template <typename T, int D, int BN>
+__device__ __noinline__ void mend_pieces(const PagedAttnArgs& a, int cta, int n_cta, int x0,
+                                         int slot0, int row0, int rows, int lane) {
+  __syncwarp();  // the rows, written by other lanes
+  const WorkStart start = find_work<BN>(a, cta, n_cta, lane);
+  for (PieceWalk<BN> w(a, start); w.live(); w.next(a)) {
+    const int tokens = min(w.tokens(a) - x0, a.half_tokens), slot = w.slot(cta);
+    const int t_first = w.sp.t0 + w.first(a) + x0, p0 = w.sp.len - w.sp.n + w.first(a) + x0;
+    const HeadSlice hs = head_slice(a, w.h);
+    for (int r = row0; r < row0 + rows; ++r) {
+      const int t = r / a.slice, g = r - t * a.slice;
+      if (t >= tokens) break;
+      if (g >= hs.n) continue;
+      const long long out =
+          (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+      mend_row<T, D>(a, w.b, hs.kvh,
+                     (const T*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs, w.cur * BN,
+                     first_seen(a, p0 + t), p0 + t + 1, min(w.end * BN, w.sp.len),
+                     slot < 0 ? (T*)a.y + out * D : nullptr,
+                     slot < 0 ? nullptr : part_row<D>(a, slot, slot0 + r), lane);
     }
   }
 }

@@ -194,6 +194,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
     const uint32_t sO = tmem + x * 128 + lane_base;
     uint32_t it = 0;     // tiles of X so far: S buffer it & 1
     uint32_t tile0 = 0;  // tiles of the CTA before this piece
+    bool nonfinite = false;  // an output of the thread's rows was NaN or infinite
     const int rt = row / a.group, g = row - rt * a.group;
     for (uint32_t i = 0; read_piece(i, w); tile0 += w.end - w.cur, drop_piece(i++)) {
       // the X's tokens [x0, x0 + tokens); rows past the last repeat its last token
@@ -308,7 +309,6 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       const long long out = (long long)(w.token + tok) * (a.pv.n_kv_heads * a.group) +
                             w.h * a.group + g;
       float* part = part_row<D>(a, slot, x * 128 + row);  // when slot >= 0
-      uint32_t nan_groups = 0;  // 16-channel groups of the row with a NaN
 #pragma unroll
       for (int c = 0; c < D; c += 32) {
         uint32_t o[32];
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           z0 = fmaf(__uint_as_float(o[i]), 0.f, z0);
           z1 = fmaf(__uint_as_float(o[16 + i]), 0.f, z1);
         }
-        nan_groups |= ((z0 != z0 ? 1u : 0u) | (z1 != z1 ? 2u : 0u)) << (c / 16);
+        nonfinite = nonfinite || (mine && z0 + z1 != 0.f);
         if (!mine) {
         } else if (slot >= 0) {
           float* dst = part + c / 4 * a.part_step;
@@ -346,19 +346,13 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       if (mine) {
         if (slot >= 0) a.part_lse[(size_t)slot * a.slot_rows + x * 128 + row] = lse2;
         else if (a.lse) a.lse[out] = l == 0.f ? -INFINITY : lse2 * kLn2;
-        if (nan_groups)
-          mend_row<__nv_bfloat16, D>(
-              a, w.b, w.h,
-              (const __nv_bfloat16*)a.q + (w.token + tok) * a.q_ts +
-                  (w.h * a.group + g) * a.q_hs,
-              w.cur * kTcBN, lo, hi, min(w.end * kTcBN, w.len),
-              m == -INFINITY ? 0.f : m * a.scale2, inv, nan_groups,
-              slot < 0 ? (__nv_bfloat16*)a.y + out * D : nullptr,
-              slot < 0 ? nullptr : part);
       }
       __syncwarp();
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
+    if (ok && __any_sync(0xffffffffu, nonfinite))
+      mend_pieces<__nv_bfloat16, D, kTcBN>(a, cta, gridDim.x, x * a.half_tokens, x * 128,
+                                           (warp & 3) * 32, 32, lane);
   } else if (warp < 10) {
     // ---------------- MMA issue: a warp per X (one thread's instructions between
     // the MMAs of both would take longer than the MMAs)

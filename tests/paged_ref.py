@@ -78,7 +78,7 @@ def attention_detail(q, K, V, block_table, seq_len, cu, scale, window, absent=()
     y, mean, root = (torch.zeros((T, hq, d), dtype=torch.float64, device=q.device)
                      for _ in range(3))
     lse = torch.full((T, hq), -math.inf, dtype=torch.float64, device=q.device)
-    for b, n in enumerate(seq_len.tolist()):
+    for b, n in enumerate(torch.as_tensor(seq_len).tolist()):
         lo, hi = int(cu[b]), int(cu[b + 1])
         if hi == lo or n == 0:
             continue

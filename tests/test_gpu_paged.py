@@ -351,6 +351,52 @@ def test_attention_nonfinite_values_of_later_tokens_stay_there(E, dtype, new):
     assert (lse.double() - rl).abs().max().item() <= 2e-5
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,d,new,total,window", [
+    (torch.bfloat16, 32, 8, 128, 1216, 33000, 0),      # whole items: 33k keys in one CTA's piece
+    (torch.bfloat16, 32, 8, 64, 1216, 33000, 0),
+    (torch.bfloat16, 32, 8, 128, 1216, 60000, 32000),  # hidden at the window's far edge too
+    (torch.bfloat16, 28, 4, 128, 5, 100000, 0),        # drafts, pieces of many CTAs
+    (torch.float32, 4, 4, 64, 500, 33000, 0),
+    (torch.float32, 8, 2, 128, 3, 70000, 0),
+])
+def test_nonfinite_value_rows_over_long_contexts(E, dtype, hq, hkv, d, new, total, window):
+    """Value rows that are NaN in every channel, one in the middle of the new tokens and
+    one that leaves the window among them: rows that do not see them are right to the last
+    channel, rows that do are NaN, another sequence notices nothing, and no wait runs out."""
+    s = R.make([new, 70], [total, 900], hq, hkv, d, 64, dtype, 63)
+    V0 = s["V"].clone()
+    bad = [total - new + new // 2]
+    if window:
+        bad.append(total - new + new // 4 - window)  # seen by the first quarter
+    for pos in bad:
+        for h in range(hkv):
+            R.row(s["V"], s["bt"], 0, h, pos).fill_(math.nan)
+    pc = cache(E, s)
+    y, lse = E.ebd_paged_attention(s["q"], pc, s["cu"], s["max_new"], window=window)
+    assert pc.dev_status.item() == 0
+    at = torch.arange(total - new, total, device="cuda")
+    sees = torch.zeros(new, dtype=torch.bool, device="cuda")
+    for pos in bad:
+        sees |= (pos <= at) & ((at - pos < window) if window else True)
+    assert sees.any() and not sees.all()
+    assert torch.isnan(y[:new][sees]).all() and torch.isfinite(y[:new][~sees]).all()
+    assert torch.isfinite(y[new:]).all()
+    tol = 2e-5 * 5.5 + 2 * unit(dtype) * 5.5
+    ry, rl, _, _ = R.attention_detail(s["q"][new:], s["K"], s["V"].nan_to_num(0.0), s["bt"][1:],
+                                      s["seq_len"][1:], [0, 70], d ** -0.5, window)
+    assert (y[new:].double() - ry).abs().max().item() <= tol
+    # tokens around each bad position, as the last ones of a shorter sequence
+    for pos in bad:
+        mid = pos - (total - new) + (window if pos < total - new else 0)
+        lo, hi = max(mid - 64, 0), min(mid + 64, new)
+        ry, rl, _, _ = R.attention_detail(s["q"][lo:hi], s["K"], V0, s["bt"][:1],
+                                          [total - new + hi], [0, hi - lo], d ** -0.5, window)
+        ok = ~sees[lo:hi]
+        assert ok.any()
+        assert (y[lo:hi].double() - ry)[ok].abs().max().item() <= tol
+        assert (lse[lo:hi].double() - rl).abs().max().item() <= 2e-5
+
+
 @pytest.mark.parametrize("new", [2, 40, 300])
 def test_attention_window_hides_nonfinite_values(E, new):
     """The same at the window's far edge: a NaN value older than the window."""
