@@ -105,6 +105,21 @@ def attention_detail(q, K, V, block_table, seq_len, cu, scale, window, absent=()
     return y, lse, mean, root
 
 
+def attention_bound(y, mean, root, dtype):
+    """Bound of each output's error from attention_detail()'s results.
+
+    bfloat16 weights are off by 2^-8 relative at most (8 significant bits, half a unit),
+    so the sum is off by 2^-8 sum p |v| at most; with roundings of independent signs it
+    exceeds 7 2^-8 (sum p^2 v^2)^1/2 with probability 2 e^(-49 / 2) = 5e-11 (Hoeffding).  The
+    result is rounded once, 2^-8 |y|.  Float32: a logit is off by 2e-5 at most (the bound
+    of the log-sum-exp), which changes a weight and the sum of weights by 2e-5 each,
+    4e-5 sum p |v|; exponentials, sums and joins are far below, 1e-4 sum p |v| is asked."""
+    bound = 1e-4 * mean
+    if dtype == torch.bfloat16:
+        bound = bound + 2.0 ** -8 * (torch.minimum(mean, 7 * root) + y.abs() + bound)
+    return bound
+
+
 def make(new, total, hq, hkv, d, page, dtype, seed, order="head", spare=3, stale=0.0,
          max_blocks=None):
     """Inputs of one call.  new / total: new tokens and lengths per sequence.

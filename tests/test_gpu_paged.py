@@ -300,6 +300,38 @@ def test_items_split_over_many_ctas(E, dtype, d, group, new, total):
     assert torch.equal(y0, y1) and torch.equal(l0, l1)
 
 
+CLOSE = ATTN + [  # as ATTN; long contexts, where a lost tile changes little
+    ([1], [5003], 1, 1, 32, 0),
+    ([1], [5003], 28, 4, 16, 0),
+    ([2], [4100], 16, 1, 32, 0),
+    ([1, 150], [2900, 1300], 128, 1, 32, 0),
+    ([1, 1, 1], [30000, 20011, 7777], 8, 2, 64, 0),
+    ([5, 5], [16379, 6139], 32, 8, 64, 0),
+    ([300], [9000], 8, 2, 128, 0),
+    ([300, 7], [9000, 12345], 14, 2, 16, 4000),
+    ([1] * 300, [i * 53 % 400 + 1 for i in range(300)], 4, 2, 16, 0),
+    ([i % 3 for i in range(1025)], [i * 17 % 90 + 2 for i in range(1025)], 4, 1, 8, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("case", range(len(CLOSE)))
+def test_attention_to_the_size_of_its_roundings(E, dtype, d, case):
+    """Every output within the roundings of its own weights and value, however small it
+    is against the largest value."""
+    new, total, hq, hkv, page, window = CLOSE[case]
+    s = R.make(new, total, hq, hkv, d, page, dtype, 400 + case, stale=math.nan)
+    pc = cache(E, s)
+    y, lse = E.ebd_paged_attention(s["q"], pc, s["cu"], s["max_new"], window=window)
+    K, V = s["K"].nan_to_num(0.0), s["V"].nan_to_num(0.0)
+    ry, rl, mean, root = R.attention_detail(s["q"], K, V, s["bt"].clamp(min=0), s["seq_len"],
+                                            s["cu"], d ** -0.5, window)
+    assert ((y.double() - ry).abs() <= R.attention_bound(ry, mean, root, dtype)).all()
+    assert ((lse.double() - rl).abs() <= 2e-5).all()
+    assert pc.dev_status.item() == 0
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["row", "side"])
 @pytest.mark.parametrize("new", [1, 70])

@@ -238,3 +238,29 @@ def test_workspace_is_taken_from_the_streams_pool(E, monkeypatch):
     assert E._workspace(256, "cpu", ws, "side") == (ws.data_ptr(), 300) and len(made) == 2
     with pytest.raises(ValueError, match="too small"):
         E._workspace(301, "cpu", ws, "side")
+
+
+# ---------------------------------------------------------------- the tests' own bound
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d,hq,n", [(64, 1, 5003), (128, 1, 5003), (128, 8, 30000)])
+def test_attention_bound_sees_one_wrong_value_tile(dtype, d, hq, n):
+    """A 64-key value tile that is zeros, or another tile's, goes past the bound of the
+    attention tests at any place of a long context; exact results with rounded weights
+    and outputs do not."""
+    import paged_ref as R
+    g = torch.Generator().manual_seed(7)
+    page = 64
+    blocks = -(-n // page)
+    K, V = (torch.randn((blocks, 1, page, d), generator=g).to(dtype) for _ in range(2))
+    q = torch.randn((1, hq, d), generator=g).to(dtype)
+    bt, cu = torch.arange(blocks).int()[None], [0, 1]
+    y, lse, mean, root = R.attention_detail(q, K, V, bt, [n], cu, d ** -0.5, 0)
+    bound = R.attention_bound(y, mean, root, dtype)
+    k, v = R.rows(K, bt, 0, 0, n), R.rows(V, bt, 0, 0, n)
+    p = ((q[0].double() @ k.T) * d ** -0.5 - lse[0][:, None]).exp()
+    for block in range(blocks - 1):
+        at = slice(block * page, (block + 1) * page)
+        for wrong in (torch.zeros_like(v[at]), V[(block + 5) % (blocks - 1), 0].double()):
+            assert ((p[:, at] @ (wrong - v[at])).abs() > bound[0]).any(), block
+    w = p.to(dtype).double()
+    assert (((w @ v).to(dtype).double() - y[0]).abs() <= bound[0]).all()
