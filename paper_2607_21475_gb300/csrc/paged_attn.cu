@@ -155,19 +155,29 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
       if (j + 2 < w.end && threadIdx.x < BN) row = find_row(j + 2);
       if (live) {
         float s[4][NK] = {};
-#pragma unroll 4
-        for (int c = 0; c < D; c += 4) {
-          float q[4][4], k[NK][4];
+        // sums of 16 channels, then of those: one running sum of 128 has 2.3 times the
+        // rounding error
+#pragma unroll 1
+        for (int c0 = 0; c0 < D; c0 += 16) {
+          float part[4][NK] = {};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
+          for (int c = c0; c < c0 + 16; c += 4) {
+            float q[4][4], k[NK][4];
 #pragma unroll
-          for (int e = 0; e < NK; ++e) load4(Ks + (tx + 16 * e) * (D + 4) + c, k[e]);
+            for (int i = 0; i < 4; ++i) load4(Qs + (ty * 4 + i) * (D + 4) + c, q[i]);
+#pragma unroll
+            for (int e = 0; e < NK; ++e) load4(Ks + (tx + 16 * e) * (D + 4) + c, k[e]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int e = 0; e < NK; ++e)
+#pragma unroll
+                for (int z = 0; z < 4; ++z) part[i][e] = fmaf(q[i][z], k[e][z], part[i][e]);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int e = 0; e < NK; ++e)
-#pragma unroll
-              for (int z = 0; z < 4; ++z) s[i][e] = fmaf(q[i][z], k[e][z], s[i][e]);
+            for (int e = 0; e < NK; ++e) s[i][e] += part[i][e];
         }
         const uint32_t absent = absent_s[j & 3];
         bool all = absent == 0;  // every row of the warp sees every key of the tile
@@ -181,19 +191,21 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
           for (int e = 0; e < NK; ++e) {
             const int pos = k0 + tx + 16 * e;
             s[i][e] = all || (pos >= lo[i] && pos < hi[i] && !(absent >> (tx + 16 * e) & 1))
-                          ? s[i][e] * a.scale2
+                          ? s[i][e]
                           : -INFINITY;
             top = fmaxf(top, s[i][e]);
           }
 #pragma unroll
           for (int x = 8; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-          const float base = top == -INFINITY ? 0.f : top;  // nothing seen yet: every weight is 0
-          const float f = exp2f(m[i] - base);
+          // nothing seen yet: every weight is 0
+          const float base = top == -INFINITY ? 0.f : __fmul_rn(top, a.scale2);
+          const float f = exp2f(__fmul_rn(m[i], a.scale2) - base);
           m[i] = top;
           float sum = 0.f;
 #pragma unroll
           for (int e = 0; e < NK; ++e) {
-            const float p = exp2f(s[i][e] - base);
+            // fused: a logit of 16 rounded first would leave 7e-7 in the largest weights
+            const float p = exp2f(fmaf(s[i][e], a.scale2, -base));
             sum += p;
             Ps[(ty * 4 + i) * (BN + 4) + tx + 16 * e] = p;
           }
@@ -247,7 +259,8 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
         }
         if (mine) store4(dst + (c * 16 + tx) * step, x);
       }
-      const float lse2 = l[i] == 0.f ? -INFINITY : m[i] + log2f(l[i]);
+      const float lse2 =
+          l[i] == 0.f ? -INFINITY : __fmul_rn(m[i], a.scale2) + log2f(l[i]);
       if (mine && tx == 0 && slot >= 0) a.part_lse[(size_t)slot * a.slot_rows + r] = lse2;
       if (mine && tx == 0 && slot < 0 && a.lse) a.lse[out] = lse2 * kLn2;
     }

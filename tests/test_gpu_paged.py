@@ -332,6 +332,26 @@ def test_attention_to_the_size_of_its_roundings(E, dtype, d, case):
     assert pc.dev_status.item() == 0
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (32, 8)])
+@pytest.mark.parametrize("new,total", [(1, 92), (1, 601), (1, 2801), (2, 9002), (1, 30001),
+                                       (40, 1240)])
+def test_float32_attention_keeps_its_digits(E, hq, hkv, new, total):
+    """Relative error of the whole output, logits of standard deviation 2 over 128
+    channels.  A logit summed as 8 sums of 16 products (of size 2 each) is off by
+    2^-24 / 3^1/2 x 2 x (8 x 16^2 / 2 + 16 x 36)^1/2 x 128^-1/2 = 2.4e-7 (one sum of 128: 5.5e-7),
+    and more where the logit is large and its weight counts; the exponential, its
+    argument and the sums over keys add about 4e-7.  1e-6 is asked, of every seed."""
+    for seed in range(4):
+        s = R.make([new], [total], hq, hkv, 128, 64, torch.float32, 500 + seed, stale=math.nan)
+        q = (s["q"] * 2).contiguous()
+        y, lse = E.ebd_paged_attention(q, cache(E, s), s["cu"], new)
+        ry, rl, _, _ = R.attention_detail(q, s["K"].nan_to_num(0.0), s["V"].nan_to_num(0.0),
+                                          s["bt"].clamp(min=0), s["seq_len"], s["cu"],
+                                          128 ** -0.5, 0)
+        assert ((y.double() - ry).norm() / ry.norm()).item() <= 1e-6
+        assert ((lse.double() - rl).norm() / rl.norm()).item() <= 3e-7
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("order", ["row", "side"])
 @pytest.mark.parametrize("new", [1, 70])
