@@ -5,8 +5,9 @@
 // K and V together), so HBM bounds it, if enough rows are in flight: the chain
 // index -> page number -> row is three dependent loads, which a warp goes
 // through for 8 rows at once (4 rows: 26.0 us, 16 rows: 22.6 us).  Measured: a
-// quarter of 8 caches of 12-16k tokens (4 heads x 128, bf16) 22.7 us, 5.0 TB/s (74%
-// of the measured copy peak); one small cache 3.2 us.
+// quarter of 8 caches of 12-16k tokens (4 heads x 128, bf16) 22.6 us, 5.0 TB/s (74%
+// of the measured copy peak) as a kernel, 24.1 us, 4.7 TB/s in a row of calls; one
+// small cache 3.1 us.
 #include <cuda_runtime.h>
 
 #include "common.cuh"

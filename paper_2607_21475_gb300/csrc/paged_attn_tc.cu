@@ -14,12 +14,13 @@
 // holds it to 2/3 of the MMA rate (1280 cycles of MMA work per 64 keys).
 //
 // What bounds it: a chunk of 4096 tokens over 16k positions (28/4 heads, d = 128)
-// runs at 1.69 PFLOP/s (88% of the measured bf16 peak) in isolation and 1.59 (530 us)
-// under the power cap of a long run; a decode batch of 32 sequences streams its
-// cache at 7.0 TB/s (at the copy peak); head_dim 64 and short windows are bound by
-// the softmax warps (mixed batch with a window of 1024: 42 us, 1370 cycles per tile of
-// two X, 1070 of one); one sequence of 6k tokens by latencies (12.4 us, of which
-// about 8000 cycles pass before the first product).
+// runs at 1.71 PFLOP/s (493 us, 89% of the measured bf16 peak) at the full clock and
+// at 1.55-1.6 (525-541 us) under the power cap of a long run; a decode batch of 32
+// sequences streams its cache at 6.9-7.0 TB/s (at the copy peak); head_dim 64 and short
+// windows are bound by the softmax warps (mixed batch with a window of 1024: 42 us,
+// 1370 cycles per tile of two X, 1070 of one; decode of 32 x 16k at 64 channels: 209 us,
+// 5.1 TB/s); one sequence of 6k tokens by latencies (12.7 us, of which about 8000 cycles
+// pass before the first product).
 //
 // The softmax keeps one row per thread.  Its reference m moves only when a
 // tile's maximum exceeds it by more than 2^8 (in the weight), so that O_X is
@@ -706,7 +707,11 @@ ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,
   a.half_tokens = 128 / a.group;
   a.tokens = 2 * a.half_tokens;
   // measured: 1070 cycles per tile of one X, 1370 of two (64 channels); equal weights
-  // left CTAs between 52k and 82k cycles of work in the mixed batch, these 64k to 77k
+  // left CTAs between 52k and 82k cycles of work in the mixed batch, these 64k to 77k.
+  // 16 mixed sequences of up to 5k tokens, half of them single steps, 2 : 3 against equal
+  // weights (and 2 : 4), us: 64 channels with a window of 1024 41.4 / 43.5 (46.2), without
+  // 67 / 70 (81); 128 channels with the window 54.2 / 55.0 (62.4), without 89 / 86 (108), and
+  // over 3-16k positions 413-423 / 350-390 (510): there equal weights are better
   a.tile_work = 2;
   a.full_work = 3;
   a.min_share = 8;  // more than a tile: a CTA in the middle of an item has one at least

@@ -307,7 +307,8 @@ static ebd_status launch_rotary_v(RotaryArgs a, int head_dim, cudaStream_t s) {
 }
 
 // 16-byte accesses where every row and the rotated part allow them; otherwise
-// single elements (half) or single pairs (pairs).
+// single elements (half) or single pairs (pairs).  16384 tokens x 28 heads x 80 channels in
+// bf16, half layout: 32 rotated 27 us (5.4 TB/s), 20 rotated, by elements, 46 us (3.2 TB/s).
 template <typename T, bool APPEND>
 static ebd_status launch_rotary_t(const RotaryArgs& a, int head_dim, bool pairs, bool cache_ok,
                                   cudaStream_t s) {

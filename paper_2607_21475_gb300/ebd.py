@@ -659,8 +659,9 @@ def rotary_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "n
       the fastest stays;
     - "parts": a pair that makes at least `fast_turns` turns over
       `original_positions` stays, one that makes at most `slow_turns` slows by
-      `factor`, in between the two are mixed linearly in the pair's index; the
-      table grows by mscale = 0.1 ln(factor) + 1."""
+      `factor`, in between the two are mixed linearly in the pair's index, from the
+      last index that stays to the first that slows in full (either may lie
+      outside 0 .. R / 2 - 1); the table grows by mscale = 0.1 ln(factor) + 1."""
     if rotary_dim < 2 or rotary_dim % 2:
         raise ValueError("rotary_dim must be even and at least 2")
     if not base > 1 or not factor >= 1:
