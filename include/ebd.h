@@ -568,6 +568,170 @@ ebd_status ebd_paged_gather(const ebd_paged_cache* cache, const int32_t* idx_c,
                             const int32_t* n_kept, int32_t capacity, void* K_c, void* V_c,
                             int32_t* dev_status, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * A speculative decoding step over the paged cache: pages dealt to the sequences,
+ * queries and keys normalised per head on their way, a drafted tree of tokens
+ * attended, the accepted path kept.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Pages, offsets, positions and slots of a step from the sequences' lengths, on the device.
+ * Sequence b has seq_len[b] cached tokens and holds the pages of blocks
+ * [held[b][0], held[b][1]) of its row of block_table.  n_new[b] tokens are to join them
+ * (0: none; negative: the sequence leaves, its row is free afterwards).  In this order:
+ *   - given back: all pages of a sequence that leaves; with a window > 0 the blocks that
+ *     end at or before position seq_len[b] - window (no new token sees them).  They are
+ *     added to the end of free_pages[0 .. n_free), by sequence and block;
+ *   - a sequence needs pages for the blocks from held[b][1] up to the one of its last new
+ *     token.  In order of sequence it is served if its row of the table has room, the
+ *     wanted pages up to and including its own are there (it needs none, or) and so is
+ *     room for the new tokens up to and including its own in n_tokens packed ones: a
+ *     sequence that does not fit holds back those after it that need pages or tokens
+ *     past what is left, and nothing of it changes (EBD_DEV_CAPACITY, served[b] = 0).
+ *     A request too long for its row is left out of that count;
+ *   - pages are taken from the end of the list, by sequence and block, and entered into
+ *     the table; entries of blocks not held keep what they hold;
+ *   - seq_len_out[b] = seq_len[b] + n_new[b] where served, held_out and n_free_out alike,
+ *     cu_new the packed offsets of the served sequences' new tokens; positions[t] and
+ *     slots[t] = page * page_size + row of packed token t; 0 and -1 past the last one.
+ * The outputs seq_len_out, held_out, n_free_out may be the inputs.  Entries outside their
+ * ranges are clamped (EBD_DEV_RANGE); a page belongs to one sequence.
+ *   n_new, seq_len   device [B]       held        device [B][2]     n_free  device [1]
+ *   free_pages       device [n_pages] block_table device [B, max_blocks]
+ *   cu_new           device [B+1] out served      device [B] out, nullable
+ *   positions        device [n_tokens] int32 out, nullable
+ *   slots            device [n_tokens] int64 out, nullable
+ *   dev_status       device int32, required
+ */
+ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max_blocks,
+                          int32_t n_tokens, int32_t window, const int32_t* n_new,
+                          const int32_t* seq_len, const int32_t* held, const int32_t* n_free,
+                          int32_t* free_pages, int32_t* block_table, int32_t* seq_len_out,
+                          int32_t* held_out, int32_t* n_free_out, int32_t* cu_new, int32_t* served,
+                          int32_t* positions, int64_t* slots, int32_t* dev_status, void* stream);
+
+/*
+ * Norm per head and rotation in one pass: with r = (mean_c x_c^2 + eps)^(-1/2) of a row,
+ *   y[t, h] = R(w[h] * x[t, h] * r),
+ * R the rotation of ebd_rotary to positions[t] (table NULL: none; positions, n_pos,
+ * rotary_dim, layout unused).  Float32 arithmetic, one rounding.
+ *   x, y         device (dtype), strided as for ebd_rotary; y may be x (same strides)
+ *   weight       device: element (h, c) at h * weight_head_stride + c; stride 0: one
+ *                weight for all heads.  weight_dtype is EBD_F32 or dtype
+ *   eps          positive
+ *   positions    device [n_tokens]; outside [0, n_pos): as for ebd_rotary
+ * d <= 512 (EBD_ERR_UNSUPPORTED otherwise).  Alignment as for ebd_rotary.
+ */
+ebd_status ebd_norm_rotary(ebd_dtype dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
+                           const void* x, int64_t x_token_stride, int64_t x_head_stride,
+                           const void* weight, ebd_dtype weight_dtype, int64_t weight_head_stride,
+                           float eps, const int32_t* positions, const float* table, int32_t n_pos,
+                           int32_t rotary_dim, ebd_rotary_layout layout, void* y,
+                           int64_t y_token_stride, int64_t y_head_stride, int32_t* dev_status,
+                           void* stream);
+
+/*
+ * Its gradient: with u = R^T dy[t, h] and z = x r,
+ *   dx[t, h] = r (u w - z mean_c(u w z)),   dweight = sum of u z over the rows of a weight.
+ *   dy, x, dx    device (dtype), strided; dx may be dy or x (same strides)
+ *   dweight      device float32 [d] (weight_head_stride 0) or [n_heads, d] out; zeros
+ *                without tokens
+ * The sums run in a fixed order (reproducible bit for bit on a given GPU).  Needs workspace
+ * of ebd_norm_rotary_backward_workspace_bytes(...) bytes.
+ */
+size_t ebd_norm_rotary_backward_workspace_bytes(int32_t n_heads, int32_t head_dim,
+                                                int32_t per_head);
+ebd_status ebd_norm_rotary_backward(
+    ebd_dtype dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim, const void* dy,
+    int64_t dy_token_stride, int64_t dy_head_stride, const void* x, int64_t x_token_stride,
+    int64_t x_head_stride, const void* weight, ebd_dtype weight_dtype, int64_t weight_head_stride,
+    float eps, const int32_t* positions, const float* table, int32_t n_pos, int32_t rotary_dim,
+    ebd_rotary_layout layout, void* dx, int64_t dx_token_stride, int64_t dx_head_stride,
+    float* dweight, int32_t* dev_status, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * ebd_paged_append with the norm of keys and queries on the way, and tokens placed by their
+ * offsets or by their slots (one of cu_new and slots):
+ *   cu_new     as for ebd_paged_append; positions (nullable) then say where a token is
+ *              turned to when that is not its place in the sequence (a drafted tree)
+ *   slots      device [n_tokens] int64, page * page_size + row (ebd_paged_deal); -1: no
+ *              token here, nothing of it is written; another one outside the pool:
+ *              dropped as by ebd_paged_append (EBD_DEV_RANGE).  Needs positions with a
+ *              table; block_table and seq_len are not read
+ *   k_weight, q_weight  as for ebd_norm_rotary; NULL: not normalised
+ * With neither table nor q_weight n_q_heads is 0.  The rest as for ebd_paged_append.
+ */
+ebd_status ebd_paged_append_norm(
+    const ebd_paged_cache* cache, int32_t n_tokens, const int32_t* cu_new, const int64_t* slots,
+    const int32_t* positions, const void* k_new, int64_t k_token_stride, int64_t k_head_stride,
+    const void* v_new, int64_t v_token_stride, int64_t v_head_stride, const void* k_weight,
+    int64_t k_weight_head_stride, const void* q_weight, int64_t q_weight_head_stride,
+    ebd_dtype weight_dtype, float eps, const float* table, int32_t n_pos, int32_t rotary_dim,
+    ebd_rotary_layout layout, int32_t n_q_heads, const void* q, int64_t q_token_stride,
+    int64_t q_head_stride, void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+    int32_t* dev_status, void* stream);
+
+/*
+ * Masks and positions of drafted trees.  A sequence's new tokens are a tree (or several) that
+ * grows from its last cached token; token i of them names its parent's number in
+ * parents, a smaller one, or -1 for a child of the last cached token (anything else:
+ * EBD_DEV_RANGE, taken for -1).  Bit j % 32 of mask[t][j / 32] is set when the token
+ * sees new token j of its sequence: itself and its ancestors, with a window > 0 those
+ * fewer than `window` generations away; positions[t] = seq_len[b] - (new tokens of b) +
+ * depth, depth 0 for a child of the last cached token.
+ *   parents    device [n_tokens]
+ *   seq_len    device [B], new tokens included
+ *   max_new    as for ebd_paged_attention; at most 32 mask_words and 1024
+ *   mask       device [n_tokens][mask_words] out;  positions  device [n_tokens] out
+ *   dev_status device int32, nullable
+ * Tokens that cu_new gives to no sequence, or past max_new, keep what both held
+ * (EBD_DEV_RANGE).
+ */
+ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t max_new, const int32_t* parents,
+                          const int32_t* cu_new, const int32_t* seq_len, int32_t window,
+                          uint32_t* mask, int32_t mask_words, int32_t* positions,
+                          int32_t* dev_status, void* stream);
+
+/*
+ * Attention of drafted trees over the paged cache: ebd_paged_attention, but a new token
+ * sees, of its sequence's new tokens, those up to itself whose bit of its mask row is set
+ * (itself too only if its own is), and of the earlier positions j, with a window > 0,
+ * those with j > positions[t] - window.  A token with nothing to see gets y = 0,
+ * lse = -inf.
+ *   mask       device [n_tokens][mask_words], max_new <= 32 mask_words
+ *   positions  device [n_tokens], needed with a window: from the tree's beginning, base =
+ *              seq_len[b] - (new tokens of b), to base + the token's number
+ *              (otherwise clamped, EBD_DEV_RANGE)
+ * Everything else, the workspace too, as for ebd_paged_attention.
+ */
+ebd_status ebd_paged_tree_attention(const ebd_paged_cache* cache, int32_t n_tokens,
+                                    int32_t max_new, int32_t n_q_heads, const int32_t* cu_new,
+                                    const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                    float scale, int32_t window, const uint32_t* mask,
+                                    int32_t mask_words, const int32_t* positions, void* y,
+                                    float* lse, int32_t* dev_status, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/*
+ * Keeps an accepted path of each tree: with base as above, the cached row of position
+ * base + path[b][i] moves to base + i, for i < n_accepted[b], in every KV head of n_layers
+ * caches that share the block table (layer l's pools begin l * layer_stride elements
+ * after K_pages and V_pages), and seq_len_out[b] = base + n_accepted[b].  Keys stay turned
+ * as they are: the i-th token of a path stood at position base + i already.
+ *   cu_new      device [B+1]: offsets of the trees (only their differences are read)
+ *   path        device [B, max_path] numbers of new tokens, rising; the path ends before the
+ *               first that does not rise or is none (EBD_DEV_RANGE)
+ *   n_accepted  device [B], 0 .. min(max_path, new tokens) (clamped, EBD_DEV_RANGE)
+ *   seq_len_out device [B] out, nullable; apart from the cache's seq_len (EBD_ERR_INVALID)
+ *   dev_status  device int32, required
+ * A row on a page outside the pool, or bound for one, does not move (EBD_DEV_RANGE).
+ * Alignment as for ebd_paged_gather, layer_stride too.
+ */
+ebd_status ebd_paged_keep(const ebd_paged_cache* cache, int32_t n_layers, int64_t layer_stride,
+                          const int32_t* cu_new, const int32_t* path, int32_t max_path,
+                          const int32_t* n_accepted, int32_t* seq_len_out, int32_t* dev_status,
+                          void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -55,7 +55,8 @@ __device__ __forceinline__ void cp_async16_or_zero(void* dst, const void* src, b
                : "memory");
 }
 
-template <int D>
+// TREE: new tokens see each other by a mask.
+template <int D, bool TREE>
 __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     paged_attn_f32_kernel(const PagedAttnArgs a) {
   using L = SimtLayout<D>;
@@ -83,7 +84,8 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     const HeadSlice hs = head_slice(a, w.h);
     const int tokens = w.tokens(a), t_first = w.sp.t0 + w.first(a);
     const int p0 = w.sp.len - w.sp.n + w.first(a);  // position of the item's first token
-    const int seen = first_seen(a, p0);  // pages before it may have been released
+    const int base = w.sp.len - w.sp.n;  // tree: where it begins
+    const int seen = first_seen(a, TREE ? base : p0);  // pages before it may have been released
     // Row threadIdx.x of key tile j: its offset in the pools; -1 past the sequence's
     // end, where nothing is read
     auto find_row = [&](int j) {
@@ -130,9 +132,9 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     int hi[4], lo[4];  // keys that this thread's rows see
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int p = p0 + min((ty * 4 + i) / a.slice, tokens - 1);
-      hi[i] = p + 1;
-      lo[i] = first_seen(a, p);
+      const int tok = min((ty * 4 + i) / a.slice, tokens - 1), p = p0 + tok;
+      hi[i] = TREE ? base : p + 1;  // up to here every key from lo on is seen
+      lo[i] = TREE ? tree_first_seen(a, t_first + tok, base, p - base, bad) : first_seen(a, p);
     }
     float m[4], l[4], o[4][D / 16];
 #pragma unroll
@@ -188,12 +190,16 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float top = m[i];
+          uint32_t visible = 0;
+          if (TREE && !all) {
+            const int tok = min((ty * 4 + i) / a.slice, tokens - 1);
+            visible = (uint32_t)tree_visible<BN>(a, t_first + tok, p0 + tok - base, base, lo[i], k0);
+          }
 #pragma unroll
           for (int e = 0; e < NK; ++e) {
             const int pos = k0 + tx + 16 * e;
-            s[i][e] = all || (pos >= lo[i] && pos < hi[i] && !(absent >> (tx + 16 * e) & 1))
-                          ? s[i][e]
-                          : -INFINITY;
+            const bool sees = TREE ? visible >> (tx + 16 * e) & 1 : pos >= lo[i] && pos < hi[i];
+            s[i][e] = all || (sees && !(absent >> (tx + 16 * e) & 1)) ? s[i][e] : -INFINITY;
             top = fmaxf(top, s[i][e]);
           }
 #pragma unroll
@@ -286,8 +292,8 @@ static int f32_ctas(int head_dim) {
 template <int D>
 static ebd_status launch_paged_f32(PagedAttnArgs a, int n_cta, cudaStream_t s) {
   const int smem = SimtLayout<D>::kFloats * 4;
-  if (cudaFuncSetAttribute(paged_attn_f32_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           smem) != cudaSuccess)
+  auto kern = a.mask ? paged_attn_f32_kernel<D, true> : paged_attn_f32_kernel<D, false>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
   const int slice = f32_slice(a.group);
   a.slices = (a.group + slice - 1) / slice;
@@ -299,7 +305,7 @@ static ebd_status launch_paged_f32(PagedAttnArgs a, int n_cta, cudaStream_t s) {
   a.item_cost = 1;
   if (!line_fits(a, SimtLayout<D>::kKeys)) return EBD_ERR_UNSUPPORTED;
   const ebd_status st =
-      launch_dependent(paged_attn_f32_kernel<D>, dim3(n_cta), kAttnThreads, smem, s, a);
+      launch_dependent(kern, dim3(n_cta), kAttnThreads, smem, s, a);
   if (st != EBD_OK) return st;
   return launch_paged_merge(a, false, D, n_cta, s);
 }
@@ -334,13 +340,13 @@ extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cac
                            cache->head_dim);
 }
 
-extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens,
-                                          int32_t max_new, int32_t n_q_heads,
-                                          const int32_t* cu_new, const void* q,
-                                          int64_t q_token_stride, int64_t q_head_stride,
-                                          float scale, int32_t window, void* y, float* lse,
-                                          int32_t* dev_status, void* workspace, size_t ws_bytes,
-                                          void* stream) {
+// Both forms; mask null: causal.
+static ebd_status attention(const ebd_paged_cache* cache, int32_t n_tokens, int32_t max_new,
+                            int32_t n_q_heads, const int32_t* cu_new, const void* q,
+                            int64_t q_token_stride, int64_t q_head_stride, float scale,
+                            int32_t window, const uint32_t* mask, int32_t mask_words,
+                            const int32_t* positions, void* y, float* lse, int32_t* dev_status,
+                            void* workspace, size_t ws_bytes, void* stream) {
   const ebd_status st = check_paged(cache);
   if (st != EBD_OK) return st;
   if (n_tokens < 0 || max_new < (n_tokens > 0) || n_q_heads < 1 ||
@@ -375,6 +381,10 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
   a.group = group;
   a.window = window;
   a.scale2 = scale * kLog2e;
+  a.mask = mask;
+  a.mask_words = mask_words;
+  a.positions = positions;
+  a.in_line = mask ? 0 : 1;
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
   const int n_cta = attention_ctas(*cache);
@@ -384,4 +394,29 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
     return cache->head_dim == 128 ? launch_paged_f32<128>(a, n_cta, s)
                                   : launch_paged_f32<64>(a, n_cta, s);
   return launch_paged_tc(a, *cache, n_cta, s);
+}
+
+extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t n_tokens,
+                                          int32_t max_new, int32_t n_q_heads,
+                                          const int32_t* cu_new, const void* q,
+                                          int64_t q_token_stride, int64_t q_head_stride,
+                                          float scale, int32_t window, void* y, float* lse,
+                                          int32_t* dev_status, void* workspace, size_t ws_bytes,
+                                          void* stream) {
+  return attention(cache, n_tokens, max_new, n_q_heads, cu_new, q, q_token_stride, q_head_stride,
+                   scale, window, nullptr, 0, nullptr, y, lse, dev_status, workspace, ws_bytes,
+                   stream);
+}
+
+extern "C" ebd_status ebd_paged_tree_attention(
+    const ebd_paged_cache* cache, int32_t n_tokens, int32_t max_new, int32_t n_q_heads,
+    const int32_t* cu_new, const void* q, int64_t q_token_stride, int64_t q_head_stride,
+    float scale, int32_t window, const uint32_t* mask, int32_t mask_words,
+    const int32_t* positions, void* y, float* lse, int32_t* dev_status, void* workspace,
+    size_t ws_bytes, void* stream) {
+  if (mask_words < 1 || max_new > 32ll * mask_words) return EBD_ERR_INVALID;
+  if (n_tokens > 0 && (!mask || (window > 0 && !positions))) return EBD_ERR_INVALID;
+  return attention(cache, n_tokens, max_new, n_q_heads, cu_new, q, q_token_stride, q_head_stride,
+                   scale, window, mask, mask_words, positions, y, lse, dev_status, workspace,
+                   ws_bytes, stream);
 }

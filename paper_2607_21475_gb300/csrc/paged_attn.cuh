@@ -61,6 +61,13 @@ struct PagedAttnArgs {
   int full_work;     // and of a larger item
   int min_share;     // least work per CTA
   int item_cost;     // work of an item beside its key tiles
+  // Tree attention: which of its sequence's new tokens each one sees, in place of those
+  // up to it, and where each stands (for the window over the earlier positions).
+  const uint32_t* mask;      // [n_tokens][mask_words]; null: causal
+  const int32_t* positions;  // [n_tokens]; needed with a window
+  int mask_words;
+  int in_line;               // 1: new token i stands i positions after the first; 0: a tree's
+                             // tokens may all stand where it begins
 };
 
 // KV head, first query head and number of query heads of (sliced) head h.
@@ -81,6 +88,51 @@ __device__ __forceinline__ int first_seen(const PagedAttnArgs& a, int p) {
   return a.window > 0 && p >= a.window ? p - a.window + 1 : 0;
 }
 
+// The first position that a tree's token t sees before the tree, which begins at position
+// base; it is the tree's token number i, and stands between base and base + i.
+__device__ __forceinline__ int tree_first_seen(const PagedAttnArgs& a, int t, int base, int i,
+                                               bool& bad) {
+  if (a.window == 0) return 0;
+  const int p = a.positions[t], at = min(max(p, base), base + i);
+  bad |= p != at;
+  return min(first_seen(a, at), max(base, 0));
+}
+
+// Mask words w, w + 1 of new token t, as one.
+__device__ __forceinline__ uint64_t tree_words(const PagedAttnArgs& a, int t, int w) {
+  const uint32_t* row = a.mask + (size_t)t * a.mask_words;
+  const uint32_t lo = w < a.mask_words ? __ldg(row + w) : 0u;
+  const uint32_t hi = w + 1 < a.mask_words ? __ldg(row + w + 1) : 0u;
+  return (uint64_t)hi << 32 | lo;
+}
+
+// Which of the BN = 32 or 64 keys from position k0 on (bit j: key k0 + j) the tree's token t
+// sees: lo and later before the tree, and those of its mask up to itself (number i).
+template <int BN>
+__device__ __forceinline__ uint64_t tree_visible(const PagedAttnArgs& a, int t, int i, int base,
+                                                 int lo, int k0) {
+  const int at = k0 - base;  // number of the first key as a new token
+  uint64_t bits = 0;
+  if (at > -BN) {
+    if (at >= 0) {
+      bits = tree_words(a, t, at >> 5) >> (at & 31);
+      if (BN == 64 && (at & 31))
+        bits |= tree_words(a, t, (at >> 5) + 2) << (64 - (at & 31));
+    } else {
+      bits = tree_words(a, t, 0) << -at;
+    }
+    const int own = i - at;  // (numbers after its own are hidden)
+    if (own < 63) bits &= own < 0 ? 0 : (2ull << own) - 1;
+  }
+  const int skip = lo - k0, end = -at;  // earlier positions: keys skip .. end - 1
+  if (end > 0) {
+    uint64_t early = end >= 64 ? ~0ull : (1ull << end) - 1;
+    if (skip > 0) early &= skip >= 64 ? 0 : ~0ull << skip;
+    bits |= early;
+  }
+  return bits;
+}
+
 // Key tiles [kb, ke) of m-tile m; an item with nothing to see keeps one (fully
 // masked) tile, so that its rows get written.
 template <int BN>
@@ -91,7 +143,7 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
   kb = 0;
   ke = 1;
   if (k_end > 0) {
-    kb = first_seen(a, p0 + first) / BN;
+    kb = first_seen(a, p0 + first * a.in_line) / BN;
     ke = (k_end + BN - 1) / BN;
   }
 }
@@ -326,15 +378,16 @@ __device__ __forceinline__ void load_row(const T* p, float (&x)[C]) {
 // value has weight 0 in the tile's product, and 0 times NaN or infinity is NaN.  The
 // channels that are NaN and in which a hidden value of the piece's positions
 // [tile_lo, tile_hi) (at most a few hundred at either end are hidden) is not finite are
-// recomputed from those that the row sees, [lo, hi) of them, 32 keys at a time with one
+// recomputed from those that the row sees, [lo, hi) of them and of a tree, which begins at
+// position base, its token's (number i, packed t), 32 keys at a time with one
 // set of weights for all channels; a NaN in any other channel is the row's own.  It
 // stops once every such channel has met a NaN of its own.  q: the row's query; y or part
 // (part_row): the output, as written.  Whole warp: lane i has channels C i .. + C - 1,
 // and key i of 32.
 template <typename T, int D>
 __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
-                                         int tile_lo, int lo, int hi, int tile_hi, T* y,
-                                         float* part, int lane) {
+                                         int tile_lo, int lo, int hi, int tile_hi, int base,
+                                         int t, int i, T* y, float* part, int lane) {
   constexpr int C = D / 32;
   const int c0 = lane * C;
   auto at = [&](int c) { return part + (c0 + c) / 4 * a.part_step + (c0 + c) % 4; };
@@ -350,11 +403,16 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
     const int page = there ? page_of(a.pv, b, pos) : -1;
     return page < 0 ? -1ll : slot_offset(a.pv, page, kvh, pos);
   };
+  // whether the row sees its position pos, lo <= pos < hi
+  auto sees = [&](int pos) {
+    return !a.mask || pos < base || (tree_words(a, t, (pos - base) >> 5) >> ((pos - base) & 31) & 1);
+  };
   const int k_lo = min(max(lo, tile_lo), tile_hi), k_hi = max(min(hi, tile_hi), k_lo);  // seen
   uint32_t mend = 0;
-  auto look = [&](int from, int to) {  // hidden positions [from, to)
+  auto look = [&](int from, int to, bool tree) {  // hidden positions of [from, to)
     for (int p0 = from; p0 < to; p0 += 32) {
-      const long long off = place(p0 + lane, p0 + lane < to);
+      const int pos = p0 + lane;
+      const long long off = place(pos, pos < to && (!tree || !sees(pos)));
 #pragma unroll 8
       for (int i = 0; i < 32; ++i) {
         const long long o = __shfl_sync(0xffffffffu, off, i);
@@ -365,14 +423,15 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
       }
     }
   };
-  look(tile_lo, k_lo);
-  look(k_hi, tile_hi);
+  look(tile_lo, k_lo, false);
+  look(k_hi, tile_hi, false);
+  if (a.mask) look(max(base, k_lo), k_hi, true);
   mend &= nan;
   if (!__any_sync(0xffffffffu, mend)) return;
   float m = -INFINITY, l = 0.f, acc[C] = {};
   for (int top = k_hi; top > k_lo; top -= 32) {
     const int pos = top - 1 - lane;
-    const long long off = place(pos, pos >= k_lo);
+    const long long off = place(pos, pos >= k_lo && sees(pos));
     float s = -INFINITY;
     if (off >= 0) {
       constexpr int W = 16 / sizeof(T);
@@ -391,7 +450,7 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
     float m1 = fmaxf(m, s);
 #pragma unroll
     for (int x = 16; x > 0; x >>= 1) m1 = fmaxf(m1, __shfl_xor_sync(0xffffffffu, m1, x));
-    const float base = m1 == -INFINITY ? 0.f : m1, f = exp2f(m - base), p = exp2f(s - base);
+    const float ref = m1 == -INFINITY ? 0.f : m1, f = exp2f(m - ref), p = exp2f(s - ref);
     m = m1;
     l = l * f + p;  // this lane's share
 #pragma unroll
@@ -438,15 +497,19 @@ __device__ __noinline__ void mend_pieces(const PagedAttnArgs& a, int cta, int n_
     const int tokens = min(w.tokens(a) - x0, a.half_tokens), slot = w.slot(cta);
     const int t_first = w.sp.t0 + w.first(a) + x0, p0 = w.sp.len - w.sp.n + w.first(a) + x0;
     const HeadSlice hs = head_slice(a, w.h);
+    const int base = w.sp.len - w.sp.n;  // tree: where it begins
     for (int r = row0; r < row0 + rows; ++r) {
       const int t = r / a.slice, g = r - t * a.slice;
       if (t >= tokens) break;
       if (g >= hs.n) continue;
       const long long out =
           (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
+      bool bad;
+      const int lo = a.mask ? tree_first_seen(a, t_first + t, base, p0 + t - base, bad)
+                            : first_seen(a, p0 + t);
       mend_row<T, D>(a, w.b, hs.kvh,
                      (const T*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs, w.cur * BN,
-                     first_seen(a, p0 + t), p0 + t + 1, min(w.end * BN, w.sp.len),
+                     lo, p0 + t + 1, min(w.end * BN, w.sp.len), base, t_first + t, p0 + t - base,
                      slot < 0 ? (T*)a.y + out * D : nullptr,
                      slot < 0 ? nullptr : part_row<D>(a, slot, slot0 + r), lane);
     }

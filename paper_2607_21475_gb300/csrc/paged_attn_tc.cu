@@ -80,6 +80,7 @@ struct Piece {
   int pos;          // its position
   int tokens;
   int slot;         // partial result, -1: the output itself
+  int first;        // number of the first token among the sequence's new ones
   int absent;       // a key that it sees has no page; told with q_full, so that the softmax
                     // asks once a piece (once a tile: mixed batch 41.5 -> 42.9 us,
                     // 4096-token chunk 490 -> 503 us at the full clock)
@@ -114,7 +115,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <int D>
+// TREE: new tokens see each other by a mask.  A row's 64 bits for a tile that touches the
+// tree are found while the tile's product runs, and select its logits.
+template <int D, bool TREE>
 __global__ void __launch_bounds__(kTcAttnThreads, 1)
     paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                          const __grid_constant__ CUtensorMap tmK,
@@ -203,7 +206,12 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       if (tokens <= 0) continue;
       const int tok = x0 + min(rt, tokens - 1);
       const int pos = w.pos + tok;
-      const int hi = pos + 1, lo = first_seen(a, pos);
+      const int base = w.pos - w.first;  // tree: where it begins
+      bool astray = false;
+      const int hi = TREE ? base : pos + 1;  // up to here every key from lo on is seen
+      const int lo = TREE ? tree_first_seen(a, w.token + tok, base, w.first + tok, astray)
+                          : first_seen(a, pos);
+      if (TREE && astray) raise_status(a.dev_status, EBD_DEV_RANGE);
       // (whether keys are absent is known by the first product)
       if (!mbar_wait_warp(&bar->s_full[x][it & 1], (it >> 1) & 1)) {
         ok = false;
@@ -215,6 +223,9 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       for (int j = w.cur; j < w.end; ++j, ++it) {
         const int k0 = j * kTcBN;
         const uint32_t buf = sS + (it & 1) * 64;
+        uint64_t visible = 0;
+        if (TREE && __any_sync(0xffffffffu, hi - k0 < kTcBN || edge > k0))
+          visible = tree_visible<kTcBN>(a, w.token + tok, w.first + tok, base, lo, k0);
         if (!mbar_wait_warp(&bar->s_full[x][it & 1], (it >> 1) & 1)) {
           ok = false;
           break;
@@ -224,10 +235,17 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         tmem_ld64(buf, s);
         tmem_ld_wait();
         if (__any_sync(0xffffffffu, hi - k0 < kTcBN || edge > k0)) {
-          const int chi = hi - k0, clo = lo - k0;
+          if (TREE) {
+            const uint32_t v0 = (uint32_t)visible, v1 = (uint32_t)(visible >> 32);
 #pragma unroll
-          for (int i = 0; i < 64; ++i)
-            if (i >= chi || i < clo) s[i] = __float_as_uint(-INFINITY);
+            for (int i = 0; i < 64; ++i)
+              if (!((i < 32 ? v0 : v1) >> (i & 31) & 1)) s[i] = __float_as_uint(-INFINITY);
+          } else {
+            const int chi = hi - k0, clo = lo - k0;
+#pragma unroll
+            for (int i = 0; i < 64; ++i)
+              if (i >= chi || i < clo) s[i] = __float_as_uint(-INFINITY);
+          }
           if (absent_keys) {
             const uint64_t absent = bar->absent[(tile0 + (j - w.cur)) % kAbsentSlots];
 #pragma unroll
@@ -456,7 +474,8 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       // where the table names a page outside.
       const int bx = lane / L::kHalves, half = lane - bx * L::kHalves;
       int block0 = 0, entry = 0, held = 0;  // pages of blocks block0 .. + held - 1
-      const int seen = first_seen(a, w.pos);  // pages before it may have been released
+      // pages before it may have been released
+      const int seen = first_seen(a, TREE ? w.pos - w.first : w.pos);
       auto page_at = [&](int j) {
         const int first = (j * kTcBN) >> a.pv.page_shift;
         const int last = (j * kTcBN + kTcBN - 1) >> a.pv.page_shift;
@@ -542,6 +561,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
           p.token = walk.sp.t0 + walk.first(a);
           p.pos = walk.sp.len - walk.sp.n + walk.first(a);
           p.tokens = walk.tokens(a);
+          p.first = walk.first(a);
           p.slot = walk.slot(cta);
           record_piece(a, record, walk, pushed == 0);
         } else if (lane == 0) {
@@ -586,7 +606,8 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
         const uint32_t at = items + turn;
         if (!ok || at + all >= pushed) break;
         const Piece& p = bar->piece[at % kPieceSlots];
-        const int first = max(p.cur * kTcBN, first_seen(a, p.pos)) >> a.pv.page_shift;
+        const int seen = first_seen(a, TREE ? p.pos - p.first : p.pos);
+        const int first = max(p.cur * kTcBN, seen) >> a.pv.page_shift;
         const int past = min(p.end * kTcBN, p.len);
         bool out = false;
 #pragma unroll 4
@@ -691,11 +712,10 @@ static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, 
   if (!encode_queries(&tmQ, a, D) || !encode_pool(&tmK, c, c.K_pages, box) || !encode_pool(&tmV, c, c.V_pages, box))
     return EBD_ERR_CUDA;
   constexpr int smem = PagedTcLayout<D>::kBytes;
-  if (cudaFuncSetAttribute(paged_attn_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           smem) != cudaSuccess)
+  auto kern = a.mask ? paged_attn_tc_kernel<D, true> : paged_attn_tc_kernel<D, false>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  return launch_dependent(paged_attn_tc_kernel<D>, dim3(n_cta), kTcAttnThreads, smem, s, tmQ, tmK,
-                          tmV, a);
+  return launch_dependent(kern, dim3(n_cta), kTcAttnThreads, smem, s, tmQ, tmK, tmV, a);
 }
 
 ebd_status launch_paged_tc(PagedAttnArgs a, const ebd_paged_cache& c, int n_cta,

@@ -37,6 +37,9 @@ __all__ = [
     "EBD_DEV_RANGE", "EBD_ROTARY_HALF", "EBD_ROTARY_PAIRS", "EbdPagedCache", "PagedCache",
     "alloc_paged", "rotary_frequencies", "ebd_rotary_table", "ebd_rotary", "ebd_paged_append",
     "ebd_paged_attention_workspace_bytes", "ebd_paged_attention", "ebd_paged_gather",
+    "PagePool", "alloc_page_pool", "ebd_paged_deal", "ebd_norm_rotary",
+    "ebd_norm_rotary_backward_workspace_bytes", "ebd_norm_rotary_backward",
+    "ebd_paged_append_norm", "ebd_tree_masks", "ebd_paged_tree_attention", "ebd_paged_keep",
 ]
 
 EBD_OK = 0
@@ -56,6 +59,9 @@ ABI_FUNCTIONS = (
     "ebd_gather_queries", "ebd_variance_contributions", "ebd_block_scores",
     "ebd_check_stalled_wait", "ebd_rotary_table", "ebd_rotary", "ebd_paged_append",
     "ebd_paged_attention_workspace_bytes", "ebd_paged_attention", "ebd_paged_gather",
+    "ebd_paged_deal", "ebd_norm_rotary", "ebd_norm_rotary_backward_workspace_bytes",
+    "ebd_norm_rotary_backward", "ebd_paged_append_norm", "ebd_tree_masks",
+    "ebd_paged_tree_attention", "ebd_paged_keep",
 )
 
 
@@ -167,6 +173,27 @@ def lib():
                                                    c_void_p, sz, c_void_p]),
             "ebd_paged_gather": (ctypes.c_int, [C, c_void_p, c_void_p, i32, c_void_p, c_void_p,
                                                 c_void_p, c_void_p]),
+            "ebd_paged_deal": (ctypes.c_int, [i32] * 6 + [c_void_p] * 15),
+            "ebd_norm_rotary": (ctypes.c_int, [
+                ctypes.c_int, i32, i32, i32, c_void_p, i64, i64, c_void_p, ctypes.c_int, i64, f32,
+                c_void_p, c_void_p, i32, i32, ctypes.c_int, c_void_p, i64, i64, c_void_p,
+                c_void_p]),
+            "ebd_norm_rotary_backward_workspace_bytes": (sz, [i32, i32, i32]),
+            "ebd_norm_rotary_backward": (ctypes.c_int, [
+                ctypes.c_int, i32, i32, i32, c_void_p, i64, i64, c_void_p, i64, i64, c_void_p,
+                ctypes.c_int, i64, f32, c_void_p, c_void_p, i32, i32, ctypes.c_int, c_void_p, i64,
+                i64, c_void_p, c_void_p, c_void_p, sz, c_void_p]),
+            "ebd_paged_append_norm": (ctypes.c_int, [
+                C, i32, c_void_p, c_void_p, c_void_p, c_void_p, i64, i64, c_void_p, i64, i64,
+                c_void_p, i64, c_void_p, i64, ctypes.c_int, f32, c_void_p, i32, i32, ctypes.c_int,
+                i32, c_void_p, i64, i64, c_void_p, i64, i64, c_void_p, c_void_p]),
+            "ebd_tree_masks": (ctypes.c_int, [i32, i32, i32, c_void_p, c_void_p, c_void_p, i32,
+                                              c_void_p, i32, c_void_p, c_void_p, c_void_p]),
+            "ebd_paged_tree_attention": (ctypes.c_int, [
+                C, i32, i32, i32, c_void_p, c_void_p, i64, i64, f32, i32, c_void_p, i32, c_void_p,
+                c_void_p, c_void_p, c_void_p, c_void_p, sz, c_void_p]),
+            "ebd_paged_keep": (ctypes.c_int, [C, i32, i64, c_void_p, c_void_p, i32, c_void_p,
+                                              c_void_p, c_void_p, c_void_p]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(L, name)
@@ -215,6 +242,13 @@ def _stream(stream):
     if _raw_stream is not None and torch.cuda.is_initialized():
         return _raw_stream(torch._C._cuda_getDevice())
     return torch.cuda.current_stream().cuda_stream
+
+
+def _here(t, stream, name):
+    """Refuses a tensor of another device than the one that the call launches on."""
+    at = stream.device_index if stream is not None else torch._C._cuda_getDevice()
+    if t.is_cuda and t.device.index != at:
+        raise ValueError(f"{name} is on {t.device}, the call's stream on cuda:{at}")
 
 
 def _check(name, code):
@@ -795,3 +829,288 @@ def ebd_paged_gather(pc: PagedCache, out: CompactCache, stream=None) -> CompactC
         _ptr(out.K_c, dt, (B, H, cap, d), "K_c"), _ptr(out.V_c, dt, (B, H, cap, d), "V_c"),
         _ptr(out.dev_status, torch.int32, (1,), "dev_status"), _stream(stream)))
     return out
+
+
+# ---------------------------------------------------------------- speculative steps
+@dataclass
+class PagePool:
+    """The pages of a paged cache that nobody holds, and who holds which blocks.
+
+    free_pages [n_pages] int32, of which the first n_free[0] are free; held [B, 2] int32:
+    sequence b holds the pages of blocks held[b, 0] .. held[b, 1] - 1 of its row of the
+    block table."""
+    free_pages: torch.Tensor
+    n_free: torch.Tensor
+    held: torch.Tensor
+
+
+def alloc_page_pool(batch, n_pages, device) -> PagePool:
+    """Caller-side allocation: every page free, no sequence holds any."""
+    i = torch.int32
+    return PagePool(torch.arange(n_pages, dtype=i, device=device),
+                    torch.full((1,), n_pages, dtype=i, device=device),
+                    torch.zeros((batch, 2), dtype=i, device=device))
+
+
+def ebd_paged_deal(pool: PagePool, pc: PagedCache, n_new: torch.Tensor, n_tokens: int,
+                   window: int = 0, cu_new=None, positions=None, slots=None, served=None,
+                   seq_len_out=None, held_out=None, n_free_out=None, stream=None):
+    """Deal pages for n_new [B] (int32; negative: the sequence leaves) more tokens, at
+    most n_tokens in all: (cu_new [B + 1], positions [n_tokens] int32, slots [n_tokens]
+    int64, served [B]).  pc.seq_len counts the cached tokens before the call and, like
+    pool.held and pool.n_free, is brought up to date in place unless another output is
+    given; pc.block_table and pool.free_pages always are.  A sequence that is not served
+    (EBD_DEV_CAPACITY in dev_status) stays as it was and has no new tokens in cu_new."""
+    c = _paged(pc)
+    B, i32 = c.batch, torch.int32
+    dev = pc.seq_len.device
+    _here(pc.seq_len, stream, "seq_len")
+    if cu_new is None:
+        cu_new = _result((B + 1,), i32, dev, stream)
+    if positions is None:
+        positions = _result((n_tokens,), i32, dev, stream)
+    if slots is None:
+        slots = _result((n_tokens,), torch.int64, dev, stream)
+    if served is None:
+        served = _result((B,), i32, dev, stream)
+    held, free = pool.held, pool.n_free
+    _check("ebd_paged_deal", lib().ebd_paged_deal(
+        B, c.page_size, c.n_pages, c.max_blocks, int(n_tokens), int(window),
+        _ptr(n_new, i32, (B,), "n_new"), c.seq_len, _ptr(held, i32, (B, 2), "held"),
+        _ptr(free, i32, (1,), "n_free"), _ptr(pool.free_pages, i32, (c.n_pages,), "free_pages"),
+        c.block_table, _ptr(pc.seq_len if seq_len_out is None else seq_len_out, i32, (B,),
+                            "seq_len_out"),
+        _ptr(held if held_out is None else held_out, i32, (B, 2), "held_out"),
+        _ptr(free if n_free_out is None else n_free_out, i32, (1,), "n_free_out"),
+        _ptr(cu_new, i32, (B + 1,), "cu_new"), _ptr(served, i32, (B,), "served"),
+        _ptr(positions, i32, (n_tokens,), "positions"),
+        _ptr(slots, torch.int64, (n_tokens,), "slots"),
+        _ptr(pc.dev_status, i32, (1,), "dev_status"), _stream(stream)))
+    return cu_new, positions, slots, served
+
+
+def _norm_weight(w, dtype, heads, d, name):
+    """(address, type code, head stride) of a norm's weight, [d] or [heads, d]."""
+    if not isinstance(w, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if not w.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if w.dtype != torch.float32 and w.dtype != dtype:
+        raise TypeError(f"{name} has dtype {w.dtype}, expected {dtype} or float32")
+    if w.shape != (d,) and w.shape != (heads, d):
+        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {(d,)} or {(heads, d)}")
+    if d > 1 and w.stride(-1) != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous")
+    hs = w.stride(0) if w.dim() == 2 else 0
+    if w.dim() == 2 and hs < 1:
+        raise ValueError(f"{name} must have a row of its own for every head")
+    return w.data_ptr(), _dtype_code(w), hs
+
+
+def _norm_table(table, positions, n_tokens):
+    """(positions, table, n_pos, rotary_dim) of a norm with or without a rotation."""
+    if table is None:
+        return None, None, 0, 0
+    if positions is None:
+        raise ValueError("a rotation needs positions")
+    tab, n_pos, rot = _rotary_rows(table)
+    return _ptr(positions, torch.int32, (n_tokens,), "positions"), tab, n_pos, rot
+
+
+def ebd_norm_rotary(x: torch.Tensor, weight: torch.Tensor, positions=None, table=None, out=None,
+                    layout: int = EBD_ROTARY_HALF, eps: float = 1e-6, dev_status=None,
+                    stream=None) -> torch.Tensor:
+    """x [T, H, d] (any token and head strides) divided by each row's root mean square,
+    times weight ([d] or [H, d], x's type or float32), and, with a table, turned to
+    positions [T] (int32).  out may be x."""
+    if x.dim() != 3:
+        raise ValueError("x must be [T, H, d]")
+    T, H, d = x.shape
+    _here(x, stream, "x")
+    wp, wt, wh = _norm_weight(weight, x.dtype, H, d, "weight")
+    if out is None:
+        out = _result((T, H, d), x.dtype, x.device, stream)
+    pos, tab, n_pos, rot = _norm_table(table, positions, T)
+    xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
+    yp, yt, yh = _rows(out, x.dtype, T, H, d, "out")
+    _check("ebd_norm_rotary", lib().ebd_norm_rotary(
+        _dtype_code(x), T, H, d, xp, xt, xh, wp, wt, wh, float(eps), pos, tab, n_pos, rot,
+        int(layout), yp, yt, yh, _ptr(dev_status, torch.int32, (1,), "dev_status"),
+        _stream(stream)))
+    return out
+
+
+def ebd_norm_rotary_backward_workspace_bytes(n_heads: int, head_dim: int, per_head: bool) -> int:
+    return int(lib().ebd_norm_rotary_backward_workspace_bytes(int(n_heads), int(head_dim),
+                                                              1 if per_head else 0))
+
+
+def ebd_norm_rotary_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
+                             positions=None, table=None, dx=None, dweight=None,
+                             layout: int = EBD_ROTARY_HALF, eps: float = 1e-6, workspace=None,
+                             dev_status=None, stream=None):
+    """Gradients of ebd_norm_rotary at x, given dy: dx [T, H, d] in x's type and dweight,
+    float32 in the weight's shape.  dx may be dy or x."""
+    if x.dim() != 3:
+        raise ValueError("x must be [T, H, d]")
+    T, H, d = x.shape
+    _here(x, stream, "x")
+    wp, wt, wh = _norm_weight(weight, x.dtype, H, d, "weight")
+    if dx is None:
+        dx = _result((T, H, d), x.dtype, x.device, stream)
+    if dweight is None:
+        dweight = _result(weight.shape, torch.float32, x.device, stream)
+    pos, tab, n_pos, rot = _norm_table(table, positions, T)
+    xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
+    gp, gt, gh = _rows(dy, x.dtype, T, H, d, "dy")
+    op, ot, oh = _rows(dx, x.dtype, T, H, d, "dx")
+    L = lib()
+    ws, wsb = _workspace(L.ebd_norm_rotary_backward_workspace_bytes(H, d, 1 if wh else 0),
+                         x.device, workspace, stream)
+    _check("ebd_norm_rotary_backward", L.ebd_norm_rotary_backward(
+        _dtype_code(x), T, H, d, gp, gt, gh, xp, xt, xh, wp, wt, wh, float(eps), pos, tab, n_pos,
+        rot, int(layout), op, ot, oh, _ptr(dweight, torch.float32, weight.shape, "dweight"),
+        _ptr(dev_status, torch.int32, (1,), "dev_status"), ws, wsb, _stream(stream)))
+    return dx, dweight
+
+
+def ebd_paged_append_norm(pc: PagedCache, k_new: torch.Tensor, v_new: torch.Tensor, k_weight=None,
+                          q=None, q_weight=None, q_out=None, cu_new=None, slots=None,
+                          positions=None, table=None, layout: int = EBD_ROTARY_HALF,
+                          eps: float = 1e-6, stream=None) -> PagedCache:
+    """ebd_paged_append with keys and queries normalised on the way (weights as for
+    ebd_norm_rotary; None: not normalised), tokens placed by cu_new [B + 1] or by their
+    slots [T] (int64, ebd_paged_deal; -1: no token).  positions [T]: where each is turned
+    to; needed with slots and a table, otherwise a token's place in its sequence."""
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    T, H, d = k_new.shape[0], c.n_kv_heads, c.head_dim
+    _here(pc.K_pages, stream, "K_pages")
+    kp, kt, kh = _rows(k_new, dt, T, H, d, "k_new")
+    vp, vt, vh = _rows(v_new, dt, T, H, d, "v_new")
+    if (cu_new is None) == (slots is None):
+        raise ValueError("tokens are placed by cu_new or by slots, one of the two")
+    if table is None:
+        tab, n_pos, rot = None, 0, 0
+    else:
+        tab, n_pos, rot = _rotary_rows(table)
+        if positions is None and cu_new is None:
+            raise ValueError("slots tell no positions: a rotation needs them")
+    hq, qp, qt, qh, op, ot, oh = 0, None, 0, 0, None, 0, 0
+    kw, wt, kwh = (None, EBD_F32, 0) if k_weight is None else _norm_weight(k_weight, dt, H, d,
+                                                                           "k_weight")
+    qw, qwh = None, 0
+    if q is not None:
+        if q.dim() != 3 or q_out is None:
+            raise ValueError("q must be [T, Hq, d] and come with q_out")
+        hq = q.shape[1]
+        qp, qt, qh = _rows(q, dt, T, hq, d, "q")
+        op, ot, oh = _rows(q_out, dt, T, hq, d, "q_out")
+        if q_weight is not None:
+            qw, qwt, qwh = _norm_weight(q_weight, dt, hq, d, "q_weight")
+            if k_weight is not None and qwt != wt:
+                raise TypeError("k_weight and q_weight must have one dtype")
+            wt = qwt
+    _check("ebd_paged_append_norm", lib().ebd_paged_append_norm(
+        ctypes.byref(c), T, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"),
+        _ptr(slots, torch.int64, (T,), "slots"), _ptr(positions, torch.int32, (T,), "positions"),
+        kp, kt, kh, vp, vt, vh, kw, kwh, qw, qwh, wt, float(eps), tab, n_pos, rot, int(layout), hq,
+        qp, qt, qh, op, ot, oh, _ptr(pc.dev_status, torch.int32, (1,), "dev_status"),
+        _stream(stream)))
+    return pc
+
+
+def ebd_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.Tensor,
+                   max_new: int, window: int = 0, mask=None, positions=None, dev_status=None,
+                   stream=None):
+    """(mask [T, W] int32, positions [T] int32) of drafted trees from the parents [T] (int32)
+    of their tokens: bit j of a token's row, W = ceil(max_new / 32) words, is set where it
+    sees new token j of its sequence."""
+    if parents.dim() != 1 or seq_len.dim() != 1:
+        raise ValueError("parents must be [T] and seq_len [B]")
+    T, B, words, i32 = parents.shape[0], seq_len.shape[0], -(-int(max_new) // 32), torch.int32
+    _here(parents, stream, "parents")
+    if mask is None:
+        mask = _result((T, words), i32, parents.device, stream)
+    if positions is None:
+        positions = _result((T,), i32, parents.device, stream)
+    _check("ebd_tree_masks", lib().ebd_tree_masks(
+        B, T, int(max_new), _ptr(parents, i32, name="parents"),
+        _ptr(cu_new, i32, (B + 1,), "cu_new"), _ptr(seq_len, i32, name="seq_len"), int(window),
+        _ptr(mask, i32, (T, words), "mask"), words, _ptr(positions, i32, (T,), "positions"),
+        _ptr(dev_status, i32, (1,), "dev_status"), _stream(stream)))
+    return mask, positions
+
+
+def ebd_paged_tree_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, max_new: int,
+                             mask: torch.Tensor, positions=None, y=None, lse=None, scale=None,
+                             window: int = 0, workspace=None, stream=None):
+    """ebd_paged_attention of drafted trees: a new token sees the earlier positions and
+    those new tokens of its sequence whose bits its row of mask [T, W] (int32,
+    ebd_tree_masks) has; positions [T] are needed with a window."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T, Hq, d]")
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    T, hq, d = q.shape[0], q.shape[1], c.head_dim
+    _here(q, stream, "q")
+    qp, qt, qh = _rows(q, dt, T, hq, d, "q")
+    if mask.dim() != 2:
+        raise ValueError("mask must be [T, W]")
+    words = mask.shape[1]
+    if y is None:
+        y = _result((T, hq, d), dt, q.device, stream)
+    if lse is None:
+        lse = _result((T, hq), torch.float32, q.device, stream)
+    L = lib()
+    ref = ctypes.byref(c)
+    ws, wsb = _workspace(L.ebd_paged_attention_workspace_bytes(ref, hq, int(max_new)), q.device,
+                         workspace, stream)
+    _check("ebd_paged_tree_attention", L.ebd_paged_tree_attention(
+        ref, T, int(max_new), hq, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"), qp, qt, qh,
+        d ** -0.5 if scale is None else float(scale), int(window),
+        _ptr(mask, torch.int32, (T, words), "mask"), words,
+        _ptr(positions, torch.int32, (T,), "positions"), _ptr(y, dt, (T, hq, d), "y"),
+        _ptr(lse, torch.float32, (T, hq), "lse"),
+        _ptr(pc.dev_status, torch.int32, (1,), "dev_status"), ws, wsb, _stream(stream)))
+    return y, lse
+
+
+def ebd_paged_keep(pc: PagedCache, cu_new: torch.Tensor, path: torch.Tensor,
+                   n_accepted: torch.Tensor, seq_len_out=None, K_layers=None, V_layers=None,
+                   stream=None) -> torch.Tensor:
+    """Move the cached rows of each tree's accepted path (path [B, max_path] int32, rising
+    numbers of new tokens; n_accepted [B]) to the places behind the tree's beginning,
+    and return the new lengths [B].  K_layers, V_layers [L, n_pages, Hkv, page_size, d]:
+    the pools of all layers, pc's among them as the first, moved in the same launch."""
+    c = _paged(pc)
+    dt = pc.K_pages.dtype
+    _here(pc.K_pages, stream, "K_pages")
+    layers, stride = 1, 0
+    if (K_layers is None) != (V_layers is None):
+        raise ValueError("K_layers and V_layers come together")
+    if K_layers is not None:
+        shape = pc.K_pages.shape
+        for name, t, first in (("K_layers", K_layers, pc.K_pages), ("V_layers", V_layers,
+                                                                    pc.V_pages)):
+            if t.dtype != dt:
+                raise TypeError(f"{name} has dtype {t.dtype}, expected {dt}")
+            if t.dim() != 5 or t.shape[1:] != shape or t.stride()[1:] != first.stride():
+                raise ValueError(f"{name} must be [L, n_pages, Hkv, page_size, d] with the "
+                                 "strides of the cache's pools")
+            if t.data_ptr() != first.data_ptr():
+                raise ValueError(f"the cache's pool must be the first of {name}")
+        layers, stride = K_layers.shape[0], K_layers.stride(0)
+        if V_layers.shape[0] != layers or V_layers.stride(0) != stride:
+            raise ValueError("K_layers and V_layers must have one shape and one layer stride")
+    if path.dim() != 2:
+        raise ValueError("path must be [B, max_path]")
+    if seq_len_out is None:
+        seq_len_out = _result((c.batch,), torch.int32, pc.seq_len.device, stream)
+    B, i32 = c.batch, torch.int32
+    _check("ebd_paged_keep", lib().ebd_paged_keep(
+        ctypes.byref(c), layers, stride, _ptr(cu_new, i32, (B + 1,), "cu_new"),
+        _ptr(path, i32, (B, path.shape[1]), "path"), path.shape[1],
+        _ptr(n_accepted, i32, (B,), "n_accepted"), _ptr(seq_len_out, i32, (B,), "seq_len_out"),
+        _ptr(pc.dev_status, i32, (1,), "dev_status"), _stream(stream)))
+    return seq_len_out
