@@ -2,7 +2,9 @@
 
 Each CUDA translation unit is compiled for sm_103a in parallel, then linked
 into ``paper_2607_21475_gb300/_build/libebd.so``.  A content hash of the
-sources and flags skips the build when nothing changed.
+sources and flags skips the build when nothing changed.  The marshalling of the serving
+calls (csrc/binding.cpp) is a Python extension beside it, ``_build/ebd_call.so``,
+compiled by g++ against the headers of the torch that is installed.
 """
 from __future__ import annotations
 
@@ -11,6 +13,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -19,6 +22,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(BUILD, "libebd.so")
+CALL = os.path.join(BUILD, "ebd_call.so")
+BINDING = os.path.join(CSRC, "binding.cpp")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--use_fast_math",
@@ -36,9 +41,39 @@ def _sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
+def _torch_root() -> str:
+    from importlib.util import find_spec
+    spec = find_spec("torch")
+    if spec is None or not spec.origin:
+        raise RuntimeError("torch not found; the binding is compiled against its headers")
+    return os.path.dirname(spec.origin)
+
+
+def _compile_binding() -> None:
+    """The extension of csrc/binding.cpp, for this interpreter and this torch."""
+    root, nvcc = _torch_root(), _nvcc()
+    cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
+    tmp = CALL + ".tmp"
+    include = [os.path.join(root, "include"),
+               os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    lib = os.path.join(root, "lib")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+           *[x for d in include for x in ("-isystem", d)], BINDING, "-o", tmp, "-L", lib,
+           "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
+           f"-Wl,-rpath,{lib}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"the binding failed to compile:\n{r.stderr[-4000:]}")
+    os.replace(tmp, CALL)
+
+
 def _digest(extra_flags) -> str:
     h = hashlib.sha256()
-    files = _sources() + sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
+    # the binding is for one interpreter and one torch
+    h.update((sys.version + _torch_root()).encode())
+    version = os.path.join(_torch_root(), "version.py")
+    files = [BINDING] + ([version] if os.path.exists(version) else []) + _sources() + sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
                                 if f.endswith((".cuh", ".h")))
     files.append(os.path.join(INCLUDE, "ebd.h"))
     for f in files:
@@ -54,7 +89,7 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     os.makedirs(BUILD, exist_ok=True)
     stamp = os.path.join(BUILD, "libebd.stamp")
     dig = _digest(extra_flags)
-    if not force and os.path.exists(LIB) and os.path.exists(stamp):
+    if not force and os.path.exists(LIB) and os.path.exists(CALL) and os.path.exists(stamp):
         with open(stamp) as fh:
             if fh.read().strip() == dig:
                 return LIB
@@ -72,8 +107,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
             sys.stderr.write(r.stderr)
         return obj
 
-    with ThreadPoolExecutor(max_workers=min(len(srcs), os.cpu_count() or 4)) as ex:
+    with ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
+        binding = ex.submit(_compile_binding)
         list(ex.map(compile_one, zip(srcs, objs)))
+        binding.result()
     tmp = LIB + ".tmp"
     cmd = [nvcc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

@@ -18,11 +18,14 @@
 #include <cuda_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "decode_tile.cuh"
 #include "internal.h"
 #include "paged.cuh"
 #include "paged_attn.cuh"
+#include "ptx.cuh"
 #include "rotary.cuh"
 
 namespace ebd {
@@ -65,42 +68,125 @@ struct NormArgs {
   int32_t* dev_status;
 };
 
-// The weight of channels c .. c + VEC - 1 of a head.
+// Packed float32 pairs: two operations to an instruction (the passes would be bound by
+// their instructions otherwise).
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// A lane's part of a row, 2 VEC channels: lo[i] and hi[i] turn together.  Half layout: the
+// unit's first and second chunk; pairs layout: the even and odd channels of both.
 template <int VEC>
-__device__ __forceinline__ void load_weight(const NormWeight& w, int h, int c, float* out) {
-  const long long at = h * w.hs + c;
-  if (w.f32) {
-    const float* p = (const float*)w.p + at;
-    if (VEC % 4 == 0 && w.wide) {
+struct Part {
+  float lo[VEC], hi[VEC];
+};
+
+template <typename T, int VEC, bool PAIRS>
+__device__ __forceinline__ void widen(const Piece<T, VEC>& r, Part<VEC>& x) {
 #pragma unroll
-      for (int i = 0; i + 3 < VEC; i += 4) {
-        const float4 f = __ldg(reinterpret_cast<const float4*>(p + i));
-        out[i] = f.x, out[i + 1] = f.y, out[i + 2] = f.z, out[i + 3] = f.w;
-      }
+  for (int i = 0; i < VEC; ++i) {
+    if (!PAIRS) {
+      x.lo[i] = to_f32(r.a.e[i]);
+      x.hi[i] = to_f32(r.b.e[i]);
     } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) out[i] = __ldg(p + i);
+      const Chunk<T, VEC>& c = i < VEC / 2 ? r.a : r.b;
+      x.lo[i] = to_f32(c.e[2 * i % VEC]);
+      x.hi[i] = to_f32(c.e[2 * i % VEC + 1]);
     }
+  }
+}
+// Two neighbouring elements from float32.
+__device__ __forceinline__ void from_f32x2(float x, float y, float& a, float& b) { a = x, b = y; }
+__device__ __forceinline__ void from_f32x2(float x, float y, __nv_bfloat16& a, __nv_bfloat16& b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+  a = v.x;
+  b = v.y;
+}
+template <typename T, int VEC, bool PAIRS>
+__device__ __forceinline__ void narrow(const Part<VEC>& x, Piece<T, VEC>& r) {
+  if constexpr (VEC == 1) {
+    from_f32(x.lo[0], r.a.e[0]);
+    from_f32(x.hi[0], r.b.e[0]);
   } else {
-    const __nv_bfloat16* p = (const __nv_bfloat16*)w.p + at;
-    if (VEC % 4 == 0 && w.wide) {
 #pragma unroll
-      for (int i = 0; i + 3 < VEC; i += 4) {
-        const uint2 f = __ldg(reinterpret_cast<const uint2*>(p + i));
-        out[i] = bf16_lo(f.x), out[i + 1] = bf16_hi(f.x);
-        out[i + 2] = bf16_lo(f.y), out[i + 3] = bf16_hi(f.y);
+    for (int i = 0; i < VEC; i += 2) {
+      if (!PAIRS) {
+        from_f32x2(x.lo[i], x.lo[i + 1], r.a.e[i], r.a.e[i + 1]);
+        from_f32x2(x.hi[i], x.hi[i + 1], r.b.e[i], r.b.e[i + 1]);
+      } else {
+        from_f32x2(x.lo[i / 2], x.hi[i / 2], r.a.e[i], r.a.e[i + 1]);
+        from_f32x2(x.lo[(VEC + i) / 2], x.hi[(VEC + i) / 2], r.b.e[i], r.b.e[i + 1]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) out[i] = __bfloat162float(p[i]);
     }
   }
 }
 
-// Cosines and sines of unit u's pairs at row tpos of the table.
+// f(i, lo pair i, hi pair i) for every two of a part's pairs of channels, packed; VEC = 1:
+// one in a pair's first half.
+template <int VEC, typename F>
+__device__ __forceinline__ void each_two(Part<VEC>& x, F f) {
+  if constexpr (VEC == 1) {
+    float2 lo = make_float2(x.lo[0], 0.f), hi = make_float2(x.hi[0], 0.f);
+    f(0, lo, hi);
+    x.lo[0] = lo.x;
+    x.hi[0] = hi.x;
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 2) {
+      float2 lo = make_float2(x.lo[i], x.lo[i + 1]), hi = make_float2(x.hi[i], x.hi[i + 1]);
+      f(i, lo, hi);
+      x.lo[i] = lo.x, x.lo[i + 1] = lo.y;
+      x.hi[i] = hi.x, x.hi[i + 1] = hi.y;
+    }
+  }
+}
+template <int VEC>
+__device__ __forceinline__ float2 two(const float (&v)[VEC], int i) {
+  if constexpr (VEC == 1) return make_float2(v[0], 0.f);
+  else return make_float2(v[i], v[i + 1]);
+}
+
+// Cosines and sines of a unit's pairs.
+template <int VEC>
+struct Angles {
+  float c[VEC], s[VEC];
+};
+
+// A lane's place in a row: U units, the j-th of them with chunks at channels c1, c2.
+template <int VEC, bool PAIRS, int U>
+struct Place {
+  int c1[U], c2[U];  // -1: the row has none
+  __device__ __forceinline__ Place(const NormArgs& a, int sub) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      c1[j] = c2[j] = -1;
+      if (sub + a.lanes * j < a.units) unit_channels<VEC, PAIRS>(a, sub + a.lanes * j, c1[j], c2[j]);
+    }
+  }
+};
+
+// The unit's pairs that turn: none, the first chunk's (pairs layout), all.
 template <int VEC, bool PAIRS>
-__device__ __forceinline__ void load_unit_angles(const NormArgs& a, int tpos, int u,
-                                                 float (&cs)[VEC], float (&sn)[VEC]) {
+__device__ __forceinline__ void turn(const NormArgs& a, int u, int c2, const Angles<VEC>& t,
+                                     float sign, Part<VEC>& x) {
+  if (u >= a.rot_units) return;
+  const bool all = !PAIRS || (c2 >= 0 && c2 < a.rot);
+  each_two<VEC>(x, [&](int i, float2& lo, float2& hi) {
+    float2 c = two(t.c, i), s = two(t.s, i);
+    s.x *= sign, s.y *= sign;
+    const float2 ns = make_float2(-s.x, -s.y);
+    // VEC = 2 in the pairs layout: one pair of each chunk
+    const float2 lo1 = __ffma2_rn(lo, c, __fmul2_rn(hi, ns));
+    const float2 hi1 = __ffma2_rn(lo, s, __fmul2_rn(hi, c));
+    if (PAIRS && VEC == 2) {
+      lo.x = lo1.x, hi.x = hi1.x;
+      if (all) lo.y = lo1.y, hi.y = hi1.y;
+    } else if (all || i < VEC / 2) {
+      lo = lo1, hi = hi1;
+    }
+  });
+}
+
+template <int VEC, bool PAIRS>
+__device__ __forceinline__ void load_angles(const NormArgs& a, int tpos, int u, Angles<VEC>& t) {
   if (u >= a.rot_units) return;
   const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * VEC;
   const int n = PAIRS ? min(VEC, a.rot / 2 - u * VEC) : VEC;
@@ -109,131 +195,192 @@ __device__ __forceinline__ void load_unit_angles(const NormArgs& a, int tpos, in
     for (int i = 0; i + 1 < VEC; i += 2) {
       if (PAIRS && i >= n) break;
       const float4 f = __ldg(reinterpret_cast<const float4*>(row + i));
-      cs[i] = f.x;
-      sn[i] = f.y;
-      cs[i + 1] = f.z;
-      sn[i + 1] = f.w;
+      t.c[i] = f.x, t.s[i] = f.y;
+      t.c[i + 1] = f.z, t.s[i + 1] = f.w;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) {
       if (PAIRS && i >= n) break;
       const float2 f = __ldg(row + i);
-      cs[i] = f.x;
-      sn[i] = f.y;
+      t.c[i] = f.x, t.s[i] = f.y;
     }
   }
 }
 
-// Turns the pairs of a unit's two chunks (p: the first, q: the second), rot: the first
-// channel that stays, c2 the second chunk's channel.
-template <int VEC, bool PAIRS>
-__device__ __forceinline__ void turn_unit(float (&p)[VEC], float (&q)[VEC], const float (&cs)[VEC],
-                                          const float (&sn)[VEC], float sign, int c2, int rot) {
-  auto turn = [&](float& e0, float& e1, int i) {
-    const float a = e0, b = e1, s = sn[i] * sign;
-    e0 = a * cs[i] - b * s;
-    e1 = b * cs[i] + a * s;
+// The weight of a unit's channels in a head.
+template <typename T, int VEC, bool PAIRS>
+__device__ __forceinline__ void load_weight(const NormWeight& w, int h, int c1, int c2,
+                                            Part<VEC>& out) {
+  if (c1 < 0) return;
+  auto load = [&](auto piece) {
+    using P = decltype(piece);
+    using Elem = std::remove_reference_t<decltype(piece.a.e[0])>;
+    const Elem* p = (const Elem*)w.p + h * w.hs;
+    auto chunk = [&](int c, auto& to) {
+      constexpr int kBytes = VEC * sizeof(Elem);
+      if (kBytes % 16 == 0 && w.wide) {
+#pragma unroll
+        for (int i = 0; i < kBytes / 16; ++i)
+          reinterpret_cast<uint4*>(&to)[i] = __ldg(reinterpret_cast<const uint4*>(p + c) + i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) to.e[i] = p[c + i];
+      }
+    };
+    P r = piece;
+    chunk(c1, r.a);
+    if (c2 >= 0) chunk(c2, r.b);
+    widen<Elem, VEC, PAIRS>(r, out);
   };
-  if (PAIRS) {
-#pragma unroll
-    for (int i = 0; i < VEC / 2; ++i) turn(p[2 * i], p[2 * i + 1], i);
-    if (c2 >= 0 && c2 < rot) {
-#pragma unroll
-      for (int i = 0; i < VEC / 2; ++i) turn(q[2 * i], q[2 * i + 1], VEC / 2 + i);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) turn(p[i], q[i], i);
-  }
+  if (w.f32) load(Piece<float, VEC>{});
+  else load(Piece<__nv_bfloat16, VEC>{});
 }
 
 // Sum over the L lanes that share a row.
 __device__ __forceinline__ float row_sum(float v, int lanes) {
-  for (int o = 1; o < lanes; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
 // 2^-64: rows whose sum of squares leaves float32's range are scaled by it first.
 constexpr float kRowScale = 5.421010862427522e-20f;
 
-template <typename T, int VEC>
-__device__ __forceinline__ void scale_chunk(Chunk<T, VEC>& c, float f) {
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) from_f32(to_f32(c.e[i]) * f, c.e[i]);
-}
+// Rows on their way to a warp, N of them to a step (the backward pass: x and dy): kAhead
+// steps are asked for ahead.  Wide chunks wait in shared memory, where their number costs
+// no registers; every lane reads back what it asked for, so nothing is synchronised.
+// Elements and pairs wait in registers, one step ahead.
+template <typename T, int VEC, int U, int N>
+struct RowRing {
+  static constexpr bool kShared = VEC * sizeof(T) == 16;
+  static constexpr int kStages = U == 1 ? 4 : 2;
+  static constexpr int kAhead = kShared ? kStages - 1 : 1;
+  static constexpr int kBytes = kShared ? kNormWarps * kStages * N * U * 2 * 512 : 0;
+  static constexpr int kStageBytes = N * U * 2 * 512;
+  unsigned char* base;     // this lane's part of the warp's first stage
+  int in = 0, out = 0;     // stages' offsets
+  Piece<T, VEC> next[kShared ? 1 : 2][N][U];  // (by elements)
 
-template <typename T, int VEC>
-__device__ __forceinline__ void widen(const Chunk<T, VEC>& c, float (&x)[VEC]) {
+  // smem: kBytes for the block
+  __device__ __forceinline__ explicit RowRing(void* smem)
+      : base((unsigned char*)smem + (threadIdx.x >> 5) * kStages * kStageBytes +
+             (threadIdx.x & 31) * 16) {}
+  // src: the rows; null: none
+  template <typename P>
+  __device__ __forceinline__ void fetch(const P& place, const T* const (&src)[N]) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) x[i] = to_f32(c.e[i]);
-}
-template <typename T, int VEC>
-__device__ __forceinline__ void narrow(const float (&x)[VEC], Chunk<T, VEC>& c) {
+    for (int n = 0; n < N; ++n) {
 #pragma unroll
-  for (int i = 0; i < VEC; ++i) from_f32(x[i], c.e[i]);
-}
+      for (int j = 0; j < U; ++j) {
+        if constexpr (kShared) {
+          unsigned char* to = base + in + (n * U + j) * 1024;
+          if (src[n] != nullptr && place.c1[j] >= 0) cp_async16(to, src[n] + place.c1[j]);
+          if (src[n] != nullptr && place.c2[j] >= 0) cp_async16(to + 512, src[n] + place.c2[j]);
+        } else {
+          next[0][n][j] = next[1][n][j];
+          if (src[n] == nullptr) continue;
+          if (place.c1[j] >= 0) load_chunk<T, VEC>(src[n] + place.c1[j], next[1][n][j].a);
+          if (place.c2[j] >= 0) load_chunk<T, VEC>(src[n] + place.c2[j], next[1][n][j].b);
+        }
+      }
+    }
+    if constexpr (kShared) {
+      cp_async_commit();
+      in = in + kStageBytes == kStages * kStageBytes ? 0 : in + kStageBytes;
+    }
+  }
+  // The step fetched kAhead fetches ago; zeros where a row has no chunk.
+  template <typename P>
+  __device__ __forceinline__ void take(const P& place, Piece<T, VEC> (&r)[N][U]) {
+    if constexpr (kShared) cp_async_wait<kAhead>();
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        if constexpr (kShared) {
+          const unsigned char* from = base + out + (n * U + j) * 1024;
+          uint4 v = *reinterpret_cast<const uint4*>(from);
+          uint4 w = *reinterpret_cast<const uint4*>(from + 512);
+          if (place.c1[j] < 0) v = make_uint4(0, 0, 0, 0);
+          if (place.c2[j] < 0) w = make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(&r[n][j].a) = v;
+          *reinterpret_cast<uint4*>(&r[n][j].b) = w;
+        } else {
+          r[n][j] = next[0][n][j];
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            if (place.c1[j] < 0) from_f32(0.f, r[n][j].a.e[i]);
+            if (place.c2[j] < 0) from_f32(0.f, r[n][j].b.e[i]);
+          }
+        }
+      }
+    if constexpr (kShared) out = out + kStageBytes == kStages * kStageBytes ? 0 : out + kStageBytes;
+  }
+  // Forgets the steps that were asked for past the last one.
+  __device__ __forceinline__ void restart() {
+    if constexpr (kShared) out = in;
+  }
+  __device__ __forceinline__ void drain() {
+    if constexpr (kShared) cp_async_wait<0>();
+  }
+};
 
 template <typename T, int VEC, bool PAIRS, bool APPEND, int U>
 __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, VEC))
     norm_rotary_kernel(const NormArgs a) {
+  using Ring = RowRing<T, VEC, U, 1>;
+  __shared__ uint4 ring_s[Ring::kBytes / 16 + 1];
   const int lane = threadIdx.x & 31;
   const long long w = (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5);
   const int t = a.parts == 1 ? (int)w : (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
   if (t >= a.n_tokens) return;
-  const int L = a.lanes, sub = lane & (L - 1), per_warp = 32 / L;
+  const int L = a.lanes, sub = lane & (L - 1), per_warp = 32 / L, g = lane / L;
   const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
   const int step = per_warp * a.parts;
   int hb = part * per_warp;  // first head of the warp's step
-  const int g = lane / L;
+  const Place<VEC, PAIRS, U> place(a, sub);
   const T* xp = (const T*)a.x.p + t * a.x.ts;
   const T* kp = (const T*)a.k.p + t * a.k.ts;
   const T* vp = (const T*)a.v.p + t * a.v.ts;
-  auto load = [&](int h, Piece<T, VEC> (&r)[U]) {
-    if (h >= heads) return;
-    const T* src = !APPEND || h < a.n_x  ? xp + h * a.x.hs
-                   : h < a.n_x + a.n_kv ? kp + (h - a.n_x) * a.k.hs
-                                        : vp + (h - a.n_x - a.n_kv) * a.v.hs;
-#pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int u = sub + L * j;
-      if (u >= a.units) break;
-      int c1, c2;
-      unit_channels<VEC, PAIRS>(a, u, c1, c2);
-      load_chunk<T, VEC>(src + c1, r[j].a);
-      if (c2 >= 0) load_chunk<T, VEC>(src + c2, r[j].b);
-    }
+  Ring ring(ring_s);
+  int hf = hb + g;  // the next head to fetch
+  auto fetch = [&]() {
+    const T* p = nullptr;
+    if (hf < heads)
+      p = !APPEND || hf < a.n_x  ? xp + hf * a.x.hs
+          : hf < a.n_x + a.n_kv ? kp + (hf - a.n_x) * a.k.hs
+                                : vp + (hf - a.n_x - a.n_kv) * a.v.hs;
+    const T* const src[1] = {p};
+    ring.fetch(place, src);
+    hf += step;
   };
-  Piece<T, VEC> r0[U], r1[U];
-  load(hb + g, r0);
-  load(hb + g + step, r1);
+#pragma unroll
+  for (int k = 0; k < Ring::kAhead; ++k) fetch();
 
   // 0: x, 1: keys, 2: values
   auto set_of = [&](int h) { return !APPEND || h < a.n_x ? 0 : h < a.n_x + a.n_kv ? 1 : 2; };
-  float wt[U][2 * VEC];
+  Part<VEC> wt[U];
   int held = -1;  // the set whose weight is in wt
   auto load_weights = [&](int h, int set) {
     const NormWeight& w = set == 0 ? a.wx : a.wk;
-    if (!w.p || (held == set && w.hs == 0)) return;
+    if (set > 1 || !w.p || (held == set && w.hs == 0)) return;
     held = set;
-    const int head = set == 0 ? h : h - a.n_x;
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int u = sub + L * j;
-      if (u >= a.units) break;
-      int c1, c2;
-      unit_channels<VEC, PAIRS>(a, u, c1, c2);
-      load_weight<VEC>(w, head, c1, &wt[j][0]);
-      if (c2 >= 0) load_weight<VEC>(w, head, c2, &wt[j][VEC]);
-    }
+    for (int j = 0; j < U; ++j)
+      load_weight<T, VEC, PAIRS>(w, set == 0 ? h : h - a.n_x, place.c1[j], place.c2[j], wt[j]);
   };
-  if (hb + g < heads && set_of(hb + g) < 2) load_weights(hb + g, set_of(hb + g));
+  if (hb + g < heads) load_weights(hb + g, set_of(hb + g));
 
   int pos = 0, page = -1;
   long long at = -1;  // the token's row of head 0 in the pools
   if (APPEND && a.slots) {
     const int64_t slot = a.slots[t];
-    if (slot == -1) return;  // no token here
+    if (slot == -1) {  // no token here
+      ring.drain();
+      return;
+    }
     pos = a.positions ? a.positions[t] : 0;
     const int64_t page64 = slot >> a.pv.page_shift;
     if (slot >= 0 && page64 < a.pv.n_pages) {
@@ -251,7 +398,10 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
     none |= t < c0;
     odd |= none | (c_first != 0) | (c_last != a.n_tokens);
     if (lane == 0 && odd) raise_status(a.dev_status, EBD_DEV_RANGE);
-    if (none) return;
+    if (none) {
+      ring.drain();
+      return;
+    }
     pos = len - (min(c1, a.n_tokens) - t);
     page = page_of(a.pv, b, pos);
     if (page >= 0) at = slot_offset(a.pv, page, 0, pos);
@@ -260,94 +410,73 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
     pos = a.positions[t];
   }
   const int tpos = a.table ? min(max(pos, 0), a.n_pos - 1) : 0;
-  float cs[U][VEC], sn[U][VEC];
+  Angles<VEC> angles[U];
 #pragma unroll
-  for (int j = 0; j < U; ++j) load_unit_angles<VEC, PAIRS>(a, tpos, sub + L * j, cs[j], sn[j]);
+  for (int j = 0; j < U; ++j) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
   if (lane == 0 && ((APPEND && page < 0) || (a.table && tpos != pos)))
     raise_status(a.dev_status, EBD_DEV_RANGE);
   T* yp = (T*)a.y.p + t * a.y.ts;
 
-  // normalises, turns and stores one row's pieces; whole warp
-  auto store = [&](int h, Piece<T, VEC> (&r)[U]) {
+  for (; hb < heads; hb += step) {
+    fetch();
+    Piece<T, VEC> r[1][U];
+    ring.take(place, r);
+    const int h = hb + g, set = set_of(h);
     const bool live = h < heads;
-    const int set = set_of(h);
-    const bool normed = live && set < 2 && (set == 0 ? a.wx.p : a.wk.p) != nullptr;
+    Part<VEC> x[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) widen<T, VEC, PAIRS>(r[0][j], x[j]);
     auto squares = [&]() {
-      float ss = 0.f;
-      if (normed) {
+      float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-          const int u = sub + L * j;
-          if (u >= a.units) break;
-          int c1, c2;
-          unit_channels<VEC, PAIRS>(a, u, c1, c2);
-          float x[VEC];
-          widen(r[j].a, x);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
-          if (c2 >= 0) {
-            widen(r[j].b, x);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
-          }
-        }
-      }
-      return row_sum(ss, L);
+      for (int j = 0; j < U; ++j)
+        each_two<VEC>(x[j], [&](int, float2& lo, float2& hi) {
+          s0 = __ffma2_rn(lo, lo, s0);
+          s1 = __ffma2_rn(hi, hi, s1);
+        });
+      const float2 s = __fadd2_rn(s0, s1);
+      return row_sum(live ? s.x + s.y : 0.f, L);
     };
     float ss = squares(), eps = a.eps;
-    if (__any_sync(0xffffffffu, !(ss < INFINITY))) {
-      if (!(ss < INFINITY)) {
+    const bool normed = live && set < 2 && (set == 0 ? a.wx.p : a.wk.p) != nullptr;
+    if (__any_sync(0xffffffffu, normed && !(ss < INFINITY))) {
+      if (normed && !(ss < INFINITY)) {
         eps = 0.f;  // below the sum's rounding
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-          scale_chunk(r[j].a, kRowScale);
-          scale_chunk(r[j].b, kRowScale);
-        }
+        for (int j = 0; j < U; ++j)
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
       }
       ss = squares();
     }
-    if (!live) return;
-    const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
-    if (normed) load_weights(h, set);
+    if (!live) continue;
     T* dst;
     if (!APPEND || set == 0) {
       dst = yp + h * a.y.hs;
     } else {
-      if (at < 0) return;
+      if (at < 0) continue;
       const int kh = h - a.n_x - (set == 2 ? a.n_kv : 0);
       dst = (T*)(set == 2 ? a.V_pages : a.K_pages) + at + kh * a.pv.head_stride;
     }
+    if (normed) {
+      load_weights(h, set);
+      const float2 inv = both(__frsqrt_rn(fmaf(ss, a.inv_d, eps)));
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
+          lo = __fmul2_rn(lo, __fmul2_rn(two(wt[j].lo, i), inv));
+          hi = __fmul2_rn(hi, __fmul2_rn(two(wt[j].hi, i), inv));
+        });
+    }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      const int u = sub + L * j;
-      if (u >= a.units) break;
-      int c1, c2;
-      unit_channels<VEC, PAIRS>(a, u, c1, c2);
       if (set < 2) {
-        float p[VEC], q[VEC];
-        widen(r[j].a, p);
-        widen(r[j].b, q);
-        if (normed) {
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            p[i] *= inv * wt[j][i];
-            q[i] *= inv * wt[j][VEC + i];
-          }
-        }
-        if (u < a.rot_units) turn_unit<VEC, PAIRS>(p, q, cs[j], sn[j], 1.f, c2, a.rot);
-        narrow(p, r[j].a);
-        narrow(q, r[j].b);
+        turn<VEC, PAIRS>(a, sub + L * j, place.c2[j], angles[j], 1.f, x[j]);
+        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
       }
-      store_chunk<T, VEC>(dst + c1, r[j].a);
-      if (c2 >= 0) store_chunk<T, VEC>(dst + c2, r[j].b);
+      if (place.c1[j] >= 0) store_chunk<T, VEC>(dst + place.c1[j], r[0][j].a);
+      if (place.c2[j] >= 0) store_chunk<T, VEC>(dst + place.c2[j], r[0][j].b);
     }
-  };
-  for (; hb < heads; hb += 2 * step) {
-    store(hb + g, r0);
-    load(hb + g + 2 * step, r0);
-    if (hb + step >= heads) break;
-    store(hb + g + step, r1);
-    load(hb + g + 3 * step, r1);
   }
 }
 
@@ -357,29 +486,24 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
 template <typename T, int VEC, bool PAIRS, int U, bool PER_HEAD>
 __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, U, VEC))
     norm_backward_kernel(const NormArgs a, float* __restrict__ partial) {
-  extern __shared__ float red[];  // [warps][units of all lanes][2 VEC]
+  extern __shared__ __align__(16) unsigned char smem[];  // the rows' ring; then, in its place:
+  float* red = reinterpret_cast<float*>(smem);           // [warps][units of all lanes][2 VEC]
+  using Ring = RowRing<T, VEC, U, 2>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int L = a.lanes, sub = lane & (L - 1), per_warp = 32 / L, g = lane / L;
   const long long items =
       PER_HEAD ? (a.n_tokens + per_warp - 1) / per_warp : (long long)a.n_tokens * a.parts;
   const int step = per_warp * a.parts;
-
-  float wt[U][2 * VEC], acc[U][2 * VEC];
-  int ch1[U], ch2[U];
+  const Place<VEC, PAIRS, U> place(a, sub);
+  Part<VEC> wt[U], acc[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
-    const int u = sub + L * j;
-    ch1[j] = ch2[j] = -1;
-    if (u < a.units) {
-      unit_channels<VEC, PAIRS>(a, u, ch1[j], ch2[j]);
-      const int head = PER_HEAD ? blockIdx.y : 0;
-      load_weight<VEC>(a.wx, head, ch1[j], &wt[j][0]);
-      if (ch2[j] >= 0) load_weight<VEC>(a.wx, head, ch2[j], &wt[j][VEC]);
-    }
 #pragma unroll
-    for (int i = 0; i < 2 * VEC; ++i) acc[j][i] = 0.f;
+    for (int i = 0; i < VEC; ++i) wt[j].lo[i] = wt[j].hi[i] = acc[j].lo[i] = acc[j].hi[i] = 0.f;
+    load_weight<T, VEC, PAIRS>(a.wx, PER_HEAD ? blockIdx.y : 0, place.c1[j], place.c2[j], wt[j]);
   }
 
+  Ring ring(smem);
   for (long long item = (long long)blockIdx.x * kNormWarps + warp; item < items;
        item += (long long)gridDim.x * kNormWarps) {
     int t, h;
@@ -392,68 +516,48 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     }
     const int hend = PER_HEAD ? h + 1 : a.n_x;
     const bool there = t < a.n_tokens;
-    auto load = [&](int h, Piece<T, VEC> (&x)[U], Piece<T, VEC> (&dy)[U]) {
-      if (!there || h >= hend) return;
-      const T* xp = (const T*)a.x.p + t * a.x.ts + h * a.x.hs;
-      const T* dp = (const T*)a.dy.p + t * a.dy.ts + h * a.dy.hs;
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        if (ch1[j] < 0) break;
-        load_chunk<T, VEC>(xp + ch1[j], x[j].a);
-        load_chunk<T, VEC>(dp + ch1[j], dy[j].a);
-        if (ch2[j] >= 0) {
-          load_chunk<T, VEC>(xp + ch2[j], x[j].b);
-          load_chunk<T, VEC>(dp + ch2[j], dy[j].b);
-        }
-      }
+    int hf = h;  // the next head to fetch
+    auto fetch = [&]() {
+      const bool live = there && hf < hend;
+      const T* const src[2] = {live ? (const T*)a.x.p + t * a.x.ts + hf * a.x.hs : nullptr,
+                               live ? (const T*)a.dy.p + t * a.dy.ts + hf * a.dy.hs : nullptr};
+      ring.fetch(place, src);
+      hf += step;
     };
-    Piece<T, VEC> x0[U], d0[U], x1[U], d1[U];
-    load(h, x0, d0);
+#pragma unroll
+    for (int k = 0; k < Ring::kAhead; ++k) fetch();
     const int pos = there && a.positions ? a.positions[t] : 0;
     const int tpos = a.table ? min(max(pos, 0), a.n_pos - 1) : 0;
     if (there && sub == 0 && a.table && tpos != pos) raise_status(a.dev_status, EBD_DEV_RANGE);
-    float cs[U][VEC], sn[U][VEC];
+    Angles<VEC> angles[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) load_unit_angles<VEC, PAIRS>(a, tpos, sub + L * j, cs[j], sn[j]);
-    // one row; whole warp
-    auto row = [&](int h, Piece<T, VEC> (&x)[U], Piece<T, VEC> (&dy)[U]) {
+    for (int j = 0; j < U; ++j) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
+    // (h - g: the warp's step is the same in all lanes)
+    for (int h0 = PER_HEAD ? h : h - g; h0 < hend; h0 += step, h += step) {
+      fetch();
+      Piece<T, VEC> r[2][U];
+      ring.take(place, r);
       const bool live = there && h < hend;
-      float u[U][2 * VEC];  // R^T dy
+      Part<VEC> x[U], u[U];  // u: R^T dy
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        if (!live || ch1[j] < 0) break;
-        float p[VEC], q[VEC];
-        widen(dy[j].a, p);
-        widen(dy[j].b, q);
-        if (sub + L * j < a.rot_units)
-          turn_unit<VEC, PAIRS>(p, q, cs[j], sn[j], -1.f, ch2[j], a.rot);
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) u[j][i] = p[i], u[j][VEC + i] = q[i];
+        widen<T, VEC, PAIRS>(r[0][j], x[j]);
+        widen<T, VEC, PAIRS>(r[1][j], u[j]);
+        turn<VEC, PAIRS>(a, sub + L * j, place.c2[j], angles[j], -1.f, u[j]);
       }
       float ss, gx;
       auto sums = [&]() {
-        ss = gx = 0.f;
+        float2 s0 = make_float2(0.f, 0.f), s1 = s0;
 #pragma unroll
-        for (int j = 0; j < U; ++j) {
-          if (!live || ch1[j] < 0) break;
-          float v[VEC];
-          widen(x[j].a, v);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            ss = fmaf(v[i], v[i], ss);
-            gx = fmaf(u[j][i] * wt[j][i], v[i], gx);
-          }
-          if (ch2[j] >= 0) {
-            widen(x[j].b, v);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-              ss = fmaf(v[i], v[i], ss);
-              gx = fmaf(u[j][VEC + i] * wt[j][VEC + i], v[i], gx);
-            }
-          }
-        }
-        ss = row_sum(ss, L);
-        gx = row_sum(gx, L);
+        for (int j = 0; j < U; ++j)
+          each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
+            s0 = __ffma2_rn(lo, lo, s0);
+            s0 = __ffma2_rn(hi, hi, s0);
+            s1 = __ffma2_rn(__fmul2_rn(two(u[j].lo, i), two(wt[j].lo, i)), lo, s1);
+            s1 = __ffma2_rn(__fmul2_rn(two(u[j].hi, i), two(wt[j].hi, i)), hi, s1);
+          });
+        ss = row_sum(live ? s0.x + s0.y : 0.f, L);
+        gx = row_sum(live ? s1.x + s1.y : 0.f, L);
       };
       sums();
       float eps = a.eps, scale = 1.f;
@@ -462,77 +566,63 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
           eps = 0.f;
           scale = kRowScale;
 #pragma unroll
-          for (int j = 0; j < U; ++j) {
-            scale_chunk(x[j].a, kRowScale);
-            scale_chunk(x[j].b, kRowScale);
-          }
+          for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
         }
         sums();
       }
-      if (!live) return;
+      if (!live) continue;
       const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
-      const float mean = gx * inv * a.inv_d;  // of g z
-      const float back = inv * scale;
+      const float2 inv2 = both(inv), mean = both(-gx * inv * a.inv_d);  // -mean of g z
+      const float2 back = both(inv * scale);
       T* out = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
 #pragma unroll
       for (int j = 0; j < U; ++j) {
-        if (ch1[j] < 0) break;
-        float v[VEC];
-        auto half = [&](Chunk<T, VEC>& c, int o) {
-          widen(c, v);
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) {
-            const float z = v[i] * inv, uu = u[j][o + i];
-            acc[j][o + i] = fmaf(uu, z, acc[j][o + i]);
-            v[i] = (uu * wt[j][o + i] - z * mean) * back;
-          }
-          narrow(v, c);
-        };
-        half(x[j].a, 0);
-        store_chunk<T, VEC>(out + ch1[j], x[j].a);
-        if (ch2[j] >= 0) {
-          half(x[j].b, VEC);
-          store_chunk<T, VEC>(out + ch2[j], x[j].b);
-        }
-      }
-    };
-    if (PER_HEAD) {
-      row(h, x0, d0);
-    } else {
-      // (h - g: the warp's step is the same in all lanes)
-      load(h + step, x1, d1);
-      for (; h - g < a.n_x; h += 2 * step) {
-        row(h, x0, d0);
-        load(h + 2 * step, x0, d0);
-        if (h - g + step >= a.n_x) break;
-        row(h + step, x1, d1);
-        load(h + 3 * step, x1, d1);
+        each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
+          const float2 z0 = __fmul2_rn(lo, inv2), z1 = __fmul2_rn(hi, inv2);
+          const float2 u0 = two(u[j].lo, i), u1 = two(u[j].hi, i);
+          const float2 a0 = __ffma2_rn(u0, z0, two(acc[j].lo, i));
+          const float2 a1 = __ffma2_rn(u1, z1, two(acc[j].hi, i));
+          acc[j].lo[i] = a0.x, acc[j].hi[i] = a1.x;
+          if constexpr (VEC > 1) acc[j].lo[i + 1] = a0.y, acc[j].hi[i + 1] = a1.y;
+          lo = __fmul2_rn(__ffma2_rn(z0, mean, __fmul2_rn(u0, two(wt[j].lo, i))), back);
+          hi = __fmul2_rn(__ffma2_rn(z1, mean, __fmul2_rn(u1, two(wt[j].hi, i))), back);
+        });
+        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
+        if (place.c1[j] >= 0) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
+        if (place.c2[j] >= 0) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);
       }
     }
+    ring.restart();
   }
 
   // the block's sum, in a fixed order: lanes, then warps
+  __syncthreads();
   const int wide = L * U * 2 * VEC;
 #pragma unroll
   for (int j = 0; j < U; ++j)
 #pragma unroll
     for (int i = 0; i < 2 * VEC; ++i) {
-      float v = acc[j][i];
+      float v = i < VEC ? acc[j].lo[i % VEC] : acc[j].hi[i % VEC];
       for (int o = L; o < 32; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
       if (g == 0) red[warp * wide + (sub + L * j) * 2 * VEC + i] = v;
     }
   __syncthreads();
   float* dst = partial + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.head_dim;
   for (int k = threadIdx.x; k < wide; k += kNormWarps * 32) {
-    const int u = k / (2 * VEC), i = k - u * 2 * VEC;
+    const int u = k / (2 * VEC), i = k - u * 2 * VEC, e = i % VEC;
     if (u >= a.units) continue;
     int c1, c2;
     unit_channels<VEC, PAIRS>(a, u, c1, c2);
-    if (i >= VEC && c2 < 0) continue;
+    // lo[e] (i < VEC) and hi[e]: chunk and element
+    const bool second = PAIRS ? e >= VEC / 2 : i >= VEC;
+    if (second && c2 < 0) continue;
+    const int c = (second ? c2 : c1) + (PAIRS ? 2 * e % VEC + (i >= VEC) : e);
     float v = 0.f;
 #pragma unroll
     for (int x = 0; x < kNormWarps; ++x) v += red[x * wide + k];
-    dst[i < VEC ? c1 + i : c2 + i - VEC] = v;
+    dst[c] = v;
   }
 }
 
@@ -611,12 +701,15 @@ static ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStr
       per_head ? (a.n_tokens + per_warp - 1) / per_warp : (long long)a.n_tokens * a.parts;
   const int blocks = norm_back_blocks(items, per_head ? a.n_x : 1);
   const int total = (per_head ? a.n_x : 1) * a.head_dim;
-  const int smem = kNormWarps * a.lanes * U * 2 * VEC * 4;
+  const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4, ring = RowRing<T, VEC, U, 2>::kBytes;
+  const int smem = sums > ring ? sums : ring;
   const dim3 grid(blocks, per_head ? a.n_x : 1);
-  if (per_head)
-    norm_backward_kernel<T, VEC, PAIRS, U, true><<<grid, kNormWarps * 32, smem, s>>>(a, bw.partial);
-  else
-    norm_backward_kernel<T, VEC, PAIRS, U, false><<<grid, kNormWarps * 32, smem, s>>>(a, bw.partial);
+  auto kern = per_head ? norm_backward_kernel<T, VEC, PAIRS, U, true>
+                       : norm_backward_kernel<T, VEC, PAIRS, U, false>;
+  if (smem > 48 * 1024 &&
+      cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    return EBD_ERR_CUDA;
+  kern<<<grid, kNormWarps * 32, smem, s>>>(a, bw.partial);
   const ebd_status st = launch_status();
   if (st != EBD_OK) return st;
   return launch_dependent(norm_weight_reduce_kernel, dim3((total + 31) / 32), 256, 0, s,

@@ -14,13 +14,15 @@ is no fallback implementation.
 from __future__ import annotations
 
 import ctypes
+import importlib.machinery
+import importlib.util
 import math
 import os
 from dataclasses import dataclass
 
 import torch
 
-from .build import LIB
+from .build import CALL, LIB
 
 __all__ = [
     "EbdError", "EbdDesign", "EBD_F32", "EBD_BF16", "EBD_RANGE_BOUND", "EBD_RANGE_EXACT",
@@ -203,6 +205,27 @@ def lib():
     return _LIB
 
 
+_CALL = None
+
+
+def _call():
+    """The extension that marshals the serving calls (csrc/binding.cpp), bound to the
+    library once; raises if it has not been built."""
+    global _CALL
+    if _CALL is None:
+        L = lib()
+        if not os.path.exists(CALL):
+            raise RuntimeError(f"{CALL} is not built; run `python -c \"import __graft_entry__ as "
+                               f"g; g.build()\"` (no fallback exists)")
+        loader = importlib.machinery.ExtensionFileLoader("ebd_call", CALL)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("ebd_call", loader))
+        loader.exec_module(m)
+        m.bind({name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value
+                for name in ABI_FUNCTIONS})
+        _CALL = m
+    return _CALL
+
+
 # ----------------------------------------------------------------- helpers
 def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
@@ -242,13 +265,6 @@ def _stream(stream):
     if _raw_stream is not None and torch.cuda.is_initialized():
         return _raw_stream(torch._C._cuda_getDevice())
     return torch.cuda.current_stream().cuda_stream
-
-
-def _here(t, stream, name):
-    """Refuses a tensor of another device than the one that the call launches on."""
-    at = stream.device_index if stream is not None else torch._C._cuda_getDevice()
-    if t.is_cuda and t.device.index != at:
-        raise ValueError(f"{name} is on {t.device}, the call's stream on cuda:{at}")
 
 
 def _check(name, code):
@@ -861,10 +877,7 @@ def ebd_paged_deal(pool: PagePool, pc: PagedCache, n_new: torch.Tensor, n_tokens
     pool.held and pool.n_free, is brought up to date in place unless another output is
     given; pc.block_table and pool.free_pages always are.  A sequence that is not served
     (EBD_DEV_CAPACITY in dev_status) stays as it was and has no new tokens in cu_new."""
-    c = _paged(pc)
-    B, i32 = c.batch, torch.int32
-    dev = pc.seq_len.device
-    _here(pc.seq_len, stream, "seq_len")
+    B, i32, dev = pc.block_table.shape[0], torch.int32, pc.seq_len.device
     if cu_new is None:
         cu_new = _result((B + 1,), i32, dev, stream)
     if positions is None:
@@ -873,48 +886,13 @@ def ebd_paged_deal(pool: PagePool, pc: PagedCache, n_new: torch.Tensor, n_tokens
         slots = _result((n_tokens,), torch.int64, dev, stream)
     if served is None:
         served = _result((B,), i32, dev, stream)
-    held, free = pool.held, pool.n_free
-    _check("ebd_paged_deal", lib().ebd_paged_deal(
-        B, c.page_size, c.n_pages, c.max_blocks, int(n_tokens), int(window),
-        _ptr(n_new, i32, (B,), "n_new"), c.seq_len, _ptr(held, i32, (B, 2), "held"),
-        _ptr(free, i32, (1,), "n_free"), _ptr(pool.free_pages, i32, (c.n_pages,), "free_pages"),
-        c.block_table, _ptr(pc.seq_len if seq_len_out is None else seq_len_out, i32, (B,),
-                            "seq_len_out"),
-        _ptr(held if held_out is None else held_out, i32, (B, 2), "held_out"),
-        _ptr(free if n_free_out is None else n_free_out, i32, (1,), "n_free_out"),
-        _ptr(cu_new, i32, (B + 1,), "cu_new"), _ptr(served, i32, (B,), "served"),
-        _ptr(positions, i32, (n_tokens,), "positions"),
-        _ptr(slots, torch.int64, (n_tokens,), "slots"),
-        _ptr(pc.dev_status, i32, (1,), "dev_status"), _stream(stream)))
+    held, free, n = pool.held, pool.n_free, pc.seq_len
+    _check("ebd_paged_deal", (_CALL or _call()).deal(
+        pool.free_pages, free, held, pc.K_pages, pc.V_pages, pc.block_table, n, pc.dev_status,
+        n_new, n_tokens, window, cu_new, positions, slots, served,
+        n if seq_len_out is None else seq_len_out, held if held_out is None else held_out,
+        free if n_free_out is None else n_free_out, stream))
     return cu_new, positions, slots, served
-
-
-def _norm_weight(w, dtype, heads, d, name):
-    """(address, type code, head stride) of a norm's weight, [d] or [heads, d]."""
-    if not isinstance(w, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if not w.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if w.dtype != torch.float32 and w.dtype != dtype:
-        raise TypeError(f"{name} has dtype {w.dtype}, expected {dtype} or float32")
-    if w.shape != (d,) and w.shape != (heads, d):
-        raise ValueError(f"{name} has shape {tuple(w.shape)}, expected {(d,)} or {(heads, d)}")
-    if d > 1 and w.stride(-1) != 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    hs = w.stride(0) if w.dim() == 2 else 0
-    if w.dim() == 2 and hs < 1:
-        raise ValueError(f"{name} must have a row of its own for every head")
-    return w.data_ptr(), _dtype_code(w), hs
-
-
-def _norm_table(table, positions, n_tokens):
-    """(positions, table, n_pos, rotary_dim) of a norm with or without a rotation."""
-    if table is None:
-        return None, None, 0, 0
-    if positions is None:
-        raise ValueError("a rotation needs positions")
-    tab, n_pos, rot = _rotary_rows(table)
-    return _ptr(positions, torch.int32, (n_tokens,), "positions"), tab, n_pos, rot
 
 
 def ebd_norm_rotary(x: torch.Tensor, weight: torch.Tensor, positions=None, table=None, out=None,
@@ -923,20 +901,10 @@ def ebd_norm_rotary(x: torch.Tensor, weight: torch.Tensor, positions=None, table
     """x [T, H, d] (any token and head strides) divided by each row's root mean square,
     times weight ([d] or [H, d], x's type or float32), and, with a table, turned to
     positions [T] (int32).  out may be x."""
-    if x.dim() != 3:
-        raise ValueError("x must be [T, H, d]")
-    T, H, d = x.shape
-    _here(x, stream, "x")
-    wp, wt, wh = _norm_weight(weight, x.dtype, H, d, "weight")
     if out is None:
-        out = _result((T, H, d), x.dtype, x.device, stream)
-    pos, tab, n_pos, rot = _norm_table(table, positions, T)
-    xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
-    yp, yt, yh = _rows(out, x.dtype, T, H, d, "out")
-    _check("ebd_norm_rotary", lib().ebd_norm_rotary(
-        _dtype_code(x), T, H, d, xp, xt, xh, wp, wt, wh, float(eps), pos, tab, n_pos, rot,
-        int(layout), yp, yt, yh, _ptr(dev_status, torch.int32, (1,), "dev_status"),
-        _stream(stream)))
+        out = _result(x.shape, x.dtype, x.device, stream)
+    _check("ebd_norm_rotary", (_CALL or _call()).norm(x, weight, positions, table, out, layout, eps,
+                                                      dev_status, stream))
     return out
 
 
@@ -951,26 +919,12 @@ def ebd_norm_rotary_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Te
                              dev_status=None, stream=None):
     """Gradients of ebd_norm_rotary at x, given dy: dx [T, H, d] in x's type and dweight,
     float32 in the weight's shape.  dx may be dy or x."""
-    if x.dim() != 3:
-        raise ValueError("x must be [T, H, d]")
-    T, H, d = x.shape
-    _here(x, stream, "x")
-    wp, wt, wh = _norm_weight(weight, x.dtype, H, d, "weight")
     if dx is None:
-        dx = _result((T, H, d), x.dtype, x.device, stream)
+        dx = _result(x.shape, x.dtype, x.device, stream)
     if dweight is None:
         dweight = _result(weight.shape, torch.float32, x.device, stream)
-    pos, tab, n_pos, rot = _norm_table(table, positions, T)
-    xp, xt, xh = _rows(x, x.dtype, T, H, d, "x")
-    gp, gt, gh = _rows(dy, x.dtype, T, H, d, "dy")
-    op, ot, oh = _rows(dx, x.dtype, T, H, d, "dx")
-    L = lib()
-    ws, wsb = _workspace(L.ebd_norm_rotary_backward_workspace_bytes(H, d, 1 if wh else 0),
-                         x.device, workspace, stream)
-    _check("ebd_norm_rotary_backward", L.ebd_norm_rotary_backward(
-        _dtype_code(x), T, H, d, gp, gt, gh, xp, xt, xh, wp, wt, wh, float(eps), pos, tab, n_pos,
-        rot, int(layout), op, ot, oh, _ptr(dweight, torch.float32, weight.shape, "dweight"),
-        _ptr(dev_status, torch.int32, (1,), "dev_status"), ws, wsb, _stream(stream)))
+    _check("ebd_norm_rotary_backward", (_CALL or _call()).norm_backward(
+        dy, x, weight, positions, table, dx, dweight, layout, eps, workspace, dev_status, stream))
     return dx, dweight
 
 
@@ -982,41 +936,9 @@ def ebd_paged_append_norm(pc: PagedCache, k_new: torch.Tensor, v_new: torch.Tens
     ebd_norm_rotary; None: not normalised), tokens placed by cu_new [B + 1] or by their
     slots [T] (int64, ebd_paged_deal; -1: no token).  positions [T]: where each is turned
     to; needed with slots and a table, otherwise a token's place in its sequence."""
-    c = _paged(pc)
-    dt = pc.K_pages.dtype
-    T, H, d = k_new.shape[0], c.n_kv_heads, c.head_dim
-    _here(pc.K_pages, stream, "K_pages")
-    kp, kt, kh = _rows(k_new, dt, T, H, d, "k_new")
-    vp, vt, vh = _rows(v_new, dt, T, H, d, "v_new")
-    if (cu_new is None) == (slots is None):
-        raise ValueError("tokens are placed by cu_new or by slots, one of the two")
-    if table is None:
-        tab, n_pos, rot = None, 0, 0
-    else:
-        tab, n_pos, rot = _rotary_rows(table)
-        if positions is None and cu_new is None:
-            raise ValueError("slots tell no positions: a rotation needs them")
-    hq, qp, qt, qh, op, ot, oh = 0, None, 0, 0, None, 0, 0
-    kw, wt, kwh = (None, EBD_F32, 0) if k_weight is None else _norm_weight(k_weight, dt, H, d,
-                                                                           "k_weight")
-    qw, qwh = None, 0
-    if q is not None:
-        if q.dim() != 3 or q_out is None:
-            raise ValueError("q must be [T, Hq, d] and come with q_out")
-        hq = q.shape[1]
-        qp, qt, qh = _rows(q, dt, T, hq, d, "q")
-        op, ot, oh = _rows(q_out, dt, T, hq, d, "q_out")
-        if q_weight is not None:
-            qw, qwt, qwh = _norm_weight(q_weight, dt, hq, d, "q_weight")
-            if k_weight is not None and qwt != wt:
-                raise TypeError("k_weight and q_weight must have one dtype")
-            wt = qwt
-    _check("ebd_paged_append_norm", lib().ebd_paged_append_norm(
-        ctypes.byref(c), T, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"),
-        _ptr(slots, torch.int64, (T,), "slots"), _ptr(positions, torch.int32, (T,), "positions"),
-        kp, kt, kh, vp, vt, vh, kw, kwh, qw, qwh, wt, float(eps), tab, n_pos, rot, int(layout), hq,
-        qp, qt, qh, op, ot, oh, _ptr(pc.dev_status, torch.int32, (1,), "dev_status"),
-        _stream(stream)))
+    _check("ebd_paged_append_norm", (_CALL or _call()).append_norm(
+        pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len, pc.dev_status, k_new, v_new, k_weight,
+        q, q_weight, q_out, cu_new, slots, positions, table, layout, eps, stream))
     return pc
 
 
@@ -1026,19 +948,13 @@ def ebd_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.T
     """(mask [T, W] int32, positions [T] int32) of drafted trees from the parents [T] (int32)
     of their tokens: bit j of a token's row, W = ceil(max_new / 32) words, is set where it
     sees new token j of its sequence."""
-    if parents.dim() != 1 or seq_len.dim() != 1:
-        raise ValueError("parents must be [T] and seq_len [B]")
-    T, B, words, i32 = parents.shape[0], seq_len.shape[0], -(-int(max_new) // 32), torch.int32
-    _here(parents, stream, "parents")
+    T, i32 = parents.shape[0], torch.int32
     if mask is None:
-        mask = _result((T, words), i32, parents.device, stream)
+        mask = _result((T, -(-int(max_new) // 32)), i32, parents.device, stream)
     if positions is None:
         positions = _result((T,), i32, parents.device, stream)
-    _check("ebd_tree_masks", lib().ebd_tree_masks(
-        B, T, int(max_new), _ptr(parents, i32, name="parents"),
-        _ptr(cu_new, i32, (B + 1,), "cu_new"), _ptr(seq_len, i32, name="seq_len"), int(window),
-        _ptr(mask, i32, (T, words), "mask"), words, _ptr(positions, i32, (T,), "positions"),
-        _ptr(dev_status, i32, (1,), "dev_status"), _stream(stream)))
+    _check("ebd_tree_masks", (_CALL or _call()).tree_masks(
+        parents, cu_new, seq_len, max_new, window, mask, positions, dev_status, stream))
     return mask, positions
 
 
@@ -1048,31 +964,13 @@ def ebd_paged_tree_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tens
     """ebd_paged_attention of drafted trees: a new token sees the earlier positions and
     those new tokens of its sequence whose bits its row of mask [T, W] (int32,
     ebd_tree_masks) has; positions [T] are needed with a window."""
-    if q.dim() != 3:
-        raise ValueError("q must be [T, Hq, d]")
-    c = _paged(pc)
-    dt = pc.K_pages.dtype
-    T, hq, d = q.shape[0], q.shape[1], c.head_dim
-    _here(q, stream, "q")
-    qp, qt, qh = _rows(q, dt, T, hq, d, "q")
-    if mask.dim() != 2:
-        raise ValueError("mask must be [T, W]")
-    words = mask.shape[1]
     if y is None:
-        y = _result((T, hq, d), dt, q.device, stream)
+        y = _result(q.shape, pc.K_pages.dtype, q.device, stream)
     if lse is None:
-        lse = _result((T, hq), torch.float32, q.device, stream)
-    L = lib()
-    ref = ctypes.byref(c)
-    ws, wsb = _workspace(L.ebd_paged_attention_workspace_bytes(ref, hq, int(max_new)), q.device,
-                         workspace, stream)
-    _check("ebd_paged_tree_attention", L.ebd_paged_tree_attention(
-        ref, T, int(max_new), hq, _ptr(cu_new, torch.int32, (c.batch + 1,), "cu_new"), qp, qt, qh,
-        d ** -0.5 if scale is None else float(scale), int(window),
-        _ptr(mask, torch.int32, (T, words), "mask"), words,
-        _ptr(positions, torch.int32, (T,), "positions"), _ptr(y, dt, (T, hq, d), "y"),
-        _ptr(lse, torch.float32, (T, hq), "lse"),
-        _ptr(pc.dev_status, torch.int32, (1,), "dev_status"), ws, wsb, _stream(stream)))
+        lse = _result(q.shape[:2], torch.float32, q.device, stream)
+    _check("ebd_paged_tree_attention", (_CALL or _call()).tree_attention(
+        pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len, pc.dev_status, q, cu_new, max_new,
+        mask, positions, y, lse, scale, window, workspace, stream))
     return y, lse
 
 
@@ -1083,34 +981,9 @@ def ebd_paged_keep(pc: PagedCache, cu_new: torch.Tensor, path: torch.Tensor,
     numbers of new tokens; n_accepted [B]) to the places behind the tree's beginning,
     and return the new lengths [B].  K_layers, V_layers [L, n_pages, Hkv, page_size, d]:
     the pools of all layers, pc's among them as the first, moved in the same launch."""
-    c = _paged(pc)
-    dt = pc.K_pages.dtype
-    _here(pc.K_pages, stream, "K_pages")
-    layers, stride = 1, 0
-    if (K_layers is None) != (V_layers is None):
-        raise ValueError("K_layers and V_layers come together")
-    if K_layers is not None:
-        shape = pc.K_pages.shape
-        for name, t, first in (("K_layers", K_layers, pc.K_pages), ("V_layers", V_layers,
-                                                                    pc.V_pages)):
-            if t.dtype != dt:
-                raise TypeError(f"{name} has dtype {t.dtype}, expected {dt}")
-            if t.dim() != 5 or t.shape[1:] != shape or t.stride()[1:] != first.stride():
-                raise ValueError(f"{name} must be [L, n_pages, Hkv, page_size, d] with the "
-                                 "strides of the cache's pools")
-            if t.data_ptr() != first.data_ptr():
-                raise ValueError(f"the cache's pool must be the first of {name}")
-        layers, stride = K_layers.shape[0], K_layers.stride(0)
-        if V_layers.shape[0] != layers or V_layers.stride(0) != stride:
-            raise ValueError("K_layers and V_layers must have one shape and one layer stride")
-    if path.dim() != 2:
-        raise ValueError("path must be [B, max_path]")
     if seq_len_out is None:
-        seq_len_out = _result((c.batch,), torch.int32, pc.seq_len.device, stream)
-    B, i32 = c.batch, torch.int32
-    _check("ebd_paged_keep", lib().ebd_paged_keep(
-        ctypes.byref(c), layers, stride, _ptr(cu_new, i32, (B + 1,), "cu_new"),
-        _ptr(path, i32, (B, path.shape[1]), "path"), path.shape[1],
-        _ptr(n_accepted, i32, (B,), "n_accepted"), _ptr(seq_len_out, i32, (B,), "seq_len_out"),
-        _ptr(pc.dev_status, i32, (1,), "dev_status"), _stream(stream)))
+        seq_len_out = _result(pc.seq_len.shape, torch.int32, pc.seq_len.device, stream)
+    _check("ebd_paged_keep", (_CALL or _call()).keep(
+        pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len, pc.dev_status, cu_new, path, n_accepted,
+        seq_len_out, K_layers, V_layers, stream))
     return seq_len_out
