@@ -31,7 +31,9 @@
 namespace ebd {
 
 constexpr int kNormWarps = 8;
-constexpr int kNormBlocks = 3, kNormBackBlocks = 2;  // resident blocks of 256 threads
+// resident blocks of 256 threads (prompt of 16k tokens: 4 blocks, with spills, 46 us against
+// 39 with 3; ragged chunks appended: 3 blocks 38.6 us against 37.6 with 2)
+constexpr int kNormBlocks = 3, kAppendNormBlocks = 2, kNormBackBlocks = 2;
 constexpr int kNormMaxDim = 512;
 // (fewer where a lane holds several pairs of a row: its arrays would spill)
 constexpr int norm_blocks(int blocks, int u, int vec) {
@@ -150,25 +152,50 @@ struct Angles {
   float c[VEC], s[VEC];
 };
 
-// A lane's place in a row: U units, the j-th of them with chunks at channels c1, c2.
-template <int VEC, bool PAIRS, int U>
+// A lane's place in a row: U units, the j-th of them with chunks at channels c1, c2 = c1 +
+// gap.  FL > 0: rows of FL lanes, each with one unit of two chunks that turn.
+template <int VEC, bool PAIRS, int U, int FL>
 struct Place {
+  static constexpr bool kFull = FL > 0;
+  int lanes, sub;
   int c1[U], c2[U];  // -1: the row has none
-  __device__ __forceinline__ Place(const NormArgs& a, int sub) {
+  bool turns[U], all[U];  // the unit does; its second chunk too (pairs layout)
+  __device__ __forceinline__ Place(const NormArgs& a, int lane)
+      : lanes(kFull ? FL : a.lanes), sub(lane & (lanes - 1)) {
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      c1[j] = c2[j] = -1;
-      if (sub + a.lanes * j < a.units) unit_channels<VEC, PAIRS>(a, sub + a.lanes * j, c1[j], c2[j]);
+      const int u = sub + lanes * j;
+      if (kFull) {
+        c1[j] = PAIRS ? 2 * VEC * sub : VEC * sub;
+        c2[j] = c1[j] + (PAIRS ? VEC : VEC * FL);
+        turns[j] = all[j] = true;
+      } else {
+        c1[j] = c2[j] = -1;
+        if (u < a.units) unit_channels<VEC, PAIRS>(a, u, c1[j], c2[j]);
+        turns[j] = u < a.rot_units;
+        all[j] = !PAIRS || (c2[j] >= 0 && c2[j] < a.rot);
+      }
     }
+  }
+  __device__ __forceinline__ int per_warp() const { return 32 / lanes; }
+  __device__ __forceinline__ bool first(int j) const { return kFull || c1[j] >= 0; }
+  __device__ __forceinline__ bool second(int j) const { return kFull || c2[j] >= 0; }
+  __device__ __forceinline__ bool turn(int j) const { return kFull || turns[j]; }
+  __device__ __forceinline__ bool turn_all(int j) const { return kFull || all[j]; }
+  // Sum over the lanes that share a row.
+  __device__ __forceinline__ float row_sum(float v) const {
+#pragma unroll
+    for (int o = 1; o < (kFull ? FL : 32); o <<= 1) {
+      const float u = __shfl_xor_sync(0xffffffffu, v, o);
+      if (kFull || o < lanes) v += u;
+    }
+    return v;
   }
 };
 
 // The unit's pairs that turn: none, the first chunk's (pairs layout), all.
 template <int VEC, bool PAIRS>
-__device__ __forceinline__ void turn(const NormArgs& a, int u, int c2, const Angles<VEC>& t,
-                                     float sign, Part<VEC>& x) {
-  if (u >= a.rot_units) return;
-  const bool all = !PAIRS || (c2 >= 0 && c2 < a.rot);
+__device__ __forceinline__ void turn(const Angles<VEC>& t, bool all, float sign, Part<VEC>& x) {
   each_two<VEC>(x, [&](int i, float2& lo, float2& hi) {
     float2 c = two(t.c, i), s = two(t.s, i);
     s.x *= sign, s.y *= sign;
@@ -187,7 +214,6 @@ __device__ __forceinline__ void turn(const NormArgs& a, int u, int c2, const Ang
 
 template <int VEC, bool PAIRS>
 __device__ __forceinline__ void load_angles(const NormArgs& a, int tpos, int u, Angles<VEC>& t) {
-  if (u >= a.rot_units) return;
   const float2* row = a.table + (size_t)tpos * (a.rot / 2) + u * VEC;
   const int n = PAIRS ? min(VEC, a.rot / 2 - u * VEC) : VEC;
   if (VEC % 2 == 0 && a.wide_table) {
@@ -207,6 +233,52 @@ __device__ __forceinline__ void load_angles(const NormArgs& a, int tpos, int u, 
     }
   }
 }
+
+// A unit's turn with the weight in it: lo' = ll lo + lh hi, hi' = hl lo + hh hi, in the order
+// of the plain rotation's roundings (without a weight the two agree bit for bit).
+template <int VEC>
+struct Factors {
+  float ll[VEC], lh[VEC], hl[VEC], hh[VEC];
+
+  __device__ __forceinline__ void set(const Angles<VEC>& t, const Part<VEC>& w, bool turns) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      ll[i] = turns ? t.c[i] * w.lo[i] : w.lo[i];
+      lh[i] = -t.s[i] * w.hi[i];
+      hl[i] = t.s[i] * w.lo[i];
+      hh[i] = turns ? t.c[i] * w.hi[i] : w.hi[i];
+    }
+  }
+  // (a chunk that stays beside one that turns, pairs layout: its factors are the weight)
+  __device__ __forceinline__ void second_stays(const Part<VEC>& w) {
+#pragma unroll
+    for (int i = VEC / 2; i < VEC; ++i) ll[i] = w.lo[i], hh[i] = w.hi[i];
+  }
+  // turns: the unit does; all: its second chunk too (pairs layout).
+  template <bool PAIRS>
+  __device__ __forceinline__ void turn(bool turns, bool all, float by, Part<VEC>& x) const {
+    const float2 by2 = both(by);
+    if (!turns) {
+      each_two<VEC>(x, [&](int i, float2& lo, float2& hi) {
+        lo = __fmul2_rn(__fmul2_rn(lo, two(ll, i)), by2);
+        hi = __fmul2_rn(__fmul2_rn(hi, two(hh, i)), by2);
+      });
+      return;
+    }
+    each_two<VEC>(x, [&](int i, float2& lo, float2& hi) {
+      const float2 h = __fmul2_rn(hi, two(hh, i));
+      float2 l1 = __ffma2_rn(lo, two(ll, i), __fmul2_rn(hi, two(lh, i)));
+      float2 h1 = __ffma2_rn(lo, two(hl, i), h);
+      if (PAIRS && !all && i >= VEC / 2) l1 = __fmul2_rn(lo, two(ll, i)), h1 = h;
+      if (PAIRS && !all && VEC == 2) {  // one pair of each chunk
+        l1.y = lo.y * ll[1];
+        h1.y = h.y;
+      }
+      lo = __fmul2_rn(l1, by2);
+      hi = __fmul2_rn(h1, by2);
+    });
+  }
+};
 
 // The weight of a unit's channels in a head.
 template <typename T, int VEC, bool PAIRS>
@@ -237,14 +309,6 @@ __device__ __forceinline__ void load_weight(const NormWeight& w, int h, int c1, 
   else load(Piece<__nv_bfloat16, VEC>{});
 }
 
-// Sum over the L lanes that share a row.
-__device__ __forceinline__ float row_sum(float v, int lanes) {
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1)
-    if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-
 // 2^-64: rows whose sum of squares leaves float32's range are scaled by it first.
 constexpr float kRowScale = 5.421010862427522e-20f;
 
@@ -267,22 +331,22 @@ struct RowRing {
   __device__ __forceinline__ explicit RowRing(void* smem)
       : base((unsigned char*)smem + (threadIdx.x >> 5) * kStages * kStageBytes +
              (threadIdx.x & 31) * 16) {}
-  // src: the rows; null: none
+  // src: the rows, if there are any
   template <typename P>
-  __device__ __forceinline__ void fetch(const P& place, const T* const (&src)[N]) {
+  __device__ __forceinline__ void fetch(const P& place, const T* const (&src)[N], bool any) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         if constexpr (kShared) {
           unsigned char* to = base + in + (n * U + j) * 1024;
-          if (src[n] != nullptr && place.c1[j] >= 0) cp_async16(to, src[n] + place.c1[j]);
-          if (src[n] != nullptr && place.c2[j] >= 0) cp_async16(to + 512, src[n] + place.c2[j]);
+          if (any && place.first(j)) cp_async16(to, src[n] + place.c1[j]);
+          if (any && place.second(j)) cp_async16(to + 512, src[n] + place.c2[j]);
         } else {
           next[0][n][j] = next[1][n][j];
-          if (src[n] == nullptr) continue;
-          if (place.c1[j] >= 0) load_chunk<T, VEC>(src[n] + place.c1[j], next[1][n][j].a);
-          if (place.c2[j] >= 0) load_chunk<T, VEC>(src[n] + place.c2[j], next[1][n][j].b);
+          if (!any) continue;
+          if (place.first(j)) load_chunk<T, VEC>(src[n] + place.c1[j], next[1][n][j].a);
+          if (place.second(j)) load_chunk<T, VEC>(src[n] + place.c2[j], next[1][n][j].b);
         }
       }
     }
@@ -303,16 +367,16 @@ struct RowRing {
           const unsigned char* from = base + out + (n * U + j) * 1024;
           uint4 v = *reinterpret_cast<const uint4*>(from);
           uint4 w = *reinterpret_cast<const uint4*>(from + 512);
-          if (place.c1[j] < 0) v = make_uint4(0, 0, 0, 0);
-          if (place.c2[j] < 0) w = make_uint4(0, 0, 0, 0);
+          if (!place.first(j)) v = make_uint4(0, 0, 0, 0);
+          if (!place.second(j)) w = make_uint4(0, 0, 0, 0);
           *reinterpret_cast<uint4*>(&r[n][j].a) = v;
           *reinterpret_cast<uint4*>(&r[n][j].b) = w;
         } else {
           r[n][j] = next[0][n][j];
 #pragma unroll
           for (int i = 0; i < VEC; ++i) {
-            if (place.c1[j] < 0) from_f32(0.f, r[n][j].a.e[i]);
-            if (place.c2[j] < 0) from_f32(0.f, r[n][j].b.e[i]);
+            if (!place.first(j)) from_f32(0.f, r[n][j].a.e[i]);
+            if (!place.second(j)) from_f32(0.f, r[n][j].b.e[i]);
           }
         }
       }
@@ -327,8 +391,8 @@ struct RowRing {
   }
 };
 
-template <typename T, int VEC, bool PAIRS, bool APPEND, int U>
-__global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, VEC))
+template <typename T, int VEC, bool PAIRS, bool APPEND, int U, int FL>
+__global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(APPEND ? kAppendNormBlocks : kNormBlocks, U, VEC))
     norm_rotary_kernel(const NormArgs a) {
   using Ring = RowRing<T, VEC, U, 1>;
   __shared__ uint4 ring_s[Ring::kBytes / 16 + 1];
@@ -336,42 +400,30 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
   const long long w = (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5);
   const int t = a.parts == 1 ? (int)w : (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
   if (t >= a.n_tokens) return;
-  const int L = a.lanes, sub = lane & (L - 1), per_warp = 32 / L, g = lane / L;
   const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
-  const int step = per_warp * a.parts;
-  int hb = part * per_warp;  // first head of the warp's step
-  const Place<VEC, PAIRS, U> place(a, sub);
+  const Place<VEC, PAIRS, U, FL> place(a, lane);
+  const int sub = place.sub, g = lane / place.lanes, step = place.per_warp() * a.parts;
+  int hb = part * place.per_warp();  // first head of the warp's step
   const T* xp = (const T*)a.x.p + t * a.x.ts;
   const T* kp = (const T*)a.k.p + t * a.k.ts;
   const T* vp = (const T*)a.v.p + t * a.v.ts;
   Ring ring(ring_s);
-  int hf = hb + g;  // the next head to fetch
+  int hf = hb + g;  // the next head to fetch, and (not append) its row
+  const T* xf = xp + hf * a.x.hs;
+  const long long x_step = step * a.x.hs;
   auto fetch = [&]() {
-    const T* p = nullptr;
-    if (hf < heads)
-      p = !APPEND || hf < a.n_x  ? xp + hf * a.x.hs
+    const T* p = xf;
+    if (APPEND)
+      p = hf < a.n_x         ? xp + hf * a.x.hs
           : hf < a.n_x + a.n_kv ? kp + (hf - a.n_x) * a.k.hs
                                 : vp + (hf - a.n_x - a.n_kv) * a.v.hs;
     const T* const src[1] = {p};
-    ring.fetch(place, src);
+    ring.fetch(place, src, hf < heads);
     hf += step;
+    xf += x_step;
   };
 #pragma unroll
   for (int k = 0; k < Ring::kAhead; ++k) fetch();
-
-  // 0: x, 1: keys, 2: values
-  auto set_of = [&](int h) { return !APPEND || h < a.n_x ? 0 : h < a.n_x + a.n_kv ? 1 : 2; };
-  Part<VEC> wt[U];
-  int held = -1;  // the set whose weight is in wt
-  auto load_weights = [&](int h, int set) {
-    const NormWeight& w = set == 0 ? a.wx : a.wk;
-    if (set > 1 || !w.p || (held == set && w.hs == 0)) return;
-    held = set;
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      load_weight<T, VEC, PAIRS>(w, set == 0 ? h : h - a.n_x, place.c1[j], place.c2[j], wt[j]);
-  };
-  if (hb + g < heads) load_weights(hb + g, set_of(hb + g));
 
   int pos = 0, page = -1;
   long long at = -1;  // the token's row of head 0 in the pools
@@ -410,14 +462,35 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
     pos = a.positions[t];
   }
   const int tpos = a.table ? min(max(pos, 0), a.n_pos - 1) : 0;
-  Angles<VEC> angles[U];
+  // 0: x, 1: keys, 2: values
+  auto set_of = [&](int h) { return !APPEND || h < a.n_x ? 0 : h < a.n_x + a.n_kv ? 1 : 2; };
+  Factors<VEC> f[U];
+  int held = -1;  // the set whose factors are in f
+  auto load_factors = [&](int h, int set) {
+    const NormWeight& w = set == 0 ? a.wx : a.wk;
+    if (set > 1 || (held == set && w.hs == 0)) return;
+    held = set;
 #pragma unroll
-  for (int j = 0; j < U; ++j) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
+    for (int j = 0; j < U; ++j) {
+      Angles<VEC> t;
+      if (place.turn(j)) load_angles<VEC, PAIRS>(a, tpos, sub + place.lanes * j, t);
+      Part<VEC> wt;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) wt.lo[i] = wt.hi[i] = 1.f;
+      if (w.p)
+        load_weight<T, VEC, PAIRS>(w, set == 0 ? h : h - a.n_x, place.c1[j], place.c2[j], wt);
+      f[j].set(t, wt, place.turn(j));
+      if (PAIRS && !place.turn_all(j)) f[j].second_stays(wt);
+    }
+  };
+  if (hb + g < heads) load_factors(hb + g, set_of(hb + g));
   if (lane == 0 && ((APPEND && page < 0) || (a.table && tpos != pos)))
     raise_status(a.dev_status, EBD_DEV_RANGE);
   T* yp = (T*)a.y.p + t * a.y.ts;
+  T* yh = yp + (hb + g) * a.y.hs;  // (not append) the step's row
+  const long long y_step = step * a.y.hs;
 
-  for (; hb < heads; hb += step) {
+  for (; hb < heads; hb += step, yh += y_step) {
     fetch();
     Piece<T, VEC> r[1][U];
     ring.take(place, r);
@@ -435,7 +508,7 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
           s1 = __ffma2_rn(hi, hi, s1);
         });
       const float2 s = __fadd2_rn(s0, s1);
-      return row_sum(live ? s.x + s.y : 0.f, L);
+      return place.row_sum(live ? s.x + s.y : 0.f);
     };
     float ss = squares(), eps = a.eps;
     const bool normed = live && set < 2 && (set == 0 ? a.wx.p : a.wk.p) != nullptr;
@@ -451,31 +524,28 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
     }
     if (!live) continue;
     T* dst;
-    if (!APPEND || set == 0) {
+    if (!APPEND) {
+      dst = yh;
+    } else if (set == 0) {
       dst = yp + h * a.y.hs;
     } else {
       if (at < 0) continue;
       const int kh = h - a.n_x - (set == 2 ? a.n_kv : 0);
       dst = (T*)(set == 2 ? a.V_pages : a.K_pages) + at + kh * a.pv.head_stride;
     }
-    if (normed) {
-      load_weights(h, set);
-      const float2 inv = both(__frsqrt_rn(fmaf(ss, a.inv_d, eps)));
+    if (set < 2) {
+      load_factors(h, set);
+      const float inv = normed ? __frsqrt_rn(fmaf(ss, a.inv_d, eps)) : 1.f;
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-        each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
-          lo = __fmul2_rn(lo, __fmul2_rn(two(wt[j].lo, i), inv));
-          hi = __fmul2_rn(hi, __fmul2_rn(two(wt[j].hi, i), inv));
-        });
+      for (int j = 0; j < U; ++j) {
+        f[j].template turn<PAIRS>(place.turn(j), place.turn_all(j), inv, x[j]);
+        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
+      }
     }
 #pragma unroll
     for (int j = 0; j < U; ++j) {
-      if (set < 2) {
-        turn<VEC, PAIRS>(a, sub + L * j, place.c2[j], angles[j], 1.f, x[j]);
-        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
-      }
-      if (place.c1[j] >= 0) store_chunk<T, VEC>(dst + place.c1[j], r[0][j].a);
-      if (place.c2[j] >= 0) store_chunk<T, VEC>(dst + place.c2[j], r[0][j].b);
+      if (place.first(j)) store_chunk<T, VEC>(dst + place.c1[j], r[0][j].a);
+      if (place.second(j)) store_chunk<T, VEC>(dst + place.c2[j], r[0][j].b);
     }
   }
 }
@@ -483,18 +553,18 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBlocks, U, V
 // PER_HEAD: a block has one head (blockIdx.y), a warp's groups of lanes have tokens; else
 // they have heads of a token.  Leaves the block's sum of the weight's gradient in
 // partial[blockIdx.x][blockIdx.y][d].
-template <typename T, int VEC, bool PAIRS, int U, bool PER_HEAD>
+template <typename T, int VEC, bool PAIRS, int U, bool PER_HEAD, int FL>
 __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, U, VEC))
     norm_backward_kernel(const NormArgs a, float* __restrict__ partial) {
   extern __shared__ __align__(16) unsigned char smem[];  // the rows' ring; then, in its place:
   float* red = reinterpret_cast<float*>(smem);           // [warps][units of all lanes][2 VEC]
   using Ring = RowRing<T, VEC, U, 2>;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int L = a.lanes, sub = lane & (L - 1), per_warp = 32 / L, g = lane / L;
+  const Place<VEC, PAIRS, U, FL> place(a, lane);
+  const int L = place.lanes, sub = place.sub, per_warp = place.per_warp(), g = lane / L;
   const long long items =
       PER_HEAD ? (a.n_tokens + per_warp - 1) / per_warp : (long long)a.n_tokens * a.parts;
   const int step = per_warp * a.parts;
-  const Place<VEC, PAIRS, U> place(a, sub);
   Part<VEC> wt[U], acc[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
@@ -503,7 +573,9 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     load_weight<T, VEC, PAIRS>(a.wx, PER_HEAD ? blockIdx.y : 0, place.c1[j], place.c2[j], wt[j]);
   }
 
+  grid_launch_dependents();  // the sum over blocks, which waits for this kernel's end
   Ring ring(smem);
+  const long long x_step = step * a.x.hs, dy_step = step * a.dy.hs, dx_step = step * a.y.hs;
   for (long long item = (long long)blockIdx.x * kNormWarps + warp; item < items;
        item += (long long)gridDim.x * kNormWarps) {
     int t, h;
@@ -516,13 +588,15 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     }
     const int hend = PER_HEAD ? h + 1 : a.n_x;
     const bool there = t < a.n_tokens;
-    int hf = h;  // the next head to fetch
+    int hf = there ? h : hend;  // the next head to fetch, and its rows
+    const T* src[2] = {(const T*)a.x.p + t * a.x.ts + h * a.x.hs,
+                       (const T*)a.dy.p + t * a.dy.ts + h * a.dy.hs};
+    T* out = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
     auto fetch = [&]() {
-      const bool live = there && hf < hend;
-      const T* const src[2] = {live ? (const T*)a.x.p + t * a.x.ts + hf * a.x.hs : nullptr,
-                               live ? (const T*)a.dy.p + t * a.dy.ts + hf * a.dy.hs : nullptr};
-      ring.fetch(place, src);
+      ring.fetch(place, src, hf < hend);
       hf += step;
+      src[0] += x_step;
+      src[1] += dy_step;
     };
 #pragma unroll
     for (int k = 0; k < Ring::kAhead; ++k) fetch();
@@ -531,9 +605,10 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     if (there && sub == 0 && a.table && tpos != pos) raise_status(a.dev_status, EBD_DEV_RANGE);
     Angles<VEC> angles[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
+    for (int j = 0; j < U; ++j)
+      if (place.turn(j)) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
     // (h - g: the warp's step is the same in all lanes)
-    for (int h0 = PER_HEAD ? h : h - g; h0 < hend; h0 += step, h += step) {
+    for (int h0 = PER_HEAD ? h : h - g; h0 < hend; h0 += step, h += step, out += dx_step) {
       fetch();
       Piece<T, VEC> r[2][U];
       ring.take(place, r);
@@ -543,7 +618,7 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
       for (int j = 0; j < U; ++j) {
         widen<T, VEC, PAIRS>(r[0][j], x[j]);
         widen<T, VEC, PAIRS>(r[1][j], u[j]);
-        turn<VEC, PAIRS>(a, sub + L * j, place.c2[j], angles[j], -1.f, u[j]);
+        if (place.turn(j)) turn<VEC, PAIRS>(angles[j], place.turn_all(j), -1.f, u[j]);
       }
       float ss, gx;
       auto sums = [&]() {
@@ -556,8 +631,8 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
             s1 = __ffma2_rn(__fmul2_rn(two(u[j].lo, i), two(wt[j].lo, i)), lo, s1);
             s1 = __ffma2_rn(__fmul2_rn(two(u[j].hi, i), two(wt[j].hi, i)), hi, s1);
           });
-        ss = row_sum(live ? s0.x + s0.y : 0.f, L);
-        gx = row_sum(live ? s1.x + s1.y : 0.f, L);
+        ss = place.row_sum(live ? s0.x + s0.y : 0.f);
+        gx = place.row_sum(live ? s1.x + s1.y : 0.f);
       };
       sums();
       float eps = a.eps, scale = 1.f;
@@ -574,9 +649,8 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
       }
       if (!live) continue;
       const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
-      const float2 inv2 = both(inv), mean = both(-gx * inv * a.inv_d);  // -mean of g z
-      const float2 back = both(inv * scale);
-      T* out = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
+      const float2 inv2 = both(inv), back = both(inv * scale);
+      const float2 mean = both(-gx * inv * a.inv_d * (inv * scale));  // -r mean of g z
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
@@ -586,12 +660,12 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
           const float2 a1 = __ffma2_rn(u1, z1, two(acc[j].hi, i));
           acc[j].lo[i] = a0.x, acc[j].hi[i] = a1.x;
           if constexpr (VEC > 1) acc[j].lo[i + 1] = a0.y, acc[j].hi[i + 1] = a1.y;
-          lo = __fmul2_rn(__ffma2_rn(z0, mean, __fmul2_rn(u0, two(wt[j].lo, i))), back);
-          hi = __fmul2_rn(__ffma2_rn(z1, mean, __fmul2_rn(u1, two(wt[j].hi, i))), back);
+          lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), back));
+          hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), back));
         });
         narrow<T, VEC, PAIRS>(x[j], r[0][j]);
-        if (place.c1[j] >= 0) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
-        if (place.c2[j] >= 0) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);
+        if (place.first(j)) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
+        if (place.second(j)) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);
       }
     }
     ring.restart();
@@ -627,26 +701,27 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
 }
 
 // dweight[i] = sum over the n blocks of partial[block][i], i < total; 32 columns per block,
-// warp w sums the blocks w, w + 8, ..
-__global__ void __launch_bounds__(256)
+// warp w sums the blocks w, w + 32, .., and the warps' sums are added in a fixed order.
+constexpr int kReduceWarps = 32;
+__global__ void __launch_bounds__(kReduceWarps * 32)
     norm_weight_reduce_kernel(const float* __restrict__ partial, int n, int total,
                               float* __restrict__ dweight) {
-  __shared__ float s[8][32];
+  __shared__ float s[kReduceWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
   grid_dependency_wait();
   float v = 0.f;
   if (i < total) {
-#pragma unroll 8
-    for (int k = warp; k < n; k += 8) v += partial[(size_t)k * total + i];
+#pragma unroll 5
+    for (int k = warp; k < n; k += kReduceWarps) v += partial[(size_t)k * total + i];
   }
   s[warp][lane] = v;
   __syncthreads();
-  if (warp == 0 && i < total) {
-    v = 0.f;
+  // warp w has columns w of the block: a lane per warp's sum
+  const int col = blockIdx.x * 32 + warp;
+  v = s[lane][warp];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v += s[k][lane];
-    dweight[i] = v;
-  }
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (lane == 0 && col < total) dweight[col] = v;
 }
 
 // Shape of a row's lanes for chunks of VEC elements; false: too many units.
@@ -662,7 +737,7 @@ static bool norm_shape(NormArgs& a, bool pairs, int max_u) {
   return a.units <= a.lanes * max_u;
 }
 
-template <typename T, int VEC, bool PAIRS, bool APPEND, int U>
+template <typename T, int VEC, bool PAIRS, bool APPEND, int U, int FL>
 static ebd_status launch_norm_u(NormArgs a, cudaStream_t s) {
   const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
   // one row per lane while the call has fewer warps than the GPU holds (latency), up to
@@ -671,7 +746,7 @@ static ebd_status launch_norm_u(NormArgs a, cudaStream_t s) {
   a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
   const long long blocks = ((long long)a.n_tokens * a.parts + kNormWarps - 1) / kNormWarps;
   if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
-  norm_rotary_kernel<T, VEC, PAIRS, APPEND, U>
+  norm_rotary_kernel<T, VEC, PAIRS, APPEND, U, FL>
       <<<(unsigned)blocks, kNormWarps * 32, 0, s>>>(a);
   return launch_status();
 }
@@ -688,7 +763,7 @@ struct NormBackward {
   float *partial, *dweight;
 };
 
-template <typename T, int VEC, bool PAIRS, int U>
+template <typename T, int VEC, bool PAIRS, int U, int FL>
 static ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s) {
   const bool per_head = a.wx.hs != 0;
   const int per_warp = 32 / a.lanes;
@@ -704,15 +779,15 @@ static ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStr
   const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4, ring = RowRing<T, VEC, U, 2>::kBytes;
   const int smem = sums > ring ? sums : ring;
   const dim3 grid(blocks, per_head ? a.n_x : 1);
-  auto kern = per_head ? norm_backward_kernel<T, VEC, PAIRS, U, true>
-                       : norm_backward_kernel<T, VEC, PAIRS, U, false>;
+  auto kern = per_head ? norm_backward_kernel<T, VEC, PAIRS, U, true, FL>
+                       : norm_backward_kernel<T, VEC, PAIRS, U, false, FL>;
   if (smem > 48 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
   kern<<<grid, kNormWarps * 32, smem, s>>>(a, bw.partial);
   const ebd_status st = launch_status();
   if (st != EBD_OK) return st;
-  return launch_dependent(norm_weight_reduce_kernel, dim3((total + 31) / 32), 256, 0, s,
+  return launch_dependent(norm_weight_reduce_kernel, dim3((total + 31) / 32), kReduceWarps * 32, 0, s,
                           (const float*)bw.partial, blocks, total, bw.dweight);
 }
 
@@ -726,13 +801,27 @@ static ebd_status launch_norm_v(NormArgs a, const NormBackward* bw, cudaStream_t
   constexpr int kLess = kWide ? 1 : 2;
   if (!norm_shape<VEC>(a, PAIRS, kMore)) return EBD_ERR_UNSUPPORTED;
   const bool less = a.units <= a.lanes * kLess;
-  if constexpr (!APPEND) {
-    if (bw)
-      return less ? launch_norm_back_u<T, VEC, PAIRS, kLess>(a, *bw, s)
-                  : launch_norm_back_u<T, VEC, PAIRS, kMore>(a, *bw, s);
+  auto launch = [&](auto u, auto fl) {
+    constexpr int U = decltype(u)::value, FL = decltype(fl)::value;
+    if constexpr (!APPEND) {
+      if (bw) return launch_norm_back_u<T, VEC, PAIRS, U, FL>(a, *bw, s);
+    }
+    return launch_norm_u<T, VEC, PAIRS, APPEND, U, FL>(a, s);
+  };
+  using std::integral_constant;
+  using One = integral_constant<int, 1>;
+  if constexpr (kWide) {
+    // whole heads of 64, 128 and 256 channels turn: nothing is asked of a lane's chunks
+    constexpr int L64 = 64 / (2 * VEC);
+    if (a.rot == a.head_dim) {
+      if (a.head_dim == 64) return launch(One{}, integral_constant<int, L64>{});
+      if (a.head_dim == 128) return launch(One{}, integral_constant<int, 2 * L64>{});
+      if (a.head_dim == 256) return launch(One{}, integral_constant<int, 4 * L64>{});
+    }
   }
-  return less ? launch_norm_u<T, VEC, PAIRS, APPEND, kLess>(a, s)
-              : launch_norm_u<T, VEC, PAIRS, APPEND, kMore>(a, s);
+  using None = integral_constant<int, 0>;
+  return less ? launch(integral_constant<int, kLess>{}, None{})
+              : launch(integral_constant<int, kMore>{}, None{});
 }
 
 // 16-byte accesses where every row and the rotated part allow them; otherwise
