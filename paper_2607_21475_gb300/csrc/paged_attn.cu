@@ -71,14 +71,14 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   static_assert(sizeof(WorkStart) <= 12 * 4, "start");
   grid_dependency_wait();
   if (threadIdx.x < 32) {
-    const WorkStart w = find_work<BN>(a, blockIdx.x, gridDim.x, threadIdx.x);
+    const WorkStart w = find_work<BN, TREE>(a, blockIdx.x, gridDim.x, threadIdx.x);
     if (threadIdx.x == 0) *start_s = w;
   }
   __syncthreads();
   bool bad = false, first = true;
   bool nan = false;  // a NaN in this thread's outputs
   PieceRecord record = {0, 0, 0, 0};
-  for (PieceWalk<BN> w(a, *start_s); w.live(); w.next(a)) {
+  for (PieceWalk<BN, TREE> w(a, *start_s); w.live(); w.next(a)) {
     record_piece(a, record, w, first);
     first = false;
     const HeadSlice hs = head_slice(a, w.h);
@@ -198,8 +198,12 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
 #pragma unroll
           for (int e = 0; e < NK; ++e) {
             const int pos = k0 + tx + 16 * e;
-            const bool sees = TREE ? visible >> (tx + 16 * e) & 1 : pos >= lo[i] && pos < hi[i];
-            s[i][e] = all || (sees && !(absent >> (tx + 16 * e) & 1)) ? s[i][e] : -INFINITY;
+            if (TREE)
+              s[i][e] = all || (visible & ~absent) >> (tx + 16 * e) & 1 ? s[i][e] : -INFINITY;
+            else
+              s[i][e] = all || (pos >= lo[i] && pos < hi[i] && !(absent >> (tx + 16 * e) & 1))
+                            ? s[i][e]
+                            : -INFINITY;
             top = fmaxf(top, s[i][e]);
           }
 #pragma unroll
@@ -273,7 +277,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     }
   }
   if (__any_sync(0xffffffffu, nan))
-    mend_pieces<float, D, BN>(a, blockIdx.x, gridDim.x, 0, 0, (threadIdx.x >> 5) * 8, 8,
+    mend_pieces<float, D, BN, TREE>(a, blockIdx.x, gridDim.x, 0, 0, (threadIdx.x >> 5) * 8, 8,
                               threadIdx.x & 31);
   if (threadIdx.x == 0) a.rec[blockIdx.x] = record;
   if (bad) raise_status(a.dev_status, EBD_DEV_RANGE);
@@ -384,7 +388,6 @@ static ebd_status attention(const ebd_paged_cache* cache, int32_t n_tokens, int3
   a.mask = mask;
   a.mask_words = mask_words;
   a.positions = positions;
-  a.in_line = mask ? 0 : 1;
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
   const int n_cta = attention_ctas(*cache);

@@ -66,8 +66,6 @@ struct PagedAttnArgs {
   const uint32_t* mask;      // [n_tokens][mask_words]; null: causal
   const int32_t* positions;  // [n_tokens]; needed with a window
   int mask_words;
-  int in_line;               // 1: new token i stands i positions after the first; 0: a tree's
-                             // tokens may all stand where it begins
 };
 
 // KV head, first query head and number of query heads of (sliced) head h.
@@ -135,7 +133,7 @@ __device__ __forceinline__ uint64_t tree_visible(const PagedAttnArgs& a, int t, 
 
 // Key tiles [kb, ke) of m-tile m; an item with nothing to see keeps one (fully
 // masked) tile, so that its rows get written.
-template <int BN>
+template <int BN, bool TREE>
 __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int len, int m, int& kb,
                                            int& ke) {
   const int first = m * a.tokens, last = min(n, first + a.tokens) - 1, p0 = len - n;
@@ -143,7 +141,8 @@ __device__ __forceinline__ void item_range(const PagedAttnArgs& a, int n, int le
   kb = 0;
   ke = 1;
   if (k_end > 0) {
-    kb = first_seen(a, p0 + first * a.in_line) / BN;
+    // (a tree's tokens may all stand where it begins)
+    kb = first_seen(a, TREE ? p0 : p0 + first) / BN;
     ke = (k_end + BN - 1) / BN;
   }
 }
@@ -178,7 +177,7 @@ __device__ __forceinline__ int warp_scan_add(int v, int lane) {
 }
 
 // Work of one head of the sequences base + lane (lane = 0..31), their spans and m-tiles.
-template <int BN>
+template <int BN, bool TREE>
 __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, int lane,
                                              bool report, SeqSpan& sp, int& mt) {
   const int b = base + lane;
@@ -191,7 +190,7 @@ __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, i
   int c = 0;
   for (int m = 0; m < min(mt, 4); ++m) {
     int kb, ke;
-    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+    item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
     c += (ke - kb) * tile_work(a, sp.n, m) + a.item_cost;
   }
   // long chunks: the warp walks the remaining m-tiles of one sequence together
@@ -202,7 +201,7 @@ __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, i
     int sum = 0;
     for (int m = 4 + lane; m < k; m += 32) {
       int kb, ke;
-      item_range<BN>(a, n, len, m, kb, ke);
+      item_range<BN, TREE>(a, n, len, m, kb, ke);
       sum += (ke - kb) * tile_work(a, n, m) + a.item_cost;
     }
     sum = __reduce_add_sync(0xffffffffu, sum);
@@ -212,14 +211,14 @@ __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, i
 }
 
 // Where CTA `cta` begins on the line, and how much of it is its own; one whole warp.
-template <int BN>
+template <int BN, bool TREE>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
   const int H = a.heads;
   SeqSpan sp;
   int total = 0, c = 0, upto = 0, mt = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
-    c = sequence_work<BN>(a, base, lane, cta == 0, sp, mt);
+    c = sequence_work<BN, TREE>(a, base, lane, cta == 0, sp, mt);
     upto = warp_scan_add(c * H, lane);
     total += __shfl_sync(0xffffffffu, upto, 31);
   }
@@ -230,7 +229,7 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
   const int count = min(share, total - at);
   for (int base = 0; base < a.pv.batch; base += 32) {
     if (a.pv.batch > 32) {
-      c = sequence_work<BN>(a, base, lane, false, sp, mt);
+      c = sequence_work<BN, TREE>(a, base, lane, false, sp, mt);
       upto = warp_scan_add(c * H, lane);
     }
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
@@ -259,7 +258,7 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
     int work = 0;
     if (base + lane < w.mt) {
       int kb, ke;
-      item_range<BN>(a, w.sp.n, w.sp.len, base + lane, kb, ke);
+      item_range<BN, TREE>(a, w.sp.n, w.sp.len, base + lane, kb, ke);
       work = (ke - kb) * tile_work(a, w.sp.n, base + lane) + a.item_cost;
     }
     const int end = warp_scan_add(work, lane);
@@ -276,7 +275,7 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
 }
 
 // Walks a CTA's pieces; every role of the CTA walks the same ones.
-template <int BN>
+template <int BN, bool TREE>
 struct PieceWalk {
   int b, h, m, mt;
   SeqSpan sp;
@@ -290,14 +289,14 @@ struct PieceWalk {
       left = -1;
       return;
     }
-    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+    item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
     take(a, w.off);
     if (cur == end) next(a);
   }
   __device__ __forceinline__ void load(const PagedAttnArgs& a) {
     sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
     mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);
-    item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+    item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
   }
   // This CTA's tiles of the item, of which earlier CTAs have the first `off` of its
   // work: an item's own cost comes first, so a share that ends within it has no
@@ -326,7 +325,7 @@ struct PieceWalk {
         return;
       }
       if (++m < mt) {
-        item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+        item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
       } else {
         m = 0;
         if (++h == a.heads) {
@@ -339,7 +338,7 @@ struct PieceWalk {
             load(a);
           } while (mt == 0);
         } else {
-          item_range<BN>(a, sp.n, sp.len, m, kb, ke);
+          item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
         }
       }
       take(a, 0);
@@ -348,9 +347,9 @@ struct PieceWalk {
 };
 
 // Enters a piece into the CTA's record.
-template <int BN>
+template <int BN, bool TREE>
 __device__ __forceinline__ void record_piece(const PagedAttnArgs& a, PieceRecord& r,
-                                             const PieceWalk<BN>& p, bool first) {
+                                             const PieceWalk<BN, TREE>& p, bool first) {
   if (first && p.cur > p.kb) {
     r.cont = p.end < p.ke ? 1 : 2;
   } else if (p.end < p.ke) {
@@ -384,7 +383,7 @@ __device__ __forceinline__ void load_row(const T* p, float (&x)[C]) {
 // stops once every such channel has met a NaN of its own.  q: the row's query; y or part
 // (part_row): the output, as written.  Whole warp: lane i has channels C i .. + C - 1,
 // and key i of 32.
-template <typename T, int D>
+template <typename T, int D, bool TREE>
 __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh, const T* q,
                                          int tile_lo, int lo, int hi, int tile_hi, int base,
                                          int t, int i, T* y, float* part, int lane) {
@@ -405,7 +404,7 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
   };
   // whether the row sees its position pos, lo <= pos < hi
   auto sees = [&](int pos) {
-    return !a.mask || pos < base || (tree_words(a, t, (pos - base) >> 5) >> ((pos - base) & 31) & 1);
+    return !TREE || pos < base || (tree_words(a, t, (pos - base) >> 5) >> ((pos - base) & 31) & 1);
   };
   const int k_lo = min(max(lo, tile_lo), tile_hi), k_hi = max(min(hi, tile_hi), k_lo);  // seen
   uint32_t mend = 0;
@@ -425,7 +424,7 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
   };
   look(tile_lo, k_lo, false);
   look(k_hi, tile_hi, false);
-  if (a.mask) look(max(base, k_lo), k_hi, true);
+  if (TREE) look(max(base, k_lo), k_hi, true);
   mend &= nan;
   if (!__any_sync(0xffffffffu, mend)) return;
   float m = -INFINITY, l = 0.f, acc[C] = {};
@@ -488,12 +487,12 @@ __device__ __forceinline__ void mend_row(const PagedAttnArgs& a, int b, int kvh,
 // 32/8 heads x 128, bf16: the call takes 113 (690) ms instead of 0.46 (1.5); with every value
 // NaN 5.5 (6.5) ms.  With 4 rows to a pass over the keys it took 37 (229) ms, but its 168
 // registers and its size made every call 1-2% slower.
-template <typename T, int D, int BN>
+template <typename T, int D, int BN, bool TREE>
 __device__ __noinline__ void mend_pieces(const PagedAttnArgs& a, int cta, int n_cta, int x0,
                                          int slot0, int row0, int rows, int lane) {
   __syncwarp();  // the rows, written by other lanes
-  const WorkStart start = find_work<BN>(a, cta, n_cta, lane);
-  for (PieceWalk<BN> w(a, start); w.live(); w.next(a)) {
+  const WorkStart start = find_work<BN, TREE>(a, cta, n_cta, lane);
+  for (PieceWalk<BN, TREE> w(a, start); w.live(); w.next(a)) {
     const int tokens = min(w.tokens(a) - x0, a.half_tokens), slot = w.slot(cta);
     const int t_first = w.sp.t0 + w.first(a) + x0, p0 = w.sp.len - w.sp.n + w.first(a) + x0;
     const HeadSlice hs = head_slice(a, w.h);
@@ -505,9 +504,9 @@ __device__ __noinline__ void mend_pieces(const PagedAttnArgs& a, int cta, int n_
       const long long out =
           (long long)(t_first + t) * (a.pv.n_kv_heads * a.group) + hs.q0 + g;
       bool bad;
-      const int lo = a.mask ? tree_first_seen(a, t_first + t, base, p0 + t - base, bad)
+      const int lo = TREE ? tree_first_seen(a, t_first + t, base, p0 + t - base, bad)
                             : first_seen(a, p0 + t);
-      mend_row<T, D>(a, w.b, hs.kvh,
+      mend_row<T, D, TREE>(a, w.b, hs.kvh,
                      (const T*)a.q + (t_first + t) * a.q_ts + (hs.q0 + g) * a.q_hs, w.cur * BN,
                      lo, p0 + t + 1, min(w.end * BN, w.sp.len), base, t_first + t, p0 + t - base,
                      slot < 0 ? (T*)a.y + out * D : nullptr,

@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   fence_proxy_async_smem();
   grid_dependency_wait();  // nothing of the caller's was read or written so far
   WorkStart start = {};
-  if (warp == 11) start = find_work<kTcBN>(a, cta, gridDim.x, lane);
+  if (warp == 11) start = find_work<kTcBN, TREE>(a, cta, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       tc_fence_before();  // the reads of O_X, before the next item's first product
     }
     if (ok && __any_sync(0xffffffffu, nonfinite))
-      mend_pieces<__nv_bfloat16, D, kTcBN>(a, cta, gridDim.x, x * a.half_tokens, x * 128,
+      mend_pieces<__nv_bfloat16, D, kTcBN, TREE>(a, cta, gridDim.x, x * a.half_tokens, x * 128,
                                            (warp & 3) * 32, 32, lane);
   } else if (warp < 10) {
     // ---------------- MMA issue: a warp per X (one thread's instructions between
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
       mbar_wait_bounded(&bar->v_full[i % KS], (i / KS) & 1);
   } else {
     // ---------------- the CTA's pieces; query rows; value rows past the end
-    PieceWalk<kTcBN> walk(a, start);
+    PieceWalk<kTcBN, TREE> walk(a, start);
     uint32_t items = 0, pushed = 0, tile0 = 0;  // tile0: tiles before this piece
     bool all = false;  // the end of the work was told
     PieceRecord record = {0, 0, 0, 0};
