@@ -9,8 +9,8 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAFunctions.h>
-#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -160,32 +160,31 @@ struct Stream {
   }
 };
 
-// A call's workspace: the given one, or a buffer from the pool of the call's stream.
+// A call's workspace: the given one, or a buffer from the pool of the call's stream, which
+// gets it back in stream order when the call returns.
 struct Workspace {
-  at::Tensor buffer;
-  void* p = nullptr;
+  void *p = nullptr, *own = nullptr;
   size_t bytes = 0;
 
   Workspace(size_t need, PyObject* given, const Stream& s) {
     if (need == 0) return;
-    if (given != Py_None) {
-      const at::Tensor& t = tensor(given, "workspace");
-      if (!t.is_cuda()) bad_value("workspace must be a CUDA tensor");
-      if (!t.is_contiguous()) bad_value("workspace must be contiguous");
-      if ((size_t)t.nbytes() < need)
-        bad_value("workspace too small: " + std::to_string(t.nbytes()) + " < " +
-                  std::to_string(need));
-      p = t.data_ptr();
-      bytes = t.nbytes();
+    if (given == Py_None) {
+      p = own = c10::cuda::CUDACachingAllocator::raw_alloc_with_stream(need, (cudaStream_t)s.raw);
+      bytes = need;
       return;
     }
-    c10::cuda::OptionalCUDAStreamGuard guard;
-    if (s.given)
-      guard.reset_stream(c10::cuda::getStreamFromExternal((cudaStream_t)s.raw, s.device));
-    buffer = at::empty({(int64_t)need}, at::TensorOptions().dtype(at::kByte).device(
-                                            at::Device(at::kCUDA, s.device)));
-    p = buffer.data_ptr();
-    bytes = need;
+    const at::Tensor& t = tensor(given, "workspace");
+    if (!t.is_cuda()) bad_value("workspace must be a CUDA tensor");
+    if (!t.is_contiguous()) bad_value("workspace must be contiguous");
+    if ((size_t)t.nbytes() < need)
+      bad_value("workspace too small: " + std::to_string(t.nbytes()) + " < " +
+                std::to_string(need));
+    p = t.data_ptr();
+    bytes = t.nbytes();
+  }
+  Workspace(const Workspace&) = delete;
+  ~Workspace() {
+    if (own) c10::cuda::CUDACachingAllocator::raw_delete(own);
   }
 };
 

@@ -382,10 +382,6 @@ struct RowRing {
       }
     if constexpr (kShared) out = out + kStageBytes == kStages * kStageBytes ? 0 : out + kStageBytes;
   }
-  // Forgets the steps that were asked for past the last one.
-  __device__ __forceinline__ void restart() {
-    if constexpr (kShared) out = in;
-  }
   __device__ __forceinline__ void drain() {
     if constexpr (kShared) cp_async_wait<0>();
   }
@@ -397,6 +393,8 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(APPEND ? kAppendN
   using Ring = RowRing<T, VEC, U, 1>;
   __shared__ uint4 ring_s[Ring::kBytes / 16 + 1];
   const int lane = threadIdx.x & 31;
+  grid_launch_dependents();
+  grid_dependency_wait();
   const long long w = (long long)blockIdx.x * kNormWarps + (threadIdx.x >> 5);
   const int t = a.parts == 1 ? (int)w : (int)(w / a.parts), part = (int)(w - (long long)t * a.parts);
   if (t >= a.n_tokens) return;
@@ -562,9 +560,8 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const Place<VEC, PAIRS, U, FL> place(a, lane);
   const int L = place.lanes, sub = place.sub, per_warp = place.per_warp(), g = lane / L;
-  const long long items =
-      PER_HEAD ? (a.n_tokens + per_warp - 1) / per_warp : (long long)a.n_tokens * a.parts;
-  const int step = per_warp * a.parts;
+  grid_launch_dependents();  // the sum over blocks, which waits for this kernel's end
+  grid_dependency_wait();
   Part<VEC> wt[U], acc[U];
 #pragma unroll
   for (int j = 0; j < U; ++j) {
@@ -573,102 +570,119 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     load_weight<T, VEC, PAIRS>(a.wx, PER_HEAD ? blockIdx.y : 0, place.c1[j], place.c2[j], wt[j]);
   }
 
-  grid_launch_dependents();  // the sum over blocks, which waits for this kernel's end
-  Ring ring(smem);
-  const long long x_step = step * a.x.hs, dy_step = step * a.dy.hs, dx_step = step * a.y.hs;
-  for (long long item = (long long)blockIdx.x * kNormWarps + warp; item < items;
-       item += (long long)gridDim.x * kNormWarps) {
-    int t, h;
+  // Steps of the call: 32 / L heads of a token, or tokens of the block's head, one after
+  // another; a warp has an even share of them, its rows asked for from token to token.
+  const int per_token = PER_HEAD ? 1 : (a.n_x + per_warp - 1) / per_warp;
+  const long long steps = PER_HEAD ? (a.n_tokens + per_warp - 1) / per_warp
+                                   : (long long)a.n_tokens * per_token;
+  const long long warps = (long long)gridDim.x * kNormWarps, w = (long long)warp * gridDim.x + blockIdx.x;
+  const long long q0 = steps * w / warps, q1 = steps * (w + 1) / warps;
+  struct At {
+    int t, h;  // a step's token and head for these lanes
+  };
+  auto first_at = [&](long long q) {
+    At p;
+    p.t = PER_HEAD ? (int)q * per_warp + g : (int)(q / per_token);
+    p.h = PER_HEAD ? blockIdx.y : (int)(q - (long long)p.t * per_token) * per_warp + g;
+    return p;
+  };
+  auto next_at = [&](At& p) {
     if (PER_HEAD) {
-      t = (int)(item * per_warp) + g;
-      h = blockIdx.y;
-    } else {
-      t = (int)(item / a.parts);
-      h = (int)(item - (long long)t * a.parts) * per_warp + g;
+      p.t += per_warp;
+    } else if ((p.h += per_warp) - g >= a.n_x) {
+      p.h = g;
+      ++p.t;
     }
-    const int hend = PER_HEAD ? h + 1 : a.n_x;
-    const bool there = t < a.n_tokens;
-    int hf = there ? h : hend;  // the next head to fetch, and its rows
-    const T* src[2] = {(const T*)a.x.p + t * a.x.ts + h * a.x.hs,
-                       (const T*)a.dy.p + t * a.dy.ts + h * a.dy.hs};
-    T* out = (T*)a.y.p + t * a.y.ts + h * a.y.hs;
-    auto fetch = [&]() {
-      ring.fetch(place, src, hf < hend);
-      hf += step;
-      src[0] += x_step;
-      src[1] += dy_step;
+  };
+  auto there = [&](const At& p) { return p.t < a.n_tokens && p.h < a.n_x; };
+  Ring ring(smem);
+  At ahead = first_at(q0);
+  long long qf = q0;  // the next step to fetch
+  auto fetch = [&]() {
+    const T* const src[2] = {(const T*)a.x.p + ahead.t * a.x.ts + ahead.h * a.x.hs,
+                             (const T*)a.dy.p + ahead.t * a.dy.ts + ahead.h * a.dy.hs};
+    ring.fetch(place, src, qf < q1 && there(ahead));
+    next_at(ahead);
+    ++qf;
+  };
+#pragma unroll
+  for (int k = 0; k < Ring::kAhead; ++k) fetch();
+  At at = first_at(q0);
+  Angles<VEC> angles[U];
+  int token = -1;  // whose angles these are
+  int pos = 0;     // position of the next token
+  if (a.positions && q0 < q1 && at.t < a.n_tokens) pos = a.positions[at.t];
+  for (long long q = q0; q < q1; ++q, next_at(at)) {
+    if (at.t != token) {
+      token = at.t;
+      const int tpos = a.table ? min(max(pos, 0), a.n_pos - 1) : 0;
+      if (there(at) && sub == 0 && a.table && tpos != pos)
+        raise_status(a.dev_status, EBD_DEV_RANGE);
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (place.turn(j)) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
+      const int after = PER_HEAD ? token + per_warp : token + 1;
+      if (a.positions && after < a.n_tokens) pos = a.positions[after];
+    }
+    fetch();
+    Piece<T, VEC> r[2][U];
+    ring.take(place, r);
+    const bool live = there(at);
+    Part<VEC> x[U], u[U];  // u: R^T dy
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      widen<T, VEC, PAIRS>(r[0][j], x[j]);
+      widen<T, VEC, PAIRS>(r[1][j], u[j]);
+      if (place.turn(j)) turn<VEC, PAIRS>(angles[j], place.turn_all(j), -1.f, u[j]);
+    }
+    float ss, gx;
+    auto sums = [&]() {
+      float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
+          s0 = __ffma2_rn(lo, lo, s0);
+          s0 = __ffma2_rn(hi, hi, s0);
+          s1 = __ffma2_rn(__fmul2_rn(two(u[j].lo, i), two(wt[j].lo, i)), lo, s1);
+          s1 = __ffma2_rn(__fmul2_rn(two(u[j].hi, i), two(wt[j].hi, i)), hi, s1);
+        });
+      ss = place.row_sum(live ? s0.x + s0.y : 0.f);
+      gx = place.row_sum(live ? s1.x + s1.y : 0.f);
     };
-#pragma unroll
-    for (int k = 0; k < Ring::kAhead; ++k) fetch();
-    const int pos = there && a.positions ? a.positions[t] : 0;
-    const int tpos = a.table ? min(max(pos, 0), a.n_pos - 1) : 0;
-    if (there && sub == 0 && a.table && tpos != pos) raise_status(a.dev_status, EBD_DEV_RANGE);
-    Angles<VEC> angles[U];
-#pragma unroll
-    for (int j = 0; j < U; ++j)
-      if (place.turn(j)) load_angles<VEC, PAIRS>(a, tpos, sub + L * j, angles[j]);
-    // (h - g: the warp's step is the same in all lanes)
-    for (int h0 = PER_HEAD ? h : h - g; h0 < hend; h0 += step, h += step, out += dx_step) {
-      fetch();
-      Piece<T, VEC> r[2][U];
-      ring.take(place, r);
-      const bool live = there && h < hend;
-      Part<VEC> x[U], u[U];  // u: R^T dy
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        widen<T, VEC, PAIRS>(r[0][j], x[j]);
-        widen<T, VEC, PAIRS>(r[1][j], u[j]);
-        if (place.turn(j)) turn<VEC, PAIRS>(angles[j], place.turn_all(j), -1.f, u[j]);
-      }
-      float ss, gx;
-      auto sums = [&]() {
-        float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+    sums();
+    float eps = a.eps, scale = 1.f;
+    if (__any_sync(0xffffffffu, !(ss < INFINITY))) {
+      if (!(ss < INFINITY)) {
+        eps = 0.f;
+        scale = kRowScale;
 #pragma unroll
         for (int j = 0; j < U; ++j)
-          each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
-            s0 = __ffma2_rn(lo, lo, s0);
-            s0 = __ffma2_rn(hi, hi, s0);
-            s1 = __ffma2_rn(__fmul2_rn(two(u[j].lo, i), two(wt[j].lo, i)), lo, s1);
-            s1 = __ffma2_rn(__fmul2_rn(two(u[j].hi, i), two(wt[j].hi, i)), hi, s1);
-          });
-        ss = place.row_sum(live ? s0.x + s0.y : 0.f);
-        gx = place.row_sum(live ? s1.x + s1.y : 0.f);
-      };
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
+      }
       sums();
-      float eps = a.eps, scale = 1.f;
-      if (__any_sync(0xffffffffu, !(ss < INFINITY))) {
-        if (!(ss < INFINITY)) {
-          eps = 0.f;
-          scale = kRowScale;
-#pragma unroll
-          for (int j = 0; j < U; ++j)
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
-        }
-        sums();
-      }
-      if (!live) continue;
-      const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
-      const float2 inv2 = both(inv), back = both(inv * scale);
-      const float2 mean = both(-gx * inv * a.inv_d * (inv * scale));  // -r mean of g z
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
-          const float2 z0 = __fmul2_rn(lo, inv2), z1 = __fmul2_rn(hi, inv2);
-          const float2 u0 = two(u[j].lo, i), u1 = two(u[j].hi, i);
-          const float2 a0 = __ffma2_rn(u0, z0, two(acc[j].lo, i));
-          const float2 a1 = __ffma2_rn(u1, z1, two(acc[j].hi, i));
-          acc[j].lo[i] = a0.x, acc[j].hi[i] = a1.x;
-          if constexpr (VEC > 1) acc[j].lo[i + 1] = a0.y, acc[j].hi[i + 1] = a1.y;
-          lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), back));
-          hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), back));
-        });
-        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
-        if (place.first(j)) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
-        if (place.second(j)) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);
-      }
     }
-    ring.restart();
+    if (!live) continue;
+    T* out = (T*)a.y.p + at.t * a.y.ts + at.h * a.y.hs;
+    const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
+    const float2 inv2 = both(inv), back = both(inv * scale);
+    const float2 mean = both(-gx * inv * a.inv_d * (inv * scale));  // -r mean of g z
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
+        const float2 z0 = __fmul2_rn(lo, inv2), z1 = __fmul2_rn(hi, inv2);
+        const float2 u0 = two(u[j].lo, i), u1 = two(u[j].hi, i);
+        const float2 a0 = __ffma2_rn(u0, z0, two(acc[j].lo, i));
+        const float2 a1 = __ffma2_rn(u1, z1, two(acc[j].hi, i));
+        acc[j].lo[i] = a0.x, acc[j].hi[i] = a1.x;
+        if constexpr (VEC > 1) acc[j].lo[i + 1] = a0.y, acc[j].hi[i + 1] = a1.y;
+        lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), back));
+        hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), back));
+      });
+      narrow<T, VEC, PAIRS>(x[j], r[0][j]);
+      if (place.first(j)) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
+      if (place.second(j)) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);
+    }
   }
 
   // the block's sum, in a fixed order: lanes, then warps
@@ -708,6 +722,7 @@ __global__ void __launch_bounds__(kReduceWarps * 32)
                               float* __restrict__ dweight) {
   __shared__ float s[kReduceWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
+  grid_launch_dependents();
   grid_dependency_wait();
   float v = 0.f;
   if (i < total) {
@@ -746,14 +761,13 @@ static ebd_status launch_norm_u(NormArgs a, cudaStream_t s) {
   a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
   const long long blocks = ((long long)a.n_tokens * a.parts + kNormWarps - 1) / kNormWarps;
   if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
-  norm_rotary_kernel<T, VEC, PAIRS, APPEND, U, FL>
-      <<<(unsigned)blocks, kNormWarps * 32, 0, s>>>(a);
-  return launch_status();
+  return launch_dependent(norm_rotary_kernel<T, VEC, PAIRS, APPEND, U, FL>, dim3((unsigned)blocks),
+                          kNormWarps * 32, 0, s, a);
 }
 
 // Blocks of the backward pass along its rows (times the heads where each has a weight).
-static int norm_back_blocks(long long items, int heads) {
-  const long long want = (items + kNormWarps - 1) / kNormWarps;
+static int norm_back_blocks(long long steps, int heads) {
+  const long long want = (steps + kNormWarps - 1) / kNormWarps;
   long long most = (long long)sm_count() * kNormBackBlocks / heads;
   if (most < 1) most = 1;
   return (int)(want < most ? want : most);
@@ -767,14 +781,9 @@ template <typename T, int VEC, bool PAIRS, int U, int FL>
 static ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s) {
   const bool per_head = a.wx.hs != 0;
   const int per_warp = 32 / a.lanes;
-  // whole tokens per warp, unless there are too few for every warp of the GPU
-  const int steps = (a.n_x + per_warp - 1) / per_warp;
-  const long long warps = (long long)sm_count() * kNormBackBlocks * kNormWarps;
-  long long parts = (warps + a.n_tokens - 1) / a.n_tokens;
-  a.parts = (int)(parts < steps ? parts : steps);
-  const long long items =
-      per_head ? (a.n_tokens + per_warp - 1) / per_warp : (long long)a.n_tokens * a.parts;
-  const int blocks = norm_back_blocks(items, per_head ? a.n_x : 1);
+  const long long steps = per_head ? (a.n_tokens + per_warp - 1) / per_warp
+                                   : (long long)a.n_tokens * ((a.n_x + per_warp - 1) / per_warp);
+  const int blocks = norm_back_blocks(steps, per_head ? a.n_x : 1);
   const int total = (per_head ? a.n_x : 1) * a.head_dim;
   const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4, ring = RowRing<T, VEC, U, 2>::kBytes;
   const int smem = sums > ring ? sums : ring;
@@ -784,8 +793,7 @@ static ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStr
   if (smem > 48 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  kern<<<grid, kNormWarps * 32, smem, s>>>(a, bw.partial);
-  const ebd_status st = launch_status();
+  const ebd_status st = launch_dependent(kern, grid, kNormWarps * 32, smem, s, a, bw.partial);
   if (st != EBD_OK) return st;
   return launch_dependent(norm_weight_reduce_kernel, dim3((total + 31) / 32), kReduceWarps * 32, 0, s,
                           (const float*)bw.partial, blocks, total, bw.dweight);
@@ -865,7 +873,8 @@ static ebd_status check_norm(ebd_dtype dtype, int n_tokens, int head_dim, ebd_ro
   if (layout != EBD_ROTARY_HALF && layout != EBD_ROTARY_PAIRS) return EBD_ERR_INVALID;
   if (n_tokens < 0 || head_dim < 1) return EBD_ERR_INVALID;
   if (!(eps > 0.f) || !(eps < INFINITY)) return EBD_ERR_INVALID;
-  if (head_dim > kNormMaxDim) return EBD_ERR_UNSUPPORTED;
+  // (token numbers a step past the last one still fit 31 bits)
+  if (head_dim > kNormMaxDim || n_tokens > 0x7fffff00) return EBD_ERR_UNSUPPORTED;
   if (!table) {
     rot = 0;
     return EBD_OK;

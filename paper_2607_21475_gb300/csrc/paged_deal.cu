@@ -22,6 +22,7 @@
 #include <cuda_runtime.h>
 
 #include "common.cuh"
+#include "decode_tile.cuh"
 #include "internal.h"
 #include "paged.cuh"
 #include "ptx.cuh"
@@ -159,6 +160,8 @@ __global__ void __launch_bounds__(kDealThreads, 1) paged_deal_kernel(const DealA
   const int threads = blockDim.x * ranks;
   const int tid = ((threadIdx.x >> 5) * ranks + rank) * 32 + (threadIdx.x & 31);
   const DealSums of(sums_s, a.batch);
+  grid_launch_dependents();
+  grid_dependency_wait();
   const int b0 = min((int)threadIdx.x * PER, a.batch), mine = min(PER, a.batch - b0);
   bool bad = false, short_of = false;
 
@@ -372,6 +375,8 @@ __device__ __forceinline__ void cluster_scan(long long (&x)[N], long long (&tota
 __global__ void __launch_bounds__(kDealThreads, 1) paged_deal_many_kernel(const DealArgs a) {
   __shared__ long long warp_sums[2][32][3], part[2][3];
   __shared__ int cu_s[kDealOffsets + 1];
+  grid_launch_dependents();
+  grid_dependency_wait();
   const uint32_t ranks = gridDim.x, rank = cluster_rank();
   const int lane = threadIdx.x & 31;
   const int threads = kDealThreads * ranks, tid = rank * kDealThreads + threadIdx.x;
@@ -581,11 +586,13 @@ extern "C" ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n
       return EBD_ERR_CUDA;
   }
   cfg.stream = (cudaStream_t)stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cfg.gridDim.x;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = 2;
   return cuda_status(cudaLaunchKernelEx(&cfg, kern, a));
 }

@@ -13,11 +13,16 @@
 // walks the path upwards: path[i] >= i, so no source is overwritten before it is read,
 // neither within a step of kKeepFlight loads and then their stores nor by earlier ones.
 // HBM and the chain lengths -> path -> pages -> rows bound it.
+//
+// Both are programmatic dependents of what precedes them on the stream, and let the next
+// kernel of that kind begin.
 #include <cuda_runtime.h>
 
 #include "common.cuh"
+#include "decode_tile.cuh"
 #include "internal.h"
 #include "paged.cuh"
+#include "paged_attn.cuh"
 
 namespace ebd {
 
@@ -35,6 +40,8 @@ __global__ void __launch_bounds__(kTreeWarps * 32)
                       int32_t* __restrict__ positions, int32_t* dev_status) {
   __shared__ int parent_s[kTreeMost];
   const int b = blockIdx.y, lane = threadIdx.x & 31, first = blockIdx.x * kTreeWarps;
+  grid_launch_dependents();
+  grid_dependency_wait();
   const int c0 = cu[b], c1 = cu[b + 1], len = seq_len[b];
   const int t0 = min(max(c0, 0), n_tokens), t1 = min(max(c1, t0), n_tokens);
   const int n = min(t1 - t0, max_new);
@@ -75,6 +82,8 @@ __global__ void __launch_bounds__(kKeepThreads)
   __shared__ long long from_s[kKeepMoves], to_s[kKeepMoves];
   __shared__ int kept_s, moves_s;
   const int b = blockIdx.x, lane = threadIdx.x & 31;
+  grid_launch_dependents();
+  grid_dependency_wait();
   const int c0 = cu[b], c1 = cu[b + 1], len_b = v.seq_len[b], kept_b = n_kept[b];
   const long long most = (long long)v.max_blocks << v.page_shift;
   const int len = (int)min((long long)max(len_b, 0), most);
@@ -158,10 +167,9 @@ extern "C" ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t ma
     return EBD_ERR_UNSUPPORTED;
   if (n_tokens == 0) return EBD_OK;
   if (!parents || !cu_new || !seq_len || !mask || !positions) return EBD_ERR_INVALID;
-  tree_masks_kernel<<<dim3((max_new + kTreeWarps - 1) / kTreeWarps, batch), kTreeWarps * 32, 0,
-                      (cudaStream_t)stream>>>(parents, cu_new, seq_len, batch, n_tokens, max_new,
-                                              mask_words, window, mask, positions, dev_status);
-  return launch_status();
+  return launch_dependent(tree_masks_kernel, dim3((max_new + kTreeWarps - 1) / kTreeWarps, batch),
+                          kTreeWarps * 32, 0, (cudaStream_t)stream, parents, cu_new, seq_len, batch,
+                          n_tokens, max_new, mask_words, window, mask, positions, dev_status);
 }
 
 extern "C" ebd_status ebd_paged_keep(const ebd_paged_cache* cache, int32_t n_layers,
@@ -188,9 +196,9 @@ extern "C" ebd_status ebd_paged_keep(const ebd_paged_cache* cache, int32_t n_lay
   v.page_stride /= wide;
   v.head_stride /= wide;
   v.row_stride /= wide;
-  paged_keep_kernel<<<dim3((unsigned)cache->batch, (unsigned)n_layers), kKeepThreads, 0,
-                      (cudaStream_t)stream>>>(
-      (uint4*)cache->K_pages, (uint4*)cache->V_pages, v, n_layers > 1 ? layer_stride / wide : 0,
-      cache->head_dim / wide, cu_new, path, n_accepted, max_path, seq_len_out, dev_status);
-  return launch_status();
+  return launch_dependent(
+      paged_keep_kernel, dim3((unsigned)cache->batch, (unsigned)n_layers), kKeepThreads, 0,
+      (cudaStream_t)stream, (uint4*)cache->K_pages, (uint4*)cache->V_pages, v,
+      n_layers > 1 ? layer_stride / wide : 0ll, cache->head_dim / wide, cu_new, path, n_accepted,
+      max_path, seq_len_out, dev_status);
 }
