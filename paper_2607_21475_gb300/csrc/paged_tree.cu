@@ -84,6 +84,9 @@ __global__ void __launch_bounds__(kKeepThreads)
   const int b = blockIdx.x, lane = threadIdx.x & 31;
   grid_launch_dependents();
   grid_dependency_wait();
+  // the path's first entries do not wait for the lengths
+  const int32_t* row = path + (size_t)b * max_path;
+  const int p_first = lane < max_path ? row[lane] : 0;
   const int c0 = cu[b], c1 = cu[b + 1], len_b = v.seq_len[b], kept_b = n_kept[b];
   const long long most = (long long)v.max_blocks << v.page_shift;
   const int len = (int)min((long long)max(len_b, 0), most);
@@ -93,14 +96,15 @@ __global__ void __launch_bounds__(kKeepThreads)
   bool bad = len != len_b || c1 - c0 != n || kept_b != k;
   K += blockIdx.y * layer_stride;
   V += blockIdx.y * layer_stride;
-  const int32_t* row = path + (size_t)b * max_path;
   const int columns = 2 * v.n_kv_heads * cpr;
   // the path is good up to the first entry that does not rise or is no new token
   int kept = k;
   for (int i0 = 0; i0 < kept; i0 += kKeepMoves) {
     if (threadIdx.x < 32) {
       const int i = i0 + lane;
-      const int p = i < kept ? row[i] : 0, before = i > 0 && i < kept ? row[i - 1] : -1;
+      int p = p_first, before = __shfl_up_sync(0xffffffffu, p_first, 1);
+      if (i0 > 0) p = i < kept ? row[i] : 0, before = i < kept ? row[i - 1] : -1;
+      if (i == 0) before = -1;
       const uint32_t wrong =
           __ballot_sync(0xffffffffu, i < kept && (p <= before || p >= n || p < 0));
       const int good = wrong ? i0 + __ffs(wrong) - 1 : kept;
