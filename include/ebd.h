@@ -618,7 +618,7 @@ ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n_pages, int
  *   x, y         device (dtype), strided as for ebd_rotary; y may be x (same strides)
  *   weight       device: element (h, c) at h * weight_head_stride + c; stride 0: one
  *                weight for all heads.  weight_dtype is EBD_F32 or dtype
- *   eps          positive
+ *   eps          at least the smallest normal float32
  *   positions    device [n_tokens]; outside [0, n_pos): as for ebd_rotary
  * d <= 512 (EBD_ERR_UNSUPPORTED otherwise).  Alignment as for ebd_rotary.
  */
@@ -657,7 +657,7 @@ ebd_status ebd_norm_rotary_backward(
  *   slots      device [n_tokens] int64, page * page_size + row (ebd_paged_deal); -1: no
  *              token here, nothing of it is written; another one outside the pool:
  *              dropped as by ebd_paged_append (EBD_DEV_RANGE).  Needs positions with a
- *              table; block_table and seq_len are not read
+ *              table; block_table and seq_len are not read; no slot twice
  *   k_weight, q_weight  as for ebd_norm_rotary; NULL: not normalised
  * With neither table nor q_weight n_q_heads is 0.  The rest as for ebd_paged_append.
  */
@@ -725,6 +725,7 @@ ebd_status ebd_paged_tree_attention(const ebd_paged_cache* cache, int32_t n_toke
  *   seq_len_out device [B] out, nullable; apart from the cache's seq_len (EBD_ERR_INVALID)
  *   dev_status  device int32, required
  * A row on a page outside the pool, or bound for one, does not move (EBD_DEV_RANGE).
+ * V_pages may be K_pages.
  * Alignment as for ebd_paged_gather, layer_stride too.
  */
 ebd_status ebd_paged_keep(const ebd_paged_cache* cache, int32_t n_layers, int64_t layer_stride,

@@ -16,6 +16,7 @@
 // of one token at a time, keeps the token's angles and the weight in registers and
 // has two steps' rows in flight.
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 
 #include <type_traits>
@@ -872,7 +873,8 @@ static ebd_status check_norm(ebd_dtype dtype, int n_tokens, int head_dim, ebd_ro
   if (weight_dtype != EBD_F32 && weight_dtype != dtype) return EBD_ERR_INVALID;
   if (layout != EBD_ROTARY_HALF && layout != EBD_ROTARY_PAIRS) return EBD_ERR_INVALID;
   if (n_tokens < 0 || head_dim < 1) return EBD_ERR_INVALID;
-  if (!(eps > 0.f) || !(eps < INFINITY)) return EBD_ERR_INVALID;
+  // (a subnormal eps would be flushed, and a row of zeros divided by zero)
+  if (!(eps >= FLT_MIN) || !(eps < INFINITY)) return EBD_ERR_INVALID;
   // (token numbers a step past the last one still fit 31 bits)
   if (head_dim > kNormMaxDim || n_tokens > 0x7fffff00) return EBD_ERR_UNSUPPORTED;
   if (!table) {

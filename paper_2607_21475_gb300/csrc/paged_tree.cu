@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kTreeWarps * 32)
 // Block (x, layer): sequence x.  The view's strides and layer_stride are in chunks of 16
 // bytes, `cpr` of them to a row.
 __global__ void __launch_bounds__(kKeepThreads)
-    paged_keep_kernel(uint4* __restrict__ K, uint4* __restrict__ V, PagedView v,
+    paged_keep_kernel(uint4* K, uint4* V, PagedView v,
                       long long layer_stride, int cpr, const int32_t* __restrict__ cu,
                       const int32_t* __restrict__ path, const int32_t* __restrict__ n_kept,
                       int max_path, int32_t* __restrict__ seq_len_out, int32_t* dev_status) {
@@ -96,7 +96,8 @@ __global__ void __launch_bounds__(kKeepThreads)
   bool bad = len != len_b || c1 - c0 != n || kept_b != k;
   K += blockIdx.y * layer_stride;
   V += blockIdx.y * layer_stride;
-  const int columns = 2 * v.n_kv_heads * cpr;
+  // (one pool for both: its rows move once)
+  const int columns = (K == V ? 1 : 2) * v.n_kv_heads * cpr;
   // the path is good up to the first entry that does not rise or is no new token
   int kept = k;
   for (int i0 = 0; i0 < kept; i0 += kKeepMoves) {

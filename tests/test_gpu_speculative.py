@@ -831,6 +831,113 @@ def test_keep_long_path_over_a_chain_moves_every_row_down(E):
     assert torch.equal(s["K"], rk[0]) and torch.equal(s["V"], rv[0])
 
 
+def test_keep_of_one_pool_for_keys_and_values(E):
+    """K and V in the same memory: every row moves once, though each is a later source."""
+    n = 300
+    s = R.make([n], [n + 9], 1, 1, 64, 16, torch.float32, 44)
+    path = [list(range(1, n))]
+    rk, _, _ = keep_ref(s["K"][None], s["K"][None], s["bt"], [n + 9], [0, n], path, [n - 1], 16)
+    s["V"] = s["K"]
+    E.ebd_paged_keep(cache(E, s), s["cu"], ints(path), ints([n - 1]))
+    assert torch.equal(s["K"], rk[0])
+
+
+# ---------------------------------------------------------------- the binding
+def test_calls_on_another_stream(E):
+    """Every call with stream=: after a long piece of work on that stream, into buffers that
+    the call makes itself."""
+    s = tree_case(E, 3, torch.bfloat16)
+    pc, tab = cache(E, s), table_of(E, 128, 200)
+    x, dy, w, pos = norm_inputs(33, 4, 128, torch.bfloat16, False, 5)
+    T = s["T"]
+    qo = torch.empty((T, 8, 128), dtype=torch.bfloat16, device="cuda")
+    path, kept = ints([[0, 3], [0, 0], [0, 0], [1, 2]]), ints([2, 0, 1, 2])
+
+    def all_calls(stream):
+        pool, pc2 = fresh_pool(E, 3, 20, 8, 5)
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                torch.cuda._sleep(2000000)
+        out = list(E.ebd_paged_deal(pool, pc2, ints([10, 3, 20]), 40, stream=stream))
+        out.append(E.ebd_norm_rotary(x, w, pos, tab_long, stream=stream))
+        out += E.ebd_norm_rotary_backward(dy, x, w, pos, tab_long, stream=stream)
+        m, p = E.ebd_tree_masks(s["parents"], s["cu"], s["seq_len"], 33, stream=stream)
+        E.ebd_paged_append_norm(pc, s["k"], s["v"], k_weight=w, q=s["q"], q_weight=w, q_out=qo,
+                                cu_new=s["cu"], positions=p, table=tab, stream=stream)
+        out += [m, p, *E.ebd_paged_tree_attention(qo, pc, s["cu"], 33, m, stream=stream)]
+        out.append(E.ebd_paged_keep(pc, s["cu"], path, kept, stream=stream))
+        if stream is not None:
+            torch.cuda.current_stream().wait_stream(stream)
+        return out
+
+    tab_long = table_of(E, 128, 4000)
+    K0 = s["K"].clone()
+    want = all_calls(None)
+    s["K"].copy_(K0)
+    got = all_calls(torch.cuda.Stream())
+    assert all(torch.equal(a, b) for a, b in zip(want, got)) and len(want) == len(got)
+
+
+def test_arguments_are_checked(E):
+    s = tree_case(E, 2, torch.bfloat16)
+    pc = cache(E, s)
+    x, dy, w, pos = norm_inputs(5, 2, 64, torch.bfloat16, False, 1)
+    tab = table_of(E, 64, 4000)
+
+    class Elsewhere:
+        cuda_stream, device_index = 0, 7
+
+    bad = [
+        (TypeError, lambda: E.ebd_norm_rotary(x, w.half(), pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w[:32], pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w.expand(2, 64), pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w, None, tab)),
+        (TypeError, lambda: E.ebd_norm_rotary(x, w, pos.long(), tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w, pos[:3], tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w, pos, tab[:, :, 0])),
+        (TypeError, lambda: E.ebd_norm_rotary(x.half(), w, pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x.transpose(1, 2), w, pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w, pos, tab, out=x[:4])),
+        (ValueError, lambda: E.ebd_norm_rotary(x, w, pos, tab, out=torch.empty_like(x),
+                                               stream=Elsewhere())),
+        (TypeError, lambda: E.ebd_norm_rotary_backward(dy.float(), x, w, pos, tab)),
+        (ValueError, lambda: E.ebd_norm_rotary_backward(dy, x, w, pos, tab, dweight=tab[0])),
+        (ValueError, lambda: E.ebd_norm_rotary_backward(
+            dy, x, w, pos, tab, workspace=torch.empty(16, device="cuda"))),
+        (ValueError, lambda: E.ebd_paged_append_norm(pc, s["k"], s["v"])),
+        (ValueError, lambda: E.ebd_paged_append_norm(pc, s["k"], s["v"][:1], cu_new=s["cu"])),
+        (ValueError, lambda: E.ebd_paged_append_norm(pc, s["k"], s["v"], cu_new=s["cu"][:1])),
+        (ValueError, lambda: E.ebd_paged_append_norm(pc, s["k"], s["v"], cu_new=s["cu"],
+                                                     q=s["q"])),
+        (TypeError, lambda: E.ebd_paged_append_norm(pc, s["k"], s["v"], slots=s["cu"][:1])),
+        (ValueError, lambda: E.ebd_tree_masks(s["parents"], s["cu"], s["cu"], 16)),
+        (ValueError, lambda: E.ebd_tree_masks(s["parents"], s["cu"], s["seq_len"], 16,
+                                              mask=s["mask"][:3])),
+        (ValueError, lambda: E.ebd_paged_tree_attention(s["q"], pc, s["cu"], 16, s["mask"][0])),
+        (TypeError, lambda: E.ebd_paged_tree_attention(s["q"], pc, s["cu"], 16,
+                                                       s["mask"].long())),
+        (ValueError, lambda: E.ebd_paged_tree_attention(s["q"], pc, s["cu"], 16, s["mask"][:2])),
+        (ValueError, lambda: E.ebd_paged_keep(pc, s["cu"], s["pos"], s["seq_len"])),
+        (ValueError, lambda: E.ebd_paged_keep(pc, s["cu"], s["pos"][None], s["seq_len"],
+                                              K_layers=s["K"][None])),
+        (ValueError, lambda: E.ebd_paged_keep(pc, s["cu"], s["pos"][None], s["seq_len"],
+                                              K_layers=s["K"].clone()[None],
+                                              V_layers=s["V"][None])),
+        (TypeError, lambda: E.ebd_paged_deal(E.alloc_page_pool(1, s["K"].shape[0], "cuda"), pc,
+                                             torch.ones(1, device="cuda"), 4)),
+        (ValueError, lambda: E.ebd_paged_deal(E.alloc_page_pool(1, 3, "cuda"), pc, ints([1]), 4)),
+        (E.EbdError, lambda: E.ebd_paged_tree_attention(s["q"], pc, s["cu"], 40, s["mask"])),
+        (E.EbdError, lambda: E.ebd_norm_rotary(x, w, pos, tab, eps=0.0)),
+        (E.EbdError, lambda: E.ebd_paged_keep(pc, s["cu"], s["pos"][None], s["seq_len"],
+                                              seq_len_out=s["seq_len"])),
+    ]
+    for i, (error, f) in enumerate(bad):
+        with pytest.raises(error):
+            f()
+            pytest.fail(f"call {i} was not refused")
+
+
 # ---------------------------------------------------------------- together
 @pytest.mark.parametrize("dtype,hq,hkv,d,window", [(torch.bfloat16, 8, 2, 128, 0),
                                                    (torch.float32, 4, 4, 64, 0),

@@ -53,7 +53,7 @@ NORM = dict(dtype=1, T=1, H=2, d=64, x=FAKE, xt=128, xh=64, w=FAKE, wt=1, wh=0, 
             table=FAKE, n_pos=8, rot=64, layout=0, y=FAKE, yt=128, yh=64, st=None, stream=None)
 NORM_BAD = [(dict(dtype=2), 1), (dict(T=-1), 1), (dict(H=0), 1), (dict(d=0), 1), (dict(d=513), 4),
             (dict(x=None), 1), (dict(w=None), 1), (dict(wt=2), 1), (dict(dtype=0), 1),
-            (dict(wh=-1), 1), (dict(eps=0.0), 1), (dict(eps=-1.0), 1), (dict(eps=math.nan), 1),
+            (dict(wh=-1), 1), (dict(eps=0.0), 1), (dict(eps=1e-39), 1), (dict(eps=-1.0), 1), (dict(eps=math.nan), 1),
             (dict(eps=math.inf), 1), (dict(pos=None), 1), (dict(table=FAKE + 4), 1),
             (dict(n_pos=0), 1), (dict(rot=0), 1), (dict(rot=3), 1), (dict(rot=66), 1),
             (dict(layout=2), 1), (dict(layout=1, xt=129), 4)]
@@ -131,6 +131,14 @@ def test_tree_refusals(E):
                       (dict(K_pages=FAKE + 8), 1)]:
         a["c"] = ctypes.byref(good_cache(E, **bad))
         assert call(*a.values()) == code, bad
+
+
+def test_binding_is_bound_to_every_entry_point(E):
+    m = E._call()
+    with pytest.raises(RuntimeError, match="address"):
+        m.bind({})
+    with pytest.raises(TypeError, match="arguments"):
+        m.keep(1, 2)
 
 
 def test_python_refusals(E):
