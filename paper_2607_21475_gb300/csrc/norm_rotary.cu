@@ -9,12 +9,22 @@
 // linear, its transpose is the inverse turn), g = u w and z = x r the gradient is
 //   dx = r (g - z mean(g z)),   dw = sum of u z over the rows that share w.
 //
-// Both directions move rows (forward 2, backward 3 per row; some 7 and 13 FMAs per
-// channel), so HBM bounds them at large sizes, a launch and a chain of loads at small
-// ones.  A row is shared by L lanes, L a power of two, each with U pairs of chunks that
-// turn together, so that a row's sums are log2 L shuffles; a warp takes 32 / L heads
-// of one token at a time, keeps the token's angles and the weight in registers and
-// has two steps' rows in flight.
+// Both directions move rows (forward 2, backward 3 per row), so HBM bounds them at large
+// sizes, a launch and a chain of loads at small ones; in between it is their instructions,
+// which is why the arithmetic is in packed pairs, the weight is multiplied into the turn's
+// factors once a token, and whole turning heads of 64, 128 and 256 channels have forms of
+// their own that ask nothing about a lane's chunks (16k tokens x 28 heads x 128, bf16: 413
+// instructions per warp and 4 rows and 54 us at first, 203 and 39 us now).  A row is shared
+// by L lanes, L a power of two, each with U pairs of chunks that turn together, so that a
+// row's sums are log2 L shuffles; a warp takes 32 / L heads of a token at a time and has
+// three steps' rows on their way through shared memory.  The backward pass has an even share
+// of all steps per warp, and its rows are asked for from token to token; the weight's
+// gradient is summed per lane, per warp, per block and over the blocks, in that fixed order.
+// Measured, bf16, 28 heads x 128: 16384 tokens 38.8 us, 6.3 TB/s (93% of the measured copy
+// peak); gradient of 8192 tokens 34.6 us, 5.2 TB/s (77%: instructions, 57% of the issue
+// slots, and 16 warps per SM, 128 registers each); 8 ragged chunks of 9.4k tokens in all
+// appended (28/4 heads) 37.1 us, 4.8 TB/s; append step of 32 sequences (32/8 heads) 3.3 us.
+// All are programmatic dependents of what precedes them on the stream.
 #include <cuda_runtime.h>
 #include <float.h>
 #include <math.h>

@@ -6,7 +6,9 @@ the scores as page-locked CPU tensors: the library then reads the scores and
 only the kept rows from host memory); it checks shapes, dtypes and
 contiguity, passes raw pointers plus sizes, and raises ``EbdError`` on a
 non-OK status.  Every step of the hot path runs in the library's CUDA
-kernels.  PyTorch supplies device memory and the current stream.
+kernels.  PyTorch supplies device memory and the current stream.  The calls of
+a speculative serving step go through a C++ extension that makes the same checks
+(csrc/binding.cpp); the others through ctypes.
 
 If the compiled library is missing the import of any entry point raises: there
 is no fallback implementation.
