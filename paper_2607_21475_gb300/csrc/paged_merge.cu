@@ -38,39 +38,20 @@ __device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&v)[16]
                    pack_bf16(v[8 * i + 4], v[8 * i + 5]), pack_bf16(v[8 * i + 6], v[8 * i + 7]));
 }
 
-// A lane adds FLIGHT pieces at a time, AHEAD times as many are in flight; kMergeChannels
-// channels of a row.
+// Whether a CTA's record tells of an item that it begins.
+__device__ __forceinline__ bool begins_item(const PagedAttnArgs& a, const PieceRecord& r) {
+  return r.tokens >= 1 && r.tokens <= a.tokens && r.token >= 0 && r.token <= a.n_tokens - r.tokens &&
+         (unsigned)r.h < (unsigned)a.heads;
+}
+
+// Rows row0 .. + 31 and channels kMergeChannels part .. of the item that CTA c0 begins (r), of
+// n pieces.  A lane adds FLIGHT pieces at a time, AHEAD times as many are in flight.  Whole
+// warp.
 template <typename T, int D, int FLIGHT, int AHEAD, int kMergeChannels>
-__global__ void __launch_bounds__(kMergeWarps * 32)
-    paged_merge_kernel(const PagedAttnArgs a, int n_cta) {
-  grid_dependency_wait();
-  const int c0 = blockIdx.x, lane = threadIdx.x & 31;
-  const PieceRecord r = a.rec[c0];
-  // the item goes on through the first pieces of the following CTAs: up to the
-  // first that does not just continue it (32 records at a time)
-  int c1 = c0 + 1;
-  bool on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
-  if (r.tokens < 1 || r.tokens > a.tokens || r.token < 0 || r.token > a.n_tokens - r.tokens ||
-      (unsigned)r.h >= (unsigned)a.heads)
-    return;  // none begun here
-  const int rows = r.tokens * a.slice;
-  // this warp's rows of the slot (its second half starts at row 128) and channels
-  constexpr int kParts = D / kMergeChannels;
-  const int task = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
-  const int part = task % kParts, row0 = task / kParts * 32;
-  const int half_rows = a.half_tokens * a.slice;
-  if (row0 >= (rows > half_rows ? 128 + rows - half_rows : rows)) return;
+__device__ __forceinline__ void merge_rows(const PagedAttnArgs& a, const PieceRecord& r, int c0,
+                                           int n, int row0, int part, int lane) {
   const HeadSlice hs = head_slice(a, r.h);
-  for (;;) {
-    const uint32_t off = ~__ballot_sync(0xffffffffu, on);
-    if (off) {
-      c1 += __ffs(off) - 1;
-      break;
-    }
-    c1 += 32;
-    on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
-  }
-  const int n = c1 - c0 + 1;
+  const int rows = r.tokens * a.slice, half_rows = a.half_tokens * a.slice;
   // lanes: `wide` rows, 32 / wide lanes share a row's pieces
   const int wide = rows <= 8 ? 8 : rows <= 16 ? 16 : 32;
   const int row = row0 + (lane & (wide - 1)), k0 = lane / wide, by = 32 / wide;
@@ -142,6 +123,91 @@ __global__ void __launch_bounds__(kMergeWarps * 32)
   if (a.lse && part == 0) a.lse[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
+// 32-row tasks of an item (its second half starts at row 128 of the slot).
+__device__ __forceinline__ int merge_blocks(const PagedAttnArgs& a, int tokens) {
+  const int rows = tokens * a.slice, half_rows = a.half_tokens * a.slice;
+  return ((rows > half_rows ? 128 + rows - half_rows : rows) + 31) / 32;
+}
+
+// Block (x, y): tasks kMergeWarps y .. of the item that CTA x begins, if it does.
+template <typename T, int D, int FLIGHT, int AHEAD, int kMergeChannels>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    paged_merge_kernel(const PagedAttnArgs a, int n_cta) {
+  grid_dependency_wait();
+  const int c0 = blockIdx.x, lane = threadIdx.x & 31;
+  const PieceRecord r = a.rec[c0];
+  // the item goes on through the first pieces of the following CTAs: up to the
+  // first that does not just continue it (32 records at a time)
+  int c1 = c0 + 1;
+  bool on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
+  if (!begins_item(a, r)) return;
+  constexpr int kParts = D / kMergeChannels;
+  const int task = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
+  if (task / kParts >= merge_blocks(a, r.tokens)) return;
+  for (;;) {
+    const uint32_t off = ~__ballot_sync(0xffffffffu, on);
+    if (off) {
+      c1 += __ffs(off) - 1;
+      break;
+    }
+    c1 += 32;
+    on = c1 + lane < n_cta - 1 && a.rec[c1 + lane].cont == 1;
+  }
+  merge_rows<T, D, FLIGHT, AHEAD, kMergeChannels>(a, r, c0, c1 - c0 + 1, task / kParts * 32,
+                                              task % kParts, lane);
+}
+
+// Few items of many pieces: block (x, y) has tasks of 4 channels of the x-th split item, which
+// every warp finds among all records, and 16 pieces are in flight.
+constexpr int kFewRecords = 160;
+template <typename T, int D>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+    paged_merge_few_kernel(const PagedAttnArgs a, int n_cta) {
+  grid_dependency_wait();
+  constexpr int kWords = kFewRecords / 32, kParts = D / 4;
+  const int lane = threadIdx.x & 31;
+  PieceRecord rec[kWords];
+#pragma unroll
+  for (int q = 0; q < kWords; ++q) {
+    rec[q] = PieceRecord{0, 0, 0, 0};
+    if (q * 32 + lane < n_cta) rec[q] = a.rec[q * 32 + lane];
+  }
+  int left = blockIdx.x, c0 = -1, n = 0;
+  bool open = false;  // the item may go on
+  PieceRecord r = {0, 0, 0, 0};
+#pragma unroll
+  for (int q = 0; q < kWords; ++q) {
+    const int c = q * 32 + lane;
+    uint32_t from = 0;  // of the word: records after c0
+    if (c0 < 0) {
+      uint32_t begun = __ballot_sync(0xffffffffu, c < n_cta - 1 && begins_item(a, rec[q]));
+      if (left >= __popc(begun)) {
+        left -= __popc(begun);
+        continue;
+      }
+      for (; left > 0; --left) begun &= begun - 1;
+      const int src = __ffs(begun) - 1;
+      c0 = q * 32 + src;
+      r.h = __shfl_sync(0xffffffffu, rec[q].h, src);
+      r.token = __shfl_sync(0xffffffffu, rec[q].token, src);
+      r.tokens = __shfl_sync(0xffffffffu, rec[q].tokens, src);
+      open = true;
+      n = 2;  // the piece that begins the item and the next CTA's
+      from = src + 1;
+    }
+    if (!open || from == 32) continue;
+    const uint32_t on =
+        __ballot_sync(0xffffffffu, c < n_cta - 1 && rec[q].cont == 1) >> from;
+    const int more = on == 0xffffffffu ? 32 : __ffs(~on) - 1;
+    n += min(more, 32 - (int)from);
+    open = more >= 32 - (int)from;
+  }
+  if (c0 < 0) return;
+  const int task = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
+  if (task / kParts >= merge_blocks(a, r.tokens)) return;
+  merge_rows<T, D, 2, 8, 4>(a, r, c0, n, task / kParts * 32, task % kParts, lane);
+}
+
 size_t paged_split_bytes(int n_cta, int slot_rows, int head_dim) {
   const size_t rows = (size_t)2 * n_cta * slot_rows;
   return align_up(n_cta * sizeof(PieceRecord), 256) + align_up(rows * 4, 256) +
@@ -160,28 +226,32 @@ void paged_split_layout(PagedAttnArgs& a, void* ws, int n_cta) {
 
 template <typename T, int D, int FLIGHT, int AHEAD, int CHANNELS>
 static ebd_status launch_merge_c(const PagedAttnArgs& a, int n_cta, cudaStream_t s) {
-  const int rows = a.slot_rows > 32 ? a.slot_rows : 32;
-  const int tasks = (rows + 31) / 32 * (D / CHANNELS);
-  const dim3 grid(n_cta - 1, (tasks + kMergeWarps - 1) / kMergeWarps);
-  return launch_dependent(paged_merge_kernel<T, D, FLIGHT, AHEAD, CHANNELS>, grid,
+  const int tasks = (a.slot_rows + 31) / 32 * (D / CHANNELS);
+  return launch_dependent(paged_merge_kernel<T, D, FLIGHT, AHEAD, CHANNELS>,
+                          dim3(n_cta - 1, (tasks + kMergeWarps - 1) / kMergeWarps),
                           kMergeWarps * 32, 0, s, a, n_cta);
 }
 
+// Items of few rows often have many pieces, and there are few warps then.  Where the items (a
+// bound of them is known here) are so few that each has four pieces and more, warps have four
+// channels each and more pieces in flight: a 6k-token step (7 rows an item) 12.8 -> 12.4 us,
+// with the item found among the records 13.2; a tree of 112 rows over 6k positions, 24 pieces
+// an item, 18.3 -> 16.4 and so found, in 64 blocks instead of 2416, 15.2.  Elsewhere that
+// takes longer (short float32 prompts 34.3 -> 35.7).  A result's bits do not depend on it.
 template <typename T, int D>
 static ebd_status launch_merge_t(const PagedAttnArgs& a, int n_cta, cudaStream_t s) {
-  // items of few rows often have many pieces, and there are few warps then.  Where the items
-  // (a bound of them is known here) are so few that each has four pieces and more, four
-  // channels to a warp and eight pieces in flight: a tree of 112 rows over 6k positions, 24
-  // pieces an item, 18.3 -> 16.4 us, a 6k-token step 12.8 -> 12.4.  Elsewhere the blocks
-  // that it takes cost more (short float32 prompts 34.3 -> 35.7).  A result's bits do not
-  // depend on it.
-  const int per_seq = (a.max_new + a.tokens - 1) / a.tokens;
-  const bool few = (long long)a.pv.batch * a.heads * per_seq * 4 <= n_cta;
+  const int blocks = (a.slot_rows + 31) / 32;
+  const long long items =
+      (long long)a.pv.batch * a.heads * ((a.max_new + a.tokens - 1) / a.tokens);
+  const bool few = items * 4 <= n_cta;
   if (a.slot_rows <= 32)
     return few ? launch_merge_c<T, D, 4, 2, 4>(a, n_cta, s)
                : launch_merge_c<T, D, 4, 1, 16>(a, n_cta, s);
-  return few ? launch_merge_c<T, D, 2, 4, 4>(a, n_cta, s)
-             : launch_merge_c<T, D, 2, 1, 16>(a, n_cta, s);
+  if (few && n_cta <= kFewRecords)
+    return launch_dependent(paged_merge_few_kernel<T, D>,
+                            dim3((unsigned)items, (blocks * (D / 4) + kMergeWarps - 1) / kMergeWarps),
+                            kMergeWarps * 32, 0, s, a, n_cta);
+  return launch_merge_c<T, D, 2, 1, 16>(a, n_cta, s);
 }
 
 ebd_status launch_paged_merge(const PagedAttnArgs& a, bool bf16, int head_dim, int n_cta,
