@@ -602,6 +602,7 @@ ebd_status ebd_paged_gather(const ebd_paged_cache* cache, const int32_t* idx_c,
  *   positions        device [n_tokens] int32 out, nullable
  *   slots            device [n_tokens] int64 out, nullable
  *   dev_status       device int32, required
+ * At most 65535 sequences; n_tokens and n_pages up to 2^31 - 2^16 (EBD_ERR_UNSUPPORTED).
  */
 ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n_pages, int32_t max_blocks,
                           int32_t n_tokens, int32_t window, const int32_t* n_new,
@@ -684,7 +685,8 @@ ebd_status ebd_paged_append_norm(
  *   max_new    as for ebd_paged_attention; at most 32 mask_words and 1024
  *   mask       device [n_tokens][mask_words] out;  positions  device [n_tokens] out
  *   dev_status device int32, nullable
- * Tokens that cu_new gives to no sequence, or past max_new, keep what both held
+ * Places past the last offset are empty (as ebd_paged_deal leaves them) and keep what both
+ * held; so do tokens that cu_new gives to no sequence before it, or past max_new
  * (EBD_DEV_RANGE).
  */
 ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t max_new, const int32_t* parents,
@@ -702,7 +704,8 @@ ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t max_new, cons
  *   positions  device [n_tokens], needed with a window: from the tree's beginning, base =
  *              seq_len[b] - (new tokens of b), to base + the token's number
  *              (otherwise clamped, EBD_DEV_RANGE)
- * Everything else, the workspace too, as for ebd_paged_attention.
+ * Places past the last offset are empty: y and lse stay as they were, and no status is
+ * raised.  Everything else, the workspace too, as for ebd_paged_attention.
  */
 ebd_status ebd_paged_tree_attention(const ebd_paged_cache* cache, int32_t n_tokens,
                                     int32_t max_new, int32_t n_q_heads, const int32_t* cu_new,

@@ -183,7 +183,7 @@ __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, i
   const int b = base + lane;
   sp = SeqSpan{};
   if (b < a.pv.batch) {
-    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
+    sp = seq_span<TREE>(a.pv, a.cu, b, a.n_tokens, a.max_new);
     if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
   }
   mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);

@@ -118,8 +118,8 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // TREE: new tokens see each other by a mask.  A row's 64 bits for a tile that touches the
 // tree are found while the tile's product runs, and select its logits; the other tiles take
 // the same path as causal ones, and so does the time (one 6k-token sequence, 16 drafted
-// tokens, 28/4 heads x 128: 16.4 us with either mask; trees of 40-64 tokens of 32 dialogues
-// of 2k-32k, 32/8 x 128: 422 us at the full clock, 440-500 under the power cap, tensor pipe
+// tokens, 28/4 heads x 128: 15.2 us, 14.9 causal; trees of 40-64 tokens of 32 dialogues
+// of 2k-32k, 32/8 x 128: 422 us at the full clock, 440-514 under the power cap, tensor pipe
 // 75% active, its 256-row tiles 81% filled).
 template <int D, bool TREE>
 __global__ void __launch_bounds__(kTcAttnThreads, 1)

@@ -535,6 +535,8 @@ extern "C" ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n
   if (page_size < 8 || page_size > 1024 || (page_size & (page_size - 1)) != 0)
     return EBD_ERR_UNSUPPORTED;
   if ((long long)max_blocks * page_size > 0x7ff00000LL || batch > 65535) return EBD_ERR_UNSUPPORTED;
+  // (a number a step past the last, and twice a sum's bound, still fit 31 and 32 bits)
+  if (n_tokens > 0x7fff0000 || n_pages > 0x7fff0000) return EBD_ERR_UNSUPPORTED;
   if (!n_new || !seq_len || !held || !n_free || !free_pages || !block_table || !seq_len_out ||
       !held_out || !n_free_out || !cu_new || !dev_status)
     return EBD_ERR_INVALID;

@@ -37,7 +37,7 @@ constexpr int kKeepMoves = 32;   // path entries placed at a time
 // Block (x, b): tokens kTreeWarps x .. of sequence b.
 __global__ void __launch_bounds__(kTreeWarps * 32)
     tree_masks_kernel(const int32_t* __restrict__ parents, const int32_t* __restrict__ cu,
-                      const int32_t* __restrict__ seq_len, int batch, int n_tokens, int max_new,
+                      const int32_t* __restrict__ seq_len, int n_tokens, int max_new,
                       int words, int window, uint32_t* __restrict__ mask,
                       int32_t* __restrict__ positions, int32_t* dev_status) {
   __shared__ int parent_s[kTreeMost];
@@ -47,8 +47,8 @@ __global__ void __launch_bounds__(kTreeWarps * 32)
   const int c0 = cu[b], c1 = cu[b + 1], len = seq_len[b];
   const int t0 = min(max(c0, 0), n_tokens), t1 = min(max(c1, t0), n_tokens);
   const int n = min(t1 - t0, max_new);
-  const bool odd = t0 != c0 || t0 + n != c1 || len < n || (b == 0 && c0 != 0) ||
-                   (b == batch - 1 && c1 != n_tokens);
+  // (places past the last offset are empty, as a deal leaves them)
+  const bool odd = t0 != c0 || t0 + n != c1 || len < n || (b == 0 && c0 != 0);
   if (odd && blockIdx.x == 0 && threadIdx.x == 0) raise_status(dev_status, EBD_DEV_RANGE);
   const int upto = min(n, first + kTreeWarps);  // a line of ancestors goes down
   if (first >= upto) return;
@@ -175,7 +175,7 @@ extern "C" ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t ma
   if (n_tokens == 0) return EBD_OK;
   if (!parents || !cu_new || !seq_len || !mask || !positions) return EBD_ERR_INVALID;
   return launch_dependent(tree_masks_kernel, dim3((max_new + kTreeWarps - 1) / kTreeWarps, batch),
-                          kTreeWarps * 32, 0, (cudaStream_t)stream, parents, cu_new, seq_len, batch,
+                          kTreeWarps * 32, 0, (cudaStream_t)stream, parents, cu_new, seq_len,
                           n_tokens, max_new, mask_words, window, mask, positions, dev_status);
 }
 

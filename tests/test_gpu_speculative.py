@@ -713,6 +713,29 @@ def test_rows_of_no_sequence_stay(E, dtype):
         assert (y[t] == 5).all() and (lse[t] == 6).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("case", [3, 8])
+def test_empty_places_behind_the_last_sequence(E, dtype, case):
+    """Packed arrays longer than the offsets say: the rest stays, and nothing is reported."""
+    s = tree_case(E, case, dtype)
+    pc = cache(E, s)
+    y, lse = call(E, s, pc)
+    T = s["T"]
+    q = torch.cat([s["q"], torch.full_like(s["q"][:5], math.nan)])
+    mask = torch.cat([s["mask"], torch.full_like(s["mask"][:1], -1).expand(5, -1)])
+    y2, lse2 = torch.full_like(q, 3), torch.full(q.shape[:2], 4.0, device="cuda")
+    E.ebd_paged_tree_attention(q, pc, s["cu"], s["max_new"], mask, y=y2, lse=lse2)
+    assert torch.equal(y2[:T], y) and torch.equal(lse2[:T], lse)
+    assert (y2[T:] == 3).all() and (lse2[T:] == 4).all()
+    m, p, st = torch.full_like(mask, 7), torch.full((T + 5,), 8, device="cuda").int(), ints([0])
+    parents = torch.cat([s["parents"], ints([99] * 5)])
+    E.ebd_tree_masks(parents, s["cu"], s["seq_len"], s["max_new"], mask=m, positions=p,
+                     dev_status=st)
+    assert torch.equal(m[:T], s["mask"]) and torch.equal(p[:T], s["pos"])
+    assert (m[T:] == 7).all() and (p[T:] == 8).all()
+    assert st.item() == 0 and pc.dev_status.item() == 0
+
+
 def test_graph_and_stream_of_tree_attention(E):
     """A captured step follows masks, lengths and pages; the other stream's buffers hold."""
     s = tree_case(E, 4, torch.bfloat16)
@@ -1023,6 +1046,84 @@ def test_a_served_run_of_trees(E, dtype, hq, hkv, d, window):
         pc.seq_len.copy_(E.ebd_paged_keep(pc, cu, ints(path), ints(kept)))
         assert pc.seq_len.tolist() == [len(x) for x in story]
     assert pc.dev_status.item() == 0
+
+
+@pytest.mark.parametrize("dtype,d", [(torch.bfloat16, 128), (torch.float32, 64)])
+def test_a_captured_step_is_the_eager_one(E, dtype, d):
+    """A whole step and its norms' gradient in one graph, replayed over changing requests
+    and inputs: every kernel waits for the one before it."""
+    B, hq, hkv, P, n, cap, eps = 5, 8, 2, 8, 12, 60, 1e-6
+    tab = table_of(E, d, 400)
+    w = torch.rand(d, device="cuda").to(dtype) + 0.5
+    x = {k: torch.zeros(v, dtype=t, device="cuda") for k, v, t in [
+        ("n_new", (B,), torch.int32), ("parents", (cap,), torch.int32),
+        ("path", (B, 4), torch.int32), ("kept", (B,), torch.int32),
+        ("qkv", (cap, hq + 2 * hkv, d), dtype), ("dy", (cap, hq, d), dtype)]}
+
+    def world():
+        pc = E.alloc_paged(B, hkv, 150, P, d, 40, dtype, "cuda")
+        pc.K_pages.zero_()
+        pc.V_pages.zero_()
+        o = {k: torch.zeros(v, dtype=t, device="cuda") for k, v, t in [
+            ("cu_new", (B + 1,), torch.int32), ("positions", (cap,), torch.int32),
+            ("slots", (cap,), torch.int64), ("served", (B,), torch.int32),
+            ("mask", (cap, 1), torch.int32), ("tpos", (cap,), torch.int32),
+            ("q", (cap, hq, d), dtype), ("y", (cap, hq, d), dtype),
+            ("lse", (cap, hq), torch.float32), ("len", (B,), torch.int32),
+            ("dx", (cap, hq, d), dtype), ("dw", (d,), torch.float32)]}
+        return pc, E.alloc_page_pool(B, 150, "cuda"), o
+
+    def step(pc, pool, o):
+        q, k, v = x["qkv"][:, :hq], x["qkv"][:, hq:hq + hkv], x["qkv"][:, hq + hkv:]
+        E.ebd_paged_deal(pool, pc, x["n_new"], cap, **{i: o[i] for i in (
+            "cu_new", "positions", "slots", "served")})
+        E.ebd_tree_masks(x["parents"], o["cu_new"], pc.seq_len, n, mask=o["mask"],
+                         positions=o["tpos"])
+        E.ebd_paged_append_norm(pc, k, v, k_weight=w, q=q, q_weight=w, q_out=o["q"],
+                                slots=o["slots"], positions=o["tpos"], table=tab, eps=eps)
+        E.ebd_paged_tree_attention(o["q"], pc, o["cu_new"], n, o["mask"], y=o["y"], lse=o["lse"])
+        E.ebd_norm_rotary_backward(x["dy"], q, w, o["tpos"], tab, dx=o["dx"], dweight=o["dw"])
+        E.ebd_paged_keep(pc, o["cu_new"], x["path"], x["kept"], seq_len_out=o["len"])
+        pc.seq_len.copy_(o["len"])
+
+    eager, other = world(), world()
+    first = [t.clone() for t in (other[0].K_pages, other[0].V_pages, other[0].block_table,
+                                 other[0].seq_len, other[1].free_pages, other[1].n_free,
+                                 other[1].held)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(*other)
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(*other)
+    for t, f in zip((other[0].K_pages, other[0].V_pages, other[0].block_table, other[0].seq_len,
+                     other[1].free_pages, other[1].n_free, other[1].held), first):
+        t.copy_(f)
+    for t in other[2].values():
+        t.zero_()
+    rng, gen = random.Random(3), torch.Generator(device="cuda").manual_seed(4)
+    for i in range(8):
+        new = [rng.randint(0, n) if i else n for _ in range(B)]
+        if i == 4:
+            new[2] = -1
+        par = [p for b in range(B) for p in S.random_parents([max(new[b], 0)], 7 * i + b)]
+        x["n_new"].copy_(ints(new))
+        x["parents"].zero_()
+        x["parents"][:len(par)] = ints(par)
+        x["kept"].copy_(ints([min(max(v, 0), 1 + b % 4) for b, v in enumerate(new)]))
+        x["path"].copy_(ints([[0, 1, 2, 3]] * B))
+        for k in ("qkv", "dy"):
+            x[k].copy_(torch.randn(x[k].shape, generator=gen, device="cuda"))
+        step(*eager)
+        g.replay()
+        for k in eager[2]:
+            assert torch.equal(eager[2][k], other[2][k]), (i, k)
+        assert other[0].dev_status.item() == 0  # empty places are no mistake
+        for a, b in ((eager[0].K_pages, other[0].K_pages), (eager[0].V_pages, other[0].V_pages),
+                     (eager[0].seq_len, other[0].seq_len), (eager[1].held, other[1].held)):
+            assert torch.equal(a, b), i
 
 
 def test_example_runs(E):

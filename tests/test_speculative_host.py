@@ -43,7 +43,8 @@ def test_deal_refusals(E):
     run(a, E.lib().ebd_paged_deal, [
         (dict(B=0), 1), (dict(pages=0), 1), (dict(blocks=0), 1), (dict(n=-1), 1),
         (dict(window=-1), 1), (dict(page=24), 4), (dict(page=4), 4), (dict(page=2048), 4),
-        (dict(blocks=1 << 28), 4), (dict(B=65536), 4), (dict(len_out=FAKE + 4), 1),
+        (dict(blocks=1 << 28), 4), (dict(B=65536), 4), (dict(n=0x7fff0001), 4),
+        (dict(pages=0x7fff0001), 4), (dict(len_out=FAKE + 4), 1),
         (dict(held_out=FAKE + 12), 1)] + [(dict([(k, None)]), 1) for k in (
             "new", "len", "held", "free", "list", "bt", "len_out", "held_out", "free_out", "cu",
             "st")])
@@ -51,7 +52,7 @@ def test_deal_refusals(E):
 
 NORM = dict(dtype=1, T=1, H=2, d=64, x=FAKE, xt=128, xh=64, w=FAKE, wt=1, wh=0, eps=1e-6, pos=FAKE,
             table=FAKE, n_pos=8, rot=64, layout=0, y=FAKE, yt=128, yh=64, st=None, stream=None)
-NORM_BAD = [(dict(dtype=2), 1), (dict(T=-1), 1), (dict(H=0), 1), (dict(d=0), 1), (dict(d=513), 4),
+NORM_BAD = [(dict(dtype=2), 1), (dict(T=-1), 1), (dict(T=0x7fffff01), 4), (dict(H=0), 1), (dict(d=0), 1), (dict(d=513), 4),
             (dict(x=None), 1), (dict(w=None), 1), (dict(wt=2), 1), (dict(dtype=0), 1),
             (dict(wh=-1), 1), (dict(eps=0.0), 1), (dict(eps=1e-39), 1), (dict(eps=-1.0), 1), (dict(eps=math.nan), 1),
             (dict(eps=math.inf), 1), (dict(pos=None), 1), (dict(table=FAKE + 4), 1),
