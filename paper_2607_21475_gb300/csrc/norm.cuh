@@ -21,7 +21,7 @@
 // A warp takes 32 / L heads of a token at a time and has three steps' rows on their way
 // through shared memory.  The backward pass has an even share of all steps per warp, and its
 // rows are asked for from token to token; the weight's gradient is summed per lane, per
-// warp, per block and over the blocks, in that fixed order.
+// warp, per block and over the blocks (few rows: of one cluster), in that fixed order.
 // Measured, bf16, 28 heads x 128: 16384 tokens 38.4 us in either layout, 6.3 TB/s (94% of the
 // measured copy peak), half of each head turning 43.4, a weight per head 51.9; gradient of
 // 8192 tokens 34.8 us, 5.2 TB/s (77%: instructions, 57% of the issue slots, and 16 warps per

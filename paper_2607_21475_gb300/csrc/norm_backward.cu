@@ -5,10 +5,12 @@ namespace ebd {
 
 // PER_HEAD: a block has one head (blockIdx.y), a warp's groups of lanes have tokens; else
 // they have heads of a token.  Leaves the block's sum of the weight's gradient in
-// partial[blockIdx.x][blockIdx.y][d].
+// partial[blockIdx.x][blockIdx.y][d]; without partial the grid's rows of blocks are clusters,
+// which add their blocks' sums up through distributed shared memory.
 template <typename T, int VEC, bool PAIRS, int U, bool PER_HEAD, int FL, bool ALL>
 __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, U, VEC))
-    norm_backward_kernel(const NormArgs a, float* __restrict__ partial) {
+    norm_backward_kernel(const NormArgs a, float* __restrict__ partial,
+                         float* __restrict__ dweight) {
   extern __shared__ __align__(16) unsigned char smem[];  // the rows' ring; then, in its place:
   float* red = reinterpret_cast<float*>(smem);           // [warps][units of all lanes][2 VEC]
   using Ring = RowRing<T, VEC, U, 2>;
@@ -153,7 +155,9 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
       if (g == 0) red[warp * wide + (sub + L * j) * 2 * VEC + i] = v;
     }
   __syncthreads();
-  float* dst = partial + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.head_dim;
+  float* sum = red + kNormWarps * wide;  // (clusters)
+  float* dst =
+      partial ? partial + ((size_t)blockIdx.x * gridDim.y + blockIdx.y) * a.head_dim : sum;
   for (int k = threadIdx.x; k < wide; k += kNormWarps * 32) {
     const int u = k / (2 * VEC), i = k - u * 2 * VEC, e = i % VEC;
     if (!PAIRS && u >= a.units) continue;
@@ -168,6 +172,17 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     for (int x = 0; x < kNormWarps; ++x) v += red[x * wide + k];
     dst[c] = v;
   }
+  if (partial) return;
+  __syncwarp();
+  cluster_barrier();
+  const uint32_t ranks = gridDim.x, rank = cluster_rank();
+  for (int c = rank * kNormWarps * 32 + threadIdx.x; c < a.head_dim; c += ranks * kNormWarps * 32) {
+    float v = 0.f;
+    for (uint32_t r = 0; r < ranks; ++r) v += ld_cluster_f32(cluster_map(smem_u32(sum + c), r));
+    dweight[(size_t)blockIdx.y * a.head_dim + c] = v;
+  }
+  __syncwarp();
+  cluster_barrier();  // no block leaves while another reads its sum
 }
 
 // dweight[i] = sum over the n blocks of partial[block][i], i < total; 32 columns per block,
@@ -203,24 +218,55 @@ static int norm_back_blocks(long long steps, int heads) {
   return (int)(want < most ? want : most);
 }
 
+constexpr int kNormCluster = 16;  // blocks of a cluster at most
+// Steps (of a row of blocks) that one cluster takes: beyond it the kernels of two launches
+// are shorter by more than the second launch's host time (1.5 us).  One cluster against two
+// launches, us: 28 heads x 128, bf16, 1 token 4.0 / 4.3, 8 (56 steps) 4.6 / 4.6, 36 (252)
+// 5.4 / 5.0, 146 (1022) 9.2 / 6.2; a weight per head, 4 x 64, f32, 1021 tokens (256) 4.6 /
+// 4.4, 2048 (512) 6.2 / 4.8.
+constexpr int kNormFewSteps = 256;
+
 template <typename T, int VEC, bool PAIRS, int U, int FL, bool ALL>
 ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s) {
   const bool per_head = a.wx.hs != 0;
   const int per_warp = 32 / a.lanes;
   const long long steps = per_head ? (a.n_tokens + per_warp - 1) / per_warp
                                    : (long long)a.n_tokens * ((a.n_x + per_warp - 1) / per_warp);
-  const int blocks = norm_back_blocks(steps, per_head ? a.n_x : 1);
-  const int total = (per_head ? a.n_x : 1) * a.head_dim;
-  const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4, ring = RowRing<T, VEC, U, 2>::kBytes;
-  const int smem = sums > ring ? sums : ring;
-  const dim3 grid(blocks, per_head ? a.n_x : 1);
+  const int rows = per_head ? a.n_x : 1;  // of blocks: those that share a weight's gradient
+  // Few steps: a cluster per row, which adds its sums up itself, in place of a second launch.
+  const bool few = steps <= kNormFewSteps;
+  const int most = norm_back_blocks(steps, rows);
+  const int blocks = few ? (int)((steps + kNormWarps - 1) / kNormWarps < kNormCluster
+                                     ? (steps + kNormWarps - 1) / kNormWarps
+                                     : kNormCluster)
+                         : most;
+  const int total = rows * a.head_dim;
+  const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4 + (few ? a.head_dim * 4 : 0);
+  const int ring = RowRing<T, VEC, U, 2>::kBytes, smem = sums > ring ? sums : ring;
   auto kern = per_head ? norm_backward_kernel<T, VEC, PAIRS, U, true, FL, ALL>
                        : norm_backward_kernel<T, VEC, PAIRS, U, false, FL, ALL>;
   if (smem > 48 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  const ebd_status st = launch_dependent(kern, grid, kNormWarps * 32, smem, s, a, bw.partial);
-  if (st != EBD_OK) return st;
+  if (blocks > 8 && few &&
+      cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+    return EBD_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks, rows);
+  cfg.blockDim = dim3(kNormWarps * 32);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = blocks;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = few ? 2 : 1;
+  float* partial = few ? nullptr : bw.partial;
+  const ebd_status st = cuda_status(cudaLaunchKernelEx(&cfg, kern, a, partial, bw.dweight));
+  if (st != EBD_OK || few) return st;
   return launch_dependent(norm_weight_reduce_kernel, dim3((total + 31) / 32), kReduceWarps * 32, 0, s,
                           (const float*)bw.partial, blocks, total, bw.dweight);
 }
