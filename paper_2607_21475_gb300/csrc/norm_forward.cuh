@@ -168,7 +168,11 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(norm_forward_bloc
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         f[j].template turn<PAIRS>(place.turn(j), place.turn_all(j), inv, x[j]);
-        narrow<T, VEC, PAIRS>(x[j], r[0][j]);
+        Piece<T, VEC> out;
+        narrow<T, VEC, PAIRS>(x[j], out);
+        // (what is neither normalised nor turned is copied: arithmetic would flush subnormals)
+        if (!APPEND || normed || place.turn(j)) r[0][j].a = out.a;
+        if (!APPEND || normed || place.turn_all(j)) r[0][j].b = out.b;
       }
     }
 #pragma unroll

@@ -432,6 +432,39 @@ def test_append_without_weights_is_the_plain_append(E):
     assert torch.equal(s["V"][at, :, off], V1[at, :, off])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("d,rot", [(128, 32), (128, 128), (64, 32), (80, 40), (96, 20), (10, 6), (256, 64)])
+def test_append_without_weights_copies_what_does_not_turn(E, dtype, layout, d, rot):
+    """Channels that stay come as they went, whatever they hold; the others turned (three
+    float32 roundings of their terms' size and one to the type), and in 16-byte accesses bit
+    for bit as the plain append turns them."""
+    s = R.make([5, 3], [9, 40], 2, 2, d, 16, dtype, 6)
+    pc, tab = cache(E, s), table_of(E, rot, 200)
+    lay = E.EBD_ROTARY_HALF if layout == "half" else E.EBD_ROTARY_PAIRS
+    for v in (s["q"], s["k"], s["v"]):
+        odd = [-0.0, math.inf, -math.inf, 1e-40, -3e-39, 3e38]
+        for i, x in enumerate(odd if rot < d else []):
+            v[i % 5, :, rot + i % (d - rot)] = x
+    q1, q2 = (torch.empty((8, 2, d), dtype=dtype, device="cuda") for _ in range(2))
+    E.ebd_paged_append(pc, s["k"], s["v"], s["cu"], table=tab, layout=lay, q=s["q"], q_out=q1)
+    K1, V1 = s["K"].clone(), s["V"].clone()
+    E.ebd_paged_append_norm(pc, s["k"], s["v"], cu_new=s["cu"], table=tab, layout=lay, q=s["q"],
+                            q_out=q2)
+    bits = torch.int32 if dtype == torch.float32 else torch.int16
+    wide = 128 // torch.finfo(dtype).bits  # elements of a 16-byte access
+    part = wide if layout == "pairs" else 2 * wide
+    same = d if rot % part == 0 and d % wide == 0 else d - rot
+    for a, b in ((q1, q2), (K1, s["K"]), (V1, s["V"])):
+        a, b = a[..., d - same:].contiguous(), b[..., d - same:].contiguous()
+        assert torch.equal(a.view(bits), b.view(bits))
+    pos, at, off = slots_of(s, [5, 3], [9, 40], 16)
+    cs = tab[pos.long()]
+    for x, y in ((s["q"], q2), (s["k"], s["K"][at, :, off])):
+        x, y = x[..., :rot], y[..., :rot]
+        within(y, R.rotate(x, cs, layout), 4 * U * S.magnitudes(x.double(), cs, layout) + 1e-37, dtype)
+
+
 def test_append_of_a_tree_turns_to_its_positions(E):
     """By offsets and by slots; norms of one of the two only."""
     new, total = [9, 4], [30, 4]
