@@ -347,8 +347,10 @@ __device__ __forceinline__ void load_weight(const NormWeight& w, int h, int c1, 
   else load(Piece<__nv_bfloat16, VEC>{});
 }
 
-// 2^-64: rows whose sum of squares leaves float32's range are scaled by it first.
-constexpr float kRowScale = 5.421010862427522e-20f;
+// 2^-70: rows whose sum of squares leaves float32's range are scaled by it first.  Values are
+// below 2^128, so those of a scaled row are below 2^58 and 512 squares of them below 2^125;
+// one of such a row's values is at least 2^59.5, and 2^-21 when scaled and squared.
+constexpr float kRowScale = 8.470329472543003e-22f;
 
 // Rows on their way to a warp, N of them to a step (the backward pass: x and dy): kAhead
 // steps are asked for ahead.  Wide chunks wait in shared memory, where their number costs

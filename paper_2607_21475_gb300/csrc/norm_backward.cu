@@ -123,8 +123,8 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     if (!live) continue;
     T* out = (T*)a.y.p + at.t * a.y.ts + at.h * a.y.hs;
     const float inv = __frsqrt_rn(fmaf(ss, a.inv_d, eps));
-    const float2 inv2 = both(inv), back = both(inv * scale);
-    const float2 mean = both(-gx * inv * a.inv_d * (inv * scale));  // -r mean of g z
+    const float2 inv2 = both(inv);
+    const float2 mean = both(-gx * inv * a.inv_d * inv);  // -r mean of g z, up to the row's scale
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       each_two<VEC>(x[j], [&](int i, float2& lo, float2& hi) {
@@ -134,9 +134,14 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
         const float2 a1 = __ffma2_rn(u1, z1, two(acc[j].hi, i));
         acc[j].lo[i] = a0.x, acc[j].hi[i] = a1.x;
         if constexpr (VEC > 1) acc[j].lo[i + 1] = a0.y, acc[j].hi[i + 1] = a1.y;
-        lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), back));
-        hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), back));
+        lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), inv2));
+        hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), inv2));
       });
+      if (scale != 1.f)  // (last: r itself may lie below float32's normal numbers)
+        each_two<VEC>(x[j], [&](int, float2& lo, float2& hi) {
+          lo = __fmul2_rn(lo, both(scale));
+          hi = __fmul2_rn(hi, both(scale));
+        });
       narrow<T, VEC, PAIRS>(x[j], r[0][j]);
       if (place.first(j)) store_chunk<T, VEC>(out + place.c1[j], r[0][j].a);
       if (place.second(j)) store_chunk<T, VEC>(out + place.c2[j], r[0][j].b);

@@ -1,0 +1,71 @@
+"""A speculative step's operators at the ends of their ranges, against the plain forms and
+with the bounds of test_gpu_speculative.py (u = 2^-24)."""
+import pytest
+import torch
+
+import paged_ref as R
+from test_gpu_speculative import (cache, check_grad, check_normed, norm_inputs, slots_of,
+                                  table_of)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def E():
+    from paper_2607_21475_gb300 import ebd
+    ebd.lib()
+    return ebd
+
+
+# ---------------------------------------------------------------- rows of any finite size
+# Powers of two only scale a row exactly, so the bounds of ordinary rows hold; what a row of
+# such values leaves below 1e-37 is the bounds' own slack.
+def sized_rows(x, sizes):
+    """Row t of x scaled so that its largest value has the t-th size; signs and the values'
+    proportions stay."""
+    big = x.double().abs().amax(-1, keepdim=True)
+    s = torch.tensor(sizes, dtype=torch.float64, device="cuda")[:, None, None]
+    return (x.double() / big * s).to(x.dtype)
+
+
+LARGE = [(64, 64), (128, 128), (128, 32), (80, 20), (512, 0), (512, 512)]
+
+
+def large_rows(E, d, rot, dtype, per_head=False):
+    top = torch.finfo(dtype).max
+    sizes = [2.0 ** 58, 2.0 ** 59.6, 2.0 ** 64, 1e30, 1e38, top, top, top, top, 1.0]
+    x, dy, w, pos = norm_inputs(len(sizes), 3, d, dtype, per_head, d + rot)
+    x = sized_rows(x, sizes)
+    x[6] = torch.where(x[6] < 0, -top, top).to(dtype)  # every value the largest
+    x[7] = torch.where(x[7] < 0, -1e38, 1e38).to(dtype)
+    x[8] = 1
+    x[8, :, d // 2] = -top
+    return x, dy * 1e6, w, pos, table_of(E, rot, 4000) if rot else None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("layout", ["half", "pairs"])
+@pytest.mark.parametrize("d,rot", LARGE)
+@pytest.mark.parametrize("per_head", [False, True])
+def test_norm_of_rows_up_to_the_largest_value(E, dtype, layout, d, rot, per_head):
+    x, dy, w, pos, tab = large_rows(E, d, rot, dtype, per_head)
+    lay = E.EBD_ROTARY_HALF if layout == "half" else E.EBD_ROTARY_PAIRS
+    y = E.ebd_norm_rotary(x, w, pos, tab, layout=lay)
+    check_normed(y, x, w, pos, tab, layout, dtype)
+    dx, dw = E.ebd_norm_rotary_backward(dy, x, w, pos, tab, layout=lay)
+    check_grad(dx, dw, dy, x, w, pos, tab, layout, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("d", [64, 128, 512])
+def test_append_of_rows_up_to_the_largest_value(E, dtype, d):
+    x, _, w, pos, _ = large_rows(E, d, 0, dtype)
+    T = x.shape[0]
+    s = R.make([T], [T + 5], 3, 3, d, 16, dtype, d)
+    pc = cache(E, s)
+    q_out = torch.empty((T, 3, d), dtype=dtype, device="cuda")
+    E.ebd_paged_append_norm(pc, x, s["v"], k_weight=w, q=x, q_weight=w, q_out=q_out,
+                            cu_new=s["cu"])
+    _, at, off = slots_of(s, [T], [T + 5], 16)
+    check_normed(q_out, x, w, None, None, "half", dtype)
+    assert torch.equal(s["K"][at, :, off], q_out) and pc.dev_status.item() == 0
