@@ -615,11 +615,14 @@ ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n_pages, int
  * Norm per head and rotation in one pass: with r = (mean_c x_c^2 + eps)^(-1/2) of a row,
  *   y[t, h] = R(w[h] * x[t, h] * r),
  * R the rotation of ebd_rotary to positions[t] (table NULL: none; positions, n_pos,
- * rotary_dim, layout unused).  Float32 arithmetic, one rounding.
+ * rotary_dim, layout unused).  Float32 arithmetic, one rounding; rows of any finite size.
+ * What comes out below the smallest normal float32 counts as zero, and so do subnormal
+ * inputs beside an eps of 2^-102 and more.
  *   x, y         device (dtype), strided as for ebd_rotary; y may be x (same strides)
  *   weight       device: element (h, c) at h * weight_head_stride + c; stride 0: one
  *                weight for all heads.  weight_dtype is EBD_F32 or dtype
- *   eps          at least the smallest normal float32
+ *   eps          at least the smallest normal float32 (below 2^-102 rows move by elements or
+ *                pairs, several times slower, with sums that such an eps asks for)
  *   positions    device [n_tokens]; outside [0, n_pos): as for ebd_rotary
  * d <= 512 (EBD_ERR_UNSUPPORTED otherwise).  Alignment as for ebd_rotary.
  */

@@ -86,6 +86,7 @@ struct NormArgs {
   int lanes;                 // L
   int parts;                 // warps per token
   float eps, inv_d;
+  float least;               // sums of squares below it are formed anew (rescale_row)
   bool wide_table;
   int32_t* dev_status;
 };
@@ -347,10 +348,43 @@ __device__ __forceinline__ void load_weight(const NormWeight& w, int h, int c1, 
   else load(Piece<__nv_bfloat16, VEC>{});
 }
 
-// 2^-70: rows whose sum of squares leaves float32's range are scaled by it first.  Values are
-// below 2^128, so those of a scaled row are below 2^58 and 512 squares of them below 2^125;
-// one of such a row's values is at least 2^59.5, and 2^-21 when scaled and squared.
-constexpr float kRowScale = 8.470329472543003e-22f;
+// Rows whose sum of squares leaves float32's range are scaled by a power of two first.
+// Down, 2^-70, where it is not finite: values are below 2^128, so those of a scaled row are
+// below 2^58 and 512 squares of them below 2^125; one of such a row's values is at least
+// 2^59.5, and 2^-21 when scaled and squared.
+// Up, 2^64, where squares that are flushed (below 2^-126) count beside eps: from 2^-102 on what
+// they could add to the mean changes r by 2^-25 at most; below it rows with a sum under 2^-60
+// are scaled (beside a larger sum the flushed squares do not count): values below 2^-30, eps
+// between 2^2 and 2^26 then.  Calls with such an eps take the forms by elements and pairs, the
+// only ones that ask: the second comparison cost the 16-byte forms 0.7 to 2.7% (16k tokens x
+// 28 x 80 bf16 48.2 -> 49.5 us), for an eps that is hardly ever asked for.
+constexpr float kRowDown = 8.470329472543003e-22f, kRowUp = 18446744073709551616.f;
+constexpr float kSmallEps = 1.9721522630525295e-31f, kSmallSum = 8.673617379884035e-19f;
+template <typename T, int VEC>
+constexpr bool kWideRows = VEC * sizeof(T) == 16;
+
+// Whether a row's sum of squares asks for that.
+template <typename T, int VEC>
+__device__ __forceinline__ bool out_of_range(const NormArgs& a, float ss) {
+  if (!kWideRows<T, VEC> && ss < a.least) return true;
+  return !(ss < INFINITY);
+}
+// Scales such a row, eps too; the scale.
+template <typename T, int VEC, int U>
+__device__ __forceinline__ float rescale_row(float ss, float& eps, Part<VEC> (&x)[U]) {
+  const bool up = !kWideRows<T, VEC> && ss < 1.f;
+  const float scale = up ? kRowUp : kRowDown;
+  eps = up ? eps * kRowUp * kRowUp : 0.f;  // (0: below the sum's rounding)
+  auto times = [&](float v) {              // (not flushed: a row may be of subnormal values)
+    asm("mul.rn.f32 %0, %0, %1;" : "+f"(v) : "f"(scale));
+    return v;
+  };
+#pragma unroll
+  for (int j = 0; j < U; ++j)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) x[j].lo[i] = times(x[j].lo[i]), x[j].hi[i] = times(x[j].hi[i]);
+  return scale;
+}
 
 // Rows on their way to a warp, N of them to a step (the backward pass: x and dy): kAhead
 // steps are asked for ahead.  Wide chunks wait in shared memory, where their number costs
@@ -435,6 +469,7 @@ inline bool norm_shape(NormArgs& a, bool pairs, int max_u) {
   a.rot_units = pairs ? 0 : rot_chunks / 2;
   a.units = pairs ? (chunks + 1) / 2 : a.rot_units + (chunks - rot_chunks + 1) / 2;
   a.wide_table = a.rot % 4 == 0 && (uintptr_t)a.table % 16 == 0;
+  a.least = a.eps < kSmallEps ? kSmallSum : 0.f;
   a.lanes = 1;
   while (a.lanes < 32 && a.lanes < a.units) a.lanes *= 2;
   return a.units <= a.lanes * max_u;
@@ -487,7 +522,7 @@ ebd_status launch_norm_v(NormArgs a, const NormBackward* bw, cudaStream_t s) {
               : launch(integral_constant<int, kMore>{}, None{}, std::false_type{});
 }
 
-// 16-byte accesses where every row and the rotated part allow them; otherwise
+// 16-byte accesses where every row, the rotated part and eps (kSmallEps) allow them; otherwise
 // single elements (half) or single pairs (pairs).
 template <typename T, NormPass PASS>
 ebd_status launch_norm_t(const NormArgs& a, bool pairs, const NormBackward* bw, cudaStream_t s) {
@@ -502,7 +537,8 @@ ebd_status launch_norm_t(const NormArgs& a, bool pairs, const NormBackward* bw, 
            a.pv.page_stride % vec == 0 && a.pv.head_stride % vec == 0 && a.pv.row_stride % vec == 0;
     return ok && a.head_dim % vec == 0;
   };
-  const bool wide = (pairs ? a.rot : a.rot / 2) % kWide == 0 && rows_ok(kWide);
+  const bool wide =
+      !(a.eps < kSmallEps) && (pairs ? a.rot : a.rot / 2) % kWide == 0 && rows_ok(kWide);
   if (pairs) {
     if (wide) return launch_norm_v<T, kWide, true, PASS>(a, bw, s);
     // an odd head_dim or stride would split a pair's 2-element access

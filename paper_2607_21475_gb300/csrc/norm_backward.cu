@@ -109,15 +109,9 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
     };
     sums();
     float eps = a.eps, scale = 1.f;
-    if (__any_sync(0xffffffffu, !(ss < INFINITY))) {
-      if (!(ss < INFINITY)) {
-        eps = 0.f;
-        scale = kRowScale;
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
-      }
+    const bool off = live && out_of_range<T, VEC>(a, ss);
+    if (__any_sync(0xffffffffu, off)) {
+      if (off) scale = rescale_row<T, VEC, U>(ss, eps, x);
       sums();
     }
     if (!live) continue;
@@ -137,7 +131,7 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
         lo = __ffma2_rn(z0, mean, __fmul2_rn(__fmul2_rn(u0, two(wt[j].lo, i)), inv2));
         hi = __ffma2_rn(z1, mean, __fmul2_rn(__fmul2_rn(u1, two(wt[j].hi, i)), inv2));
       });
-      if (scale != 1.f)  // (last: r itself may lie below float32's normal numbers)
+      if (off)  // (last: r itself may lie below float32's normal numbers)
         each_two<VEC>(x[j], [&](int, float2& lo, float2& hi) {
           lo = __fmul2_rn(lo, both(scale));
           hi = __fmul2_rn(hi, both(scale));

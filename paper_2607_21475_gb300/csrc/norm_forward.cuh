@@ -129,14 +129,9 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(norm_forward_bloc
     };
     float ss = squares(), eps = a.eps;
     const bool normed = live && set < 2 && (set == 0 ? a.wx.p : a.wk.p) != nullptr;
-    if (__any_sync(0xffffffffu, normed && !(ss < INFINITY))) {
-      if (normed && !(ss < INFINITY)) {
-        eps = 0.f;  // below the sum's rounding
-#pragma unroll
-        for (int j = 0; j < U; ++j)
-#pragma unroll
-          for (int i = 0; i < VEC; ++i) x[j].lo[i] *= kRowScale, x[j].hi[i] *= kRowScale;
-      }
+    const bool off = normed && out_of_range<T, VEC>(a, ss);
+    if (__any_sync(0xffffffffu, off)) {
+      if (off) rescale_row<T, VEC, U>(ss, eps, x);
       ss = squares();
     }
     if (!live) continue;

@@ -69,3 +69,32 @@ def test_append_of_rows_up_to_the_largest_value(E, dtype, d):
     _, at, off = slots_of(s, [T], [T + 5], 16)
     check_normed(q_out, x, w, None, None, "half", dtype)
     assert torch.equal(s["K"][at, :, off], q_out) and pc.dev_status.item() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("eps", [2.0 ** -126, 3e-38, 1e-35, 2.0 ** -102 * (1 - 2.0 ** -23), 2.0 ** -102,
+                                 1e-30, 1e-20])
+@pytest.mark.parametrize("d,rot,per_head", [(64, 64, False), (128, 32, True), (80, 20, False),
+                                            (512, 0, False)])
+def test_norm_of_small_rows_beside_a_small_eps(E, dtype, eps, d, rot, per_head):
+    """Squares below the smallest normal float32 count where eps is as small.  (From 2^-102 on
+    what they could add changes r by at most 2^-25, half a u.)"""
+    root = eps ** 0.5
+    sizes = [0.3 * root, root, 3 * root, 100 * root, 2.0 ** -31, 2.0 ** -29, 1.0, 30 * root]
+    if eps < 1e-37:
+        sizes += [1e-39, 2e-38]  # (r is so large that these count too)
+    x, dy, w, pos = norm_inputs(len(sizes) + 1, 3, d, dtype, per_head, d)
+    x[:-1] = sized_rows(x[:-1], sizes)
+    x[-1] = 0
+    x = x.contiguous()
+    tab = table_of(E, rot, 4000) if rot else None
+    y = E.ebd_norm_rotary(x, w, pos, tab, eps=eps)
+    check_normed(y, x, w, pos, tab, "half", dtype, eps)
+    dx, dw = E.ebd_norm_rotary_backward(dy, x, w, pos, tab, eps=eps)
+    check_grad(dx, dw, dy, x, w, pos, tab, "half", dtype, eps)
+    T = x.shape[0]
+    s = R.make([T], [T + 5], 3, 3, d, 16, dtype, d)
+    _, at, off = slots_of(s, [T], [T + 5], 16)
+    E.ebd_paged_append_norm(cache(E, s), x, s["v"], k_weight=w, cu_new=s["cu"], positions=pos,
+                            table=tab, eps=eps)
+    assert torch.equal(s["K"][at, :, off], y)
