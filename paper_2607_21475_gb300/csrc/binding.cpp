@@ -314,10 +314,11 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F body) {
 // The call itself, without the interpreter's lock: a full launch queue makes it wait.
 template <typename F>
 long launched(F call) {
-  PyThreadState* state = PyEval_SaveThread();
-  const int st = call();
-  PyEval_RestoreThread(state);
-  return st;
+  struct Unlocked {  // (an exception takes the lock again too)
+    PyThreadState* state = PyEval_SaveThread();
+    ~Unlocked() { PyEval_RestoreThread(state); }
+  } unlocked;
+  return call();
 }
 
 PyObject* bind(PyObject*, PyObject* addresses) {  // {name: address}
@@ -375,7 +376,8 @@ const int32_t* norm_positions(PyObject* o, const Table& t, int64_t T) {
 PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&] {
     const at::Tensor& xt = three(a[0], "x", "[T, H, d]");
-    const int64_t T = xt.size(0), H = xt.size(1), d = xt.size(2);
+    const int32_t T = int32_of(xt.size(0), "T"), H = int32_of(xt.size(1), "H");
+    const int32_t d = int32_of(xt.size(2), "d");
     const ScalarType dt = xt.scalar_type();
     const Rows x = rows(a[0], dt, T, H, d, "x"), y = rows(a[4], dt, T, H, d, "out");
     if (a[1] == Py_None) bad_type("weight must be a torch.Tensor");
@@ -389,9 +391,9 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const Stream s(a[8]);
     s.check(xt, "x");
     return launched([&] {
-      return L.ebd_norm_rotary(code, int32_of(T, "T"), int32_of(H, "H"), int32_of(d, "d"), x.p,
-                               x.ts, x.hs, w.p, w.dtype, w.hs, eps, pos, t.p, t.n_pos, t.rot,
-                               (ebd_rotary_layout)layout, y.p, y.ts, y.hs, status, s.raw);
+      return L.ebd_norm_rotary(code, T, H, d, x.p, x.ts, x.hs, w.p, w.dtype, w.hs, eps, pos, t.p,
+                               t.n_pos, t.rot, (ebd_rotary_layout)layout, y.p, y.ts, y.hs, status,
+                               s.raw);
     });
   });
 }
@@ -400,7 +402,8 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 12, [&] {
     const at::Tensor& xt = three(a[1], "x", "[T, H, d]");
-    const int64_t T = xt.size(0), H = xt.size(1), d = xt.size(2);
+    const int32_t T = int32_of(xt.size(0), "T"), H = int32_of(xt.size(1), "H");
+    const int32_t d = int32_of(xt.size(2), "d");
     const ScalarType dt = xt.scalar_type();
     const Rows x = rows(a[1], dt, T, H, d, "x"), dy = rows(a[0], dt, T, H, d, "dy");
     const Rows dx = rows(a[5], dt, T, H, d, "dx");
@@ -414,12 +417,11 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const float eps = real(a[8]);
     int32_t* status = ints(a[10], {1}, "dev_status");
     const ebd_dtype code = dtype_code(xt);
-    const int32_t T32 = int32_of(T, "T"), H32 = int32_of(H, "H"), d32 = int32_of(d, "d");
     const Stream s(a[11]);
     s.check(xt, "x");
-    const Workspace ws(L.ebd_norm_rotary_backward_workspace_bytes(H32, d32, w.hs != 0), a[9], s);
+    const Workspace ws(L.ebd_norm_rotary_backward_workspace_bytes(H, d, w.hs != 0), a[9], s);
     return launched([&] {
-      return L.ebd_norm_rotary_backward(code, T32, H32, d32, dy.p, dy.ts, dy.hs, x.p, x.ts, x.hs,
+      return L.ebd_norm_rotary_backward(code, T, H, d, dy.p, dy.ts, dy.hs, x.p, x.ts, x.hs,
                                         w.p, w.dtype, w.hs, eps, pos, t.p, t.n_pos, t.rot,
                                         (ebd_rotary_layout)layout, dx.p, dx.ts, dx.hs, dw, status,
                                         ws.p, ws.bytes, s.raw);

@@ -98,3 +98,16 @@ def test_norm_of_small_rows_beside_a_small_eps(E, dtype, eps, d, rot, per_head):
     E.ebd_paged_append_norm(cache(E, s), x, s["v"], k_weight=w, cu_new=s["cu"], positions=pos,
                             table=tab, eps=eps)
     assert torch.equal(s["K"][at, :, off], y)
+
+
+def test_more_rows_than_31_bits_count_are_refused(E):
+    """By the marshalling, before anything is launched: a Python error (the tensors here are
+    views of one row)."""
+    x = torch.zeros((1, 1, 8), device="cuda").to(torch.bfloat16)
+    w, dw = torch.ones(8, device="cuda").to(torch.bfloat16), torch.empty(8, device="cuda")
+    for shape in ((2 ** 31 + 8, 1, 8), (1, 2 ** 31 + 8, 8)):
+        z = x.expand(shape)
+        with pytest.raises(ValueError, match="out of range"):
+            E.ebd_norm_rotary(z, w, out=z)
+        with pytest.raises(ValueError, match="out of range"):
+            E.ebd_norm_rotary_backward(z, z, w, dx=z, dweight=dw)
