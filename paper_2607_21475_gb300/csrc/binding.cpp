@@ -152,7 +152,8 @@ struct Stream {
     if (PyErr_Occurred()) throw Refusal{nullptr, ""};
     return x;
   }
-  // Refuses a tensor of another device than the one that the call launches on.
+  // Refuses a tensor (and with it all of the call's) of another device than the one that the
+  // call launches on.
   void check(const at::Tensor& t, const char* name) const {
     if (t.is_cuda() && t.device().index() != device)
       bad_value(std::string(name) + " is on cuda:" + std::to_string(t.device().index()) +
@@ -290,11 +291,25 @@ struct {
 #undef X
 } L;
 
-// Runs body(args), its refusals and C++ exceptions raised as Python's.
-template <typename F>
-PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F body) {
-  if (n != want) {
-    PyErr_Format(PyExc_TypeError, "%zd arguments, expected %zd", n, want);
+// A call's tensors are all on one GPU (the kernels take their addresses as they are).
+void check_devices(PyObject* const* a, Py_ssize_t n, const char* const* names) {
+  int device = -1, first = 0;
+  for (int i = 0; i < n; ++i) {
+    if (!THPVariable_Check(a[i]) || !THPVariable_Unpack(a[i]).is_cuda()) continue;
+    const int at = THPVariable_Unpack(a[i]).device().index();
+    if (device < 0) device = at, first = i;
+    if (at != device)
+      bad_value(std::string(names[i]) + " is on cuda:" + std::to_string(at) + ", " + names[first] +
+                " on cuda:" + std::to_string(device));
+  }
+}
+
+// Runs body() on the arguments of these names, its refusals and C++ exceptions raised as
+// Python's.
+template <size_t N, typename F>
+PyObject* guarded(PyObject* const* a, Py_ssize_t n, const char* const (&names)[N], F body) {
+  if (n != (Py_ssize_t)N) {
+    PyErr_Format(PyExc_TypeError, "%zd arguments, expected %zd", n, (Py_ssize_t)N);
     return nullptr;
   }
   if (!L.ebd_paged_keep) {
@@ -302,6 +317,7 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F body) {
     return nullptr;
   }
   try {
+    check_devices(a, n, names);
     return PyLong_FromLong(body());
   } catch (const Refusal& r) {
     if (r.type) PyErr_SetString(r.type, r.text.c_str());
@@ -338,10 +354,11 @@ PyObject* bind(PyObject*, PyObject* addresses) {  // {name: address}
   Py_RETURN_NONE;
 }
 
-// free_pages, n_free, held, K, V, block_table, seq_len, dev_status, n_new, n_tokens, window,
-// cu_new, positions, slots, served, seq_len_out, held_out, n_free_out, stream
 PyObject* deal(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 19, [&] {
+  static const char* const names[] = {"free_pages", "n_free", "held", "K_pages", "V_pages",
+      "block_table", "seq_len", "dev_status", "n_new", "n_tokens", "window", "cu_new", "positions",
+      "slots", "served", "seq_len_out", "held_out", "n_free_out", "stream"};
+  return guarded(a, n, names, [&] {
     const ebd_paged_cache c = paged(a[3], a[4], a[5], a[6]);
     const int64_t B = c.batch;
     const int32_t T = integer(a[9], "n_tokens"), window = integer(a[10], "window");
@@ -372,9 +389,10 @@ const int32_t* norm_positions(PyObject* o, const Table& t, int64_t T) {
   return ints(o, {T}, "positions");
 }
 
-// x, weight, positions, table, out, layout, eps, dev_status, stream
 PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 9, [&] {
+  static const char* const names[] = {"x", "weight", "positions", "table", "out", "layout", "eps",
+      "dev_status", "stream"};
+  return guarded(a, n, names, [&] {
     const at::Tensor& xt = three(a[0], "x", "[T, H, d]");
     const int32_t T = int32_of(xt.size(0), "T"), H = int32_of(xt.size(1), "H");
     const int32_t d = int32_of(xt.size(2), "d");
@@ -398,9 +416,10 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// dy, x, weight, positions, table, dx, dweight, layout, eps, workspace, dev_status, stream
 PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 12, [&] {
+  static const char* const names[] = {"dy", "x", "weight", "positions", "table", "dx", "dweight",
+      "layout", "eps", "workspace", "dev_status", "stream"};
+  return guarded(a, n, names, [&] {
     const at::Tensor& xt = three(a[1], "x", "[T, H, d]");
     const int32_t T = int32_of(xt.size(0), "T"), H = int32_of(xt.size(1), "H");
     const int32_t d = int32_of(xt.size(2), "d");
@@ -429,10 +448,11 @@ PyObject* norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// K, V, block_table, seq_len, dev_status, k_new, v_new, k_weight, q, q_weight, q_out, cu_new,
-// slots, positions, table, layout, eps, stream
 PyObject* append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 18, [&] {
+  static const char* const names[] = {"K_pages", "V_pages", "block_table", "seq_len", "dev_status",
+      "k_new", "v_new", "k_weight", "q", "q_weight", "q_out", "cu_new", "slots", "positions",
+      "table", "layout", "eps", "stream"};
+  return guarded(a, n, names, [&] {
     const ebd_paged_cache c = paged(a[0], a[1], a[2], a[3]);
     const at::Tensor& Kt = THPVariable_Unpack(a[0]);
     const ScalarType dt = Kt.scalar_type();
@@ -474,9 +494,10 @@ PyObject* append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// parents, cu_new, seq_len, max_new, window, mask, positions, dev_status, stream
 PyObject* tree_masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 9, [&] {
+  static const char* const names[] = {"parents", "cu_new", "seq_len", "max_new", "window", "mask",
+      "positions", "dev_status", "stream"};
+  return guarded(a, n, names, [&] {
     const at::Tensor &pt = tensor(a[0], "parents"), &st = tensor(a[2], "seq_len");
     if (pt.dim() != 1 || st.dim() != 1) bad_value("parents must be [T] and seq_len [B]");
     const int64_t T = pt.size(0), B = st.size(0);
@@ -496,10 +517,11 @@ PyObject* tree_masks(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// K, V, block_table, seq_len, dev_status, q, cu_new, max_new, mask, positions, y, lse, scale,
-// window, workspace, stream
 PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 16, [&] {
+  static const char* const names[] = {"K_pages", "V_pages", "block_table", "seq_len", "dev_status",
+      "q", "cu_new", "max_new", "mask", "positions", "y", "lse", "scale", "window", "workspace",
+      "stream"};
+  return guarded(a, n, names, [&] {
     const ebd_paged_cache c = paged(a[0], a[1], a[2], a[3]);
     const at::Tensor& qt = three(a[5], "q", "[T, Hq, d]");
     const ScalarType dt = THPVariable_Unpack(a[0]).scalar_type();
@@ -529,10 +551,10 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// K, V, block_table, seq_len, dev_status, cu_new, path, n_accepted, seq_len_out, K_layers,
-// V_layers, stream
 PyObject* keep(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 12, [&] {
+  static const char* const names[] = {"K_pages", "V_pages", "block_table", "seq_len", "dev_status",
+      "cu_new", "path", "n_accepted", "seq_len_out", "K_layers", "V_layers", "stream"};
+  return guarded(a, n, names, [&] {
     const ebd_paged_cache c = paged(a[0], a[1], a[2], a[3]);
     int64_t layers = 1, stride = 0;
     if ((a[9] == Py_None) != (a[10] == Py_None))

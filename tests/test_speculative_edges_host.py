@@ -26,3 +26,60 @@ def test_sizes_past_31_bits_are_refused(E, shape):
         E.ebd_norm_rotary(x, w, out=x)
     with pytest.raises(ValueError, match="out of range"):
         E.ebd_norm_rotary_backward(x, x, w, dx=x, dweight=on_gpu(shape[2], dtype=torch.float32))
+
+
+def calls(E):
+    """Every call with all its tensors given: (function, arguments by name)."""
+    def i32(*shape):
+        return on_gpu(*shape, dtype=torch.int32)
+
+    def f32(*shape):
+        return on_gpu(*shape, dtype=torch.float32)
+
+    T, B, hq, hkv, d, pages, P = 5, 2, 4, 2, 64, 8, 16
+    cache = dict(K_pages=on_gpu(pages, hkv, P, d), V_pages=on_gpu(pages, hkv, P, d),
+                 block_table=i32(B, 4), seq_len=i32(B), dev_status=i32(1))
+    turn = dict(positions=i32(T), table=f32(50, d // 2, 2))
+    pool = dict(free_pages=i32(pages), n_free=i32(1), held=i32(B, 2))
+
+    def on_cache(f):
+        return lambda **a: f(pc=E.PagedCache(*(a.pop(k) for k in cache)), **a)
+
+    def deal(**a):
+        return E.ebd_paged_deal(E.PagePool(*(a.pop(k) for k in pool)),
+                                E.PagedCache(*(a.pop(k) for k in cache)), n_tokens=T, **a)
+
+    return [
+        (deal, dict(**pool, **cache, n_new=i32(B), cu_new=i32(B + 1), positions=i32(T),
+                    slots=on_gpu(T, dtype=torch.int64), served=i32(B), seq_len_out=i32(B),
+                    held_out=i32(B, 2), n_free_out=i32(1))),
+        (E.ebd_norm_rotary, dict(x=on_gpu(T, hq, d), weight=on_gpu(d), **turn, out=on_gpu(T, hq, d),
+                                 dev_status=i32(1))),
+        (E.ebd_norm_rotary_backward, dict(
+            dy=on_gpu(T, hq, d), x=on_gpu(T, hq, d), weight=on_gpu(d), **turn, dx=on_gpu(T, hq, d),
+            dweight=f32(d), workspace=f32(1 << 20), dev_status=i32(1))),
+        (on_cache(E.ebd_paged_append_norm), dict(
+            **cache, k_new=on_gpu(T, hkv, d), v_new=on_gpu(T, hkv, d), k_weight=on_gpu(d),
+            q=on_gpu(T, hq, d), q_weight=on_gpu(d), q_out=on_gpu(T, hq, d), cu_new=i32(B + 1),
+            **turn)),
+        (E.ebd_tree_masks, dict(parents=i32(T), cu_new=i32(B + 1), seq_len=i32(B), max_new=T,
+                                mask=i32(T, 1), positions=i32(T), dev_status=i32(1))),
+        (on_cache(E.ebd_paged_tree_attention), dict(**cache, q=on_gpu(T, hq, d), cu_new=i32(B + 1), max_new=T,
+                                                mask=i32(T, 1), positions=i32(T),
+                                                y=on_gpu(T, hq, d), lse=f32(T, hq),
+                                                workspace=f32(1 << 20))),
+        (on_cache(E.ebd_paged_keep), dict(**cache, cu_new=i32(B + 1), path=i32(B, 3), n_accepted=i32(B),
+                                 seq_len_out=i32(B))),
+    ]
+
+
+@pytest.mark.parametrize("which", range(7))
+def test_tensors_of_two_gpus_are_refused(E, which):
+    """Whichever of them is elsewhere: the kernels would take its address as this GPU's."""
+    call, args = calls(E)[which]
+    for name, t in args.items():
+        if not isinstance(t, torch.Tensor):
+            continue
+        elsewhere = on_gpu(*t.shape, dtype=t.dtype, device="cuda:1")
+        with pytest.raises(ValueError, match="is on cuda:"):
+            call(**dict(args, **{name: elsewhere}))
