@@ -50,14 +50,12 @@ def main(tokens=500, steps=8, B=3, hq=28, hkv=4, d=128, page=16, drafted=12, dee
         qkv = torch.empty((T, hq + 2 * hkv, d), dtype=dt, device=dev).normal_(generator=gen)
         q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
         q_rot = torch.empty((T, hq, d), dtype=dt, device=dev)
+        mask = None  # plain tokens
         if parents is not None:
             mask, positions = ebd.ebd_tree_masks(parents, cu, pc.seq_len, n)
         ebd.ebd_paged_append_norm(pc, k, v, k_weight=k_weight, q=q, q_weight=q_weight, q_out=q_rot,
                                   slots=slots, positions=positions, table=table)
-        if parents is None:
-            y, _ = ebd.ebd_paged_attention(q_rot, pc, cu, n)
-        else:
-            y, _ = ebd.ebd_paged_tree_attention(q_rot, pc, cu, n, mask)
+        y, _ = ebd.ebd_paged_tree_attention(q_rot, pc, cu, n, mask)
         return q_rot, y, cu
 
     step(tokens)  # the prompts

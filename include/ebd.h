@@ -703,7 +703,10 @@ ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t max_new, cons
  * (itself too only if its own is), and of the earlier positions j, with a window > 0,
  * those with j > positions[t] - window.  A token with nothing to see gets y = 0,
  * lse = -inf.
- *   mask       device [n_tokens][mask_words], max_new <= 32 mask_words
+ *   mask       device [n_tokens][mask_words], max_new <= 32 mask_words.  NULL with
+ *              mask_words 0: no tree, each new token sees those before it and itself as in
+ *              ebd_paged_attention, at its own place (positions unused, any max_new): dealt
+ *              steps and prompts
  *   positions  device [n_tokens], needed with a window: from the tree's beginning, base =
  *              seq_len[b] - (new tokens of b), to base + the token's number
  *              (otherwise clamped, EBD_DEV_RANGE)

@@ -527,9 +527,13 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const ScalarType dt = THPVariable_Unpack(a[0]).scalar_type();
     const int64_t T = qt.size(0), hq = qt.size(1), d = c.head_dim;
     const Rows q = rows(a[5], dt, T, hq, d, "q");
-    const at::Tensor& mt = tensor(a[8], "mask");
-    if (mt.dim() != 2) bad_value("mask must be [T, W]");
-    const int64_t words = mt.size(1);
+    int64_t words = 0;  // (no mask: causal)
+    if (a[8] != Py_None) {
+      const at::Tensor& mt = tensor(a[8], "mask");
+      if (mt.dim() != 2) bad_value("mask must be [T, W]");
+      words = mt.size(1);
+      if (words < 1 && T > 0) bad_value("mask must have a word per 32 new tokens");
+    }
     const int32_t most = integer(a[7], "max_new"), window = integer(a[13], "window");
     const int32_t* cu = ints(a[6], {c.batch + 1}, "cu_new");
     const int32_t *mask = ints(a[8], {T, words}, "mask"), *pos = ints(a[9], {T}, "positions");

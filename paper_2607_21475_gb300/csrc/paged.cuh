@@ -80,10 +80,9 @@ struct SeqSpan {
   bool bad;  // an entry was outside its range
 };
 
-// PADDED: places past the last offset are empty, no mistake.
-template <bool PADDED = false>
+// padded: places past the last offset are empty, no mistake.
 __device__ __forceinline__ SeqSpan seq_span(const PagedView& v, const int32_t* cu, int b,
-                                            int n_tokens, int max_new) {
+                                            int n_tokens, int max_new, bool padded) {
   const int c0 = cu[b], c1 = cu[b + 1], l = v.seq_len[b];
   SeqSpan s;
   s.t0 = min(max(c0, 0), n_tokens);
@@ -93,7 +92,7 @@ __device__ __forceinline__ SeqSpan seq_span(const PagedView& v, const int32_t* c
   s.len = (int)min((long long)max(l, 0), most);
   // the offsets run from 0 to n_tokens: what lies before or after is no sequence's
   s.bad = s.t0 != c0 || s.t0 + s.n != c1 || s.len != l || (b == 0 && c0 != 0) ||
-          (!PADDED && b == v.batch - 1 && c1 != n_tokens);
+          (!padded && b == v.batch - 1 && c1 != n_tokens);
   return s;
 }
 

@@ -58,7 +58,8 @@ __device__ __forceinline__ void cp_async16_or_zero(void* dst, const void* src, b
 // TREE: new tokens see each other by a mask.  (Its words asked for a tile ahead cost spills:
 // five trees of up to 33 tokens over 1k positions with a window of 200, in turn, 20.6-22.4
 // us against 17.2-19.8, both after a long chunk's heat; 15.8 on a rested GPU.)
-template <int D, bool TREE>
+// PADDED: places past the last offset are empty, no mistake.
+template <int D, bool TREE, bool PADDED>
 __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
     paged_attn_f32_kernel(const PagedAttnArgs a) {
   using L = SimtLayout<D>;
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(kAttnThreads, SimtLayout<D>::kCtasPerSm)
   static_assert(sizeof(WorkStart) <= 12 * 4, "start");
   grid_dependency_wait();
   if (threadIdx.x < 32) {
-    const WorkStart w = find_work<BN, TREE>(a, blockIdx.x, gridDim.x, threadIdx.x);
+    const WorkStart w = find_work<BN, TREE, PADDED>(a, blockIdx.x, gridDim.x, threadIdx.x);
     if (threadIdx.x == 0) *start_s = w;
   }
   __syncthreads();
@@ -298,7 +299,9 @@ static int f32_ctas(int head_dim) {
 template <int D>
 static ebd_status launch_paged_f32(PagedAttnArgs a, int n_cta, cudaStream_t s) {
   const int smem = SimtLayout<D>::kFloats * 4;
-  auto kern = a.mask ? paged_attn_f32_kernel<D, true> : paged_attn_f32_kernel<D, false>;
+  auto kern = a.mask     ? paged_attn_f32_kernel<D, true, true>
+              : a.padded ? paged_attn_f32_kernel<D, false, true>
+                         : paged_attn_f32_kernel<D, false, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
   const int slice = f32_slice(a.group);
@@ -346,13 +349,13 @@ extern "C" size_t ebd_paged_attention_workspace_bytes(const ebd_paged_cache* cac
                            cache->head_dim);
 }
 
-// Both forms; mask null: causal.
+// Both forms; mask null: causal.  padded: places past the last offset may be empty.
 static ebd_status attention(const ebd_paged_cache* cache, int32_t n_tokens, int32_t max_new,
                             int32_t n_q_heads, const int32_t* cu_new, const void* q,
                             int64_t q_token_stride, int64_t q_head_stride, float scale,
                             int32_t window, const uint32_t* mask, int32_t mask_words,
-                            const int32_t* positions, void* y, float* lse, int32_t* dev_status,
-                            void* workspace, size_t ws_bytes, void* stream) {
+                            const int32_t* positions, bool padded, void* y, float* lse,
+                            int32_t* dev_status, void* workspace, size_t ws_bytes, void* stream) {
   const ebd_status st = check_paged(cache);
   if (st != EBD_OK) return st;
   if (n_tokens < 0 || max_new < (n_tokens > 0) || n_q_heads < 1 ||
@@ -390,6 +393,7 @@ static ebd_status attention(const ebd_paged_cache* cache, int32_t n_tokens, int3
   a.mask = mask;
   a.mask_words = mask_words;
   a.positions = positions;
+  a.padded = padded;
   a.dev_status = dev_status;
   cudaStream_t s = (cudaStream_t)stream;
   const int n_cta = attention_ctas(*cache);
@@ -409,7 +413,7 @@ extern "C" ebd_status ebd_paged_attention(const ebd_paged_cache* cache, int32_t 
                                           int32_t* dev_status, void* workspace, size_t ws_bytes,
                                           void* stream) {
   return attention(cache, n_tokens, max_new, n_q_heads, cu_new, q, q_token_stride, q_head_stride,
-                   scale, window, nullptr, 0, nullptr, y, lse, dev_status, workspace, ws_bytes,
+                   scale, window, nullptr, 0, nullptr, false, y, lse, dev_status, workspace, ws_bytes,
                    stream);
 }
 
@@ -419,9 +423,12 @@ extern "C" ebd_status ebd_paged_tree_attention(
     float scale, int32_t window, const uint32_t* mask, int32_t mask_words,
     const int32_t* positions, void* y, float* lse, int32_t* dev_status, void* workspace,
     size_t ws_bytes, void* stream) {
-  if (mask_words < 1 || max_new > 32ll * mask_words) return EBD_ERR_INVALID;
-  if (n_tokens > 0 && (!mask || (window > 0 && !positions))) return EBD_ERR_INVALID;
+  const bool causal = !mask && mask_words == 0;
+  if (!causal) {
+    if (mask_words < 1 || max_new > 32ll * mask_words) return EBD_ERR_INVALID;
+    if (n_tokens > 0 && (!mask || (window > 0 && !positions))) return EBD_ERR_INVALID;
+  }
   return attention(cache, n_tokens, max_new, n_q_heads, cu_new, q, q_token_stride, q_head_stride,
-                   scale, window, mask, mask_words, positions, y, lse, dev_status, workspace,
+                   scale, window, mask, mask_words, positions, true, y, lse, dev_status, workspace,
                    ws_bytes, stream);
 }

@@ -66,6 +66,7 @@ struct PagedAttnArgs {
   const uint32_t* mask;      // [n_tokens][mask_words]; null: causal
   const int32_t* positions;  // [n_tokens]; needed with a window
   int mask_words;
+  bool padded;               // (host) places past the last offset are empty, no mistake
 };
 
 // KV head, first query head and number of query heads of (sliced) head h.
@@ -177,13 +178,13 @@ __device__ __forceinline__ int warp_scan_add(int v, int lane) {
 }
 
 // Work of one head of the sequences base + lane (lane = 0..31), their spans and m-tiles.
-template <int BN, bool TREE>
+template <int BN, bool TREE, bool PADDED>
 __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, int lane,
                                              bool report, SeqSpan& sp, int& mt) {
   const int b = base + lane;
   sp = SeqSpan{};
   if (b < a.pv.batch) {
-    sp = seq_span<TREE>(a.pv, a.cu, b, a.n_tokens, a.max_new);
+    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new, PADDED);
     if (report && sp.bad) raise_status(a.dev_status, EBD_DEV_RANGE);
   }
   mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);
@@ -211,14 +212,14 @@ __device__ __forceinline__ int sequence_work(const PagedAttnArgs& a, int base, i
 }
 
 // Where CTA `cta` begins on the line, and how much of it is its own; one whole warp.
-template <int BN, bool TREE>
+template <int BN, bool TREE, bool PADDED>
 __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, int n_cta,
                                                int lane) {
   const int H = a.heads;
   SeqSpan sp;
   int total = 0, c = 0, upto = 0, mt = 0;
   for (int base = 0; base < a.pv.batch; base += 32) {
-    c = sequence_work<BN, TREE>(a, base, lane, cta == 0, sp, mt);
+    c = sequence_work<BN, TREE, PADDED>(a, base, lane, cta == 0, sp, mt);
     upto = warp_scan_add(c * H, lane);
     total += __shfl_sync(0xffffffffu, upto, 31);
   }
@@ -229,7 +230,7 @@ __device__ __forceinline__ WorkStart find_work(const PagedAttnArgs& a, int cta, 
   const int count = min(share, total - at);
   for (int base = 0; base < a.pv.batch; base += 32) {
     if (a.pv.batch > 32) {
-      c = sequence_work<BN, TREE>(a, base, lane, false, sp, mt);
+      c = sequence_work<BN, TREE, PADDED>(a, base, lane, false, sp, mt);
       upto = warp_scan_add(c * H, lane);
     }
     const uint32_t past = __ballot_sync(0xffffffffu, upto > at);
@@ -294,7 +295,7 @@ struct PieceWalk {
     if (cur == end) next(a);
   }
   __device__ __forceinline__ void load(const PagedAttnArgs& a) {
-    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new);
+    sp = seq_span(a.pv, a.cu, b, a.n_tokens, a.max_new, true);  // (nothing is reported here)
     mt = (int)((uint32_t)(sp.n + a.tokens - 1) / (uint32_t)a.tokens);
     item_range<BN, TREE>(a, sp.n, sp.len, m, kb, ke);
   }
@@ -491,7 +492,7 @@ template <typename T, int D, int BN, bool TREE>
 __device__ __noinline__ void mend_pieces(const PagedAttnArgs& a, int cta, int n_cta, int x0,
                                          int slot0, int row0, int rows, int lane) {
   __syncwarp();  // the rows, written by other lanes
-  const WorkStart start = find_work<BN, TREE>(a, cta, n_cta, lane);
+  const WorkStart start = find_work<BN, TREE, true>(a, cta, n_cta, lane);  // (told before)
   for (PieceWalk<BN, TREE> w(a, start); w.live(); w.next(a)) {
     const int tokens = min(w.tokens(a) - x0, a.half_tokens), slot = w.slot(cta);
     const int t_first = w.sp.t0 + w.first(a) + x0, p0 = w.sp.len - w.sp.n + w.first(a) + x0;

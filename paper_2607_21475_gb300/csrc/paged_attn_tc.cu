@@ -121,7 +121,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // tokens, 28/4 heads x 128: 15.2 us, 14.9 causal; trees of 40-64 tokens of 32 dialogues
 // of 2k-32k, 32/8 x 128: 422 us at the full clock, 440-514 under the power cap, tensor pipe
 // 75% active, its 256-row tiles 81% filled).
-template <int D, bool TREE>
+// PADDED: places past the last offset are empty, no mistake (a form of its own: asked at run
+// time, the causal kernels took longer, a 4096-token chunk over 16k 493 -> 499 us).
+template <int D, bool TREE, bool PADDED>
 __global__ void __launch_bounds__(kTcAttnThreads, 1)
     paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tmQ,
                          const __grid_constant__ CUtensorMap tmK,
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(kTcAttnThreads, 1)
   fence_proxy_async_smem();
   grid_dependency_wait();  // nothing of the caller's was read or written so far
   WorkStart start = {};
-  if (warp == 11) start = find_work<kTcBN, TREE>(a, cta, gridDim.x, lane);
+  if (warp == 11) start = find_work<kTcBN, TREE, PADDED>(a, cta, gridDim.x, lane);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -716,7 +718,9 @@ static ebd_status launch_tc_t(const PagedAttnArgs& a, const ebd_paged_cache& c, 
   if (!encode_queries(&tmQ, a, D) || !encode_pool(&tmK, c, c.K_pages, box) || !encode_pool(&tmV, c, c.V_pages, box))
     return EBD_ERR_CUDA;
   constexpr int smem = PagedTcLayout<D>::kBytes;
-  auto kern = a.mask ? paged_attn_tc_kernel<D, true> : paged_attn_tc_kernel<D, false>;
+  auto kern = a.mask     ? paged_attn_tc_kernel<D, true, true>
+              : a.padded ? paged_attn_tc_kernel<D, false, true>
+                         : paged_attn_tc_kernel<D, false, false>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
   return launch_dependent(kern, dim3(n_cta), kTcAttnThreads, smem, s, tmQ, tmK, tmV, a);

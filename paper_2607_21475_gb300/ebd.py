@@ -961,12 +961,13 @@ def ebd_tree_masks(parents: torch.Tensor, cu_new: torch.Tensor, seq_len: torch.T
 
 
 def ebd_paged_tree_attention(q: torch.Tensor, pc: PagedCache, cu_new: torch.Tensor, max_new: int,
-                             mask: torch.Tensor, positions=None, y=None, lse=None, scale=None,
+                             mask, positions=None, y=None, lse=None, scale=None,
                              window: int = 0, workspace=None, stream=None):
     """ebd_paged_attention of drafted trees: a new token sees the earlier positions and
     those new tokens of its sequence whose bits its row of mask [T, W] (int32,
-    ebd_tree_masks) has; positions [T] are needed with a window.  Places past the last
-    offset (a deal's empty ones) are left alone."""
+    ebd_tree_masks) has; positions [T] are needed with a window.  mask None: no tree, every
+    token sees those before it, as in ebd_paged_attention.  Places past the last offset (a
+    deal's empty ones) are left alone."""
     if y is None:
         y = _result(q.shape, pc.K_pages.dtype, q.device, stream)
     if lse is None:

@@ -1,11 +1,13 @@
 """A speculative step's operators at the ends of their ranges, against the plain forms and
 with the bounds of test_gpu_speculative.py (u = 2^-24)."""
+import math
+
 import pytest
 import torch
 
 import paged_ref as R
-from test_gpu_speculative import (cache, check_grad, check_normed, norm_inputs, slots_of,
-                                  table_of)
+from test_gpu_speculative import (cache, check_grad, check_normed, ints, norm_inputs, slots_of,
+                                  table_of, tree_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +113,58 @@ def test_more_rows_than_31_bits_count_are_refused(E):
             E.ebd_norm_rotary(z, w, out=z)
         with pytest.raises(ValueError, match="out of range"):
             E.ebd_norm_rotary_backward(z, z, w, dx=z, dweight=dw)
+
+
+# ---------------------------------------------------------------- causal tokens after a deal
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("case", [0, 3, 4, 5, 8, 10])
+@pytest.mark.parametrize("window", [0, 9])
+def test_attention_without_a_mask_is_the_causal_one(E, dtype, case, window):
+    """Bit for bit; empty places behind the last sequence stay, and nothing is reported."""
+    s = tree_case(E, case, dtype)
+    pc, T = cache(E, s), s["T"]
+    want = E.ebd_paged_attention(s["q"], pc, s["cu"], s["max_new"], window=window)
+    got = E.ebd_paged_tree_attention(s["q"], pc, s["cu"], s["max_new"], None, window=window)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    q = torch.cat([s["q"], torch.full_like(s["q"][:7], math.nan)])
+    y, lse = torch.full_like(q, 3), torch.full(q.shape[:2], 4.0, device="cuda")
+    E.ebd_paged_tree_attention(q, pc, s["cu"], s["max_new"], None, window=window, y=y, lse=lse)
+    assert torch.equal(y[:T], want[0]) and torch.equal(lse[:T], want[1])
+    assert (y[T:] == 3).all() and (lse[T:] == 4).all() and pc.dev_status.item() == 0
+    # offsets that step back, or past the packed tokens, are still told
+    cu = s["cu"].clone()
+    cu[-1] = T + 8
+    E.ebd_paged_tree_attention(q, pc, cu, s["max_new"] + 8, None, window=window, y=y, lse=lse)
+    assert pc.dev_status.item() == E.EBD_DEV_RANGE
+    with pytest.raises(ValueError, match="word"):  # an empty mask is none
+        E.ebd_paged_tree_attention(s["q"], pc, s["cu"], s["max_new"], s["mask"][:, :0])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_dealt_prompts_and_steps_are_attended_without_a_status(E, dtype):
+    """Requests that idle, leave or wait for pages leave empty places; prompts longer than any
+    tree.  The same tokens packed tightly give the same bits."""
+    B, hkv, hq, d, P, cap = 4, 2, 4, 64, 16, 2600
+    pc = E.alloc_paged(B, hkv, 160, P, d, 130, dtype, "cuda")
+    pc.K_pages.zero_()
+    pc.V_pages.zero_()
+    pool = E.alloc_page_pool(B, 160, "cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    tab = table_of(E, d, 2100)
+    for new, served_want in [([1500, 3, 0, 900], [1, 1, 1, 1]), ([1, 1, 40, 0], [1, 1, 1, 1]),
+                             ([0, -1, 1, 1], [1, 1, 1, 1]), ([1, 700, 1, 1], [1, 0, 1, 1])]:
+        cu, pos, slots, served = E.ebd_paged_deal(pool, pc, ints(new), cap)
+        assert served.tolist() == served_want
+        short = 0 in served_want
+        assert pc.dev_status.item() == (E.EBD_DEV_CAPACITY if short else 0)
+        pc.dev_status.zero_()
+        qkv = torch.randn((cap, hq + 2 * hkv, d), generator=gen, device="cuda").to(dtype)
+        q_out = torch.full((cap, hq, d), 2.0, dtype=dtype, device="cuda")
+        E.ebd_paged_append_norm(pc, qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], q=qkv[:, :hq],
+                                q_out=q_out, slots=slots, positions=pos, table=tab)
+        y, lse = E.ebd_paged_tree_attention(q_out, pc, cu, max(new), None)
+        assert pc.dev_status.item() == 0
+        n = cu[-1].item()
+        want = E.ebd_paged_attention(q_out[:n], pc, cu, max(new))
+        assert torch.equal(y[:n], want[0]) and torch.equal(lse[:n], want[1])
+        assert pc.dev_status.item() == 0
