@@ -41,17 +41,19 @@ def _sources():
     return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cu"))
 
 
-def _torch_root() -> str:
+def _torch_root() -> str | None:
     from importlib.util import find_spec
     spec = find_spec("torch")
-    if spec is None or not spec.origin:
-        raise RuntimeError("torch not found; the binding is compiled against its headers")
-    return os.path.dirname(spec.origin)
+    return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
 
 
 def _compile_binding() -> None:
     """The extension of csrc/binding.cpp, for this interpreter and this torch."""
+    if os.path.exists(CALL):
+        os.remove(CALL)  # (one of other sources would marshal for a library that is gone)
     root, nvcc = _torch_root(), _nvcc()
+    if root is None:
+        raise RuntimeError("torch not found; the binding is compiled against its headers")
     cuda = os.path.dirname(os.path.dirname(os.path.realpath(nvcc)))
     tmp = CALL + ".tmp"
     include = [os.path.join(root, "include"),
@@ -62,7 +64,10 @@ def _compile_binding() -> None:
            *[x for d in include for x in ("-isystem", d)], BINDING, "-o", tmp, "-L", lib,
            "-ltorch_python", "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda",
            f"-Wl,-rpath,{lib}"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    try:
+        r = subprocess.run(cmd, capture_output=True, text=True)
+    except OSError as e:
+        raise RuntimeError(f"the binding needs a C++ compiler: {e}") from e
     if r.returncode != 0:
         raise RuntimeError(f"the binding failed to compile:\n{r.stderr[-4000:]}")
     os.replace(tmp, CALL)
@@ -71,10 +76,12 @@ def _compile_binding() -> None:
 def _digest(extra_flags) -> str:
     h = hashlib.sha256()
     # the binding is for one interpreter and one torch
-    h.update((sys.version + _torch_root()).encode())
-    version = os.path.join(_torch_root(), "version.py")
-    files = [BINDING] + ([version] if os.path.exists(version) else []) + _sources() + sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
-                                if f.endswith((".cuh", ".h")))
+    root = _torch_root() or ""
+    h.update((sys.version + root).encode())
+    version = os.path.join(root, "version.py")
+    files = [BINDING] + ([version] if root and os.path.exists(version) else [])
+    files += _sources() + sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC)
+                                 if f.endswith((".cuh", ".h")))
     files.append(os.path.join(INCLUDE, "ebd.h"))
     for f in files:
         h.update(f.encode())
@@ -85,7 +92,9 @@ def _digest(extra_flags) -> str:
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
-    """Compile the CUDA sources and link libebd.so; returns the library path."""
+    """Compile the CUDA sources and link libebd.so, and compile the binding; returns the
+    library path.  Where the binding does not compile, the library is there all the same:
+    the calls that go through ctypes, and C programs, do without it."""
     os.makedirs(BUILD, exist_ok=True)
     stamp = os.path.join(BUILD, "libebd.stamp")
     dig = _digest(extra_flags)
@@ -110,13 +119,15 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
     with ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
         binding = ex.submit(_compile_binding)
         list(ex.map(compile_one, zip(srcs, objs)))
-        binding.result()
     tmp = LIB + ".tmp"
     cmd = [nvcc, *ARCH, "-shared", "-cudart", "static", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link of libebd.so failed:\n{r.stderr}")
     os.replace(tmp, LIB)
+    if binding.exception() is not None:
+        raise RuntimeError(f"{LIB} is built, the binding of the serving calls is not") \
+            from binding.exception()
     with open(stamp, "w") as fh:
         fh.write(dig)
     return LIB

@@ -83,3 +83,29 @@ def test_tensors_of_two_gpus_are_refused(E, which):
         elsewhere = on_gpu(*t.shape, dtype=t.dtype, device="cuda:1")
         with pytest.raises(ValueError, match="is on cuda:"):
             call(**dict(args, **{name: elsewhere}))
+
+
+def test_the_library_is_linked_where_the_binding_does_not_compile(monkeypatch, tmp_path):
+    """And the binding of other sources does not stay beside it."""
+    import ctypes
+
+    from paper_2607_21475_gb300 import build as B
+    src = tmp_path / "one.cu"
+    src.write_text('extern "C" int one() { return 1; }\n')
+    binding = tmp_path / "binding.cpp"
+    binding.write_text("#error not here\n")
+    (tmp_path / "ebd_call.so").write_text("an older one")
+    for name, value in dict(BUILD=str(tmp_path), LIB=str(tmp_path / "libebd.so"),
+                            CALL=str(tmp_path / "ebd_call.so"), BINDING=str(binding),
+                            _sources=lambda: [str(src)]).items():
+        monkeypatch.setattr(B, name, value)
+    for how in ("sources", "compiler", "torch"):
+        if how == "compiler":
+            monkeypatch.setenv("CXX", str(tmp_path / "no-such-compiler"))
+        if how == "torch":
+            monkeypatch.setattr(B, "_torch_root", lambda: None)
+        with pytest.raises(RuntimeError, match="is built"):
+            B.build()
+        assert ctypes.CDLL(B.LIB).one() == 1
+        assert not (tmp_path / "ebd_call.so").exists()
+        (tmp_path / "libebd.so").unlink()
