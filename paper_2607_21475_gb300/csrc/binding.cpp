@@ -453,6 +453,8 @@ PyObject* append_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
       "k_new", "v_new", "k_weight", "q", "q_weight", "q_out", "cu_new", "slots", "positions",
       "table", "layout", "eps", "stream"};
   return guarded(a, n, names, [&] {
+    if (a[8] == Py_None && (a[9] != Py_None || a[10] != Py_None))
+      bad_value("q_weight or q_out without q");
     const ebd_paged_cache c = paged(a[0], a[1], a[2], a[3]);
     const at::Tensor& Kt = THPVariable_Unpack(a[0]);
     const ScalarType dt = Kt.scalar_type();

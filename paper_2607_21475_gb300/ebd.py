@@ -937,7 +937,8 @@ def ebd_paged_append_norm(pc: PagedCache, k_new: torch.Tensor, v_new: torch.Tens
     """ebd_paged_append with keys and queries normalised on the way (weights as for
     ebd_norm_rotary; None: not normalised), tokens placed by cu_new [B + 1] or by their
     slots [T] (int64, ebd_paged_deal; -1: no token).  positions [T]: where each is turned
-    to; needed with slots and a table, otherwise a token's place in its sequence."""
+    to; needed with slots and a table, otherwise a token's place in its sequence.  q_weight
+    and q_out come with q."""
     _check("ebd_paged_append_norm", (_CALL or _call()).append_norm(
         pc.K_pages, pc.V_pages, pc.block_table, pc.seq_len, pc.dev_status, k_new, v_new, k_weight,
         q, q_weight, q_out, cu_new, slots, positions, table, layout, eps, stream))

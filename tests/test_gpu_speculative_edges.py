@@ -168,3 +168,14 @@ def test_dealt_prompts_and_steps_are_attended_without_a_status(E, dtype):
         want = E.ebd_paged_attention(q_out[:n], pc, cu, max(new))
         assert torch.equal(y[:n], want[0]) and torch.equal(lse[:n], want[1])
         assert pc.dev_status.item() == 0
+
+
+def test_append_refuses_what_it_would_ignore(E):
+    s = R.make([3], [9], 4, 2, 64, 16, torch.bfloat16, 3)
+    pc, w = cache(E, s), torch.ones(64, device="cuda").to(torch.bfloat16)
+    K0 = s["K"].clone()
+    for kw in (dict(q_weight=w), dict(q_out=torch.empty_like(s["q"])),
+               dict(q_weight=w, q_out=torch.empty_like(s["q"]))):
+        with pytest.raises(ValueError, match="without q"):
+            E.ebd_paged_append_norm(pc, s["k"], s["v"], k_weight=w, cu_new=s["cu"], **kw)
+    assert torch.equal(s["K"], K0)

@@ -85,6 +85,15 @@ def test_tensors_of_two_gpus_are_refused(E, which):
             call(**dict(args, **{name: elsewhere}))
 
 
+def test_append_refuses_what_it_would_ignore(E):
+    """Queries' weight or place without queries: a slip that went unseen."""
+    call, args = calls(E)[3]
+    for left in ("q_weight", "q_out"):
+        a = {k: v for k, v in args.items() if k == left or k not in ("q", "q_weight", "q_out")}
+        with pytest.raises(ValueError, match="without q"):
+            call(**a)
+
+
 def test_the_library_is_linked_where_the_binding_does_not_compile(monkeypatch, tmp_path):
     """And the binding of other sources does not stay beside it."""
     import ctypes
