@@ -425,7 +425,7 @@ extern "C" ebd_status ebd_paged_tree_attention(
     size_t ws_bytes, void* stream) {
   const bool causal = !mask && mask_words == 0;
   if (!causal) {
-    if (mask_words < 1 || max_new > 32ll * mask_words) return EBD_ERR_INVALID;
+    if (mask_words < (n_tokens > 0) || max_new > 32ll * mask_words) return EBD_ERR_INVALID;
     if (n_tokens > 0 && (!mask || (window > 0 && !positions))) return EBD_ERR_INVALID;
   }
   return attention(cache, n_tokens, max_new, n_q_heads, cu_new, q, q_token_stride, q_head_stride,

@@ -167,7 +167,8 @@ extern "C" ebd_status ebd_tree_masks(int32_t batch, int32_t n_tokens, int32_t ma
                                      const int32_t* seq_len, int32_t window, uint32_t* mask,
                                      int32_t mask_words, int32_t* positions, int32_t* dev_status,
                                      void* stream) {
-  if (batch < 1 || n_tokens < 0 || max_new < (n_tokens > 0) || window < 0 || mask_words < 1)
+  if (batch < 1 || n_tokens < 0 || max_new < (n_tokens > 0) || window < 0 ||
+      mask_words < (n_tokens > 0))
     return EBD_ERR_INVALID;
   if (max_new > 32ll * mask_words) return EBD_ERR_INVALID;
   if (max_new > kTreeMost || mask_words > kTreeMost / 32 || batch > 65535)

@@ -179,3 +179,26 @@ def test_append_refuses_what_it_would_ignore(E):
         with pytest.raises(ValueError, match="without q"):
             E.ebd_paged_append_norm(pc, s["k"], s["v"], k_weight=w, cu_new=s["cu"], **kw)
     assert torch.equal(s["K"], K0)
+
+
+def test_a_step_without_tokens(E):
+    """Every call of a step in which no request has a token: nothing happens, nothing is
+    refused, lengths stay."""
+    s = tree_case(E, 3, torch.bfloat16)
+    pc = cache(E, s)
+    K0, none = s["K"].clone(), ints([0] * 5)
+    pool = E.alloc_page_pool(4, s["K"].shape[0], "cuda")
+    pool.held.copy_(ints([[0, 1], [0, 1], [0, 2], [0, 1]]))
+    cu, pos, slots, served = E.ebd_paged_deal(pool, pc, none[:4], 0)
+    assert cu.tolist() == [0] * 5 and served.tolist() == [1] * 4 and pos.shape == (0,)
+    mask, tpos = E.ebd_tree_masks(s["parents"][:0], cu, pc.seq_len, 0)
+    assert mask.shape == (0, 0) and tpos.shape == (0,)
+    w = torch.ones(128, device="cuda").to(torch.bfloat16)
+    q = torch.empty_like(s["q"][:0])
+    E.ebd_paged_append_norm(pc, s["k"][:0], s["v"][:0], k_weight=w, q=q, q_weight=w, q_out=q,
+                            slots=slots, positions=pos)
+    for m in (mask, None):
+        y, lse = E.ebd_paged_tree_attention(q, pc, cu, 0, m, positions=tpos, window=7)
+        assert y.shape == q.shape and lse.shape == q.shape[:2]
+    got = E.ebd_paged_keep(pc, cu, ints([[0]] * 4), none[:4])
+    assert got.tolist() == s["total"] and pc.dev_status.item() == 0 and torch.equal(s["K"], K0)

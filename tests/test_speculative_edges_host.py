@@ -1,5 +1,7 @@
 """Refusals of the speculative calls' marshalling, host only: tensors without memory stand
 for those of a GPU."""
+import ctypes
+
 import pytest
 import torch
 from torch._subclasses.fake_tensor import FakeTensorMode
@@ -94,10 +96,24 @@ def test_append_refuses_what_it_would_ignore(E):
             call(**a)
 
 
+def test_a_step_without_tokens_needs_no_mask(E):
+    """max_new 0, a mask of no words: the largest number of new tokens of no sequence."""
+    from test_speculative_host import FAKE, good_cache
+    L, c = E.lib(), good_cache(E)
+    masks = dict(B=2, T=0, most=0, parents=None, cu=FAKE, len=FAKE, window=0, mask=None, words=0,
+                 pos=None, st=None, stream=None)
+    attend = dict(c=ctypes.byref(c), n=0, most=0, hq=2, cu=FAKE, q=None, qt=128, qh=64, scale=0.1,
+                  window=4, mask=FAKE, words=0, pos=None, y=None, lse=None, st=FAKE, ws=None, wsb=0,
+                  stream=None)
+    for f, a, some in ((L.ebd_tree_masks, masks, dict(T=1, most=1)),
+                       (L.ebd_paged_tree_attention, attend, dict(n=1, most=1))):
+        assert f(*a.values()) == E.EBD_OK
+        for bad in (dict(words=-1), dict(most=-1), dict(most=1), some):
+            assert f(*dict(a, **bad).values()) == 1, bad
+
+
 def test_the_library_is_linked_where_the_binding_does_not_compile(monkeypatch, tmp_path):
     """And the binding of other sources does not stay beside it."""
-    import ctypes
-
     from paper_2607_21475_gb300 import build as B
     src = tmp_path / "one.cu"
     src.write_text('extern "C" int one() { return 1; }\n')
