@@ -624,7 +624,8 @@ ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n_pages, int
  *   eps          at least the smallest normal float32 (below 2^-102 rows move by elements or
  *                pairs, several times slower, with sums that such an eps asks for)
  *   positions    device [n_tokens]; outside [0, n_pos): as for ebd_rotary
- * d <= 512 (EBD_ERR_UNSUPPORTED otherwise).  Alignment as for ebd_rotary.
+ * d <= 512, up to 2^30 - 2^16 heads (EBD_ERR_UNSUPPORTED otherwise).  Alignment as for
+ * ebd_rotary.
  */
 ebd_status ebd_norm_rotary(ebd_dtype dtype, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
                            const void* x, int64_t x_token_stride, int64_t x_head_stride,

@@ -55,6 +55,9 @@ constexpr int norm_forward_blocks(int elem, bool all, bool heads) {
   return elem == 4 || (all && !heads) ? 3 : 2;
 }
 constexpr int kNormMaxDim = 512;
+// Heads of a token (append: with the keys' and values'): the next one that a lane asks for lies
+// up to (kAhead + 1) U / 16 times as many past the last, once at most.
+constexpr int kNormMaxHeads = 0x3fff0000;
 // (fewer where a lane holds several pairs of a row: its arrays would spill)
 constexpr int norm_blocks(int blocks, int u, int vec) {
   return u > 1 && u * vec >= 8 ? blocks - 1 : blocks;

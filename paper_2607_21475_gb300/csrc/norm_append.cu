@@ -21,6 +21,7 @@ extern "C" ebd_status ebd_paged_append_norm(
   if (st != EBD_OK) return st;
   if (n_q_heads < 0 || k_weight_head_stride < 0 || q_weight_head_stride < 0)
     return EBD_ERR_INVALID;
+  if (n_q_heads + 2ll * cache->n_kv_heads > kNormMaxHeads) return EBD_ERR_UNSUPPORTED;
   if (n_q_heads > 0 && !table && !q_weight) return EBD_ERR_INVALID;  // nothing to do to q
   if (n_tokens == 0) return EBD_OK;
   // a token's place is told by the offsets or by its slot, one of the two; a slot tells

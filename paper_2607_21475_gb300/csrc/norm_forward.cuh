@@ -183,8 +183,9 @@ ebd_status launch_norm_u(NormArgs a, cudaStream_t s) {
   const int heads = a.n_x + (APPEND ? 2 * a.n_kv : 0);
   // one row per lane while the call has fewer warps than the GPU holds (latency), up to
   // sixteen pairs of chunks per lane beyond that
-  const int many = (heads * a.lanes + 31) / 32, few = (heads * a.lanes * U + 511) / 512;
-  a.parts = (long long)a.n_tokens * many <= (long long)sm_count() * 32 ? many : few;
+  const long long units = (long long)heads * a.lanes;
+  const long long many = (units + 31) / 32, few = (units * U + 511) / 512;
+  a.parts = (int)(many * a.n_tokens <= (long long)sm_count() * 32 ? many : few);
   const long long blocks = ((long long)a.n_tokens * a.parts + kNormWarps - 1) / kNormWarps;
   if (blocks > 0x7fffffffLL) return EBD_ERR_UNSUPPORTED;
   const bool each = (a.wx.p && a.wx.hs) || (APPEND && a.wk.p && a.wk.hs);

@@ -15,6 +15,7 @@ extern "C" ebd_status ebd_norm_rotary(
       check_norm(dtype, n_tokens, head_dim, layout, eps, weight_dtype, table, n_pos, rot);
   if (st != EBD_OK) return st;
   if (n_heads < 1 || weight_head_stride < 0) return EBD_ERR_INVALID;
+  if (n_heads > kNormMaxHeads) return EBD_ERR_UNSUPPORTED;
   if (n_tokens == 0) return EBD_OK;
   if (!x || !y || !weight || (table && !positions)) return EBD_ERR_INVALID;
   NormArgs a = {};

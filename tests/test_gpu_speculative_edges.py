@@ -115,6 +115,21 @@ def test_more_rows_than_31_bits_count_are_refused(E):
             E.ebd_norm_rotary_backward(z, z, w, dx=z, dweight=dw)
 
 
+def test_norm_of_more_chunks_than_31_bits_count(E):
+    """2^28 heads of one token (69 GB out, from views of a few rows): units of work, offsets and
+    heads in 64 bits where they need them."""
+    H, d, n = 2 ** 28 + 3, 128, 4
+    x, _, w, _ = norm_inputs(1, n, d, torch.bfloat16, False, 31)
+    want = E.ebd_norm_rotary(x, w)
+    check_normed(want, x, w, None, None, "half", torch.bfloat16)
+    got = torch.empty((1, H, d), dtype=torch.bfloat16, device="cuda")
+    E.ebd_norm_rotary(x[:, :1].expand(1, H, d), w, out=got)
+    for part in got[0].split(1 << 23):
+        assert torch.equal(part, want[0, :1].expand(part.shape))
+    del got, part
+    torch.cuda.empty_cache()
+
+
 # ---------------------------------------------------------------- causal tokens after a deal
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("case", [0, 3, 4, 5, 8, 10])

@@ -112,6 +112,21 @@ def test_a_step_without_tokens_needs_no_mask(E):
             assert f(*dict(a, **bad).values()) == 1, bad
 
 
+def test_more_heads_than_31_bits_count_are_refused(E):
+    from test_speculative_host import FAKE, NORM, good_cache
+    L, most = E.lib(), 0x3fff0000
+    for h in (most + 1, 2 ** 31 - 1):
+        assert L.ebd_norm_rotary(*dict(NORM, H=h).values()) == 4
+    assert L.ebd_norm_rotary(*dict(NORM, H=most, T=0).values()) == E.EBD_OK
+    c = good_cache(E)
+    a = dict(c=ctypes.byref(c), T=0, cu=FAKE, slots=None, pos=None, k=FAKE, kt=128, kh=64, v=FAKE,
+             vt=128, vh=64, kw=FAKE, kwh=0, qw=FAKE, qwh=0, wt=1, eps=1e-6, table=None, n_pos=0,
+             rot=0, layout=0, hq=most - 3, q=FAKE, qt=128, qh=64, o=FAKE, ot=128, oh=64, st=FAKE,
+             stream=None)
+    assert L.ebd_paged_append_norm(*a.values()) == 4
+    assert L.ebd_paged_append_norm(*dict(a, hq=most - 4).values()) == E.EBD_OK
+
+
 def test_the_library_is_linked_where_the_binding_does_not_compile(monkeypatch, tmp_path):
     """And the binding of other sources does not stay beside it."""
     from paper_2607_21475_gb300 import build as B
