@@ -587,11 +587,13 @@ ebd_status ebd_paged_gather(const ebd_paged_cache* cache, const int32_t* idx_c,
  *     wanted pages up to and including its own are there (it needs none, or) and so is
  *     room for the new tokens up to and including its own in n_tokens packed ones: a
  *     sequence that does not fit holds back those after it that need pages or tokens
- *     past what is left, and nothing of it changes (EBD_DEV_CAPACITY, served[b] = 0).
+ *     past what is left (EBD_DEV_CAPACITY, served[b] = 0).  Its length, its end block
+ *     held[b][1] and its row of the table stay; held[b][0] does not, where blocks behind
+ *     its window were given back: others may have their pages by now.
  *     A request too long for its row is left out of that count;
  *   - pages are taken from the end of the list, by sequence and block, and entered into
  *     the table; entries of blocks not held keep what they hold;
- *   - seq_len_out[b] = seq_len[b] + n_new[b] where served, held_out and n_free_out alike,
+ *   - seq_len_out[b] = seq_len[b] + n_new[b] where served; held_out and n_free_out as above,
  *     cu_new the packed offsets of the served sequences' new tokens; positions[t] and
  *     slots[t] = page * page_size + row of packed token t; 0 and -1 past the last one.
  * The outputs seq_len_out, held_out, n_free_out may be the inputs.  Entries outside their

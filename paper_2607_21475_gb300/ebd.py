@@ -878,7 +878,9 @@ def ebd_paged_deal(pool: PagePool, pc: PagedCache, n_new: torch.Tensor, n_tokens
     int64, served [B]).  pc.seq_len counts the cached tokens before the call and, like
     pool.held and pool.n_free, is brought up to date in place unless another output is
     given; pc.block_table and pool.free_pages always are.  A sequence that is not served
-    (EBD_DEV_CAPACITY in dev_status) stays as it was and has no new tokens in cu_new."""
+    (EBD_DEV_CAPACITY in dev_status) has no new tokens in cu_new and keeps its length and
+    pages, but for the blocks behind its window, which are given back like any other's
+    (pool.held[b, 0] goes up; others may have been dealt their pages)."""
     B, i32, dev = pc.block_table.shape[0], torch.int32, pc.seq_len.device
     if cu_new is None:
         cu_new = _result((B + 1,), i32, dev, stream)

@@ -6,8 +6,9 @@ import pytest
 import torch
 
 import paged_ref as R
-from test_gpu_speculative import (cache, check_grad, check_normed, ints, norm_inputs, slots_of,
-                                  table_of, tree_case)
+import speculative_ref as S
+from test_gpu_speculative import (cache, check_grad, check_normed, fresh_pool, ints, norm_inputs,
+                                  slots_of, table_of, tree_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -217,3 +218,26 @@ def test_a_step_without_tokens(E):
         assert y.shape == q.shape and lse.shape == q.shape[:2]
     got = E.ebd_paged_keep(pc, cu, ints([[0]] * 4), none[:4])
     assert got.tolist() == s["total"] and pc.dev_status.item() == 0 and torch.equal(s["K"], K0)
+
+
+# ---------------------------------------------------------------- a deal that cannot serve
+def test_unserved_sequences_give_back_what_is_behind_their_window(E):
+    """Length, end block and table entries stay; the blocks behind the window are given back,
+    and others may be dealt them in the same call."""
+    P, window, n_pages = 8, 20, 10
+    pool, pc = fresh_pool(E, 2, n_pages, P, 12)
+    free, table = list(range(n_pages)), [[0] * 12, [0] * 12]
+    length, held = [0, 0], [[0, 0], [0, 0]]
+    for new, want in [([48, 0], [1, 1]), ([0, 8], [1, 1]), ([1, 60], [1, 0]), ([3, 9], [1, 1]),
+                      ([70, 8], [0, 1]), ([8, 0], [1, 1]), ([36, 0], [0, 1]),
+                      ([0, 1], [1, 1])]:
+        cu, pos, slots, served = E.ebd_paged_deal(pool, pc, ints(new), 100, window=window)
+        length, held, cu_r, served_r, pos_r, slots_r = S.deal(P, n_pages, 12, 100, window, new,
+                                                              length, held, free, table)
+        assert served.tolist() == served_r == want
+        assert pc.seq_len.tolist() == length and pool.held.tolist() == held
+        assert pc.block_table.tolist() == table and slots.tolist() == slots_r
+        n = pool.n_free.item()
+        assert pool.free_pages[:n].tolist() == free and cu.tolist() == cu_r
+        out = [p for b in range(2) for p in table[b][held[b][0]:held[b][1]]]
+        assert sorted(out + free) == list(range(n_pages))
