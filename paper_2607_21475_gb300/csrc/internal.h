@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "../../include/ebd.h"
+#include "cluster.h"
 
 namespace ebd {
 
@@ -18,6 +19,34 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // Number of SMs of the current device (cached per device).
 int sm_count();
+
+// cluster_ctas on the current device for launches of `threads` and `smem` bytes; clusters of
+// up to `most` CTAs are allowed for the kernel with the question.
+template <typename Kernel>
+int cluster_ctas(int want, int most, ClusterMemo& memo, Kernel* kern, int threads, size_t smem) {
+  int dev = -1;
+  if (want > kPortableCluster && cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+  return cluster_ctas(want, memo, dev, [&] {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(most);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = most;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
+            cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      return 0;
+    }
+    return n;
+  });
+}
 
 // Design validation shared by the eviction entry points (evict.cu).
 ebd_status check_design(const ebd_design* d);

@@ -235,10 +235,9 @@ ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s
   // Few steps: a cluster per row, which adds its sums up itself, in place of a second launch.
   const bool few = steps <= kNormFewSteps;
   const int most = norm_back_blocks(steps, rows);
-  const int blocks = few ? (int)((steps + kNormWarps - 1) / kNormWarps < kNormCluster
-                                     ? (steps + kNormWarps - 1) / kNormWarps
-                                     : kNormCluster)
-                         : most;
+  int blocks = most;
+  if (few) blocks = (int)((steps + kNormWarps - 1) / kNormWarps);
+  if (few && blocks > kNormCluster) blocks = kNormCluster;
   const int total = rows * a.head_dim;
   const int sums = kNormWarps * a.lanes * U * 2 * VEC * 4 + (few ? a.head_dim * 4 : 0);
   const int ring = RowRing<T, VEC, U, 2>::kBytes, smem = sums > ring ? sums : ring;
@@ -247,9 +246,8 @@ ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s
   if (smem > 48 * 1024 &&
       cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
     return EBD_ERR_CUDA;
-  if (blocks > 8 && few &&
-      cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
-    return EBD_ERR_CUDA;
+  static ClusterMemo memo[2];
+  if (few) blocks = cluster_ctas(blocks, kNormCluster, memo[per_head], kern, kNormWarps * 32, smem);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(blocks, rows);
   cfg.blockDim = dim3(kNormWarps * 32);

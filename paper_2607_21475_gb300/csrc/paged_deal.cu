@@ -569,18 +569,13 @@ extern "C" ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n
   // few threads, where that is enough: their barriers and sums are the cheaper
   const bool small = batch <= kDealThreads && n_tokens <= 4 * kDealThreads;
   const int threads = small && batch <= 256 && n_tokens <= 1024 ? 512 : kDealThreads;
-  const int ctas = small || batch > kDealSeqs ? kDealCluster : kDealLargeCluster;
   const int per = (batch + threads - 1) / threads;
   auto kern = batch > kDealSeqs ? paged_deal_many_kernel
               : small           ? paged_deal_kernel<1, false>
               : per == 1        ? paged_deal_kernel<1, true>
                                 : paged_deal_kernel<kDealSeqs / kDealThreads, true>;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(ctas);
   cfg.blockDim = dim3(threads);
-  if (ctas > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) !=
-                      cudaSuccess)
-    return EBD_ERR_CUDA;
   if (batch <= kDealSeqs) {
     cfg.dynamicSmemBytes = DealSums::bytes(batch);
     if (cfg.dynamicSmemBytes > 40 * 1024 &&
@@ -588,6 +583,10 @@ extern "C" ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n
                              (int)DealSums::bytes(kDealSeqs)) != cudaSuccess)
       return EBD_ERR_CUDA;
   }
+  static ClusterMemo memo[2];
+  const int want = small || batch > kDealSeqs ? kDealCluster : kDealLargeCluster;
+  cfg.gridDim = dim3(cluster_ctas(want, kDealLargeCluster, memo[per > 1], kern, threads,
+                                  cfg.dynamicSmemBytes));
   cfg.stream = (cudaStream_t)stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -149,3 +149,32 @@ def test_the_library_is_linked_where_the_binding_does_not_compile(monkeypatch, t
         assert ctypes.CDLL(B.LIB).one() == 1
         assert not (tmp_path / "ebd_call.so").exists()
         (tmp_path / "libebd.so").unlink()
+
+
+CLUSTERS = r"""
+#include "cluster.h"
+static ebd::ClusterMemo memo;
+static int asked = 0;
+extern "C" int choose(int want, int device, int active) {
+  return ebd::cluster_ctas(want, memo, device, [&] { ++asked; return active; });
+}
+extern "C" int times_asked() { return asked; }
+"""
+
+
+def test_clusters_fall_back_to_eight(tmp_path):
+    """A GPU that holds no cluster of sixteen, told by a fake of the question: eight are asked
+    for; the question is put once per device."""
+    import os
+    import subprocess
+
+    from paper_2607_21475_gb300 import build as B
+    (tmp_path / "c.cpp").write_text(CLUSTERS)
+    subprocess.run([os.environ.get("CXX", "g++"), "-std=c++17", "-fPIC", "-shared", "-I", B.CSRC,
+                    str(tmp_path / "c.cpp"), "-o", str(tmp_path / "c.so")], check=True)
+    L = ctypes.CDLL(str(tmp_path / "c.so"))
+    assert [L.choose(n, 0, 0) for n in (1, 7, 8)] == [1, 7, 8] and L.times_asked() == 0
+    assert [L.choose(n, 0, 9) for n in (9, 16)] == [9, 16] and L.times_asked() == 1
+    assert [L.choose(n, 1, 0) for n in (9, 16, 8, 3)] == [8, 8, 8, 3] and L.times_asked() == 2
+    assert L.choose(16, 0, 0) == 16 and L.choose(16, 1, 9) == 8 and L.times_asked() == 2
+    assert [L.choose(16, d, 9) for d in (-1, 64)] == [8, 8] and L.times_asked() == 2
