@@ -218,12 +218,13 @@ static int norm_back_blocks(long long steps, int heads) {
 }
 
 constexpr int kNormCluster = 16;  // blocks of a cluster at most
-// Steps (of a row of blocks) that one cluster takes: beyond it the kernels of two launches
-// are shorter by more than the second launch's host time (1.5 us).  One cluster against two
-// launches, us: 28 heads x 128, bf16, 1 token 4.0 / 4.3, 8 (56 steps) 4.6 / 4.6, 36 (252)
-// 5.4 / 5.0, 146 (1022) 9.2 / 6.2; a weight per head, 4 x 64, f32, 1021 tokens (256) 4.6 /
-// 4.4, 2048 (512) 6.2 / 4.8.
-constexpr int kNormFewSteps = 256;
+// Steps (of a row of blocks) that one cluster takes: one to each of its warps.  It then saves
+// the second launch; with a second step per warp that launch's many blocks are the quicker.  One
+// cluster against two launches, us in a graph (in a row of calls): 28 heads x 128, bf16, 7 steps
+// 3.7 / 4.1 (4.3 / 5.3), 126 4.2 / 4.5 (4.7 / 5.2), 252 5.2 / 4.6 (5.7 / 5.2), 1022 8.9 / 6.2
+// (9.5 / 6.6); a weight per head, 4 x 64, f32, 128 steps 3.6 / 3.9 (4.1 / 5.4), 256 4.5 / 4.1 (5.2 /
+// 5.3), 512 6.1 / 4.4 (7.1 / 5.3).
+constexpr int kNormFewSteps = kNormCluster * kNormWarps;
 
 template <typename T, int VEC, bool PAIRS, int U, int FL, bool ALL>
 ebd_status launch_norm_back_u(NormArgs a, const NormBackward& bw, cudaStream_t s) {

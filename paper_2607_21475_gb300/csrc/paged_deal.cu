@@ -31,6 +31,10 @@
 namespace ebd {
 
 constexpr int kDealThreads = 1024;
+// Threads where they are one per sequence and, over 8 CTAs, one per token: their barriers and
+// sums are the cheaper (one sequence 2.5 us against 2.9 with 1024, 256 3.0 / 3.4, 384 3.1 / 3.6, 512
+// 3.45 / 3.55).
+constexpr int kDealFewThreads = 512;
 // CTAs of a cluster: 8, 16 where many tokens are to be mapped (256 steps, 2000 pages given
 // back: 1 CTA 7.0 us, 2 6.0, 4 5.3, 8 4.4; 100k tokens of prompts: 4 12.0 us, 8 8.5, 16 7.5)
 constexpr int kDealCluster = 8, kDealLargeCluster = 16;
@@ -566,9 +570,8 @@ extern "C" ebd_status ebd_paged_deal(int32_t batch, int32_t page_size, int32_t n
   a.positions = positions;
   a.slots = slots;
   a.dev_status = dev_status;
-  // few threads, where that is enough: their barriers and sums are the cheaper
-  const bool small = batch <= kDealThreads && n_tokens <= 4 * kDealThreads;
-  const int threads = small && batch <= 256 && n_tokens <= 1024 ? 512 : kDealThreads;
+  const bool small = batch <= kDealThreads && n_tokens <= kDealCluster * kDealFewThreads;
+  const int threads = small && batch <= kDealFewThreads ? kDealFewThreads : kDealThreads;
   const int per = (batch + threads - 1) / threads;
   auto kern = batch > kDealSeqs ? paged_deal_many_kernel
               : small           ? paged_deal_kernel<1, false>

@@ -8,7 +8,7 @@ import torch
 import paged_ref as R
 import speculative_ref as S
 from test_gpu_speculative import (cache, check_grad, check_normed, fresh_pool, ints, norm_inputs,
-                                  slots_of, table_of, tree_case)
+                                  run_steps, slots_of, table_of, tree_case)
 
 pytestmark = pytest.mark.gpu
 
@@ -241,3 +241,23 @@ def test_unserved_sequences_give_back_what_is_behind_their_window(E):
         assert pool.free_pages[:n].tolist() == free and cu.tolist() == cu_r
         out = [p for b in range(2) for p in table[b][held[b][0]:held[b][1]]]
         assert sorted(out + free) == list(range(n_pages))
+
+
+# ---------------------------------------------------------------- where the forms change
+@pytest.mark.parametrize("B,n_tokens", [(1, 4096), (256, 4097), (257, 257), (512, 4096), (513, 600),
+                                        (1024, 4096), (1025, 2000)])
+def test_deal_at_the_ends_of_its_forms(E, B, n_tokens):
+    run_steps(E, B, 6 * B, 8, 30, n_tokens, 0, [lambda r, n: r.choice([0, 1, 2, 5, -1])] * 3, B)
+
+
+@pytest.mark.parametrize("T,H,d,dtype,per_head", [
+    (16, 32, 128, torch.bfloat16, False), (17, 32, 128, torch.bfloat16, False),  # 128, 136 steps
+    (512, 4, 64, torch.float32, True), (513, 4, 64, torch.float32, True),        # 128, 129
+    (36, 28, 128, torch.bfloat16, False), (1021, 4, 64, torch.float32, True)])   # 252, 256
+def test_norm_gradient_at_the_ends_of_its_forms(E, T, H, d, dtype, per_head):
+    x, dy, w, pos = norm_inputs(T, H, d, dtype, per_head, T)
+    tab = table_of(E, d, 4000)
+    dx, dw = E.ebd_norm_rotary_backward(dy, x, w, pos, tab)
+    check_grad(dx, dw, dy, x, w, pos, tab, "half", dtype)
+    again = E.ebd_norm_rotary_backward(dy, x, w, pos, tab)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
