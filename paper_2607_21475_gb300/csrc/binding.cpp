@@ -295,6 +295,8 @@ struct {
 void check_devices(PyObject* const* a, Py_ssize_t n, const char* const* names) {
   int device = -1, first = 0;
   for (int i = 0; i < n; ++i) {
+    // (asked whether it is a tensor, a number takes 60 ns)
+    if (a[i] == Py_None || PyLong_Check(a[i]) || PyFloat_Check(a[i])) continue;
     if (!THPVariable_Check(a[i]) || !THPVariable_Unpack(a[i]).is_cuda()) continue;
     const int at = THPVariable_Unpack(a[i]).device().index();
     if (device < 0) device = at, first = i;
