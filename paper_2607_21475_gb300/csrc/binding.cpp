@@ -297,8 +297,10 @@ void check_devices(PyObject* const* a, Py_ssize_t n, const char* const* names) {
   for (int i = 0; i < n; ++i) {
     // (asked whether it is a tensor, a number takes 60 ns)
     if (a[i] == Py_None || PyLong_Check(a[i]) || PyFloat_Check(a[i])) continue;
-    if (!THPVariable_Check(a[i]) || !THPVariable_Unpack(a[i]).is_cuda()) continue;
-    const int at = THPVariable_Unpack(a[i]).device().index();
+    if (!THPVariable_Check(a[i])) continue;
+    const c10::Device d = THPVariable_Unpack(a[i]).device();
+    if (!d.is_cuda()) continue;
+    const int at = d.index();
     if (device < 0) device = at, first = i;
     if (at != device)
       bad_value(std::string(names[i]) + " is on cuda:" + std::to_string(at) + ", " + names[first] +
