@@ -186,10 +186,10 @@ __global__ void __launch_bounds__(kNormWarps * 32, norm_blocks(kNormBackBlocks, 
 
 // dweight[i] = sum over the n blocks of partial[block][i], i < total; 32 columns per block,
 // warp w sums the blocks w, w + 32, .., and the warps' sums are added in a fixed order.
+// (It begins before the other kernel ends: its loads are not declared constant.)
 constexpr int kReduceWarps = 32;
 __global__ void __launch_bounds__(kReduceWarps * 32)
-    norm_weight_reduce_kernel(const float* __restrict__ partial, int n, int total,
-                              float* __restrict__ dweight) {
+    norm_weight_reduce_kernel(const float* partial, int n, int total, float* dweight) {
   __shared__ float s[kReduceWarps][33];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, i = blockIdx.x * 32 + lane;
   grid_launch_dependents();

@@ -97,11 +97,12 @@ __device__ __forceinline__ int tree_first_seen(const PagedAttnArgs& a, int t, in
   return min(first_seen(a, at), max(base, 0));
 }
 
-// Mask words w, w + 1 of new token t, as one.
+// Mask words w, w + 1 of new token t, as one.  (Ordinary loads: the kernel that writes them may
+// not have ended when this one begins.)
 __device__ __forceinline__ uint64_t tree_words(const PagedAttnArgs& a, int t, int w) {
   const uint32_t* row = a.mask + (size_t)t * a.mask_words;
-  const uint32_t lo = w < a.mask_words ? __ldg(row + w) : 0u;
-  const uint32_t hi = w + 1 < a.mask_words ? __ldg(row + w + 1) : 0u;
+  const uint32_t lo = w < a.mask_words ? row[w] : 0u;
+  const uint32_t hi = w + 1 < a.mask_words ? row[w + 1] : 0u;
   return (uint64_t)hi << 32 | lo;
 }
 

@@ -240,7 +240,8 @@ __global__ void __launch_bounds__(kDealThreads, 1) paged_deal_kernel(const DealA
   if (threadIdx.x == 0 && RUNS) of.run[a.batch] = (int)got.v[0];
   __syncthreads();
 
-  // Where the j-th page given back lies, and the j-th taken.
+  // Where the j-th page given back lies, and the j-th taken.  (Read by ordinary loads: the call
+  // before this one may still be writing when this kernel begins.)
   auto given = [&](int j) {
     const int o = place_in(of.back, a.batch, j);
     return a.block_table + (size_t)o * a.max_blocks + of.lo[o] + (j - of.back[o]);
@@ -252,8 +253,8 @@ __global__ void __launch_bounds__(kDealThreads, 1) paged_deal_kernel(const DealA
   // The page of a block of sequence b.
   auto page_at = [&](int b, int block) {
     const int fresh = block - of.hi[b];
-    return __ldg(fresh < 0 ? a.block_table + (size_t)b * a.max_blocks + block
-                           : taken_at(of.take[b] + fresh));
+    return *(fresh < 0 ? a.block_table + (size_t)b * a.max_blocks + block
+                       : taken_at(of.take[b] + fresh));
   };
   auto write = [&](int t, int pos, int page) {
     const bool in_pool = (unsigned)page < (unsigned)a.n_pages;
@@ -293,9 +294,9 @@ __global__ void __launch_bounds__(kDealThreads, 1) paged_deal_kernel(const DealA
         }
       }
     } else if (const int j = (int)(w - n_maps); j < n_back) {
-      a.free_pages[n_free + j] = __ldg(given(j));
+      a.free_pages[n_free + j] = *given(j);
     } else {
-      const int k = j - n_back, b = place_in(of.take, a.batch, k), page = __ldg(taken_at(k));
+      const int k = j - n_back, b = place_in(of.take, a.batch, k), page = *taken_at(k);
       bad |= (unsigned)page >= (unsigned)a.n_pages;
       a.block_table[(size_t)b * a.max_blocks + of.hi[b] + (k - of.take[b])] = page;
     }

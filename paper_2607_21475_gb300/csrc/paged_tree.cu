@@ -15,7 +15,9 @@
 // HBM and the chain lengths -> path -> pages -> rows bound it.
 //
 // Both are programmatic dependents of what precedes them on the stream, and let the next
-// kernel of that kind begin.
+// kernel of that kind begin.  Since they may begin before the kernel that writes their inputs
+// ends, nothing that it may write is declared constant (const __restrict__, __ldg): such a load
+// may be moved before the wait, or served from a cache that the wait does not clear.
 // Measured: masks of 16 to 64 tokens 2.3-3 us; paths of up to 8 of 64 tokens of 32 sequences
 // in 28 layers (8 heads x 128, bf16) 5.2 us, 16 MB of rows; one small layer 2.6 us.
 #include <cuda_runtime.h>
@@ -36,10 +38,9 @@ constexpr int kKeepMoves = 32;   // path entries placed at a time
 
 // Block (x, b): tokens kTreeWarps x .. of sequence b.
 __global__ void __launch_bounds__(kTreeWarps * 32)
-    tree_masks_kernel(const int32_t* __restrict__ parents, const int32_t* __restrict__ cu,
-                      const int32_t* __restrict__ seq_len, int n_tokens, int max_new,
-                      int words, int window, uint32_t* __restrict__ mask,
-                      int32_t* __restrict__ positions, int32_t* dev_status) {
+    tree_masks_kernel(const int32_t* parents, const int32_t* cu, const int32_t* seq_len,
+                      int n_tokens, int max_new, int words, int window, uint32_t* mask,
+                      int32_t* positions, int32_t* dev_status) {
   __shared__ int parent_s[kTreeMost];
   const int b = blockIdx.y, lane = threadIdx.x & 31, first = blockIdx.x * kTreeWarps;
   grid_launch_dependents();
@@ -78,9 +79,9 @@ __global__ void __launch_bounds__(kTreeWarps * 32)
 // bytes, `cpr` of them to a row.
 __global__ void __launch_bounds__(kKeepThreads)
     paged_keep_kernel(uint4* K, uint4* V, PagedView v,
-                      long long layer_stride, int cpr, const int32_t* __restrict__ cu,
-                      const int32_t* __restrict__ path, const int32_t* __restrict__ n_kept,
-                      int max_path, int32_t* __restrict__ seq_len_out, int32_t* dev_status) {
+                      long long layer_stride, int cpr, const int32_t* cu, const int32_t* path,
+                      const int32_t* n_kept, int max_path, int32_t* seq_len_out,
+                      int32_t* dev_status) {
   __shared__ long long from_s[kKeepMoves], to_s[kKeepMoves];
   __shared__ int kept_s, moves_s;
   const int b = blockIdx.x, lane = threadIdx.x & 31;
