@@ -24,7 +24,7 @@
 // warp, per block and over the blocks (few rows: of one cluster), in that fixed order.
 // Measured, bf16, 28 heads x 128: 16384 tokens 38.4 us in either layout, 6.3 TB/s (94% of the
 // measured copy peak), half of each head turning 43.4, a weight per head 51.9; gradient of
-// 8192 tokens 34.8 us, 5.2 TB/s (77%: instructions, 57% of the issue slots, and 16 warps per
+// 8192 tokens 34.5 us, 5.2 TB/s (77%: instructions, 57% of the issue slots, and 16 warps per
 // SM, 128 registers each), a weight per head 43.4; 8 ragged chunks of 9.4k tokens in all
 // appended (28/4 heads) 33.7 us, 5.3 TB/s; append step of 32 sequences (32/8 heads) 3.3 us.
 // All are programmatic dependents of what precedes them on the stream.
